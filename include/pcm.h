@@ -12,6 +12,8 @@
  *                           surrogate (Eq. 11; Eq. 2 when every chunk is kept) and backward
  *
  * and, to complete the actor update, pcm_adamw_clip_step applies the gradients (App. D).
+ * Around it, for policies over any vocabulary and as an optimizer for matrices: pcm_token_logprobs and its gradient,
+ * pcm_orthogonalise and pcm_muon_step.
  *
  * Conventions common to every entry point
  *   - Return value: PCM_OK or a negative pcm_status.  Nothing throws, aborts or prints.
@@ -448,6 +450,85 @@ PCM_API int pcm_adamw_clip_step_ex(int n_tensors, const int64_t* numel, const fl
                                    double beta2, double eps, double weight_decay, double max_grad_norm,
                                    const double* grad_sumsq, float* grad_norm_out, void* workspace,
                                    size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * pcm_token_logprobs -- log-probabilities of given tokens, with entropy and the likeliest alternatives, from rows of logits over
+ * any vocabulary: the old-policy pass that makes logp_old, the scoring of a rollout, what is logged of a policy.
+ *
+ * With x_j = logits[r][j] / temperature over the allowed tokens j of row r:
+ *   lse = log sum_j e^(x_j);   logp = x_token - lse;   entropy = lse - sum_j p_j x_j with p_j = e^(x_j - lse);
+ *   the `top` tokens of the largest logits, in descending order, of equal ones the lower index first, and their logp.
+ * Sums are fp32.  One pass over the logits.
+ *
+ *   logits    device [rows] rows of V values of dtype (PCM_F32 or PCM_BF16), logits_ld >= V values apart
+ *   tokens    device [rows] of token_type; a token >= V counts as V-1, a negative one marks a row without a token (logp 0)
+ *   allowed   device u8, or NULL (all tokens): zero excludes a token, whatever its logit holds; allowed_ld = 0: [V], the same for
+ *             every row, else rows of V values, allowed_ld >= V apart
+ *   temperature  > 0, with a finite reciprocal
+ *   top       0 .. PCM_MAX_TOP_TOKENS
+ *   logp, lse device f32 [rows];  entropy device f32 [rows] or NULL
+ *   top_ids   device i32 [rows, top], top_logp device f32 [rows, top]; unused if top = 0
+ * A row that allows nothing, or nothing but logits of -inf: lse -inf, entropy 0, logp -inf (an excluded token has logp -inf
+ * in every row).  Where fewer than `top` tokens are allowed the rest is id -1 and logp -inf.  A NaN or +inf among the allowed logits
+ * makes the row's lse, logp, entropy and top_logp NaN; a NaN is not among the alternatives.  Rows do not depend on one another.
+ * logits may be any rows of a larger matrix; they are only read.  rows = 0 is a valid call that does nothing.
+ *
+ * pcm_token_logprobs_backward -- the gradient of a loss in the logits, from its gradients in logp and entropy:
+ *   d x_j = [j = token] dlogp - p_j (dlogp + dentropy (log p_j + entropy)),  dlogits = d x / temperature, 0 for excluded tokens
+ *   and rows without a finite lse because nothing is allowed; a row without a token takes only the entropy's part.
+ *   lse, entropy         device f32 [rows], as the forward call left them;  entropy NULL exactly if dentropy is
+ *   dlogp, dentropy      device f32 [rows];  dentropy NULL: no gradient through the entropy
+ *   dlogits              device [rows] rows of V values of dtype, dlogits_ld >= V apart (values between rows are left as they
+ *                        are); may be the logits themselves, with the same leading dimension
+ * The other arguments as in the forward call.  Needs no workspace.
+ * ------------------------------------------------------------------------------------------ */
+#define PCM_MAX_TOP_TOKENS 64
+typedef enum { PCM_TOKEN_U8 = 0, PCM_TOKEN_I32 = 1, PCM_TOKEN_I64 = 2 } pcm_token_type;
+PCM_API size_t pcm_token_logprobs_workspace_bytes(int64_t rows, int V, int top);
+PCM_API int pcm_token_logprobs(const void* logits, int64_t logits_ld, int dtype, const void* tokens, int token_type,
+                               const uint8_t* allowed, int64_t allowed_ld, int64_t rows, int V, float temperature, int top,
+                               float* logp, float* lse, float* entropy, int32_t* top_ids, float* top_logp, void* workspace,
+                               size_t workspace_bytes, void* stream);
+PCM_API int pcm_token_logprobs_backward(const void* logits, int64_t logits_ld, int dtype, const void* tokens, int token_type,
+                                        const uint8_t* allowed, int64_t allowed_ld, int64_t rows, int V, float temperature,
+                                        const float* lse, const float* dlogp, const float* entropy, const float* dentropy,
+                                        void* dlogits, int64_t dlogits_ld, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * pcm_orthogonalise -- the matrix nearest in kind to an update whose singular values are all about one, by ns_steps steps of
+ * the Newton-Schulz iteration  X <- a X + (b A + c A^2) X,  A = X X^T,  (a, b, c) = (3.4445, -4.7750, 2.0315),  from
+ * X_0 = G / |G|_F (taken transposed where G has more rows than columns; the result is transposed back).  Every singular value s
+ * becomes a s + b s^3 + c s^5 per step: after five steps those above 0.002 |G|_F lie in [0.68, 1.21].
+ * Products are carried to fp32 accuracy (operands as pairs of fp16 values, fp32 sums).
+ *
+ *   update    device [batch] matrices of rows x cols of dtype: rows update_ld >= cols values apart, matrices update_stride
+ *   out       the same with out_ld, out_stride >= (rows - 1) out_ld + cols; may be the update itself
+ *   ns_steps  1 .. 10
+ * A matrix of zeros gives zeros; one that holds a NaN or an infinity gives NaN throughout.
+ * Limits: 1 <= rows, cols <= 2^20, the smaller of them <= 2^15.
+ *
+ * pcm_muon_step -- the optimizer step for matrices that uses it, beside pcm_adamw_clip_step.  Per tensor, in fp32:
+ *   m <- momentum_coef m + g;  u = g + momentum_coef m (nesterov) or m;  O = orthogonalise(u);
+ *   w <- w (1 - lr weight_decay) - lr scale O
+ * with scale = sqrt(max(1, cols / rows)) (PCM_MUON_SCALE_SHAPE; weights are stored [in, out]) or
+ * 0.2 sqrt(max(rows, cols)) (PCM_MUON_SCALE_RMS: updates of about the size of AdamW's).
+ *   n_tensors     1 .. PCM_MAX_OPT_TENSORS;  rows, cols host arrays [n_tensors], limits as above
+ *   grads         host array of device pointers, f32 [rows, cols]; read only
+ *   weights, momentum  host arrays of device pointers, f32 [rows, cols]; updated in place
+ *   weights_bf16  NULL, or a host array of device pointers (entries may be NULL) to bf16 [rows, cols] that receive the new
+ *                 weights rounded to nearest even
+ * Errors: PCM_EINVAL also for a hyper-parameter out of range (momentum_coef outside [0, 1), negative lr or weight decay).
+ * ------------------------------------------------------------------------------------------ */
+typedef enum { PCM_MUON_SCALE_SHAPE = 0, PCM_MUON_SCALE_RMS = 1 } pcm_muon_scale;
+PCM_API size_t pcm_orthogonalise_workspace_bytes(int batch, int rows, int cols);
+PCM_API int pcm_orthogonalise(const void* update, int64_t update_ld, int64_t update_stride, void* out, int64_t out_ld,
+                              int64_t out_stride, int batch, int rows, int cols, int dtype, int ns_steps, void* workspace,
+                              size_t workspace_bytes, void* stream);
+PCM_API size_t pcm_muon_step_workspace_bytes(int n_tensors, const int* rows, const int* cols);
+PCM_API int pcm_muon_step(int n_tensors, const int* rows, const int* cols, const float* const* grads, float* const* weights,
+                          float* const* momentum, void* const* weights_bf16, double lr, double momentum_coef, int nesterov,
+                          double weight_decay, int ns_steps, int scale_rule, void* workspace, size_t workspace_bytes,
+                          void* stream);
 
 #ifdef __cplusplus
 }

@@ -19,6 +19,8 @@ from .binding import (  # noqa: F401
     pcm_kept_phase_counts,
     pcm_label_phases,
     pcm_measure_mfma_rate,
+    pcm_muon_step,
+    pcm_orthogonalise,
     pcm_pack_head_weights,
     pcm_profile_collect,
     pcm_profile_enable,
@@ -26,6 +28,8 @@ from .binding import (  # noqa: F401
     pcm_score_phases,
     pcm_state_bytes,
     pcm_state_init,
+    pcm_token_logprobs,
+    pcm_token_logprobs_backward,
     pcm_update_keep_probs,
     pcm_version,
 )

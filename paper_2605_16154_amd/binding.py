@@ -81,6 +81,17 @@ def lib() -> C.CDLL:
     _sig(L.pcm_adamw_clip_step_ex, i32,
          [i32, C.POINTER(i64), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), i64,
           f64, f64, f64, f64, f64, f64, vp, vp, vp, sz, vp])
+    _sig(L.pcm_token_logprobs_workspace_bytes, sz, [i64, i32, i32])
+    _sig(L.pcm_token_logprobs, i32,
+         [vp, i64, i32, vp, i32, vp, i64, i64, i32, f32, i32, vp, vp, vp, vp, vp, vp, sz, vp])
+    _sig(L.pcm_token_logprobs_backward, i32,
+         [vp, i64, i32, vp, i32, vp, i64, i64, i32, f32, vp, vp, vp, vp, vp, i64, vp])
+    _sig(L.pcm_orthogonalise_workspace_bytes, sz, [i32] * 3)
+    _sig(L.pcm_orthogonalise, i32, [vp, i64, i64, vp, i64, i64, i32, i32, i32, i32, i32, vp, sz, vp])
+    _sig(L.pcm_muon_step_workspace_bytes, sz, [i32, C.POINTER(i32), C.POINTER(i32)])
+    _sig(L.pcm_muon_step, i32,
+         [i32, C.POINTER(i32), C.POINTER(i32), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), f64, f64, i32,
+          f64, i32, i32, vp, sz, vp])
     _sig(L.pcm_profile_enable, i32, [i32])
     _sig(L.pcm_profile_stage_count, i32, [])
     _sig(L.pcm_profile_stage_name, C.c_char_p, [i32])
@@ -462,6 +473,182 @@ def pcm_adamw_clip_step(grads, weights, m, v, step: int, lr: float = 1e-5, beta1
     finally:
         _give_workspace(ws, dev, stream)
     return grad_norm_out
+
+
+TOKEN_TYPES = {torch.uint8: 0, torch.int32: 1, torch.int64: 2}
+DTYPES = {torch.float32: PCM_F32, torch.bfloat16: PCM_BF16}
+
+
+def _rows_ptr(t: torch.Tensor, name: str) -> Tuple[int, int]:
+    """Address and leading dimension of a matrix whose rows are contiguous."""
+    if not t.is_cuda:
+        raise PcmError(f"{name} must live in device memory")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise PcmError(f"{name} must have contiguous rows")
+    ld = t.stride(0) if rows > 1 else cols
+    if ld < cols:
+        raise PcmError(f"{name} must have rows that do not overlap")
+    return t.data_ptr(), ld
+
+
+def _allowed_ptr(allowed: Optional[torch.Tensor], rows: int, V: int) -> Tuple[Optional[int], int]:
+    """Address and leading dimension of a mask [V] (leading dimension 0) or [rows, V]."""
+    if allowed is None:
+        return None, 0
+    if allowed.dtype not in (torch.bool, torch.uint8):
+        raise PcmError(f"allowed must be bool or uint8, got {allowed.dtype}")
+    if allowed.dim() == 1 and allowed.shape[0] == V:
+        return _ptr(allowed, None, "allowed"), 0
+    if tuple(allowed.shape) != (rows, V):
+        raise PcmError("allowed must be [V] or [rows, V]")
+    if rows > 1 and allowed.stride(0) == 0:             # one row, expanded
+        return _rows_ptr(allowed[:1], "allowed")[0], 0
+    return _rows_ptr(allowed, "allowed")
+
+
+def _logits_args(logits, tokens, allowed, temperature: float):
+    """The arguments that both directions of the token log-probabilities begin with."""
+    if logits.dim() != 2 or logits.dtype not in DTYPES:
+        raise PcmError("logits must be [rows, V] of float32 or bfloat16")
+    rows, V = logits.shape
+    if tokens.dtype not in TOKEN_TYPES or tuple(tokens.shape) != (rows,):
+        raise PcmError("tokens must be [rows] of uint8, int32 or int64")
+    p_logits, ld = _rows_ptr(logits, "logits")
+    p_allowed, allowed_ld = _allowed_ptr(allowed, rows, V)
+    return (p_logits, ld, DTYPES[logits.dtype], _ptr(tokens, None, "tokens"), TOKEN_TYPES[tokens.dtype], p_allowed, allowed_ld,
+            rows, V, temperature)
+
+
+def pcm_token_logprobs(logits, tokens, allowed: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                       want_entropy: bool = True, top: int = 0,
+                       out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """-> dict(logp f32[rows], lse f32[rows], and as asked entropy f32[rows], top_ids i32[rows, top], top_logp f32[rows, top]).
+
+    logits [rows, V], float32 or bfloat16, with contiguous rows (a view of a wider matrix will do); tokens [rows] uint8, int32 or
+    int64, negative where a row has none; allowed bool or uint8 [V] or [rows, V].  `out` may carry preallocated tensors.
+    """
+    args = _logits_args(logits, tokens, allowed, temperature)
+    rows, V = logits.shape
+    dev = logits.device
+    if top < 0:
+        raise PcmError("top must not be negative")
+    out = {} if out is None else out
+
+    def buf(name, shape, dt):
+        t = out.get(name)
+        if t is None:
+            out[name] = t = torch.empty(shape, dtype=dt, device=dev)
+        elif tuple(t.shape) != shape:
+            raise PcmError(f"out[{name!r}] has shape {tuple(t.shape)}, expected {shape}")
+        return _ptr(t, dt, name)
+
+    p_logp, p_lse = buf("logp", (rows,), _F32), buf("lse", (rows,), _F32)
+    p_entropy = buf("entropy", (rows,), _F32) if want_entropy else None
+    p_ids, p_top = (buf("top_ids", (rows, top), _I32), buf("top_logp", (rows, top), _F32)) if top else (None, None)
+    need = lib().pcm_token_logprobs_workspace_bytes(rows, V, top)
+    stream = _stream()
+    tail = (top, p_logp, p_lse, p_entropy, p_ids, p_top)
+    if need == 0:
+        _check(lib().pcm_token_logprobs(*args, *tail, None, 0, stream), "pcm_token_logprobs")
+        return out
+    ws = _take_workspace(need, dev, stream)
+    try:
+        _check(lib().pcm_token_logprobs(*args, *tail, ws.data_ptr(), ws.numel(), stream), "pcm_token_logprobs")
+    finally:
+        _give_workspace(ws, dev, stream)
+    return out
+
+
+def pcm_token_logprobs_backward(logits, tokens, lse, dlogp, entropy: Optional[torch.Tensor] = None,
+                                dentropy: Optional[torch.Tensor] = None, allowed: Optional[torch.Tensor] = None,
+                                temperature: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """-> d logits [rows, V] of the logits' dtype, from dlogp f32[rows] and, if the loss has a part in the entropy, dentropy
+    f32[rows] with the entropy of the forward call; lse as the forward call returned it.  `out` may be the logits themselves."""
+    args = _logits_args(logits, tokens, allowed, temperature)
+    rows, V = logits.shape
+    for name, t in (("lse", lse), ("dlogp", dlogp), ("entropy", entropy), ("dentropy", dentropy)):
+        if t is not None and tuple(t.shape) != (rows,):
+            raise PcmError(f"{name} must be [rows]")
+    if dentropy is not None and entropy is None:
+        raise PcmError("a gradient in the entropy needs the entropy")
+    if out is None:
+        out = torch.empty((rows, V), dtype=logits.dtype, device=logits.device)
+    elif tuple(out.shape) != (rows, V) or out.dtype != logits.dtype:
+        raise PcmError("out must have the shape and type of the logits")
+    p_out, out_ld = _rows_ptr(out, "out")
+    p_dentropy = _ptr(dentropy, _F32, "dentropy")
+    p_entropy = _ptr(entropy, _F32, "entropy") if dentropy is not None else None
+    _check(lib().pcm_token_logprobs_backward(*args, _ptr(lse, _F32, "lse"), _ptr(dlogp, _F32, "dlogp"), p_entropy, p_dentropy,
+                                             p_out, out_ld, _stream()), "pcm_token_logprobs_backward")
+    return out
+
+
+def _matrices(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
+    """Address, leading dimension and distance of the matrices of a tensor [rows, cols] or [batch, rows, cols]."""
+    p, ld = _rows_ptr(t if t.dim() == 2 else t[0], name)
+    return p, ld, (t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else 0)
+
+
+def pcm_orthogonalise(update, ns_steps: int = 5, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """-> the orthogonalised update: [rows, cols] or [batch, rows, cols] of float32 or bfloat16, rows contiguous.  `out` may be
+    the update itself."""
+    if update.dim() not in (2, 3) or update.dtype not in DTYPES:
+        raise PcmError("update must be [rows, cols] or [batch, rows, cols] of float32 or bfloat16")
+    if out is None:
+        out = torch.empty(update.shape, dtype=update.dtype, device=update.device)
+    elif out.shape != update.shape or out.dtype != update.dtype:
+        raise PcmError("out must have the shape and type of the update")
+    batch = update.shape[0] if update.dim() == 3 else 1
+    if batch == 0:
+        return out
+    rows, cols = update.shape[-2:]
+    need = lib().pcm_orthogonalise_workspace_bytes(batch, rows, cols)
+    if need == 0:
+        raise PcmError("pcm_orthogonalise: unsupported shape")
+    stream = _stream()
+    args = (*_matrices(update, "update"), *_matrices(out, "out"), batch, rows, cols, DTYPES[update.dtype], ns_steps)
+    ws = _take_workspace(need, update.device, stream)
+    try:
+        _check(lib().pcm_orthogonalise(*args, ws.data_ptr(), ws.numel(), stream), "pcm_orthogonalise")
+    finally:
+        _give_workspace(ws, update.device, stream)
+    return out
+
+
+MUON_SCALES = {"shape": 0, "rms": 1}
+
+
+def pcm_muon_step(grads, weights, momentum, lr: float = 0.02, momentum_coef: float = 0.95, nesterov: bool = True,
+                  weight_decay: float = 0.0, ns_steps: int = 5, scale: str = "shape", weights_bf16=None) -> None:
+    """Momentum, orthogonalisation and weight update over lists of fp32 matrices (weights and momentum are updated in place).
+
+    `weights_bf16`, if given, is a list (entries may be None) of bf16 tensors that receive the new weights.  scale: the size of
+    an update, "shape" sqrt(max(1, cols / rows)) or "rms" 0.2 sqrt(max(rows, cols)).
+    """
+    n = len(grads)
+    if scale not in MUON_SCALES:
+        raise PcmError(f"unknown scale {scale!r}")
+    if n == 0 or not (len(weights) == len(momentum) == n) or (weights_bf16 is not None and len(weights_bf16) != n):
+        raise PcmError("pcm_muon_step: lists must have equal length")
+    for i, (g, w, m) in enumerate(zip(grads, weights, momentum)):
+        b = weights_bf16[i] if weights_bf16 is not None else None
+        if g.dim() != 2 or not (g.shape == w.shape == m.shape) or (b is not None and b.shape != w.shape):
+            raise PcmError("pcm_muon_step: gradient, weight and momentum must be matrices of equal shape")
+    rows, cols = (C.c_int * n)(*[g.shape[0] for g in grads]), (C.c_int * n)(*[g.shape[1] for g in grads])
+    arr = lambda ts, dt, name: (C.c_void_p * n)(*[_ptr(t, dt, name) for t in ts])
+    lowp = arr(weights_bf16, torch.bfloat16, "weights_bf16") if weights_bf16 is not None else None
+    need = lib().pcm_muon_step_workspace_bytes(n, rows, cols)
+    if need == 0:
+        raise PcmError("pcm_muon_step: bad tensor list")
+    dev, stream = grads[0].device, _stream()
+    args = (n, rows, cols, arr(grads, _F32, "grads"), arr(weights, _F32, "weights"), arr(momentum, _F32, "momentum"), lowp, lr,
+            momentum_coef, int(nesterov), weight_decay, ns_steps, MUON_SCALES[scale])
+    ws = _take_workspace(need, dev, stream)
+    try:
+        _check(lib().pcm_muon_step(*args, ws.data_ptr(), ws.numel(), stream), "pcm_muon_step")
+    finally:
+        _give_workspace(ws, dev, stream)
 
 
 def pcm_measure_mfma_rate(random_operands: bool = True, milliseconds: int = 100) -> Tuple[float, float]:

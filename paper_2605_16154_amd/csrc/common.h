@@ -61,6 +61,10 @@ enum Stage : int {
     ST_OPT_ADAMW,
     ST_LABEL_PHASES,
     ST_LIVE_ROWS,
+    ST_TOKEN_LOGPROBS,
+    ST_TOKEN_LOGPROBS_GRAD,
+    ST_ORTH_PREPARE,
+    ST_ORTH_PRODUCTS,
     ST_COUNT
 };
 
