@@ -5,11 +5,12 @@
 // both.  Of a symmetric result only the tiles on and below the diagonal are computed.
 #pragma once
 
+#include "gemm_bf16.h"
 #include "pairs.h"
 
 namespace pcm {
 
-// What becomes of a product: value = alpha * sum + beta * D + gamma * (m == n), then one of
+// What becomes of a product: value = alpha * sum, with D also + beta * D + gamma * (m == n), then one of
 enum PairResult : int {
     kPairs = 0,          // C and, if Ct is set, its transpose, as pairs
     kOutF32 = 1,         // out[m, n] = value
@@ -31,12 +32,12 @@ struct PairJob {
     int64_t ld;                  // of out (lowp: the same)
     int rows, cols;              // of out
     float decay, rate;
-    int first_tile, tiles_n;     // filled in by the launch
+    int first, tiles_m, tiles_n, tiles;      // first workgroup, tiles: filled in by the launch
 };
 constexpr int kMaxPairJobs = 16;
 struct PairJobs {
     PairJob job[kMaxPairJobs];
-    int n, tiles;
+    int n, blocks;
 };
 
 // Accumulators of a wavefront: tile (i, j), register t of a lane is row 16 i + (lane & 15), column 16 j + 4 (lane >> 4) + t.
@@ -46,9 +47,9 @@ using PairAccumulators = f32x4[kW][kW];
 __device__ inline f32x4 mfma_f16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 // The wavefront's part of a tile: rows 16 (frag_m + i), columns 16 (frag_n + j).  off_diagonal: of a symmetric result, a tile whose
-// transpose no other tile computes.
+// transpose no other tile computes.  In blocks of 32 x 32, which a matrix has whole or not at all.
 template <int kW>
-__device__ __forceinline__ void pair_epilogue(const PairJob& p, const PairAccumulators<kW>& acc, int frag_m, int frag_n, bool off_diagonal) {
+__device__ __forceinline__ void store_pairs(const PairJob& p, const PairAccumulators<kW>& acc, int frag_m, int frag_n, bool off_diagonal) {
     const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
     // Unit matrices that pick one half of a fragment's columns: a product with one is that half transposed, exactly.
     f16x8 unit[2];
@@ -58,155 +59,383 @@ __device__ __forceinline__ void pair_epilogue(const PairJob& p, const PairAccumu
         unit[1][e] = e >= 4 && 4 * g + e - 4 == r ? (f16)1.f : (f16)0.f;
     }
     const bool transposed = p.Ct != nullptr && (!p.symmetric || off_diagonal);
+    static_for<kW * kW / 4>([&](auto block) __attribute__((always_inline)) {
+        constexpr int i = decltype(block)::value / (kW / 2) * 2, j = decltype(block)::value % (kW / 2) * 2;
+        const int fm = frag_m + i, fn = frag_n + j;
+        if (fm >= p.m_frags || fn >= p.n_frags) return;
+        f16x8 hi[2], lo[2];
 #pragma unroll
-    for (int i = 0; i < kW; i += 2)
+        for (int ii = 0; ii < 2; ++ii) {
+            const int64_t at = pair_fragment(fm + ii, fn / 2, p.m_frags) + lane * 8;
+            float v[8];
 #pragma unroll
-        for (int j = 0; j < kW; j += 2) {
-            const int fm = frag_m + i, fn = frag_n + j;
-            if (fm >= p.m_frags || fn >= p.n_frags) continue;
-            if (p.result == kPairs) {
-                f16x8 hi[2], lo[2];
+            for (int e = 0; e < 8; ++e) v[e] = p.alpha * acc[i + ii][j + e / 4][e % 4];
+            if (p.D != nullptr) {
+                const f16x8 dh = *reinterpret_cast<const f16x8*>(p.D + at), dl = *reinterpret_cast<const f16x8*>(p.D + at + kPairPart);
 #pragma unroll
-                for (int ii = 0; ii < 2; ++ii) {
-                    const int64_t at = pair_fragment(fm + ii, fn / 2, p.m_frags) + lane * 8;
-                    f16x8 dh = {0, 0, 0, 0, 0, 0, 0, 0}, dl = dh;
-                    if (p.D != nullptr) {
-                        dh = *reinterpret_cast<const f16x8*>(p.D + at);
-                        dl = *reinterpret_cast<const f16x8*>(p.D + at + kPairPart);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        float v = p.alpha * acc[i + ii][j + e / 4][e % 4];
-                        if (p.D != nullptr) v += p.beta * ((float)dh[e] + (float)dl[e]);
-                        if ((fm + ii) * 16 + r == fn * 16 + e / 4 * 16 + 4 * g + e % 4) v += p.gamma;
-                        f16 h, l;
-                        split_pair(v, h, l);
-                        hi[ii][e] = h;
-                        lo[ii][e] = l;
-                    }
-                    *reinterpret_cast<f16x8*>(p.C + at) = hi[ii];
-                    *reinterpret_cast<f16x8*>(p.C + at + kPairPart) = lo[ii];
+                for (int e = 0; e < 8; ++e) {
+                    v[e] += p.beta * ((float)dh[e] + (float)dl[e]);
+                    if ((fm + ii) * 16 + r == fn * 16 + e / 4 * 16 + 4 * g + e % 4) v[e] += p.gamma;
                 }
-                if (transposed) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int64_t at = pair_fragment(fn + h, fm / 2, p.n_frags) + lane * 8;
-                        f16x8 th, tl;
-#pragma unroll
-                        for (int ii = 0; ii < 2; ++ii) {
-                            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-                            const f32x4 a = mfma_f16(hi[ii], unit[h], zero), b = mfma_f16(lo[ii], unit[h], zero);
-#pragma unroll
-                            for (int t = 0; t < 4; ++t) {
-                                th[4 * ii + t] = (f16)a[t];
-                                tl[4 * ii + t] = (f16)b[t];
-                            }
-                        }
-                        *reinterpret_cast<f16x8*>(p.Ct + at) = th;
-                        *reinterpret_cast<f16x8*>(p.Ct + at + kPairPart) = tl;
-                    }
-                }
-                continue;
             }
 #pragma unroll
-            for (int ii = 0; ii < 2; ++ii)
-#pragma unroll
-                for (int jj = 0; jj < 2; ++jj) {
-                    const int m = (fm + ii) * 16 + r, n = (fn + jj) * 16 + 4 * g;
-                    if (m >= p.rows) continue;
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        if (n + t >= p.cols) continue;
-                        const int64_t at = (int64_t)m * p.ld + n + t;
-                        const float v = p.alpha * acc[i + ii][j + jj][t];
-                        if (p.result == kOutF32) {
-                            static_cast<float*>(p.out)[at] = v;
-                        } else if (p.result == kOutBf16) {
-                            static_cast<__bf16*>(p.out)[at] = (__bf16)v;
-                        } else {
-                            float* w = static_cast<float*>(p.out) + at;
-                            const float now = p.decay * *w - p.rate * v;
-                            *w = now;
-                            if (p.lowp != nullptr) reinterpret_cast<__bf16*>(p.lowp)[at] = (__bf16)now;
-                        }
-                    }
-                }
+            for (int e = 0; e < 8; ++e) {
+                f16 h, l;
+                split_pair(v[e], h, l);
+                hi[ii][e] = h;
+                lo[ii][e] = l;
+            }
+            *reinterpret_cast<f16x8*>(p.C + at) = hi[ii];
+            *reinterpret_cast<f16x8*>(p.C + at + kPairPart) = lo[ii];
         }
+        if (!transposed) return;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t at = pair_fragment(fn + h, fm / 2, p.n_frags) + lane * 8;
+            f16x8 th, tl;
+#pragma unroll
+            for (int ii = 0; ii < 2; ++ii) {
+                const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+                const f32x4 a = mfma_f16(hi[ii], unit[h], zero), b = mfma_f16(lo[ii], unit[h], zero);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    th[4 * ii + t] = (f16)a[t];
+                    tl[4 * ii + t] = (f16)b[t];
+                }
+            }
+            *reinterpret_cast<f16x8*>(p.Ct + at) = th;
+            *reinterpret_cast<f16x8*>(p.Ct + at + kPairPart) = tl;
+        }
+    });
 }
-
-// Tiles on and below the diagonal, row by row: the tile of row tm and column tn is number tm (tm + 1) / 2 + tn.
-__device__ inline void triangle_tile(int number, int& tm, int& tn) {
-    int row = (int)((sqrtf(8.f * (float)number + 1.f) - 1.f) * 0.5f);
-    while ((row + 1) * (row + 2) / 2 <= number) ++row;
-    while (row * (row + 1) / 2 > number) --row;
-    tm = row;
-    tn = number - row * (row + 1) / 2;
+template <int kW>
+__device__ __forceinline__ void store_result(const PairJob& p, const PairAccumulators<kW>& acc, int frag_m, int frag_n) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+    static_for<kW * kW>([&](auto tile) __attribute__((always_inline)) {
+        constexpr int i = decltype(tile)::value / kW, j = decltype(tile)::value % kW;
+        const int m = (frag_m + i) * 16 + r, n = (frag_n + j) * 16 + 4 * g;
+        if (m >= p.rows || n >= p.cols) return;
+        const int64_t at = (int64_t)m * p.ld + n;
+        float v[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) v[t] = p.alpha * acc[i][j][t];
+        if (p.result == kOutBf16) {
+            __bf16* const out = static_cast<__bf16*>(p.out) + at;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (n + t < p.cols) out[t] = (__bf16)v[t];
+            return;
+        }
+        float* const out = static_cast<float*>(p.out) + at;
+        const bool whole = n + 4 <= p.cols;
+        if (p.result == kOutWeights) {
+            f32x4 w = {0.f, 0.f, 0.f, 0.f};
+            if (whole) w = *reinterpret_cast<const f32x4_any*>(out);
+            else
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    if (n + t < p.cols) w[t] = out[t];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) v[t] = p.decay * w[t] - p.rate * v[t];
+            if (p.lowp != nullptr) {
+                __bf16* const low = reinterpret_cast<__bf16*>(p.lowp) + at;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    if (n + t < p.cols) low[t] = (__bf16)v[t];
+            }
+        }
+        if (whole) *reinterpret_cast<f32x4_any*>(out) = f32x4_any{v[0], v[1], v[2], v[3]};
+        else
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (n + t < p.cols) out[t] = v[t];
+    });
+}
+// kFinal: the jobs of the launch leave results, not pairs.
+template <int kW, bool kFinal>
+__device__ __forceinline__ void pair_epilogue(const PairJob& p, const PairAccumulators<kW>& acc, int frag_m, int frag_n, bool off_diagonal) {
+    if constexpr (kFinal) store_result<kW>(p, acc, frag_m, frag_n);
+    else store_pairs<kW>(p, acc, frag_m, frag_n, off_diagonal);
 }
 
 constexpr int kPairThreads = 256;
 
-// Tiles of 32 kW x 32 kW by four wavefronts (2 x 2), operands from memory straight into registers.
-template <int kW>
-__global__ __launch_bounds__(kPairThreads) void pair_product(PairJobs jobs) {
-    const int block = blockIdx.x;
-    int q = 0;
-    while (q + 1 < jobs.n && block >= jobs.job[q + 1].first_tile) ++q;
-    const PairJob& p = jobs.job[q];
-    const int number = block - p.first_tile;
-    int tm, tn;
-    if (p.symmetric) triangle_tile(number, tm, tn);
-    else { tm = number / p.tiles_n; tn = number % p.tiles_n; }
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int frag_m = (tm * 2 + (wave >> 1)) * kW, frag_n = (tn * 2 + (wave & 1)) * kW;
-
-    // fragments beyond the last one are read from it: what they give is not stored
-    const f16 *a[kW], *b[kW];
-#pragma unroll
-    for (int i = 0; i < kW; ++i) {
-        a[i] = p.A + pair_fragment(min(frag_m + i, p.m_frags - 1), 0, p.m_frags) + lane * 8;
-        b[i] = p.B + pair_fragment(min(frag_n + i, p.n_frags - 1), 0, p.n_frags) + lane * 8;
+// Tile number `l` of a launch's job.  Consecutive numbers are columns of bands of four rows of tiles, so that 32 of them are a
+// block of 4 x 8; of a symmetric result the tiles on and below the diagonal: band b has its 16 b tiles left of column 4 b, then the
+// triangle that is left.
+__device__ __forceinline__ void pair_tile_at(const PairJob& p, int tiles_m, int l, int& tm, int& tn) {
+    if (!p.symmetric) {
+        const int first = l / (4 * p.tiles_n) * 4, rows = min(4, tiles_m - first), at = l - first * p.tiles_n;
+        tm = first + at % rows;
+        tn = at / rows;
+        return;
     }
-    const int64_t a_step = pair_fragment(0, 1, p.m_frags), b_step = pair_fragment(0, 1, p.n_frags);
+    int b = (int)((sqrtf(4.f + 32.f * (float)l) - 2.f) * (1.f / 16.f));      // 8 b^2 + 2 b tiles before band b
+    while (8 * (b + 1) * (b + 1) + 2 * (b + 1) <= l) ++b;
+    while (8 * b * b + 2 * b > l) --b;
+    const int rows = min(4, tiles_m - 4 * b);
+    int at = l - (8 * b * b + 2 * b);
+    if (at < 4 * b * rows) {
+        tm = 4 * b + at % rows;
+        tn = at / rows;
+        return;
+    }
+    at -= 4 * b * rows;
+    const int row = at < 1 ? 0 : (at < 3 ? 1 : (at < 6 ? 2 : 3));
+    tm = 4 * b + row;
+    tn = 4 * b + at - row * (row + 1) / 2;
+}
+// Workgroup -> tile number, or -1: consecutive workgroups go to different XCDs, which take blocks of kBlock neighbouring tiles
+// in turn and share the rest evenly (see tile_of_workgroup).
+template <int kBlock>
+__device__ __forceinline__ int dealt_tile(int wg, int tiles) {
+    const int xcd = wg % kNumXcd, idx = wg / kNumXcd, full = tiles / (kBlock * kNumXcd);
+    if (idx < full * kBlock) return ((idx / kBlock) * kNumXcd + xcd) * kBlock + idx % kBlock;
+    const int rest = tiles - full * kBlock * kNumXcd, at = idx - full * kBlock;
+    if (at >= rest / kNumXcd + (xcd < rest % kNumXcd ? 1 : 0)) return -1;
+    return full * kBlock * kNumXcd + xcd * (rest / kNumXcd) + min(xcd, rest % kNumXcd) + at;
+}
+__device__ __forceinline__ PairJob job_of(const PairJobs& jobs, int block) {
+    int q = 0;
+    while (q + 1 < jobs.n && block >= jobs.job[q + 1].first) ++q;
+    return jobs.job[__builtin_amdgcn_readfirstlane(q)];
+}
+
+// Tiles of 32 kW x 32 kW by four wavefronts (2 x 2).
+//
+// A step is 32 of k: its four parts (hi and lo of both operands, 2 kW fragments each) are loaded once and take part in three
+// products, in the order A_hi B_lo, A_hi B_hi, A_lo B_hi ("phases" of kW x kW MFMAs), so that between two phases one operand stays:
+// the fragments of the four parts have a set of registers each, which is filled again in the phase after its last use.
+// Parts are numbered 4 s + {0: B_lo, 1: A_hi, 2: B_hi, 3: A_lo} in the order of their use and live in a ring of kSlots places in LDS, filled
+// by direct loads.  The one barrier of a step is behind its first phase: B_lo, A_hi and B_hi of the step have been read by then, so the
+// parts up to 4 s + 2 make room, and those that will be read up to the next barrier, up to 4 s + 6, must have landed.  From one barrier to
+// the next four parts are requested, 4 s + kSlots - 1 and the three after it.
+// The places of a step's parts repeat after kPairPeriod steps, which the loop is unrolled by: a scalar instruction costs a quarter of an
+// MFMA, and more than three of them between two MFMAs hold up the matrix pipe.  (4096 x 11008 over 4096: 766 -> 727 us, on tiles of 192
+// 822 -> 783.)  One workgroup per CU for kW = 8 and 6, two for 4 and 2.
+template <int kW> constexpr int kPairSlots = kW == 6 ? 12 : kW == 2 ? 16 : 10;
+template <int kW> constexpr int kPairPeriod = kW == 6 ? 3 : kW == 2 ? 4 : 5;
+template <int kW> constexpr uint32_t kPairPartBytes = 2u * kW * kPairPart * 2u;
+// Steps beyond the last one that a tile requests (and nobody reads): so far behind a matrix there has to be memory.
+constexpr int kPairStepsBeyond = 4;
+template <int kW>
+struct PairRing {
+    __attribute__((aligned(1024))) f16 data[kPairSlots<kW> * kPairPartBytes<kW> / 2];
+};
+
+__device__ __forceinline__ void mfma_pairs(f32x4& acc, f16x8 b, f16x8 a) {
+    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(b), "v"(a));
+}
+// (see mfma_16x16x32_and_load)
+template <uint32_t kLdsOffset>
+__device__ __forceinline__ void mfma_pairs_and_load(f32x4& acc, f16x8 b, f16x8 a, const char* base, uint32_t lane_offset, uint32_t lds_addr) {
+    asm volatile("s_add_u32 m0, %1, %2\n\t"
+                 "v_mfma_f32_16x16x32_f16 %0, %3, %4, %0\n\t"
+                 "global_load_lds_dwordx4 %5, %6"
+                 : "+a"(acc)
+                 : "s"(lds_addr), "n"(kLdsOffset), "v"(b), "v"(a), "v"(lane_offset), "s"(base)
+                 : "memory", "scc");
+}
+
+template <int kW, bool kFinal>
+__global__ __launch_bounds__(kPairThreads, kW >= 6 ? 1 : 2) void pair_product(PairJobs jobs) {
+    constexpr int kSlots = kPairSlots<kW>, kLoads = kW / 2;            // loads of a part per wavefront
+    constexpr uint32_t kPart = kPairPartBytes<kW>, kRing = kSlots * kPart;
+    __shared__ PairRing<kW> smem;
+    const PairJob p = job_of(jobs, blockIdx.x);
+    const int number = dealt_tile<(kW >= 6 ? 32 : 64)>(blockIdx.x - p.first, p.tiles);
+    if (number < 0) return;
+    int tm, tn;
+    pair_tile_at(p, p.tiles_m, number, tm, tn);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    const int first_m = tm * 2 * kW, first_n = tn * 2 * kW;           // fragments
+
+    // Global -> LDS: load r of a part brings in fragment kLoads * wave + r, lane l its 16 bytes l.  Fragments beyond the last one are
+    // read from it: what they give is not stored.
+    const uint32_t lds_base = (uint32_t)(uintptr_t)PCM_AS_LDS(smem.data);
+    uint32_t off[2][kLoads];
+#pragma unroll
+    for (int r = 0; r < kLoads; ++r) {
+        const int f = kLoads * wave + r;
+        off[0][r] = (uint32_t)(min(first_m + f, p.m_frags - 1) - first_m) * (kPairFragment * 2u) + (uint32_t)lane * 16u;
+        off[1][r] = (uint32_t)(min(first_n + f, p.n_frags - 1) - first_n) * (kPairFragment * 2u) + (uint32_t)lane * 16u;
+    }
+    const char* const origin_a = tile_address<true>(p.A + pair_fragment(first_m, 0, p.m_frags));
+    const char* const origin_b = tile_address<true>(p.B + pair_fragment(first_n, 0, p.n_frags));
+    // (assembly takes them in scalar registers, and the compiler may lose sight of their being the same in every lane)
+    const int64_t step_bytes[2] = {pair_fragment(0, 1, __builtin_amdgcn_readfirstlane(p.m_frags)) * 2,
+                                   pair_fragment(0, 1, __builtin_amdgcn_readfirstlane(p.n_frags)) * 2};
+    // by type of part: where the next one to be requested is
+    const char* from[4] = {origin_b + kPairPart * 2, origin_a, origin_b, origin_a + kPairPart * 2};
+    const int steps = __builtin_amdgcn_readfirstlane(p.steps);
+    constexpr auto operand = [](int type) { return type == 0 || type == 2 ? 1 : 0; };
+    const uint32_t my_lds = lds_base + (uint32_t)(kLoads * wave) * 1024u;
+
     PairAccumulators<kW> acc;
 #pragma unroll
     for (int i = 0; i < kW; ++i)
 #pragma unroll
         for (int j = 0; j < kW; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < p.steps; ++s) {
-        f16x8 ah[kW], al[kW], bh[kW], bl[kW];
+
+    f16x8 set[4][kW];                                    // fragments, by type of part
+    const uint32_t read_base[2] = {lds_base + (uint32_t)(wm * kW) * 1024u + (uint32_t)lane * 16u,
+                                   lds_base + (uint32_t)(wn * kW) * 1024u + (uint32_t)lane * 16u};
+    // fragment i of this wavefront in the part that lies at place `slot`: an address per 48 KB of LDS, the rest is the instruction's offset
+    constexpr uint32_t kReach = 48 * 1024;
+    constexpr int kBases = (kRing + kReach - 1) / kReach;
+    uint32_t at[2][kBases];
 #pragma unroll
-        for (int i = 0; i < kW; ++i) {
-            ah[i] = *reinterpret_cast<const f16x8*>(a[i]);
-            al[i] = *reinterpret_cast<const f16x8*>(a[i] + kPairPart);
-            bh[i] = *reinterpret_cast<const f16x8*>(b[i]);
-            bl[i] = *reinterpret_cast<const f16x8*>(b[i] + kPairPart);
-            a[i] += a_step;
-            b[i] += b_step;
+    for (int o = 0; o < 2; ++o)
+#pragma unroll
+        for (int q = 0; q < kBases; ++q) {
+            at[o][q] = read_base[o] + q * kReach;
+            asm volatile("" : "+v"(at[o][q]));
         }
+    auto read = [&](int o, int slot, int i) __attribute__((always_inline)) -> f16x8 {
+        const uint32_t offset = (uint32_t)slot * kPart + (uint32_t)i * 1024u;
+        return *(const __attribute__((address_space(3))) f16x8*)(uintptr_t)(at[o][offset / kReach] + offset % kReach);
+    };
+
+    // Prologue: parts 0 .. kSlots - 3; the first phase requests the next one.
 #pragma unroll
-        for (int i = 0; i < kW; ++i)
+    for (int n = 0; n < kSlots - 2; ++n) {
 #pragma unroll
-            for (int j = 0; j < kW; ++j) {
-                acc[i][j] = mfma_f16(bl[j], ah[i], acc[i][j]);
-                acc[i][j] = mfma_f16(bh[j], al[i], acc[i][j]);
-                acc[i][j] = mfma_f16(bh[j], ah[i], acc[i][j]);
-            }
+        for (int r = 0; r < kLoads; ++r) direct_load_16B(from[n & 3], off[operand(n & 3)][r], my_lds + (uint32_t)n * kPart + (uint32_t)r * 1024u);
+        from[n & 3] += step_bytes[operand(n & 3)];
     }
-    pair_epilogue<kW>(p, acc, frag_m, frag_n, tm != tn);
+    wait_direct_loads<(kSlots - 5) * kLoads>();
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kW; ++i) {
+        set[0][i] = read(1, 0, i);
+        set[1][i] = read(0, 1, i);
+    }
+
+    // A phase: kW x kW MFMAs, row by row.  first_part: the number, modulo the ring, of the first part requested meanwhile, of kParts (one or
+    // two); its loads are spread over the phase, one to an MFMA, and the pointer moves on one MFMA later.  reads(n): fragment read n of
+    // kReads, one behind an MFMA, early enough for all to have landed when the phase ends.
+    auto phase = [&](auto a_type, auto b_type, auto first_type, auto first_slot, auto n_parts, auto n_reads, auto reads) __attribute__((always_inline)) {
+        constexpr int kA = decltype(a_type)::value, kB = decltype(b_type)::value;
+        constexpr int kType = decltype(first_type)::value, kSlot = decltype(first_slot)::value;
+        constexpr int kMfmas = kW * kW, kTotal = decltype(n_parts)::value * kLoads, kReads = decltype(n_reads)::value;
+        constexpr int kEvery = kReads * 2 <= kMfmas - kW ? 2 : 1;
+        static_for<kMfmas>([&](auto number) __attribute__((always_inline)) {
+            constexpr int n = decltype(number)::value, i = n / kW, j = (i & 1) ? kW - 1 - n % kW : n % kW;
+            // load l is issued at MFMA l * kMfmas / kTotal
+            constexpr int l = (n * kTotal + kMfmas - 1) / kMfmas, type = (kType + l / kLoads) & 3;
+            if constexpr (l < kTotal && l * kMfmas / kTotal == n) {
+                constexpr uint32_t to = (uint32_t)((kSlot + l / kLoads) % kSlots) * kPart + (l % kLoads) * 1024u;
+                mfma_pairs_and_load<to>(acc[i][j], set[kB][j], set[kA][i], from[type], off[operand(type)][l % kLoads], my_lds);
+            } else {
+                mfma_pairs(acc[i][j], set[kB][j], set[kA][i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (l < kTotal && l * kMfmas / kTotal == n && l % kLoads == kLoads - 1) from[type] += step_bytes[operand(type)];
+            if constexpr (n % kEvery == 0 && n / kEvery < kReads) reads(Index<n / kEvery>{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    auto step = [&](auto which) __attribute__((always_inline)) {
+        constexpr int k0 = 4 * decltype(which)::value;                 // number of the step's first part, modulo the ring
+        phase(Index<1>{}, Index<0>{}, Index<(kSlots - 2) & 3>{}, Index<(k0 + kSlots - 2) % kSlots>{}, Index<1>{}, Index<kW>{},
+              [&](auto n) { set[2][decltype(n)::value] = read(1, (k0 + 2) % kSlots, decltype(n)::value); });
+        wait_direct_loads<(kSlots - 8) * kLoads>();
+        __syncthreads();
+        phase(Index<1>{}, Index<2>{}, Index<(kSlots - 1) & 3>{}, Index<(k0 + kSlots - 1) % kSlots>{}, Index<2>{}, Index<2 * kW>{}, [&](auto n) {
+            constexpr int f = decltype(n)::value;
+            if constexpr (f < kW) set[3][f] = read(0, (k0 + 3) % kSlots, f);
+            else set[0][f - kW] = read(1, (k0 + 4) % kSlots, f - kW);
+        });
+        phase(Index<3>{}, Index<2>{}, Index<(kSlots + 1) & 3>{}, Index<(k0 + kSlots + 1) % kSlots>{}, Index<1>{}, Index<kW>{},
+              [&](auto n) { set[1][decltype(n)::value] = read(0, (k0 + 5) % kSlots, decltype(n)::value); });
+    };
+    for (int left = steps;;) {
+        bool done = false;
+        static_for<kPairPeriod<kW>>([&](auto which) __attribute__((always_inline)) {
+            if (done) return;
+            step(which);
+            done = --left == 0;
+        });
+        if (done) break;
+    }
+    wait_direct_loads<0>();
+    // the compiler does not know how long an MFMA in inline assembly takes to write its results
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < kW; ++i)
+#pragma unroll
+        for (int j = 0; j < kW; ++j) asm volatile("" : "+a"(acc[i][j]));
+    pair_epilogue<kW, kFinal>(p, acc, first_m + wm * kW, first_n + wn * kW, tm != tn);
 }
 
+// The fewest microseconds a launch of the jobs is expected to take on tiles of 32 kW: what begins and ends it, its results at 4 TB/s, and per
+// round of workgroups its steps.  A step of a workgroup takes `alone` where few run (the matrix pipe; kW = 2: loads and barriers) and each of
+// the chip's `share` where many do: at full load the power cap sets the clock, at 1.4 PFLOP/s of fp16 products (kW = 2: the path from L2 into
+// LDS, 70 GB/s per CU).  Measured against this, in us, tiles of 64 / 128 / 192 / 256: symmetric 256 over 1024 7.5 / 15.9 / 30.3 / 50.5
+// (estimated 7.6 / 16.1 / 29.8 / 53), 1024 over 1024 8.5 / 17.2 / 33 / 54 (8.7 / 17 / 31 / 54), 2048 over 2048 38 / 36 / 62 / 98 (43 / 32 /
+// 58 / 102), 4096 over 4096 244 / 199 / 155 / 211 (266 / 215 / 188 / 206); 1024 x 2816 over 1024 23.2 / 22.4 / 37 / 57 (29 / 23 / 36 / 59),
+// 4096 x 11008 over 4096 1131 / 803 / 781 / 761 (1315 / 888 / 925 / 894).
+struct PairTiming {
+    double fixed, alone, share;
+    int slots;
+};
 template <int kW>
-inline void launch_pair_tiles(PairJobs& jobs, hipStream_t s) {
-    jobs.tiles = 0;
+constexpr PairTiming kPairTiming = kW == 8   ? PairTiming{8.0, 1.40, 9.0e-3, 256}
+                                   : kW == 6 ? PairTiming{6.0, 0.74, 5.06e-3, 256}
+                                   : kW == 4 ? PairTiming{4.4, 0.36, 2.25e-3, 512}
+                                             : PairTiming{3.5, 0.121, 0.86e-3, 512};
+template <int kW>
+inline void place_pair_jobs(PairJobs& jobs) {
+    jobs.blocks = 0;
     for (int i = 0; i < jobs.n; ++i) {
         PairJob& p = jobs.job[i];
-        const int tm = ceil_div(p.m_frags, 2 * kW), tn = ceil_div(p.n_frags, 2 * kW);
-        p.first_tile = jobs.tiles;
-        p.tiles_n = tn;
-        jobs.tiles += p.symmetric ? tm * (tm + 1) / 2 : tm * tn;
+        p.tiles_m = ceil_div(p.m_frags, 2 * kW);
+        p.tiles_n = ceil_div(p.n_frags, 2 * kW);
+        p.tiles = p.symmetric ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
+        p.first = jobs.blocks;
+        jobs.blocks += ceil_div(p.tiles, kNumXcd) * kNumXcd;
     }
-    pair_product<kW><<<(unsigned)jobs.tiles, kPairThreads, 0, s>>>(jobs);
 }
-inline void launch_pair_products(PairJobs& jobs, hipStream_t s) { launch_pair_tiles<2>(jobs, s); }
+template <int kW>
+inline double pair_time(PairJobs& jobs) {
+    constexpr PairTiming t = kPairTiming<kW>;
+    place_pair_jobs<kW>(jobs);
+    double tiles = 0.0, tile_steps = 0.0, bytes = 0.0, longest = 0.0;
+    for (int i = 0; i < jobs.n; ++i) {
+        const PairJob& p = jobs.job[i];
+        tiles += p.tiles;
+        tile_steps += (double)p.tiles * p.steps;
+        bytes += (double)p.m_frags * p.n_frags * 1024.0 * (p.Ct != nullptr && !p.symmetric ? 2 : 1);
+        longest = longest > p.steps ? longest : p.steps;
+    }
+    const double full = floor(tiles / t.slots), rest = tiles - full * t.slots;
+    auto round = [&](double n) { return n > 0.0 ? (t.alone > n * t.share ? t.alone : n * t.share) : 0.0; };
+    const double steps = (full * round(t.slots) + round(rest)) * (tile_steps / tiles), least = longest * t.alone;
+    return t.fixed + bytes / 4.0e6 + (steps > least ? steps : least);
+}
+inline double pair_time(PairJobs& jobs, int* tile = nullptr) {
+    const double at[4] = {pair_time<2>(jobs), pair_time<4>(jobs), pair_time<6>(jobs), pair_time<8>(jobs)};
+    int best = 0;
+    for (int i = 1; i < 4; ++i)
+        if (at[i] < at[best]) best = i;
+    if (tile != nullptr) *tile = 2 * best + 2;
+    return at[best];
+}
+template <int kW>
+inline void launch_pair_tiles(PairJobs& jobs, hipStream_t s) {
+    place_pair_jobs<kW>(jobs);
+    if (jobs.job[0].result != kPairs) pair_product<kW, true><<<(unsigned)jobs.blocks, kPairThreads, 0, s>>>(jobs);
+    else pair_product<kW, false><<<(unsigned)jobs.blocks, kPairThreads, 0, s>>>(jobs);
+}
+inline void launch_pair_products(PairJobs& jobs, hipStream_t s) {
+    int tile;
+    pair_time(jobs, &tile);
+    if (tile == 8) launch_pair_tiles<8>(jobs, s);
+    else if (tile == 6) launch_pair_tiles<6>(jobs, s);
+    else if (tile == 4) launch_pair_tiles<4>(jobs, s);
+    else launch_pair_tiles<2>(jobs, s);
+}
 
 }  // namespace pcm

@@ -7,6 +7,8 @@
 // Launches: the squares of the matrix (in 64 bits, and the momentum where there is one), the matrix divided by its norm
 // in both orientations as pairs (pairs.h), then three products per step; the last one writes the result or the weights.
 // Matrices of a call share the launches as long as they are small.
+#include <utility>
+
 #include "gemm_pairs.h"
 
 namespace pcm {
@@ -16,10 +18,8 @@ constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr int kMaxNsSteps = 10;
 constexpr int kMaxSide = 1 << 20, kMaxShortSide = 1 << 15;
 constexpr int kGroup = 8;                          // matrices of a launch
-// Powers of two of the pairs: entries are at most 1.3 in X and A (singular values), 3.5 in P.
-constexpr float kScaleX = 16384.f, kScaleA = 16384.f, kScaleP = 4096.f;
-
-typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;
+// Powers of two of the pairs: entries are at most 1.5 in X, A and B = A P (their largest singular value is), 3.5 in P and 3.5^3 in Q.
+constexpr float kScaleX = 16384.f, kScaleA = 16384.f, kScaleP = 4096.f, kScaleB = 8192.f, kScaleQ = 1024.f;
 
 struct Matrix {
     const void* in;              // [rows, cols] of `bf16` or fp32
@@ -187,7 +187,7 @@ struct Task {
 
 struct TaskBuffers {
     double* partial;
-    f16 *X, *Xt, *Xt2, *A, *P;
+    f16 *X, *Xt, *Xt2, *A, *B, *P, *Q, *Q2;
 };
 
 int short_side(int rows, int cols) { return rows < cols ? rows : cols; }
@@ -202,7 +202,11 @@ TaskBuffers carve_task(Carver& c, int rows, int cols) {
     b.Xt = c.take<f16>(pair_values(m, n));
     b.Xt2 = c.take<f16>(pair_values(m, n));
     b.A = c.take<f16>(pair_values(m, m));
+    b.B = c.take<f16>(pair_values(m, m));
     b.P = c.take<f16>(pair_values(m, m));
+    b.Q = c.take<f16>(pair_values(m, m));
+    b.Q2 = c.take<f16>(pair_values(m, m));
+    c.take<f16>(pair_values(n, 32 * kPairStepsBeyond));       // read, never used
     return b;
 }
 size_t task_bytes(int rows, int cols) {
@@ -234,6 +238,82 @@ PairJob symmetric_product(const f16* A, const f16* B, int m, int k, f16* C, floa
     return p;
 }
 
+// The products of ns_steps steps, in segments of at most `segment`: `launch` gets the jobs of one launch after the other.  A segment of one
+// is the step as it is written, X <- P X.  In a longer one X stands still: every P is a polynomial of A = X X^T, so Q = P_k .. P_1 is gathered
+// from m x m products and A goes on as A <- P A P, and at its end X <- Q X; all of them are symmetric.  In place of the two products over
+// the long side that a step costs this has three m x m ones (A P, (A P) P, P Q).
+template <class Launch>
+void iterate(const Task* tasks, TaskBuffers* buf, int n, int ns_steps, int segment, Launch launch) {
+    PairJobs jobs{};
+    auto each = [&](auto f) {
+        for (int i = 0; i < n; ++i) f(tasks[i], buf[i], short_side(tasks[i].in.rows, tasks[i].in.cols), long_side(tasks[i].in.rows, tasks[i].in.cols));
+    };
+    auto add = [&](const PairJob& p) { jobs.job[jobs.n++] = p; };
+    auto go = [&] {
+        launch(jobs);
+        jobs.n = 0;
+    };
+    for (int done = 0; done < ns_steps;) {
+        const int length = ns_steps - done < segment ? ns_steps - done : segment;
+        done += length;
+        each([&](const Task&, TaskBuffers& b, int m, int len) { add(symmetric_product(b.X, b.X, m, len, b.A, kScaleA / (kScaleX * kScaleX))); });
+        go();
+        for (int k = 0; k < length; ++k) {
+            // P = a I + b A + c A^2; the first is what the segment has gathered so far
+            each([&](const Task&, TaskBuffers& b, int m, int) {
+                PairJob p = symmetric_product(b.A, b.A, m, m, k == 0 ? b.Q : b.P, kNsC * kScaleP / (kScaleA * kScaleA));
+                p.D = b.A;
+                p.beta = kNsB * kScaleP / kScaleA;
+                p.gamma = kNsA * kScaleP;
+                add(p);
+            });
+            go();
+            const bool more = k + 1 < length;
+            each([&](const Task&, TaskBuffers& b, int m, int) {
+                if (more) add(symmetric_product(b.A, k == 0 ? b.Q : b.P, m, m, b.B, kScaleB / (kScaleA * kScaleP)));
+                if (k == 0) return;
+                add(symmetric_product(b.P, b.Q, m, m, b.Q2, kScaleQ / (kScaleP * (k == 1 ? kScaleP : kScaleQ))));
+                std::swap(b.Q, b.Q2);
+            });
+            if (jobs.n > 0) go();
+            if (!more) break;
+            each([&](const Task&, TaskBuffers& b, int m, int) { add(symmetric_product(b.B, k == 0 ? b.Q : b.P, m, m, b.A, kScaleA / (kScaleB * kScaleP))); });
+            go();
+        }
+        const float scale_q = length == 1 ? kScaleP : kScaleQ;
+        each([&](const Task& k, TaskBuffers& b, int m, int len) {
+            if (done < ns_steps) {
+                PairJob p = product(b.Q, b.Xt, m, len, m);
+                p.C = b.X;
+                p.Ct = b.Xt2;
+                p.alpha = 1.f / scale_q;
+                std::swap(b.Xt, b.Xt2);
+                add(p);
+                return;
+            }
+            // in the orientation of the result
+            PairJob p = k.in.tall ? product(b.Xt, b.Q, len, m, m) : product(b.Q, b.Xt, m, len, m);
+            p.result = k.result;
+            p.alpha = 1.f / (scale_q * kScaleX);
+            p.out = k.out;
+            p.lowp = k.lowp;
+            p.ld = k.out_ld;
+            p.rows = k.in.rows;
+            p.cols = k.in.cols;
+            p.decay = k.decay;
+            p.rate = k.rate;
+            add(p);
+        });
+        go();
+    }
+}
+// Longer segments save time where the long side is long or the matrix large; what is off in A in the directions that the matrix hardly has
+// grows by 3.4445^2 a step within a segment, where in X it grows by 3.4445: over three steps to 140 times 2^-22, over all five it spoils the
+// result.  In 64-bit arithmetic with rounded operands segments of three are as exact as fp32 products (0.4 to 2 times their error), and
+// a step at a time is better (0.2 to 0.6 times): so that is taken where it costs no more than a twentieth.
+constexpr int kSegment = 3;
+constexpr double kSegmentGain = 0.95;
+
 int run_group(Task* tasks, int n, int ns_steps, void* workspace, hipStream_t s) {
     Matrices list{};
     TaskBuffers buf[kGroup];
@@ -262,44 +342,15 @@ int run_group(Task* tasks, int n, int ns_steps, void* workspace, hipStream_t s) 
         update_to_pairs<<<(unsigned)tiles, kCopyThreads, 0, s>>>(list);
     }
     StageTimer t(ST_ORTH_PRODUCTS, s);
-    for (int step = 0; step < ns_steps; ++step) {
-        PairJobs gram{}, square{}, apply{};
-        gram.n = square.n = apply.n = n;
-        for (int i = 0; i < n; ++i) {
-            const Task& k = tasks[i];
-            const int m = short_side(k.in.rows, k.in.cols), len = long_side(k.in.rows, k.in.cols);
-            TaskBuffers& b = buf[i];
-            gram.job[i] = symmetric_product(b.X, b.X, m, len, b.A, kScaleA / (kScaleX * kScaleX));
-            PairJob& sq = square.job[i] = symmetric_product(b.A, b.A, m, m, b.P, kNsC * kScaleP / (kScaleA * kScaleA));
-            sq.D = b.A;
-            sq.beta = kNsB * kScaleP / kScaleA;
-            sq.gamma = kNsA * kScaleP;
-            PairJob& ap = apply.job[i];
-            if (step + 1 < ns_steps) {
-                ap = product(b.P, b.Xt, m, len, m);
-                ap.C = b.X;
-                ap.Ct = b.Xt2;
-                ap.alpha = 1.f / kScaleP;
-                f16* const old = b.Xt;
-                b.Xt = b.Xt2;
-                b.Xt2 = old;
-            } else {                 // in the orientation of the result
-                ap = k.in.tall ? product(b.Xt, b.P, len, m, m) : product(b.P, b.Xt, m, len, m);
-                ap.result = k.result;
-                ap.alpha = 1.f / (kScaleP * kScaleX);
-                ap.out = k.out;
-                ap.lowp = k.lowp;
-                ap.ld = k.out_ld;
-                ap.rows = k.in.rows;
-                ap.cols = k.in.cols;
-                ap.decay = k.decay;
-                ap.rate = k.rate;
-            }
-        }
-        launch_pair_products(gram, s);
-        launch_pair_products(square, s);
-        launch_pair_products(apply, s);
-    }
+    auto estimate = [&](int segment) {
+        TaskBuffers b[kGroup];
+        for (int i = 0; i < n; ++i) b[i] = buf[i];
+        double us = 0.0;
+        iterate(tasks, b, n, ns_steps, segment, [&](PairJobs& jobs) { us += pair_time(jobs); });
+        return us;
+    };
+    const int segment = estimate(kSegment) < kSegmentGain * estimate(1) ? kSegment : 1;
+    iterate(tasks, buf, n, ns_steps, segment, [&](PairJobs& jobs) { launch_pair_products(jobs, s); });
     return launch_status();
 }
 

@@ -24,6 +24,7 @@ namespace pcm {
 typedef _Float16 f16;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;     // global memory takes them at every multiple of four bytes
 
 constexpr int kPairRows = 16, kPairCols = 32;      // of a fragment
 constexpr int kPairPart = kPairRows * kPairCols;   // values of its hi, and of its lo
