@@ -472,6 +472,7 @@ PCM_API int pcm_adamw_clip_step_ex(int n_tensors, const int64_t* numel, const fl
  * in every row).  Where fewer than `top` tokens are allowed the rest is id -1 and logp -inf.  A NaN or +inf among the allowed logits
  * makes the row's lse, logp, entropy and top_logp NaN; a NaN is not among the alternatives.  Rows do not depend on one another.
  * logits may be any rows of a larger matrix; they are only read.  rows = 0 is a valid call that does nothing.
+ * Limits: rows < 2^31, 1 <= V <= 2^30.
  *
  * pcm_token_logprobs_backward -- the gradient of a loss in the logits, from its gradients in logp and entropy:
  *   d x_j = [j = token] dlogp - p_j (dlogp + dentropy (log p_j + entropy)),  dlogits = d x / temperature, 0 for excluded tokens

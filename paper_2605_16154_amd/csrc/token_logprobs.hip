@@ -7,16 +7,18 @@
 //
 // Gradient: d logit_j = ([j = token] d_logp - p_j (d_logp + d_entropy (log p_j + entropy))) / temperature, from lse and entropy as
 // the forward pass left them: every logit is read once and its gradient written once.
+#include <type_traits>
+
 #include "common.h"
 
 namespace pcm {
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int kTopMost = 64;                 // one list entry per lane
 constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 __device__ inline float infinity() { return __builtin_huge_valf(); }
+__device__ inline int ceil_div_device(int a, int b) { return (int)(((int64_t)a + b - 1) / b); }
 
 struct Logits {
     const void* z;
@@ -85,75 +87,81 @@ __device__ inline uint32_t load_chunk(const T* row, const uint8_t* allowed, int 
     return ok;
 }
 
-// What has been seen of a row: r the reference (a logit; -inf: none yet), s = sum 2^a, t = sum 2^a a, a = (z - r) c.  (z c - r c in one
-// instruction would save one of about ten, but r c rounds, and it overflows at logits of the lowest fp32 value.)
+// What has been seen of a row: s = sum 2^a and t = sum 2^a a with a = z c - R.  r is the logit that R = r c was made from (-inf:
+// none yet); R is rounded, which takes nothing from the sums, as it is the same in all of them.  Logits beyond 1e38, where r c could
+// overflow, have R = 0 and a = (z - r) c.
 struct Sums {
-    float r, s, t;
+    float r, R, s, t;
+    __device__ bool far() const { return fabsf(r) > 1e38f && r != -infinity(); }
 };
 // How far above the reference a logit may be, in powers of two: 2^17 such terms still fit.
 constexpr float kHeadroom = 64.f;
+// 0 * -inf would be NaN, and 2^-300 is zero
+__device__ __forceinline__ float times(float p, float a) { return p * fmaxf(a, -300.f); }
+__device__ __forceinline__ float exponent(const Sums& a, float z, float c) { return a.far() ? (z - a.r) * c : __builtin_fmaf(z, c, -a.R); }
 
-template <bool kEntropy>
+// A logit far above the reference, or the first one, becomes the reference.
+__device__ __forceinline__ void move_reference(Sums& a, float to, float c) {
+    Sums b{to, 0.f, a.s, a.t};
+    b.R = b.far() ? 0.f : to * c;
+    if (a.r != -infinity()) {
+        const float d = a.far() || b.far() ? (a.r - to) * c : a.R - b.R, f = __builtin_amdgcn_exp2f(d);
+        b.t = f * (a.t + times(a.s, d));
+        b.s = f * a.s;
+    }
+    a = b;
+}
+// How a chunk is added: kFinite every logit is finite, kAny also -inf (excluded tokens), kFar also beyond 1e38.
+enum Care : int { kFinite = 0, kAny = 1, kFar = 2 };
+template <bool kEntropy, int kCare>
 __device__ __forceinline__ void add_chunk(Sums& a, const float (&z)[8], float c) {
-    const float r = a.r == -infinity() ? 0.f : a.r;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float x = (z[e] - r) * c;
+        const float x = kCare == kFar ? exponent(a, z[e], c) : __builtin_fmaf(z[e], c, -a.R);
         const float p = __builtin_amdgcn_exp2f(x);
         a.s += p;
-        if (kEntropy) a.t = __builtin_fmaf(p, fmaxf(x, -300.f), a.t);       // 0 * -inf would be NaN; 2^-300 is zero
+        if (kEntropy) a.t = __builtin_fmaf(p, kCare == kFinite ? x : fmaxf(x, -300.f), a.t);
     }
 }
 __device__ __forceinline__ float chunk_max(const float (&z)[8]) {
-    return fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
+    return fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(z[0], z[1]), z[2]), z[3]), z[4]), z[5]), z[6]), z[7]);
 }
-// A chunk whose largest logit is far above the reference: it becomes the reference.
-__device__ __forceinline__ void move_reference(Sums& a, float to, float c) {
-    if (a.r != -infinity()) {
-        const float d = (a.r - to) * c, f = __builtin_amdgcn_exp2f(d);
-        a.t = f * (a.t + fmaxf(d, -300.f) * a.s);
-        a.s *= f;
-    }
-    a.r = to;
-}
-__device__ __forceinline__ Sums join(const Sums& a, const Sums& b, float c) {
-    const float r = fmaxf(a.r, b.r);
-    auto moved = [&](const Sums& x) {
-        if (x.r == -infinity()) return Sums{r, x.s, x.t};            // both are zero, or NaN
-        const float d = (x.r - r) * c, f = __builtin_amdgcn_exp2f(d);
-        return Sums{r, f * x.s, f * (x.t + fmaxf(d, -300.f) * x.s)};
-    };
-    const Sums ma = moved(a), mb = moved(b);
-    return Sums{r, ma.s + mb.s, ma.t + mb.t};
+__device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
+    if (a.r < b.r) { const Sums x = a; a = b; b = x; }
+    if (a.r == -infinity()) return Sums{a.r, a.R, a.s + b.s, a.t + b.t};        // zeros, or NaN
+    // b moves to a's reference; nothing is left of sums without one (but a NaN)
+    const float d = b.r == -infinity() ? -300.f : (a.far() || b.far() ? (b.r - a.r) * c : b.R - a.R), f = __builtin_amdgcn_exp2f(d);
+    return Sums{a.r, a.R, a.s + f * b.s, a.t + f * (b.t + times(b.s, d))};
 }
 
 // The largest logits met by a wavefront, lane i holding the i-th of them; of equal ones the lower index first.
 struct TopList {
     float z;
     int id;
-    int count;                   // the same in every lane
-    __device__ void clear() { z = -infinity(); id = -1; count = 0; }
-    __device__ float last_z(int k) const { return __shfl(z, k - 1, 64); }
+    int count;                   // the same in every lane, as is
+    float last;                  // the k-th of them (-inf while there are fewer)
+    __device__ void clear() { z = last = -infinity(); id = -1; count = 0; }
     // z, id: the same in every lane
-    __device__ void insert(float nz, int nid, int k) {
+    __device__ __forceinline__ void insert(float nz, int nid, int k) {
         const int lane = threadIdx.x & 63;
         const bool before = lane < count && (z > nz || (z == nz && id < nid));
         const int at = __popcll(__ballot(before));
         if (at >= k) return;
-        const float uz = __shfl_up(z, 1, 64);
-        const int uid = __shfl_up(id, 1, 64);
-        if (lane > at) { z = uz; id = uid; }
-        if (lane == at) { z = nz; id = nid; }
+        // from the lane below
+        const float uz = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, z), 0x138, 0xF, 0xF, false));
+        const int uid = __builtin_amdgcn_update_dpp(0, id, 0x138, 0xF, 0xF, false);
+        z = lane > at ? uz : (lane == at ? nz : z);
+        id = lane > at ? uid : (lane == at ? nid : id);
         count = min(count + 1, k);
+        if (count == k) last = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, z), k - 1));
     }
     // Every lane's own value, where it has one: those that belong into the list.
-    __device__ void offer(bool have, float nz, int nid, int k) {
-        const float last = last_z(k);            // (by all lanes: a shuffle does not read from lanes that are switched off)
+    __device__ __forceinline__ void offer(bool have, float nz, int nid, int k) {
         uint64_t todo = __ballot(have && !(nz != nz) && (count < k || nz >= last));
         while (todo != 0) {
             const int from = __builtin_ctzll(todo);
             todo &= todo - 1;
-            insert(__shfl(nz, from, 64), __shfl(nid, from, 64), k);
+            insert(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, nz), from)), __builtin_amdgcn_readlane(nid, from), k);
         }
     }
 };
@@ -164,66 +172,195 @@ struct ForwardOut {
     int32_t* top_ids;
     float* top_logp;
 };
+// What a part of a row leaves for the launch that joins them.
+struct Parts {
+    Sums* sums;                      // [rows, parts]
+    float* z;                        // [rows, parts, top]
+    int32_t* id;
+    int parts;
+};
 
-// A workgroup per row.
-template <class T, bool kMask, bool kEntropy>
-__global__ __launch_bounds__(kThreads) void token_logprobs_rows(Logits q, ForwardOut o) {
+// A row's results, by one lane; and logp of a logit.
+struct RowResult {
+    float lse, entropy;
+    __device__ RowResult(const Sums& a) {
+        empty = a.s == 0.f;          // nothing allowed, or only logits of -inf
+        log2_s = __builtin_amdgcn_logf(a.s);
+        lse = empty ? -infinity() : kLn2 * (a.R + log2_s);
+        entropy = empty ? 0.f : kLn2 * (log2_s - a.t / a.s);
+        sums = a;
+    }
+    __device__ float logp(float z, float c) const { return empty ? -infinity() : kLn2 * (exponent(sums, z, c) - log2_s); }
+    __device__ float lse_of(const Logits& q) const { return !empty && sums.far() ? sums.r * q.inv_t + kLn2 * log2_s : lse; }
+    bool empty;
+    float log2_s;
+    Sums sums;
+};
+template <class T>
+__device__ __forceinline__ void store_row(const Logits& q, const ForwardOut& o, int64_t row, const RowResult& res, float c) {
+    const int token = token_of(q, row);
+    float logp = 0.f;
+    if (token >= 0) {
+        const bool in = q.allowed == nullptr || q.allowed[row * q.allowed_ld + token] != 0;
+        logp = in ? res.logp(to_float<T>(static_cast<const T*>(q.z)[row * q.ld + token]), c) : -infinity();
+    }
+    o.logp[row] = logp;
+    o.lse[row] = res.lse_of(q);
+    if (o.entropy != nullptr) o.entropy[row] = res.entropy;
+}
+__device__ __forceinline__ void store_top(const ForwardOut& o, int64_t row, const TopList& list, const RowResult& res, float c) {
+    const int lane = threadIdx.x & 63;
+    if (lane >= o.top) return;
+    o.top_ids[row * o.top + lane] = lane < list.count ? list.id : -1;
+    o.top_logp[row * o.top + lane] = lane < list.count ? res.logp(list.z, c) : -infinity();
+}
+
+// A workgroup per part of a row, in chunks of eight logits per lane.
+template <class T, bool kMask, bool kEntropy, bool kTop, int kThreads>
+__global__ __launch_bounds__(kThreads) void token_logprobs_parts(Logits q, ForwardOut o, Parts parts) {
     constexpr int kWaves = kThreads / 64;
     __shared__ Sums wave_sums[kWaves];
-    __shared__ float list_z[kWaves][kTopMost];
-    __shared__ int list_id[kWaves][kTopMost];
-    const int64_t row = blockIdx.x;
+    __shared__ float list_z[kTop ? kWaves : 1][kTopMost];
+    __shared__ int list_id[kTop ? kWaves : 1][kTopMost];
+    const int64_t row = blockIdx.x / parts.parts;
+    const int part = blockIdx.x % parts.parts;
     const T* z_row = static_cast<const T*>(q.z) + row * q.ld;
     const uint8_t* allowed = kMask ? q.allowed + row * q.allowed_ld : nullptr;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float c = q.inv_t * kLog2E;
-    Sums a{-infinity(), 0.f, 0.f};
+    const float c = q.inv_t * kLog2E, room = kHeadroom / c;
+    Sums a{-infinity(), 0.f, 0.f, 0.f};
     TopList list;
     list.clear();
-    for (int j0 = 0; j0 < q.V; j0 += kThreads * 8) {
+    int care = kMask ? kAny : kFinite;                   // of the whole wavefront
+    float limit = -infinity();                           // a chunk with a logit above it has something to be seen to
+    const int units = ceil_div_device(q.V, kThreads * 8), per_part = ceil_div_device(units, parts.parts);
+    const int end = min(q.V, (part + 1) * per_part * kThreads * 8);
+    for (int j0 = part * per_part * kThreads * 8; j0 < end; j0 += kThreads * 8) {
         const int j = j0 + (int)threadIdx.x * 8;
         float z[8];
         const uint32_t ok = load_chunk<T, kMask>(z_row, allowed, j, q.V, z);
         const float most = chunk_max(z);
-        if (most > a.r + kHeadroom / c) move_reference(a, most, c);
-        add_chunk<kEntropy>(a, z, c);
-        if (o.top > 0 && (list.count < o.top || __any(most > list.last_z(o.top)))) {
+        if (__any(most > limit) || (kTop && list.count < o.top)) {
+            if (most > a.r + room) move_reference(a, most, c);
+            if (kTop) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) list.offer(ok >> e & 1, z[e], j + e, o.top);
+                for (int e = 0; e < 8; ++e) list.offer(ok >> e & 1, z[e], j + e, o.top);
+            }
+            limit = kTop ? fminf(a.r + room, list.last) : a.r + room;
+            if (__any(a.far())) care = kFar;
+        }
+        if (care == kFinite) {
+            const float s = a.s, t = a.t;
+            add_chunk<kEntropy, kFinite>(a, z, c);
+            if (kEntropy && __any(a.t != a.t)) {         // 0 * -inf: again, with care
+                a.s = s;
+                a.t = t;
+                care = kAny;
+                add_chunk<kEntropy, kAny>(a, z, c);
+            }
+        } else if (care == kAny) {
+            add_chunk<kEntropy, kAny>(a, z, c);
+        } else {
+            add_chunk<kEntropy, kFar>(a, z, c);
         }
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
-        const Sums b{__shfl_xor(a.r, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)};
+        const Sums b{__shfl_xor(a.r, d, 64), __shfl_xor(a.R, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)};
         a = join(a, b, c);
     }
-    if (lane == 0) wave_sums[wave] = a;
-    if (o.top > 0) {
-        list_z[wave][lane] = list.z;
-        list_id[wave][lane] = list.id;
-    }
-    __syncthreads();
-    if (wave != 0) return;
-    Sums all = wave_sums[0];
-    for (int w = 1; w < kWaves; ++w) all = join(all, wave_sums[w], c);
-    const bool empty = all.s == 0.f;                     // nothing allowed, or only logits of -inf
-    const float log2_s = __builtin_amdgcn_logf(all.s);
-    auto logp_of = [&](float z) { return empty ? -infinity() : (z - all.r) * q.inv_t - kLn2 * log2_s; };
-    if (lane == 0) {
-        const int token = token_of(q, row);
-        float logp = 0.f;
-        if (token >= 0) logp = kMask && allowed[token] == 0 ? -infinity() : logp_of(to_float<T>(z_row[token]));
-        o.logp[row] = logp;
-        o.lse[row] = empty ? -infinity() : all.r * q.inv_t + kLn2 * log2_s;
-        if (kEntropy) o.entropy[row] = empty ? 0.f : kLn2 * (log2_s - all.t / all.s);
-    }
-    if (o.top > 0) {
-        for (int w = 1; w < kWaves; ++w) list.offer(list_id[w][lane] >= 0, list_z[w][lane], list_id[w][lane], o.top);
-        if (lane < o.top) {
-            o.top_ids[row * o.top + lane] = lane < list.count ? list.id : -1;
-            o.top_logp[row * o.top + lane] = lane < list.count ? logp_of(list.z) : -infinity();
+    if (kWaves > 1) {
+        if (lane == 0) wave_sums[wave] = a;
+        if (kTop) {
+            list_z[wave][lane] = list.z;
+            list_id[wave][lane] = list.id;
         }
+        __syncthreads();
+        if (wave != 0) return;
+        for (int w = 1; w < kWaves; ++w) a = join(a, wave_sums[w], c);
+        if (kTop)
+            for (int w = 1; w < kWaves; ++w) list.offer(list_id[w][lane] >= 0, list_z[w][lane], list_id[w][lane], o.top);
     }
+    if (parts.parts > 1) {
+        if (lane == 0) parts.sums[blockIdx.x] = a;
+        if (kTop && lane < o.top) {
+            parts.z[(int64_t)blockIdx.x * o.top + lane] = list.z;
+            parts.id[(int64_t)blockIdx.x * o.top + lane] = lane < list.count ? list.id : -1;
+        }
+        return;
+    }
+    const RowResult res(a);
+    if (lane == 0) store_row<T>(q, o, row, res, c);
+    if (kTop) store_top(o, row, list, res, c);
+}
+
+// A wavefront per row: the parts of the row.
+template <class T>
+__global__ __launch_bounds__(64) void token_logprobs_join(Logits q, ForwardOut o, Parts parts) {
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x;
+    const float c = q.inv_t * kLog2E;
+    Sums a{-infinity(), 0.f, 0.f, 0.f};
+    for (int i = lane; i < parts.parts; i += 64) a = join(a, parts.sums[row * parts.parts + i], c);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        const Sums b{__shfl_xor(a.r, d, 64), __shfl_xor(a.R, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)};
+        a = join(a, b, c);
+    }
+    const RowResult res(a);
+    if (lane == 0) store_row<T>(q, o, row, res, c);
+    if (o.top == 0) return;
+    TopList list;
+    list.clear();
+    const int n = parts.parts * o.top;
+    for (int i0 = 0; i0 < n; i0 += 64) {
+        const int i = i0 + lane;
+        const int64_t at = row * n + i;
+        const int id = i < n ? parts.id[at] : -1;
+        list.offer(id >= 0, id >= 0 ? parts.z[at] : -infinity(), id, o.top);
+    }
+    store_top(o, row, list, res, c);
+}
+
+// Rows of up to 16 kLanes logits: kLanes lanes per row, all of it in registers, and the sums relative to its largest logit.
+template <int kLanes>
+__device__ __forceinline__ float lanes_max(float x) {
+#pragma unroll
+    for (int d = kLanes / 2; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
+    return x;
+}
+template <int kLanes>
+__device__ __forceinline__ float lanes_sum(float x) {
+#pragma unroll
+    for (int d = kLanes / 2; d > 0; d >>= 1) x += __shfl_xor(x, d, 64);
+    return x;
+}
+constexpr int kNarrowThreads = 256;
+template <class T, bool kMask, int kLanes>
+__global__ __launch_bounds__(kNarrowThreads) void token_logprobs_narrow(Logits q, ForwardOut o) {
+    const int64_t row = (int64_t)blockIdx.x * (kNarrowThreads / kLanes) + threadIdx.x / kLanes;
+    if (row >= q.rows) return;
+    const T* z_row = static_cast<const T*>(q.z) + row * q.ld;
+    const uint8_t* allowed = kMask ? q.allowed + row * q.allowed_ld : nullptr;
+    const int lane = threadIdx.x % kLanes;
+    const float c = q.inv_t * kLog2E;
+    float z[2][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load_chunk<T, kMask>(z_row, allowed, (h * kLanes + lane) * 8, q.V, z[h]);
+    Sums a{-infinity(), 0.f, 0.f, 0.f};
+    const float most = lanes_max<kLanes>(fmaxf(chunk_max(z[0]), chunk_max(z[1])));
+    move_reference(a, most, c);
+    if (most == -infinity()) a.R = 0.f;
+    if (__any(a.far())) {
+        add_chunk<true, kFar>(a, z[0], c);
+        add_chunk<true, kFar>(a, z[1], c);
+    } else {
+        add_chunk<true, kAny>(a, z[0], c);
+        add_chunk<true, kAny>(a, z[1], c);
+    }
+    a.s = lanes_sum<kLanes>(a.s);
+    a.t = lanes_sum<kLanes>(a.t);
+    if (lane == 0) store_row<T>(q, o, row, RowResult(a), c);
 }
 
 struct BackwardArgs {
@@ -259,54 +396,123 @@ __device__ inline void store_chunk<uint16_t>(uint16_t* row, int j, int V, const 
     }
 }
 
-// A workgroup per row.
-template <class T, bool kMask>
-__global__ __launch_bounds__(kThreads) void token_logprobs_gradient(Logits q, BackwardArgs b) {
-    const int64_t row = blockIdx.x;
+// kLanes lanes per row, in chunks of eight logits; kThreads / kLanes rows per workgroup, and a row in `parts` of them.
+constexpr int kGradientThreads = 256;
+template <class T, bool kMask, int kLanes>
+__global__ __launch_bounds__(kGradientThreads) void token_logprobs_gradient(Logits q, BackwardArgs b, int parts) {
+    const int64_t row = (int64_t)(blockIdx.x / parts) * (kGradientThreads / kLanes) + threadIdx.x / kLanes;
+    const int part = blockIdx.x % parts;
+    if (row >= q.rows) return;
     const T* z_row = static_cast<const T*>(q.z) + row * q.ld;
     T* dz_row = static_cast<T*>(b.dz) + row * b.dz_ld;
     const uint8_t* allowed = kMask ? q.allowed + row * q.allowed_ld : nullptr;
-    const float lse = b.lse[row];
-    const bool empty = lse == -infinity();
-    const int token = empty ? -1 : token_of(q, row);
+    float lse = b.lse[row];
+    int token = token_of(q, row);
+    if (lse == -infinity()) {                            // nothing to choose from: every p is zero
+        lse = infinity();
+        token = -1;
+    }
     const float dlogp = token < 0 ? 0.f : b.dlogp[row] * q.inv_t;
+    if (kMask && token >= 0 && allowed[token] == 0) token = -1;          // its own gradient is zero
     float along = 0.f, scale = -dlogp;                   // g = p (scale + along a), a = log2 p
     if (b.dentropy != nullptr) {
         const float dh = b.dentropy[row] * q.inv_t;
         along = -dh * kLn2;
         scale -= dh * b.entropy[row];
     }
-    for (int j = (int)threadIdx.x * 8; j < q.V; j += kThreads * 8) {
+    const int units = ceil_div_device(q.V, kLanes * 8), per_part = ceil_div_device(units, parts);
+    const int end = min(q.V, (part + 1) * per_part * kLanes * 8);
+    for (int j = part * per_part * kLanes * 8 + (int)(threadIdx.x % kLanes) * 8; j < end; j += kLanes * 8) {
         float z[8], g[8];
         const uint32_t ok = load_chunk<T, kMask>(z_row, allowed, j, q.V, z);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float a = __builtin_fmaf(z[e], q.inv_t, -lse) * kLog2E;
             const float p = __builtin_amdgcn_exp2f(a);
-            g[e] = empty || (kMask && !(ok >> e & 1)) ? 0.f : p * __builtin_fmaf(along, fmaxf(a, -300.f), scale);
-            if (j + e == token && (ok >> e & 1)) g[e] += dlogp;
+            g[e] = kMask && !(ok >> e & 1) ? 0.f : p * __builtin_fmaf(along, fmaxf(a, -300.f), scale);
+        }
+        if (token >= j && token < j + 8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] += j + e == token ? dlogp : 0.f;
         }
         store_chunk<T>(dz_row, j, q.V, g);
     }
 }
 
+// Lanes per row: a row of up to 1024 logits has 16 of them to a lane, longer ones go through workgroups of their own.
+constexpr int kNarrow = 1024;
+template <class F>
+void with_lanes(int V, F f) {
+    if (V <= 64) f(std::integral_constant<int, 4>{});
+    else if (V <= 128) f(std::integral_constant<int, 8>{});
+    else if (V <= 256) f(std::integral_constant<int, 16>{});
+    else if (V <= 512) f(std::integral_constant<int, 32>{});
+    else f(std::integral_constant<int, 64>{});
+}
+// Parts of a row: as many workgroups as fill the chip, of at least two chunks per lane.
+constexpr int kFill = 2048, kWide = 256, kWaveRow = 4096;
+int forward_parts(int64_t rows, int V) {
+    if (V <= kWaveRow) return 1;
+    const int64_t fill = kFill / (rows < 1 ? 1 : rows), most = V / (kWide * 16);
+    const int64_t parts = fill < most ? fill : most;
+    return parts < 1 ? 1 : (int)parts;
+}
+
+template <class T, bool kMask, bool kEntropy, bool kTop>
+void launch_parts(const Logits& q, const ForwardOut& o, const Parts& p, hipStream_t s) {
+    if (q.V <= kWaveRow) token_logprobs_parts<T, kMask, kEntropy, kTop, 64><<<(unsigned)q.rows, 64, 0, s>>>(q, o, p);
+    else token_logprobs_parts<T, kMask, kEntropy, kTop, kWide><<<(unsigned)(q.rows * p.parts), kWide, 0, s>>>(q, o, p);
+    if (p.parts > 1) token_logprobs_join<T><<<(unsigned)q.rows, 64, 0, s>>>(q, o, p);
+}
 template <class T, bool kMask>
-void launch_forward(const Logits& q, const ForwardOut& o, hipStream_t s) {
-    if (o.entropy != nullptr) token_logprobs_rows<T, kMask, true><<<(unsigned)q.rows, kThreads, 0, s>>>(q, o);
-    else token_logprobs_rows<T, kMask, false><<<(unsigned)q.rows, kThreads, 0, s>>>(q, o);
+void launch_forward(const Logits& q, const ForwardOut& o, const Parts& p, hipStream_t s) {
+    if (q.V <= kNarrow && o.top == 0) {
+        with_lanes(q.V, [&](auto lanes) {
+            constexpr int kLanes = decltype(lanes)::value, kRows = kNarrowThreads / kLanes;
+            token_logprobs_narrow<T, kMask, kLanes><<<(unsigned)ceil_div64(q.rows, kRows), kNarrowThreads, 0, s>>>(q, o);
+        });
+        return;
+    }
+    if (o.entropy != nullptr && o.top > 0) launch_parts<T, kMask, true, true>(q, o, p, s);
+    else if (o.entropy != nullptr) launch_parts<T, kMask, true, false>(q, o, p, s);
+    else if (o.top > 0) launch_parts<T, kMask, false, true>(q, o, p, s);
+    else launch_parts<T, kMask, false, false>(q, o, p, s);
 }
 template <class T>
-void launch_forward(const Logits& q, const ForwardOut& o, hipStream_t s) {
-    if (q.allowed != nullptr) launch_forward<T, true>(q, o, s);
-    else launch_forward<T, false>(q, o, s);
+void launch_forward(const Logits& q, const ForwardOut& o, const Parts& p, hipStream_t s) {
+    if (q.allowed != nullptr) launch_forward<T, true>(q, o, p, s);
+    else launch_forward<T, false>(q, o, p, s);
+}
+template <class T, bool kMask>
+void launch_backward(const Logits& q, const BackwardArgs& b, hipStream_t s) {
+    if (q.V <= kNarrow) {
+        with_lanes(q.V, [&](auto lanes) {
+            constexpr int kLanes = decltype(lanes)::value, kRows = kGradientThreads / kLanes;
+            token_logprobs_gradient<T, kMask, kLanes><<<(unsigned)ceil_div64(q.rows, kRows), kGradientThreads, 0, s>>>(q, b, 1);
+        });
+        return;
+    }
+    const int parts = forward_parts(q.rows, q.V);
+    token_logprobs_gradient<T, kMask, kGradientThreads><<<(unsigned)(q.rows * parts), kGradientThreads, 0, s>>>(q, b, parts);
 }
 template <class T>
 void launch_backward(const Logits& q, const BackwardArgs& b, hipStream_t s) {
-    if (q.allowed != nullptr) token_logprobs_gradient<T, true><<<(unsigned)q.rows, kThreads, 0, s>>>(q, b);
-    else token_logprobs_gradient<T, false><<<(unsigned)q.rows, kThreads, 0, s>>>(q, b);
+    if (q.allowed != nullptr) launch_backward<T, true>(q, b, s);
+    else launch_backward<T, false>(q, b, s);
+}
+
+Parts carve_parts(Carver& c, int64_t rows, int V, int top) {
+    Parts p{};
+    p.parts = top == 0 && V <= kNarrow ? 1 : forward_parts(rows, V);
+    if (p.parts == 1) return p;
+    p.sums = c.take<Sums>((size_t)(rows * p.parts));
+    p.z = c.take<float>((size_t)(rows * p.parts * top));
+    p.id = c.take<int32_t>((size_t)(rows * p.parts * top));
+    return p;
 }
 
 constexpr int64_t kMaxRows = 0x7fffffff;
+constexpr int kMaxVocabulary = 1 << 30;
 
 // The checks that both directions share.
 int check_logits(const void* logits, int64_t ld, int dtype, const void* tokens, int token_type, const uint8_t* allowed, int64_t allowed_ld,
@@ -321,7 +527,7 @@ int check_logits(const void* logits, int64_t ld, int dtype, const void* tokens, 
     if (!logits || !tokens || (reinterpret_cast<uintptr_t>(logits) & (dtype == PCM_F32 ? 3u : 1u)) != 0 ||
         (reinterpret_cast<uintptr_t>(tokens) & (token_size - 1)) != 0)
         return PCM_EINVAL;
-    return rows > kMaxRows ? PCM_EUNSUPPORTED : PCM_OK;
+    return rows > kMaxRows || V > kMaxVocabulary ? PCM_EUNSUPPORTED : PCM_OK;
 }
 bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 
@@ -333,8 +539,10 @@ using namespace pcm;
 extern "C" {
 
 PCM_API size_t pcm_token_logprobs_workspace_bytes(int64_t rows, int V, int top) {
-    (void)rows; (void)V; (void)top;
-    return 0;
+    if (rows < 1 || rows > kMaxRows || V < 1 || V > kMaxVocabulary || top < 0 || top > kTopMost) return 0;
+    Carver c(nullptr);
+    carve_parts(c, rows, V, top);
+    return c.used();
 }
 
 PCM_API int pcm_token_logprobs(const void* logits, int64_t logits_ld, int dtype, const void* tokens, int token_type,
@@ -351,9 +559,11 @@ PCM_API int pcm_token_logprobs(const void* logits, int64_t logits_ld, int dtype,
     hipStream_t s = static_cast<hipStream_t>(stream);
     const Logits q{logits, logits_ld, allowed, allowed_ld, tokens, token_type, rows, V, 1.f / temperature};
     const ForwardOut o{logp, lse, entropy, top, top_ids, top_logp};
+    Carver c(workspace);
+    const Parts p = carve_parts(c, rows, V, top);
     StageTimer t(ST_TOKEN_LOGPROBS, s);
-    if (dtype == PCM_F32) launch_forward<float>(q, o, s);
-    else launch_forward<uint16_t>(q, o, s);
+    if (dtype == PCM_F32) launch_forward<float>(q, o, p, s);
+    else launch_forward<uint16_t>(q, o, p, s);
     return launch_status();
 }
 
