@@ -50,41 +50,90 @@ typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;
 typedef __attribute__((ext_vector_type(8), aligned(2))) uint16_t u16x8_any;
 typedef __attribute__((aligned(1))) uint64_t u64_any;
 
-__device__ inline void load_eight(const float* p, float (&z)[8]) {
-    const f32x4_any a = *reinterpret_cast<const f32x4_any*>(p), b = *reinterpret_cast<const f32x4_any*>(p + 4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { z[e] = a[e]; z[4 + e] = b[e]; }
-}
-__device__ inline void load_eight(const uint16_t* p, float (&z)[8]) {
-    const u16x8_any a = *reinterpret_cast<const u16x8_any*>(p);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) z[e] = to_float<uint16_t>(a[e]);
-}
+template <class T> struct Eight;
+template <>
+struct Eight<float> {
+    f32x4_any a, b;
+    __device__ void load(const float* p) {
+        a = *reinterpret_cast<const f32x4_any*>(p);
+        b = *reinterpret_cast<const f32x4_any*>(p + 4);
+    }
+    __device__ float operator[](int e) const { return e < 4 ? a[e] : b[e - 4]; }
+};
+template <>
+struct Eight<uint16_t> {
+    u16x8_any a;
+    __device__ void load(const uint16_t* p) { a = *reinterpret_cast<const u16x8_any*>(p); }
+    __device__ float operator[](int e) const { return to_float<uint16_t>(a[e]); }
+};
+// All eight are in the row: the loads, which may be well ahead of the use, and the use.
 template <class T, bool kMask>
-__device__ inline uint32_t load_chunk(const T* row, const uint8_t* allowed, int j, int V, float (&z)[8]) {
-    uint32_t ok = 0xFF;
-    if (j + 8 <= V) {
-        load_eight(row + j, z);
+struct WholeChunk {
+    Eight<T> z;
+    uint64_t mask;
+    __device__ void load(const T* row, const uint8_t* allowed, int j) {
+        z.load(row + j);
+        if (kMask) mask = *reinterpret_cast<const u64_any*>(allowed + j);
+    }
+    __device__ uint32_t get(float (&out)[8]) const {
+        uint32_t ok = 0xFF;
         if (kMask) {
-            const uint64_t m = *reinterpret_cast<const u64_any*>(allowed + j);
             ok = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ok |= (uint32_t)((m >> (8 * e) & 0xFF) != 0) << e;
+            for (int e = 0; e < 8; ++e) ok |= (uint32_t)((mask >> (8 * e) & 0xFF) != 0) << e;
         }
-    } else {
-        ok = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const bool in = j + e < V && (!kMask || allowed[j + e] != 0);
-            z[e] = in ? to_float<T>(row[j + e]) : -infinity();
-            ok |= (uint32_t)in << e;
-        }
+        for (int e = 0; e < 8; ++e) out[e] = !kMask || (ok >> e & 1) ? z[e] : -infinity();
         return ok;
     }
-    if (kMask)
+};
+template <class T, bool kMask>
+__device__ inline uint32_t load_chunk(const T* row, const uint8_t* allowed, int j, int V, float (&z)[8]) {
+    if (j + 8 <= V) {
+        WholeChunk<T, kMask> c;
+        c.load(row, allowed, j);
+        return c.get(z);
+    }
+    uint32_t ok = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = (ok >> e & 1) ? z[e] : -infinity();
+    for (int e = 0; e < 8; ++e) {
+        const bool in = j + e < V && (!kMask || allowed[j + e] != 0);
+        z[e] = in ? to_float<T>(row[j + e]) : -infinity();
+        ok |= (uint32_t)in << e;
+    }
     return ok;
+}
+// f(j, z, ok) for the chunks from `begin` to `end` that this thread of kStride has, the loads of kAhead chunks under way while as many
+// are worked on: with one at a time a wavefront waits for each (4096 rows of 65536 bf16 164 us).
+constexpr int kAhead = 2;
+template <class T, bool kMask, int kStride, class F>
+__device__ __forceinline__ void each_chunk(const T* row, const uint8_t* allowed, int begin, int end, int V, int lane, F f) {
+    constexpr int kUnit = kStride * 8;
+    const int rounds = max(0, min(end, V) - begin) / (kAhead * kUnit);           // of chunks that are whole in every lane
+    int j = begin + lane * 8;
+    if (rounds > 0) {
+        WholeChunk<T, kMask> now[kAhead], next[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) now[u].load(row, allowed, j + u * kUnit);
+        for (int i = 0; i < rounds; ++i) {
+            if (i + 1 < rounds)
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) next[u].load(row, allowed, j + (kAhead + u) * kUnit);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                float z[8];
+                const uint32_t ok = now[u].get(z);
+                f(j + u * kUnit, z, ok);
+                now[u] = next[u];
+            }
+            j += kAhead * kUnit;
+        }
+    }
+    for (int first = begin + rounds * kAhead * kUnit; first < end; first += kUnit, j += kUnit) {
+        float z[8];
+        const uint32_t ok = load_chunk<T, kMask>(row, allowed, j, V, z);
+        f(j, z, ok);
+    }
 }
 
 // What has been seen of a row: s = sum 2^a and t = sum 2^a a with a = z c - R.  r is the logit that R = r c was made from (-inf:
@@ -134,37 +183,58 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
     return Sums{a.r, a.R, a.s + f * b.s, a.t + f * (b.t + times(b.s, d))};
 }
 
-// The largest logits met by a wavefront, lane i holding the i-th of them; of equal ones the lower index first.
-struct TopList {
-    float z;
-    int id;
-    int count;                   // the same in every lane, as is
-    float last;                  // the k-th of them (-inf while there are fewer)
-    __device__ void clear() { z = last = -infinity(); id = -1; count = 0; }
-    // z, id: the same in every lane
-    __device__ __forceinline__ void insert(float nz, int nid, int k) {
-        const int lane = threadIdx.x & 63;
-        const bool before = lane < count && (z > nz || (z == nz && id < nid));
-        const int at = __popcll(__ballot(before));
-        if (at >= k) return;
-        // from the lane below
-        const float uz = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, z), 0x138, 0xF, 0xF, false));
-        const int uid = __builtin_amdgcn_update_dpp(0, id, 0x138, 0xF, 0xF, false);
-        z = lane > at ? uz : (lane == at ? nz : z);
-        id = lane > at ? uid : (lane == at ? nid : id);
-        count = min(count + 1, k);
-        if (count == k) last = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, z), k - 1));
-    }
-    // Every lane's own value, where it has one: those that belong into the list.
-    __device__ __forceinline__ void offer(bool have, float nz, int nid, int k) {
-        uint64_t todo = __ballot(have && !(nz != nz) && (count < k || nz >= last));
-        while (todo != 0) {
-            const int from = __builtin_ctzll(todo);
-            todo &= todo - 1;
-            insert(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, nz), from)), __builtin_amdgcn_readlane(nid, from), k);
-        }
-    }
-};
+// Selection of the largest logits.  A token is one 64-bit number, its logit as an integer of the same order above the complement of
+// its index, so that of equal logits the lower index is larger; 0 stands for none.
+__device__ __forceinline__ uint64_t token_key(float z, int id) {
+    const int bits = __builtin_bit_cast(int, z + 0.f);            // -0 as 0
+    return (uint64_t)(uint32_t)(bits ^ ((bits >> 31) | (int)0x80000000)) << 32 | (uint32_t)~id;
+}
+__device__ __forceinline__ float key_logit(uint64_t key) {
+    const int bits = (int)(uint32_t)(key >> 32);
+    return __builtin_bit_cast(float, bits ^ (~(bits >> 31) | (int)0x80000000));
+}
+__device__ __forceinline__ int key_token(uint64_t key) { return (int)~(uint32_t)key; }
+
+// The value of lane ^ kD.
+template <int kD>
+__device__ __forceinline__ int lane_xor(int x) {
+    if constexpr (kD == 1) return __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, false);                 // quad_perm 1 0 3 2
+    else if constexpr (kD == 2) return __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xF, 0xF, false);            // quad_perm 2 3 0 1
+    else if constexpr (kD == 4) return __builtin_amdgcn_update_dpp(0, __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, false), 0x1B, 0xF, 0xF, false);
+    else if constexpr (kD == 8) return __builtin_amdgcn_update_dpp(0, x, 0x128, 0xF, 0xF, false);           // row_ror 8
+    else return __shfl_xor(x, kD, 64);
+}
+// A step of a sorting network: of lanes kD apart, the one with `larger` keeps the larger key.
+template <int kD>
+__device__ __forceinline__ uint64_t sort_step(uint64_t key, bool larger) {
+    const uint64_t other = (uint64_t)(uint32_t)lane_xor<kD>((int)(key >> 32)) << 32 | (uint32_t)lane_xor<kD>((int)key);
+    return (other > key) == larger ? other : key;
+}
+// Keys whose halves by lanes are sorted in opposite directions -> descending by lane (or ascending).
+template <int kD>
+__device__ __forceinline__ uint64_t sort_bitonic(uint64_t key, bool ascending) {
+    const int lane = threadIdx.x & 63;
+    key = sort_step<kD>(key, ((lane & kD) == 0) != ascending);
+    if constexpr (kD > 1) return sort_bitonic<kD / 2>(key, ascending);
+    else return key;
+}
+__device__ __forceinline__ uint64_t sort_ascending(uint64_t key) {
+    const int lane = threadIdx.x & 63;
+    key = sort_bitonic<1>(key, (lane & 2) == 0);
+    key = sort_bitonic<2>(key, (lane & 4) == 0);
+    key = sort_bitonic<4>(key, (lane & 8) == 0);
+    key = sort_bitonic<8>(key, (lane & 16) == 0);
+    key = sort_bitonic<16>(key, (lane & 32) == 0);
+    return sort_bitonic<32>(key, true);
+}
+
+__device__ __forceinline__ uint64_t key_of_lane(uint64_t x, int lane) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
+}
+// The 64 largest of 64 keys descending by lane and 64 ascending ones.
+__device__ __forceinline__ uint64_t merge_keys(uint64_t descending, uint64_t ascending) {
+    return sort_bitonic<32>(ascending > descending ? ascending : descending, false);
+}
 
 struct ForwardOut {
     float *logp, *lse, *entropy;     // entropy: or null
@@ -175,8 +245,7 @@ struct ForwardOut {
 // What a part of a row leaves for the launch that joins them.
 struct Parts {
     Sums* sums;                      // [rows, parts]
-    float* z;                        // [rows, parts, top]
-    int32_t* id;
+    uint64_t* keys;                  // [rows, parts, top]
     int parts;
 };
 
@@ -208,11 +277,89 @@ __device__ __forceinline__ void store_row(const Logits& q, const ForwardOut& o, 
     o.lse[row] = res.lse_of(q);
     if (o.entropy != nullptr) o.entropy[row] = res.entropy;
 }
-__device__ __forceinline__ void store_top(const ForwardOut& o, int64_t row, const TopList& list, const RowResult& res, float c) {
+__device__ __forceinline__ void store_top(const ForwardOut& o, int64_t row, uint64_t key, const RowResult& res, float c) {
     const int lane = threadIdx.x & 63;
     if (lane >= o.top) return;
-    o.top_ids[row * o.top + lane] = lane < list.count ? list.id : -1;
-    o.top_logp[row * o.top + lane] = lane < list.count ? res.logp(list.z, c) : -infinity();
+    o.top_ids[row * o.top + lane] = key != 0 ? key_token(key) : -1;
+    o.top_logp[row * o.top + lane] = key != 0 ? res.logp(key_logit(key), c) : -infinity();
+}
+
+// The largest chunk of every lane: its largest logit and where it is, the first of equal ones; j < 0: none yet.
+struct Best {
+    float z;
+    int j;
+    __device__ __forceinline__ void look(int at, float most, const float (&logits)[8], uint32_t ok) {
+        if (most > z) {
+            z = most;
+            j = at;
+        }
+        if (__any(j < 0)) {                              // logits of -inf count, NaN does not
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) any |= (ok >> e & 1) && logits[e] == logits[e];
+            if (j < 0 && any) j = at;
+        }
+    }
+};
+// The `top` largest tokens of a part of a row, in the first wavefront, descending by lane.  The pass over the logits has only noted the largest
+// of every lane.  The lanes that have the `top` largest of those (of equal ones the lower chunk first) hold all that is asked for: a token of
+// another lane is behind the largest of each of them.  So their logits, `top` lanes of one in kThreads, are looked at again, and those not
+// below the last of the lanes' largest are sorted.  (Kept while passing over the logits, sorted lists take 40 us of 140 at 4096 x 65536.)
+template <int kThreads>
+struct TopScratch {
+    uint64_t lists[kThreads / 64][64];
+    uint64_t found[kThreads * 8];
+    int lane_of[kTopMost];
+    int lanes, n;
+    float floor;
+};
+template <class T, bool kMask, int kThreads>
+__device__ __forceinline__ uint64_t select_top(TopScratch<kThreads>& lds, const Best& best, const T* row, const uint8_t* allowed, int begin, int end, int V,
+                                               int top) {
+    constexpr int kWaves = kThreads / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t mine = sort_ascending(best.j < 0 ? 0 : token_key(best.z, best.j));
+    if (kWaves > 1) lds.lists[wave][lane] = mine;
+    __syncthreads();
+    uint64_t key = 0;
+    if (wave == 0) {
+        key = merge_keys(0, mine);
+        for (int w = 1; w < kWaves; ++w) key = merge_keys(key, lds.lists[w][lane]);
+        const uint64_t last = key_of_lane(key, top - 1);
+        const int lanes = __popcll(__ballot(lane < top && key != 0));
+        if (lane < lanes) lds.lane_of[lane] = (key_token(key) - begin) / 8 % kThreads;
+        if (lane == 0) {
+            lds.lanes = lanes;
+            lds.n = 0;
+            lds.floor = last != 0 ? key_logit(last) : -infinity();
+        }
+        key = 0;
+    }
+    __syncthreads();
+    const int chunks = ceil_div_device(end - begin, kThreads * 8), tasks = lds.lanes * chunks;
+    for (int first = 0; first < tasks; first += kThreads) {
+        const int task = first + (int)threadIdx.x;
+        const float floor = lds.floor;
+        if (task < tasks) {
+            const int j = begin + (task % chunks * kThreads + lds.lane_of[task / chunks]) * 8;
+            float z[8];
+            const uint32_t ok = j < end ? load_chunk<T, kMask>(row, allowed, j, V, z) : 0;
+            for (int e = 0; e < 8; ++e)
+                if ((ok >> e & 1) && z[e] >= floor) lds.found[atomicAdd(&lds.n, 1)] = token_key(z[e], j + e);
+        }
+        __syncthreads();
+        if (wave == 0) {
+            const int n = lds.n;
+            for (int i = 0; i < n; i += 64) key = merge_keys(key, sort_ascending(i + lane < n ? lds.found[i + lane] : 0));
+            const uint64_t last = key_of_lane(key, top - 1);
+            if (lane == 0) {
+                lds.n = 0;
+                if (last != 0) lds.floor = key_logit(last);
+            }
+        }
+        __syncthreads();
+    }
+    return key;
 }
 
 // A workgroup per part of a row, in chunks of eight logits per lane.
@@ -220,8 +367,6 @@ template <class T, bool kMask, bool kEntropy, bool kTop, int kThreads>
 __global__ __launch_bounds__(kThreads) void token_logprobs_parts(Logits q, ForwardOut o, Parts parts) {
     constexpr int kWaves = kThreads / 64;
     __shared__ Sums wave_sums[kWaves];
-    __shared__ float list_z[kTop ? kWaves : 1][kTopMost];
-    __shared__ int list_id[kTop ? kWaves : 1][kTopMost];
     const int64_t row = blockIdx.x / parts.parts;
     const int part = blockIdx.x % parts.parts;
     const T* z_row = static_cast<const T*>(q.z) + row * q.ld;
@@ -229,26 +374,17 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_parts(Logits q, Forwa
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float c = q.inv_t * kLog2E, room = kHeadroom / c;
     Sums a{-infinity(), 0.f, 0.f, 0.f};
-    TopList list;
-    list.clear();
+    Best best{-infinity(), -1};
     int care = kMask ? kAny : kFinite;                   // of the whole wavefront
-    float limit = -infinity();                           // a chunk with a logit above it has something to be seen to
     const int units = ceil_div_device(q.V, kThreads * 8), per_part = ceil_div_device(units, parts.parts);
-    const int end = min(q.V, (part + 1) * per_part * kThreads * 8);
-    for (int j0 = part * per_part * kThreads * 8; j0 < end; j0 += kThreads * 8) {
-        const int j = j0 + (int)threadIdx.x * 8;
-        float z[8];
-        const uint32_t ok = load_chunk<T, kMask>(z_row, allowed, j, q.V, z);
+    const int begin = min(q.V, part * per_part * kThreads * 8), end = min(q.V, begin + per_part * kThreads * 8);
+    each_chunk<T, kMask, kThreads>(z_row, allowed, begin, end, q.V, threadIdx.x, [&](int j, const float (&z)[8], uint32_t ok) __attribute__((always_inline)) {
         const float most = chunk_max(z);
-        if (__any(most > limit) || (kTop && list.count < o.top)) {
+        if (__any(most > a.r + room)) {
             if (most > a.r + room) move_reference(a, most, c);
-            if (kTop) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) list.offer(ok >> e & 1, z[e], j + e, o.top);
-            }
-            limit = kTop ? fminf(a.r + room, list.last) : a.r + room;
             if (__any(a.far())) care = kFar;
         }
+        if (kTop) best.look(j, most, z, ok);
         if (care == kFinite) {
             const float s = a.s, t = a.t;
             add_chunk<kEntropy, kFinite>(a, z, c);
@@ -263,43 +399,50 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_parts(Logits q, Forwa
         } else {
             add_chunk<kEntropy, kFar>(a, z, c);
         }
-    }
+    });
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
         const Sums b{__shfl_xor(a.r, d, 64), __shfl_xor(a.R, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)};
         a = join(a, b, c);
     }
-    if (kWaves > 1) {
-        if (lane == 0) wave_sums[wave] = a;
-        if (kTop) {
-            list_z[wave][lane] = list.z;
-            list_id[wave][lane] = list.id;
-        }
+    if (kWaves > 1 && lane == 0) wave_sums[wave] = a;
+    uint64_t key = 0;
+    if constexpr (kTop) {
+        __shared__ TopScratch<kThreads> scratch;
+        key = select_top<T, kMask, kThreads>(scratch, best, z_row, allowed, begin, end, q.V, o.top);
+    } else if (kWaves > 1) {
         __syncthreads();
-        if (wave != 0) return;
-        for (int w = 1; w < kWaves; ++w) a = join(a, wave_sums[w], c);
-        if (kTop)
-            for (int w = 1; w < kWaves; ++w) list.offer(list_id[w][lane] >= 0, list_z[w][lane], list_id[w][lane], o.top);
     }
+    if (wave != 0) return;
+    for (int w = 1; w < kWaves; ++w) a = join(a, wave_sums[w], c);
     if (parts.parts > 1) {
         if (lane == 0) parts.sums[blockIdx.x] = a;
-        if (kTop && lane < o.top) {
-            parts.z[(int64_t)blockIdx.x * o.top + lane] = list.z;
-            parts.id[(int64_t)blockIdx.x * o.top + lane] = lane < list.count ? list.id : -1;
-        }
+        if (kTop && lane < o.top) parts.keys[(int64_t)blockIdx.x * o.top + lane] = key;
         return;
     }
     const RowResult res(a);
     if (lane == 0) store_row<T>(q, o, row, res, c);
-    if (kTop) store_top(o, row, list, res, c);
+    if (kTop) store_top(o, row, key, res, c);
 }
 
-// A wavefront per row: the parts of the row.
+// A workgroup per row: the parts of the row.
+constexpr int kJoinThreads = 256;
 template <class T>
-__global__ __launch_bounds__(64) void token_logprobs_join(Logits q, ForwardOut o, Parts parts) {
+__global__ __launch_bounds__(kJoinThreads) void token_logprobs_join(Logits q, ForwardOut o, Parts parts) {
+    constexpr int kWaves = kJoinThreads / 64;
+    __shared__ uint64_t lists[kWaves][64];
     const int64_t row = blockIdx.x;
-    const int lane = threadIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float c = q.inv_t * kLog2E;
+    uint64_t key = 0;
+    if (o.top > 0) {
+        const int n = parts.parts * o.top;
+        for (int first = wave * 64; first < n; first += kJoinThreads)
+            key = merge_keys(key, sort_ascending(first + lane < n ? parts.keys[row * n + first + lane] : 0));
+        lists[wave][63 - lane] = key;
+        __syncthreads();
+    }
+    if (wave != 0) return;
     Sums a{-infinity(), 0.f, 0.f, 0.f};
     for (int i = lane; i < parts.parts; i += 64) a = join(a, parts.sums[row * parts.parts + i], c);
 #pragma unroll
@@ -310,16 +453,8 @@ __global__ __launch_bounds__(64) void token_logprobs_join(Logits q, ForwardOut o
     const RowResult res(a);
     if (lane == 0) store_row<T>(q, o, row, res, c);
     if (o.top == 0) return;
-    TopList list;
-    list.clear();
-    const int n = parts.parts * o.top;
-    for (int i0 = 0; i0 < n; i0 += 64) {
-        const int i = i0 + lane;
-        const int64_t at = row * n + i;
-        const int id = i < n ? parts.id[at] : -1;
-        list.offer(id >= 0, id >= 0 ? parts.z[at] : -infinity(), id, o.top);
-    }
-    store_top(o, row, list, res, c);
+    for (int w = 1; w < kWaves; ++w) key = merge_keys(key, lists[w][lane]);
+    store_top(o, row, key, res, c);
 }
 
 // Rows of up to 16 kLanes logits: kLanes lanes per row, all of it in registers, and the sums relative to its largest logit.
@@ -421,10 +556,9 @@ __global__ __launch_bounds__(kGradientThreads) void token_logprobs_gradient(Logi
         scale -= dh * b.entropy[row];
     }
     const int units = ceil_div_device(q.V, kLanes * 8), per_part = ceil_div_device(units, parts);
-    const int end = min(q.V, (part + 1) * per_part * kLanes * 8);
-    for (int j = part * per_part * kLanes * 8 + (int)(threadIdx.x % kLanes) * 8; j < end; j += kLanes * 8) {
-        float z[8], g[8];
-        const uint32_t ok = load_chunk<T, kMask>(z_row, allowed, j, q.V, z);
+    const int begin = min(q.V, part * per_part * kLanes * 8), end = min(q.V, begin + per_part * kLanes * 8);
+    each_chunk<T, kMask, kLanes>(z_row, allowed, begin, end, q.V, threadIdx.x % kLanes, [&](int j, const float (&z)[8], uint32_t ok) __attribute__((always_inline)) {
+        float g[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float a = __builtin_fmaf(z[e], q.inv_t, -lse) * kLog2E;
@@ -436,7 +570,7 @@ __global__ __launch_bounds__(kGradientThreads) void token_logprobs_gradient(Logi
             for (int e = 0; e < 8; ++e) g[e] += j + e == token ? dlogp : 0.f;
         }
         store_chunk<T>(dz_row, j, q.V, g);
-    }
+    });
 }
 
 // Lanes per row: a row of up to 1024 logits has 16 of them to a lane, longer ones go through workgroups of their own.
@@ -462,7 +596,7 @@ template <class T, bool kMask, bool kEntropy, bool kTop>
 void launch_parts(const Logits& q, const ForwardOut& o, const Parts& p, hipStream_t s) {
     if (q.V <= kWaveRow) token_logprobs_parts<T, kMask, kEntropy, kTop, 64><<<(unsigned)q.rows, 64, 0, s>>>(q, o, p);
     else token_logprobs_parts<T, kMask, kEntropy, kTop, kWide><<<(unsigned)(q.rows * p.parts), kWide, 0, s>>>(q, o, p);
-    if (p.parts > 1) token_logprobs_join<T><<<(unsigned)q.rows, 64, 0, s>>>(q, o, p);
+    if (p.parts > 1) token_logprobs_join<T><<<(unsigned)q.rows, kJoinThreads, 0, s>>>(q, o, p);
 }
 template <class T, bool kMask>
 void launch_forward(const Logits& q, const ForwardOut& o, const Parts& p, hipStream_t s) {
@@ -506,8 +640,7 @@ Parts carve_parts(Carver& c, int64_t rows, int V, int top) {
     p.parts = top == 0 && V <= kNarrow ? 1 : forward_parts(rows, V);
     if (p.parts == 1) return p;
     p.sums = c.take<Sums>((size_t)(rows * p.parts));
-    p.z = c.take<float>((size_t)(rows * p.parts * top));
-    p.id = c.take<int32_t>((size_t)(rows * p.parts * top));
+    p.keys = c.take<uint64_t>((size_t)(rows * p.parts * top));
     return p;
 }
 
