@@ -509,15 +509,20 @@ def _allowed_ptr(allowed: Optional[torch.Tensor], rows: int, V: int) -> Tuple[Op
 
 def _logits_args(logits, tokens, allowed, temperature: float):
     """The arguments that both directions of the token log-probabilities begin with."""
-    if logits.dim() != 2 or logits.dtype not in DTYPES:
+    dtype, token_type = DTYPES.get(logits.dtype), TOKEN_TYPES.get(tokens.dtype)
+    if logits.dim() != 2 or dtype is None:
         raise PcmError("logits must be [rows, V] of float32 or bfloat16")
     rows, V = logits.shape
-    if tokens.dtype not in TOKEN_TYPES or tuple(tokens.shape) != (rows,):
+    if token_type is None or tokens.shape != (rows,):
         raise PcmError("tokens must be [rows] of uint8, int32 or int64")
     p_logits, ld = _rows_ptr(logits, "logits")
-    p_allowed, allowed_ld = _allowed_ptr(allowed, rows, V)
-    return (p_logits, ld, DTYPES[logits.dtype], _ptr(tokens, None, "tokens"), TOKEN_TYPES[tokens.dtype], p_allowed, allowed_ld,
-            rows, V, temperature)
+    p_tokens, = _ptrs(_TOKENS, tokens)
+    p_allowed, allowed_ld = (None, 0) if allowed is None else _allowed_ptr(allowed, rows, V)
+    return p_logits, ld, dtype, p_tokens, token_type, p_allowed, allowed_ld, rows, V, temperature
+
+
+_TOKENS = ((None, "tokens"),)
+_ROW_GRADS = ((_F32, "lse"), (_F32, "dlogp"), (_F32, "entropy"), (_F32, "dentropy"))
 
 
 def pcm_token_logprobs(logits, tokens, allowed: Optional[torch.Tensor] = None, temperature: float = 1.0,
@@ -528,33 +533,46 @@ def pcm_token_logprobs(logits, tokens, allowed: Optional[torch.Tensor] = None, t
     logits [rows, V], float32 or bfloat16, with contiguous rows (a view of a wider matrix will do); tokens [rows] uint8, int32 or
     int64, negative where a row has none; allowed bool or uint8 [V] or [rows, V].  `out` may carry preallocated tensors.
     """
+    entry = lib().pcm_token_logprobs
     args = _logits_args(logits, tokens, allowed, temperature)
-    rows, V = logits.shape
+    rows, V = args[7], args[8]
     dev = logits.device
     if top < 0:
         raise PcmError("top must not be negative")
-    out = {} if out is None else out
+    p_entropy = p_ids = p_top = None
+    if out is None:          # (an allocation takes 1.5 us of the dozen that a small call is issued in, so the row values share one)
+        values = torch.empty((3 if want_entropy else 2, rows), dtype=_F32, device=dev).unbind()
+        out = {"logp": values[0], "lse": values[1]}
+        p_logp, p_lse = values[0].data_ptr(), values[1].data_ptr()
+        if want_entropy:
+            out["entropy"] = values[2]
+            p_entropy = values[2].data_ptr()
+        if top:
+            out["top_ids"] = ids = torch.empty((rows, top), dtype=_I32, device=dev)
+            out["top_logp"] = best = torch.empty((rows, top), dtype=_F32, device=dev)
+            p_ids, p_top = ids.data_ptr(), best.data_ptr()
+    else:
+        def buf(name, shape, dt):
+            t = out.get(name)
+            if t is None:
+                out[name] = t = torch.empty(shape, dtype=dt, device=dev)
+            elif tuple(t.shape) != shape:
+                raise PcmError(f"out[{name!r}] has shape {tuple(t.shape)}, expected {shape}")
+            return _ptr(t, dt, name)
 
-    def buf(name, shape, dt):
-        t = out.get(name)
-        if t is None:
-            out[name] = t = torch.empty(shape, dtype=dt, device=dev)
-        elif tuple(t.shape) != shape:
-            raise PcmError(f"out[{name!r}] has shape {tuple(t.shape)}, expected {shape}")
-        return _ptr(t, dt, name)
-
-    p_logp, p_lse = buf("logp", (rows,), _F32), buf("lse", (rows,), _F32)
-    p_entropy = buf("entropy", (rows,), _F32) if want_entropy else None
-    p_ids, p_top = (buf("top_ids", (rows, top), _I32), buf("top_logp", (rows, top), _F32)) if top else (None, None)
+        p_logp, p_lse = buf("logp", (rows,), _F32), buf("lse", (rows,), _F32)
+        if want_entropy:
+            p_entropy = buf("entropy", (rows,), _F32)
+        if top:
+            p_ids, p_top = buf("top_ids", (rows, top), _I32), buf("top_logp", (rows, top), _F32)
     need = lib().pcm_token_logprobs_workspace_bytes(rows, V, top)
     stream = _stream()
-    tail = (top, p_logp, p_lse, p_entropy, p_ids, p_top)
     if need == 0:
-        _check(lib().pcm_token_logprobs(*args, *tail, None, 0, stream), "pcm_token_logprobs")
+        _check(entry(*args, top, p_logp, p_lse, p_entropy, p_ids, p_top, None, 0, stream), "pcm_token_logprobs")
         return out
     ws = _take_workspace(need, dev, stream)
     try:
-        _check(lib().pcm_token_logprobs(*args, *tail, ws.data_ptr(), ws.numel(), stream), "pcm_token_logprobs")
+        _check(entry(*args, top, p_logp, p_lse, p_entropy, p_ids, p_top, ws.data_ptr(), ws.numel(), stream), "pcm_token_logprobs")
     finally:
         _give_workspace(ws, dev, stream)
     return out
@@ -565,22 +583,23 @@ def pcm_token_logprobs_backward(logits, tokens, lse, dlogp, entropy: Optional[to
                                 temperature: float = 1.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """-> d logits [rows, V] of the logits' dtype, from dlogp f32[rows] and, if the loss has a part in the entropy, dentropy
     f32[rows] with the entropy of the forward call; lse as the forward call returned it.  `out` may be the logits themselves."""
+    entry = lib().pcm_token_logprobs_backward
     args = _logits_args(logits, tokens, allowed, temperature)
-    rows, V = logits.shape
-    for name, t in (("lse", lse), ("dlogp", dlogp), ("entropy", entropy), ("dentropy", dentropy)):
-        if t is not None and tuple(t.shape) != (rows,):
-            raise PcmError(f"{name} must be [rows]")
-    if dentropy is not None and entropy is None:
+    rows, V = args[7], args[8]
+    if dentropy is None:
+        entropy = None
+    elif entropy is None:
         raise PcmError("a gradient in the entropy needs the entropy")
+    p = _ptrs(_ROW_GRADS, lse, dlogp, entropy, dentropy)
+    for t in (lse, dlogp) if dentropy is None else (lse, dlogp, entropy, dentropy):
+        if t.shape != (rows,):
+            raise PcmError("lse, dlogp, entropy and dentropy must be [rows]")
     if out is None:
         out = torch.empty((rows, V), dtype=logits.dtype, device=logits.device)
-    elif tuple(out.shape) != (rows, V) or out.dtype != logits.dtype:
+    elif out.shape != (rows, V) or out.dtype != logits.dtype:
         raise PcmError("out must have the shape and type of the logits")
     p_out, out_ld = _rows_ptr(out, "out")
-    p_dentropy = _ptr(dentropy, _F32, "dentropy")
-    p_entropy = _ptr(entropy, _F32, "entropy") if dentropy is not None else None
-    _check(lib().pcm_token_logprobs_backward(*args, _ptr(lse, _F32, "lse"), _ptr(dlogp, _F32, "dlogp"), p_entropy, p_dentropy,
-                                             p_out, out_ld, _stream()), "pcm_token_logprobs_backward")
+    _check(entry(*args, *p, p_out, out_ld, _stream()), "pcm_token_logprobs_backward")
     return out
 
 
