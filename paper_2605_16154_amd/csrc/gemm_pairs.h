@@ -20,24 +20,31 @@ enum PairResult : int {
 
 struct PairJob {
     const f16 *A, *B;
-    int m_frags, n_frags;        // fragments of rows of the operands (even)
-    int steps;                   // of 32 of k
-    int symmetric;               // C = C^T: only tiles with n <= m, the others through Ct (= C)
-    int result;
-    f16 *C, *Ct;
-    const f16* D;                // as C, or null
-    float alpha, beta, gamma;
-    void* out;
-    uint16_t* lowp;
-    int64_t ld;                  // of out (lowp: the same)
-    int rows, cols;              // of out
-    float decay, rate;
-    int first, tiles_m, tiles_n, tiles;      // first workgroup, tiles: filled in by the launch
+    union { f16* C; void* out; };
+    union { f16* Ct; int64_t ld; };              // ld: of out (lowp: the same)
+    union { const f16* D; uint16_t* lowp; };     // D: as C, or null
+    int m_frags, n_frags;                        // fragments of rows of the operands (even)
+    int steps;                                   // of 32 of k
+    int16_t symmetric;                           // C = C^T: only tiles with n <= m, the others through Ct (= C)
+    int16_t result;
+    float alpha;
+    union { float beta, decay; };
+    union { float gamma, rate; };
+    int rows, cols;                              // of out
+    int first, tiles_m, tiles_n;                 // first workgroup, tiles: filled in by the launch
+    __host__ __device__ int tiles() const { return symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n; }
 };
 constexpr int kMaxPairJobs = 16;
-struct PairJobs {
-    PairJob job[kMaxPairJobs];
-    int n, blocks;
+// The argument of a launch.  A launch with 2.7 KB of arguments takes two microseconds longer than one with 256 bytes, so few jobs on small
+// tiles go as kFewPairJobs.
+constexpr int kFewPairJobs = 4;
+template <int kMax>
+struct PairJobList {
+    PairJob job[kMax];
+    int n;
+};
+struct PairJobs : PairJobList<kMaxPairJobs> {
+    int blocks;
 };
 
 // Accumulators of a wavefront: tile (i, j), register t of a lane is row 16 i + (lane & 15), column 16 j + 4 (lane >> 4) + t.
@@ -110,45 +117,50 @@ __device__ __forceinline__ void store_pairs(const PairJob& p, const PairAccumula
 }
 template <int kW>
 __device__ __forceinline__ void store_result(const PairJob& p, const PairAccumulators<kW>& acc, int frag_m, int frag_n) {
-    const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-    static_for<kW * kW>([&](auto tile) __attribute__((always_inline)) {
-        constexpr int i = decltype(tile)::value / kW, j = decltype(tile)::value % kW;
-        const int m = (frag_m + i) * 16 + r, n = (frag_n + j) * 16 + 4 * g;
-        if (m >= p.rows || n >= p.cols) return;
-        const int64_t at = (int64_t)m * p.ld + n;
+    const int lane = threadIdx.x & 63;
+    const int m0 = frag_m * 16 + (lane & 15), n0 = frag_n * 16 + 4 * (lane >> 4), rows = p.rows, cols = p.cols, result = p.result;
+    const float alpha = p.alpha, decay = p.decay, rate = p.rate;
+    void* const out = p.out;
+    __bf16* const lowp = reinterpret_cast<__bf16*>(p.lowp);
+    const int64_t ld = p.ld;
+    auto store = [&](int i, int j, const f32x4& sum) __attribute__((always_inline)) {
+        const int m = m0 + 16 * i, n = n0 + 16 * j;
+        if (m >= rows || n >= cols) return;
+        const int64_t at = (int64_t)m * ld + n;
         float v[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) v[t] = p.alpha * acc[i][j][t];
-        if (p.result == kOutBf16) {
-            __bf16* const out = static_cast<__bf16*>(p.out) + at;
+        for (int t = 0; t < 4; ++t) v[t] = alpha * sum[t];
+        if (result == kOutBf16) {
+            __bf16* const to = static_cast<__bf16*>(out) + at;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                if (n + t < p.cols) out[t] = (__bf16)v[t];
+                if (n + t < cols) to[t] = (__bf16)v[t];
             return;
         }
-        float* const out = static_cast<float*>(p.out) + at;
-        const bool whole = n + 4 <= p.cols;
-        if (p.result == kOutWeights) {
+        float* const to = static_cast<float*>(out) + at;
+        const bool whole = n + 4 <= cols;
+        if (result == kOutWeights) {
             f32x4 w = {0.f, 0.f, 0.f, 0.f};
-            if (whole) w = *reinterpret_cast<const f32x4_any*>(out);
+            if (whole) w = *reinterpret_cast<const f32x4_any*>(to);
             else
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
-                    if (n + t < p.cols) w[t] = out[t];
+                    if (n + t < cols) w[t] = to[t];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) v[t] = p.decay * w[t] - p.rate * v[t];
-            if (p.lowp != nullptr) {
-                __bf16* const low = reinterpret_cast<__bf16*>(p.lowp) + at;
+            for (int t = 0; t < 4; ++t) v[t] = decay * w[t] - rate * v[t];
+            if (lowp != nullptr)
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
-                    if (n + t < p.cols) low[t] = (__bf16)v[t];
-            }
+                    if (n + t < cols) lowp[at + t] = (__bf16)v[t];
         }
-        if (whole) *reinterpret_cast<f32x4_any*>(out) = f32x4_any{v[0], v[1], v[2], v[3]};
+        if (whole) *reinterpret_cast<f32x4_any*>(to) = f32x4_any{v[0], v[1], v[2], v[3]};
         else
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                if (n + t < p.cols) out[t] = v[t];
+                if (n + t < cols) to[t] = v[t];
+    };
+    static_for<kW>([&](auto i) __attribute__((always_inline)) {
+        static_for<kW>([&](auto j) __attribute__((always_inline)) { store(decltype(i)::value, decltype(j)::value, acc[decltype(i)::value][decltype(j)::value]); });
     });
 }
 // kFinal: the jobs of the launch leave results, not pairs.
@@ -195,7 +207,8 @@ __device__ __forceinline__ int dealt_tile(int wg, int tiles) {
     if (at >= rest / kNumXcd + (xcd < rest % kNumXcd ? 1 : 0)) return -1;
     return full * kBlock * kNumXcd + xcd * (rest / kNumXcd) + min(xcd, rest % kNumXcd) + at;
 }
-__device__ __forceinline__ PairJob job_of(const PairJobs& jobs, int block) {
+template <int kMax>
+__device__ __forceinline__ PairJob job_of(const PairJobList<kMax>& jobs, int block) {
     int q = 0;
     while (q + 1 < jobs.n && block >= jobs.job[q + 1].first) ++q;
     return jobs.job[__builtin_amdgcn_readfirstlane(q)];
@@ -237,13 +250,13 @@ __device__ __forceinline__ void mfma_pairs_and_load(f32x4& acc, f16x8 b, f16x8 a
                  : "memory", "scc");
 }
 
-template <int kW, bool kFinal>
-__global__ __launch_bounds__(kPairThreads, kW >= 6 ? 1 : 2) void pair_product(PairJobs jobs) {
+template <int kW, bool kFinal, int kMax>
+__global__ __launch_bounds__(kPairThreads, kW >= 6 ? 1 : 2) void pair_product(PairJobList<kMax> jobs) {
     constexpr int kSlots = kPairSlots<kW>, kLoads = kW / 2;            // loads of a part per wavefront
     constexpr uint32_t kPart = kPairPartBytes<kW>, kRing = kSlots * kPart;
     __shared__ PairRing<kW> smem;
     const PairJob p = job_of(jobs, blockIdx.x);
-    const int number = dealt_tile<(kW >= 6 ? 32 : 64)>(blockIdx.x - p.first, p.tiles);
+    const int number = dealt_tile<(kW >= 6 ? 32 : 64)>(blockIdx.x - p.first, p.tiles());
     if (number < 0) return;
     int tm, tn;
     pair_tile_at(p, p.tiles_m, number, tm, tn);
@@ -393,9 +406,8 @@ inline void place_pair_jobs(PairJobs& jobs) {
         PairJob& p = jobs.job[i];
         p.tiles_m = ceil_div(p.m_frags, 2 * kW);
         p.tiles_n = ceil_div(p.n_frags, 2 * kW);
-        p.tiles = p.symmetric ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
         p.first = jobs.blocks;
-        jobs.blocks += ceil_div(p.tiles, kNumXcd) * kNumXcd;
+        jobs.blocks += ceil_div(p.tiles(), kNumXcd) * kNumXcd;
     }
 }
 template <int kW>
@@ -405,9 +417,9 @@ inline double pair_time(PairJobs& jobs) {
     double tiles = 0.0, tile_steps = 0.0, bytes = 0.0, longest = 0.0;
     for (int i = 0; i < jobs.n; ++i) {
         const PairJob& p = jobs.job[i];
-        tiles += p.tiles;
-        tile_steps += (double)p.tiles * p.steps;
-        bytes += (double)p.m_frags * p.n_frags * 1024.0 * (p.Ct != nullptr && !p.symmetric ? 2 : 1);
+        tiles += p.tiles();
+        tile_steps += (double)p.tiles() * p.steps;
+        bytes += (double)p.m_frags * p.n_frags * 1024.0 * (p.result == kPairs && !p.symmetric ? 2 : 1);
         longest = longest > p.steps ? longest : p.steps;
     }
     const double full = floor(tiles / t.slots), rest = tiles - full * t.slots;
@@ -423,11 +435,20 @@ inline double pair_time(PairJobs& jobs, int* tile = nullptr) {
     if (tile != nullptr) *tile = 2 * best + 2;
     return at[best];
 }
+template <int kW, int kMax>
+inline void launch_pair_list(const PairJobs& jobs, hipStream_t s) {
+    PairJobList<kMax> list{};
+    list.n = jobs.n;
+    for (int i = 0; i < jobs.n; ++i) list.job[i] = jobs.job[i];
+    if (jobs.job[0].result != kPairs) pair_product<kW, true, kMax><<<(unsigned)jobs.blocks, kPairThreads, 0, s>>>(list);
+    else pair_product<kW, false, kMax><<<(unsigned)jobs.blocks, kPairThreads, 0, s>>>(list);
+}
 template <int kW>
 inline void launch_pair_tiles(PairJobs& jobs, hipStream_t s) {
     place_pair_jobs<kW>(jobs);
-    if (jobs.job[0].result != kPairs) pair_product<kW, true><<<(unsigned)jobs.blocks, kPairThreads, 0, s>>>(jobs);
-    else pair_product<kW, false><<<(unsigned)jobs.blocks, kPairThreads, 0, s>>>(jobs);
+    if constexpr (kW <= 4)
+        if (jobs.n <= kFewPairJobs) return launch_pair_list<kW, kFewPairJobs>(jobs, s);
+    launch_pair_list<kW, kMaxPairJobs>(jobs, s);
 }
 inline void launch_pair_products(PairJobs& jobs, hipStream_t s) {
     int tile;
