@@ -10,6 +10,7 @@
 #include <utility>
 
 #include "gemm_pairs.h"
+#include "orthogonalise.h"
 
 namespace pcm {
 namespace {
@@ -17,26 +18,8 @@ namespace {
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr int kMaxNsSteps = 10;
 constexpr int kMaxSide = 1 << 20, kMaxShortSide = 1 << 15;
-constexpr int kGroup = 8;                          // matrices of a launch
 // Powers of two of the pairs: entries are at most 1.5 in X, A and B = A P (their largest singular value is), 3.5 in P and 3.5^3 in Q.
 constexpr float kScaleX = 16384.f, kScaleA = 16384.f, kScaleP = 4096.f, kScaleB = 8192.f, kScaleQ = 1024.f;
-
-struct Matrix {
-    const void* in;              // [rows, cols] of `bf16` or fp32
-    float* momentum;             // or null: the iteration is on `in`
-    int64_t ld;
-    int rows, cols, bf16, tall;  // tall: more rows than columns, X is the transpose
-    float mu;
-    int nesterov;
-    double* partial;
-    int parts, first_part;       // of the launch of the squares
-    int tiles_c, tiles, first_tile;
-    f16 *X, *Xt;                 // [m, n] and [n, m] with m <= n
-};
-struct Matrices {
-    Matrix m[kGroup];
-    int n;
-};
 
 constexpr int kCopyTile = 64, kCopyThreads = 256;
 constexpr int kMaxParts = 1024;
@@ -44,7 +27,7 @@ constexpr int kMaxParts = 1024;
 // Four columns of a row of what is to be orthogonalised, from column c on; zero beyond the matrix.  write: the momentum is
 // brought up to date first.
 template <bool kWrite>
-__device__ __forceinline__ f32x4 update_values(const Matrix& q, int r, int c) {
+__device__ __forceinline__ f32x4 update_values(const UpdateMatrix& q, int r, int c) {
     f32x4 u = {0.f, 0.f, 0.f, 0.f};
     if (r >= q.rows || c >= q.cols) return u;
     const int64_t at = (int64_t)r * q.ld + c;
@@ -98,11 +81,11 @@ __device__ inline double workgroup_sum(double x, double* lds) {
     return total;
 }
 
-__global__ __launch_bounds__(kCopyThreads) void update_squares(Matrices list) {
+__global__ __launch_bounds__(kCopyThreads) void update_squares(UpdateMatrices list) {
     __shared__ double lds[kCopyThreads / 64];
     int k = 0;
     while (k + 1 < list.n && (int)blockIdx.x >= list.m[k + 1].first_part) ++k;
-    const Matrix& q = list.m[k];
+    const UpdateMatrix& q = list.m[k];
     const int part = blockIdx.x - q.first_part;
     double sq = 0.0;
     for (int tile = part; tile < q.tiles; tile += q.parts) {
@@ -119,12 +102,12 @@ __global__ __launch_bounds__(kCopyThreads) void update_squares(Matrices list) {
 }
 
 // A tile of 64 x 64: 8 fragments in each orientation.
-__global__ __launch_bounds__(kCopyThreads) void update_to_pairs(Matrices list) {
+__global__ __launch_bounds__(kCopyThreads) void update_to_pairs(UpdateMatrices list) {
     __shared__ double lds[kCopyThreads / 64];
     __shared__ float tile[kCopyTile][kCopyTile + 1];
     int k = 0;
     while (k + 1 < list.n && (int)blockIdx.x >= list.m[k + 1].first_tile) ++k;
-    const Matrix& q = list.m[k];
+    const UpdateMatrix& q = list.m[k];
     const int number = blockIdx.x - q.first_tile;
     const int r0 = number / q.tiles_c * kCopyTile, c0 = number % q.tiles_c * kCopyTile;
     double sq = 0.0;
@@ -177,7 +160,7 @@ __global__ __launch_bounds__(kCopyThreads) void update_to_pairs(Matrices list) {
 
 // A matrix of the call: where it comes from, and what becomes of it.
 struct Task {
-    Matrix in;
+    UpdateMatrix in;
     int result;                  // PairResult
     void* out;
     uint16_t* lowp;
@@ -315,13 +298,13 @@ constexpr int kSegment = 3;
 constexpr double kSegmentGain = 0.95;
 
 int run_group(Task* tasks, int n, int ns_steps, void* workspace, hipStream_t s) {
-    Matrices list{};
-    TaskBuffers buf[kGroup];
+    UpdateMatrices list{};
+    TaskBuffers buf[kOrthGroup];
     list.n = n;
     Carver c(workspace);
     int parts = 0, tiles = 0;
     for (int i = 0; i < n; ++i) {
-        Matrix& q = tasks[i].in;
+        UpdateMatrix& q = tasks[i].in;
         buf[i] = carve_task(c, q.rows, q.cols);
         q.tall = q.rows > q.cols;
         q.tiles_c = ceil_div(q.cols, kCopyTile);
@@ -343,7 +326,7 @@ int run_group(Task* tasks, int n, int ns_steps, void* workspace, hipStream_t s) 
     }
     StageTimer t(ST_ORTH_PRODUCTS, s);
     auto estimate = [&](int segment) {
-        TaskBuffers b[kGroup];
+        TaskBuffers b[kOrthGroup];
         for (int i = 0; i < n; ++i) b[i] = buf[i];
         double us = 0.0;
         iterate(tasks, b, n, ns_steps, segment, [&](PairJobs& jobs) { us += pair_time(jobs); });
@@ -359,7 +342,7 @@ template <class Shape>
 int group_length(int first, int n, Shape shape, size_t& bytes) {
     int count = 0;
     bytes = 0;
-    while (count < kGroup && first + count < n) {
+    while (count < kOrthGroup && first + count < n) {
         int rows, cols;
         shape(first + count, rows, cols);
         const size_t more = task_bytes(rows, cols);
@@ -391,7 +374,7 @@ extern "C" {
 
 PCM_API size_t pcm_orthogonalise_workspace_bytes(int batch, int rows, int cols) {
     if (batch < 1 || !shape_ok(rows, cols) || !shape_supported(rows, cols)) return 0;
-    const int same = batch < kGroup ? batch : kGroup;        // every later group is as long or shorter
+    const int same = batch < kOrthGroup ? batch : kOrthGroup;        // every later group is as long or shorter
     return groups_bytes(same, [&](int, int& r, int& c) { r = rows; c = cols; });
 }
 
@@ -413,7 +396,7 @@ PCM_API int pcm_orthogonalise(const void* update, int64_t update_ld, int64_t upd
     for (int first = 0; first < batch;) {
         size_t bytes;
         const int n = group_length(first, batch, shape, bytes);
-        Task tasks[kGroup] = {};
+        Task tasks[kOrthGroup] = {};
         for (int i = 0; i < n; ++i) {
             Task& t = tasks[i];
             t.in.in = static_cast<const char*>(update) + (int64_t)(first + i) * update_stride * size;
@@ -460,7 +443,7 @@ PCM_API int pcm_muon_step(int n_tensors, const int* rows, const int* cols, const
     for (int first = 0; first < n_tensors;) {
         size_t bytes;
         const int n = group_length(first, n_tensors, shape, bytes);
-        Task tasks[kGroup] = {};
+        Task tasks[kOrthGroup] = {};
         for (int i = 0; i < n; ++i) {
             const int j = first + i;
             const double m = rows[j], k = cols[j];

@@ -9,7 +9,7 @@
 // the forward pass left them: every logit is read once and its gradient written once.
 #include <type_traits>
 
-#include "common.h"
+#include "token_logprobs.h"
 
 namespace pcm {
 namespace {
@@ -19,18 +19,6 @@ constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 
 __device__ inline float infinity() { return __builtin_huge_valf(); }
 __device__ inline int ceil_div_device(int a, int b) { return (int)(((int64_t)a + b - 1) / b); }
-
-struct Logits {
-    const void* z;
-    int64_t ld;
-    const uint8_t* allowed;      // or null
-    int64_t allowed_ld;          // 0: the same tokens for every row
-    const void* tokens;
-    int token_type;
-    int64_t rows;
-    int V;
-    float inv_t;
-};
 
 // The token of a row: -1 where it has none, V - 1 where it is beyond the last.
 __device__ inline int token_of(const Logits& q, int64_t row) {
@@ -136,22 +124,15 @@ __device__ __forceinline__ void each_chunk(const T* row, const uint8_t* allowed,
     }
 }
 
-// What has been seen of a row: s = sum 2^a and t = sum 2^a a with a = z c - R.  r is the logit that R = r c was made from (-inf:
-// none yet); R is rounded, which takes nothing from the sums, as it is the same in all of them.  Logits beyond 1e38, where r c could
-// overflow, have R = 0 and a = (z - r) c.
-struct Sums {
-    float r, R, s, t;
-    __device__ bool far() const { return fabsf(r) > 1e38f && r != -infinity(); }
-};
 // How far above the reference a logit may be, in powers of two: 2^17 such terms still fit.
 constexpr float kHeadroom = 64.f;
 // 0 * -inf would be NaN, and 2^-300 is zero
 __device__ __forceinline__ float times(float p, float a) { return p * fmaxf(a, -300.f); }
-__device__ __forceinline__ float exponent(const Sums& a, float z, float c) { return a.far() ? (z - a.r) * c : __builtin_fmaf(z, c, -a.R); }
+__device__ __forceinline__ float exponent(const RowSums& a, float z, float c) { return a.far() ? (z - a.r) * c : __builtin_fmaf(z, c, -a.R); }
 
 // A logit far above the reference, or the first one, becomes the reference.
-__device__ __forceinline__ void move_reference(Sums& a, float to, float c) {
-    Sums b{to, 0.f, a.s, a.t};
+__device__ __forceinline__ void move_reference(RowSums& a, float to, float c) {
+    RowSums b{to, 0.f, a.s, a.t};
     b.R = b.far() ? 0.f : to * c;
     if (a.r != -infinity()) {
         const float d = a.far() || b.far() ? (a.r - to) * c : a.R - b.R, f = __builtin_amdgcn_exp2f(d);
@@ -163,7 +144,7 @@ __device__ __forceinline__ void move_reference(Sums& a, float to, float c) {
 // How a chunk is added: kFinite every logit is finite, kAny also -inf (excluded tokens), kFar also beyond 1e38.
 enum Care : int { kFinite = 0, kAny = 1, kFar = 2 };
 template <bool kEntropy, int kCare>
-__device__ __forceinline__ void add_chunk(Sums& a, const float (&z)[8], float c) {
+__device__ __forceinline__ void add_chunk(RowSums& a, const float (&z)[8], float c) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float x = kCare == kFar ? exponent(a, z[e], c) : __builtin_fmaf(z[e], c, -a.R);
@@ -175,12 +156,12 @@ __device__ __forceinline__ void add_chunk(Sums& a, const float (&z)[8], float c)
 __device__ __forceinline__ float chunk_max(const float (&z)[8]) {
     return fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(z[0], z[1]), z[2]), z[3]), z[4]), z[5]), z[6]), z[7]);
 }
-__device__ __forceinline__ Sums join(Sums a, Sums b, float c) {
-    if (a.r < b.r) { const Sums x = a; a = b; b = x; }
-    if (a.r == -infinity()) return Sums{a.r, a.R, a.s + b.s, a.t + b.t};        // zeros, or NaN
+__device__ __forceinline__ RowSums join(RowSums a, RowSums b, float c) {
+    if (a.r < b.r) { const RowSums x = a; a = b; b = x; }
+    if (a.r == -infinity()) return RowSums{a.r, a.R, a.s + b.s, a.t + b.t};        // zeros, or NaN
     // b moves to a's reference; nothing is left of sums without one (but a NaN)
     const float d = b.r == -infinity() ? -300.f : (a.far() || b.far() ? (b.r - a.r) * c : b.R - a.R), f = __builtin_amdgcn_exp2f(d);
-    return Sums{a.r, a.R, a.s + f * b.s, a.t + f * (b.t + times(b.s, d))};
+    return RowSums{a.r, a.R, a.s + f * b.s, a.t + f * (b.t + times(b.s, d))};
 }
 
 // Selection of the largest logits.  A token is one 64-bit number, its logit as an integer of the same order above the complement of
@@ -236,23 +217,10 @@ __device__ __forceinline__ uint64_t merge_keys(uint64_t descending, uint64_t asc
     return sort_bitonic<32>(ascending > descending ? ascending : descending, false);
 }
 
-struct ForwardOut {
-    float *logp, *lse, *entropy;     // entropy: or null
-    int top;
-    int32_t* top_ids;
-    float* top_logp;
-};
-// What a part of a row leaves for the launch that joins them.
-struct Parts {
-    Sums* sums;                      // [rows, parts]
-    uint64_t* keys;                  // [rows, parts, top]
-    int parts;
-};
-
 // A row's results, by one lane; and logp of a logit.
 struct RowResult {
     float lse, entropy;
-    __device__ RowResult(const Sums& a) {
+    __device__ RowResult(const RowSums& a) {
         empty = a.s == 0.f;          // nothing allowed, or only logits of -inf
         log2_s = __builtin_amdgcn_logf(a.s);
         lse = empty ? -infinity() : kLn2 * (a.R + log2_s);
@@ -263,10 +231,10 @@ struct RowResult {
     __device__ float lse_of(const Logits& q) const { return !empty && sums.far() ? sums.r * q.inv_t + kLn2 * log2_s : lse; }
     bool empty;
     float log2_s;
-    Sums sums;
+    RowSums sums;
 };
 template <class T>
-__device__ __forceinline__ void store_row(const Logits& q, const ForwardOut& o, int64_t row, const RowResult& res, float c) {
+__device__ __forceinline__ void store_row(const Logits& q, const LogprobsOut& o, int64_t row, const RowResult& res, float c) {
     const int token = token_of(q, row);
     float logp = 0.f;
     if (token >= 0) {
@@ -277,7 +245,7 @@ __device__ __forceinline__ void store_row(const Logits& q, const ForwardOut& o, 
     o.lse[row] = res.lse_of(q);
     if (o.entropy != nullptr) o.entropy[row] = res.entropy;
 }
-__device__ __forceinline__ void store_top(const ForwardOut& o, int64_t row, uint64_t key, const RowResult& res, float c) {
+__device__ __forceinline__ void store_top(const LogprobsOut& o, int64_t row, uint64_t key, const RowResult& res, float c) {
     const int lane = threadIdx.x & 63;
     if (lane >= o.top) return;
     o.top_ids[row * o.top + lane] = key != 0 ? key_token(key) : -1;
@@ -364,16 +332,16 @@ __device__ __forceinline__ uint64_t select_top(TopScratch<kThreads>& lds, const 
 
 // A workgroup per part of a row, in chunks of eight logits per lane.
 template <class T, bool kMask, bool kEntropy, bool kTop, int kThreads>
-__global__ __launch_bounds__(kThreads) void token_logprobs_parts(Logits q, ForwardOut o, Parts parts) {
+__global__ __launch_bounds__(kThreads) void token_logprobs_parts(Logits q, LogprobsOut o, RowParts parts) {
     constexpr int kWaves = kThreads / 64;
-    __shared__ Sums wave_sums[kWaves];
+    __shared__ RowSums wave_sums[kWaves];
     const int64_t row = blockIdx.x / parts.parts;
     const int part = blockIdx.x % parts.parts;
     const T* z_row = static_cast<const T*>(q.z) + row * q.ld;
     const uint8_t* allowed = kMask ? q.allowed + row * q.allowed_ld : nullptr;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float c = q.inv_t * kLog2E, room = kHeadroom / c;
-    Sums a{-infinity(), 0.f, 0.f, 0.f};
+    RowSums a{-infinity(), 0.f, 0.f, 0.f};
     Best best{-infinity(), -1};
     int care = kMask ? kAny : kFinite;                   // of the whole wavefront
     const int units = ceil_div_device(q.V, kThreads * 8), per_part = ceil_div_device(units, parts.parts);
@@ -402,7 +370,7 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_parts(Logits q, Forwa
     });
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
-        const Sums b{__shfl_xor(a.r, d, 64), __shfl_xor(a.R, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)};
+        const RowSums b{__shfl_xor(a.r, d, 64), __shfl_xor(a.R, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)};
         a = join(a, b, c);
     }
     if (kWaves > 1 && lane == 0) wave_sums[wave] = a;
@@ -428,7 +396,7 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_parts(Logits q, Forwa
 // A workgroup per row: the parts of the row.
 constexpr int kJoinThreads = 256;
 template <class T>
-__global__ __launch_bounds__(kJoinThreads) void token_logprobs_join(Logits q, ForwardOut o, Parts parts) {
+__global__ __launch_bounds__(kJoinThreads) void token_logprobs_join(Logits q, LogprobsOut o, RowParts parts) {
     constexpr int kWaves = kJoinThreads / 64;
     __shared__ uint64_t lists[kWaves][64];
     const int64_t row = blockIdx.x;
@@ -443,11 +411,11 @@ __global__ __launch_bounds__(kJoinThreads) void token_logprobs_join(Logits q, Fo
         __syncthreads();
     }
     if (wave != 0) return;
-    Sums a{-infinity(), 0.f, 0.f, 0.f};
+    RowSums a{-infinity(), 0.f, 0.f, 0.f};
     for (int i = lane; i < parts.parts; i += 64) a = join(a, parts.sums[row * parts.parts + i], c);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
-        const Sums b{__shfl_xor(a.r, d, 64), __shfl_xor(a.R, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)};
+        const RowSums b{__shfl_xor(a.r, d, 64), __shfl_xor(a.R, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)};
         a = join(a, b, c);
     }
     const RowResult res(a);
@@ -472,7 +440,7 @@ __device__ __forceinline__ float lanes_sum(float x) {
 }
 constexpr int kNarrowThreads = 256;
 template <class T, bool kMask, int kLanes>
-__global__ __launch_bounds__(kNarrowThreads) void token_logprobs_narrow(Logits q, ForwardOut o) {
+__global__ __launch_bounds__(kNarrowThreads) void token_logprobs_narrow(Logits q, LogprobsOut o) {
     const int64_t row = (int64_t)blockIdx.x * (kNarrowThreads / kLanes) + threadIdx.x / kLanes;
     if (row >= q.rows) return;
     const T* z_row = static_cast<const T*>(q.z) + row * q.ld;
@@ -482,7 +450,7 @@ __global__ __launch_bounds__(kNarrowThreads) void token_logprobs_narrow(Logits q
     float z[2][8];
 #pragma unroll
     for (int h = 0; h < 2; ++h) load_chunk<T, kMask>(z_row, allowed, (h * kLanes + lane) * 8, q.V, z[h]);
-    Sums a{-infinity(), 0.f, 0.f, 0.f};
+    RowSums a{-infinity(), 0.f, 0.f, 0.f};
     const float most = lanes_max<kLanes>(fmaxf(chunk_max(z[0]), chunk_max(z[1])));
     move_reference(a, most, c);
     if (most == -infinity()) a.R = 0.f;
@@ -497,12 +465,6 @@ __global__ __launch_bounds__(kNarrowThreads) void token_logprobs_narrow(Logits q
     a.t = lanes_sum<kLanes>(a.t);
     if (lane == 0) store_row<T>(q, o, row, RowResult(a), c);
 }
-
-struct BackwardArgs {
-    const float *lse, *dlogp, *entropy, *dentropy;       // the last two: both or none
-    void* dz;
-    int64_t dz_ld;
-};
 
 template <class T>
 __device__ inline void store_chunk(T* row, int j, int V, const float (&g)[8]);
@@ -534,7 +496,7 @@ __device__ inline void store_chunk<uint16_t>(uint16_t* row, int j, int V, const 
 // kLanes lanes per row, in chunks of eight logits; kThreads / kLanes rows per workgroup, and a row in `parts` of them.
 constexpr int kGradientThreads = 256;
 template <class T, bool kMask, int kLanes>
-__global__ __launch_bounds__(kGradientThreads) void token_logprobs_gradient(Logits q, BackwardArgs b, int parts) {
+__global__ __launch_bounds__(kGradientThreads) void token_logprobs_gradient(Logits q, LogprobsGradient b, int parts) {
     const int64_t row = (int64_t)(blockIdx.x / parts) * (kGradientThreads / kLanes) + threadIdx.x / kLanes;
     const int part = blockIdx.x % parts;
     if (row >= q.rows) return;
@@ -593,13 +555,13 @@ int forward_parts(int64_t rows, int V) {
 }
 
 template <class T, bool kMask, bool kEntropy, bool kTop>
-void launch_parts(const Logits& q, const ForwardOut& o, const Parts& p, hipStream_t s) {
+void launch_parts(const Logits& q, const LogprobsOut& o, const RowParts& p, hipStream_t s) {
     if (q.V <= kWaveRow) token_logprobs_parts<T, kMask, kEntropy, kTop, 64><<<(unsigned)q.rows, 64, 0, s>>>(q, o, p);
     else token_logprobs_parts<T, kMask, kEntropy, kTop, kWide><<<(unsigned)(q.rows * p.parts), kWide, 0, s>>>(q, o, p);
     if (p.parts > 1) token_logprobs_join<T><<<(unsigned)q.rows, kJoinThreads, 0, s>>>(q, o, p);
 }
 template <class T, bool kMask>
-void launch_forward(const Logits& q, const ForwardOut& o, const Parts& p, hipStream_t s) {
+void launch_forward(const Logits& q, const LogprobsOut& o, const RowParts& p, hipStream_t s) {
     if (q.V <= kNarrow && o.top == 0) {
         with_lanes(q.V, [&](auto lanes) {
             constexpr int kLanes = decltype(lanes)::value, kRows = kNarrowThreads / kLanes;
@@ -613,12 +575,12 @@ void launch_forward(const Logits& q, const ForwardOut& o, const Parts& p, hipStr
     else launch_parts<T, kMask, false, false>(q, o, p, s);
 }
 template <class T>
-void launch_forward(const Logits& q, const ForwardOut& o, const Parts& p, hipStream_t s) {
+void launch_forward(const Logits& q, const LogprobsOut& o, const RowParts& p, hipStream_t s) {
     if (q.allowed != nullptr) launch_forward<T, true>(q, o, p, s);
     else launch_forward<T, false>(q, o, p, s);
 }
 template <class T, bool kMask>
-void launch_backward(const Logits& q, const BackwardArgs& b, hipStream_t s) {
+void launch_backward(const Logits& q, const LogprobsGradient& b, hipStream_t s) {
     if (q.V <= kNarrow) {
         with_lanes(q.V, [&](auto lanes) {
             constexpr int kLanes = decltype(lanes)::value, kRows = kGradientThreads / kLanes;
@@ -630,16 +592,16 @@ void launch_backward(const Logits& q, const BackwardArgs& b, hipStream_t s) {
     token_logprobs_gradient<T, kMask, kGradientThreads><<<(unsigned)(q.rows * parts), kGradientThreads, 0, s>>>(q, b, parts);
 }
 template <class T>
-void launch_backward(const Logits& q, const BackwardArgs& b, hipStream_t s) {
+void launch_backward(const Logits& q, const LogprobsGradient& b, hipStream_t s) {
     if (q.allowed != nullptr) launch_backward<T, true>(q, b, s);
     else launch_backward<T, false>(q, b, s);
 }
 
-Parts carve_parts(Carver& c, int64_t rows, int V, int top) {
-    Parts p{};
+RowParts carve_parts(Carver& c, int64_t rows, int V, int top) {
+    RowParts p{};
     p.parts = top == 0 && V <= kNarrow ? 1 : forward_parts(rows, V);
     if (p.parts == 1) return p;
-    p.sums = c.take<Sums>((size_t)(rows * p.parts));
+    p.sums = c.take<RowSums>((size_t)(rows * p.parts));
     p.keys = c.take<uint64_t>((size_t)(rows * p.parts * top));
     return p;
 }
@@ -691,9 +653,9 @@ PCM_API int pcm_token_logprobs(const void* logits, int64_t logits_ld, int dtype,
     if (!workspace_ok(workspace, workspace_bytes, pcm_token_logprobs_workspace_bytes(rows, V, top))) return PCM_EWORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const Logits q{logits, logits_ld, allowed, allowed_ld, tokens, token_type, rows, V, 1.f / temperature};
-    const ForwardOut o{logp, lse, entropy, top, top_ids, top_logp};
+    const LogprobsOut o{logp, lse, entropy, top, top_ids, top_logp};
     Carver c(workspace);
-    const Parts p = carve_parts(c, rows, V, top);
+    const RowParts p = carve_parts(c, rows, V, top);
     StageTimer t(ST_TOKEN_LOGPROBS, s);
     if (dtype == PCM_F32) launch_forward<float>(q, o, p, s);
     else launch_forward<uint16_t>(q, o, p, s);
@@ -713,7 +675,7 @@ PCM_API int pcm_token_logprobs_backward(const void* logits, int64_t logits_ld, i
     if (rc != PCM_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const Logits q{logits, logits_ld, allowed, allowed_ld, tokens, token_type, rows, V, 1.f / temperature};
-    const BackwardArgs b{lse, dlogp, entropy, dentropy, dlogits, dlogits_ld};
+    const LogprobsGradient b{lse, dlogp, entropy, dentropy, dlogits, dlogits_ld};
     StageTimer t(ST_TOKEN_LOGPROBS_GRAD, s);
     if (dtype == PCM_F32) launch_backward<float>(q, b, s);
     else launch_backward<uint16_t>(q, b, s);
