@@ -32,6 +32,7 @@ struct PairJob {
     union { float gamma, rate; };
     int rows, cols;                              // of out
     int first, tiles_m, tiles_n;                 // first workgroup, tiles: filled in by the launch
+    int splits, first_part;                      // parts that a tile's reduction is done in, number of the first: as well
     __host__ __device__ int tiles() const { return symmetric ? tiles_m * (tiles_m + 1) / 2 : tiles_m * tiles_n; }
 };
 constexpr int kMaxPairJobs = 16;
@@ -42,10 +43,14 @@ template <int kMax>
 struct PairJobList {
     PairJob job[kMax];
     int n;
+    f32x4* parts;                                // sums of the parts of tiles, or null
 };
 struct PairJobs : PairJobList<kMaxPairJobs> {
     int blocks;
 };
+// Reductions in parts are done on tiles of 64: by at most as many workgroups as run side by side, which is what the buffer of parts holds.
+constexpr int kPairPartTile = 2, kPairParts = 512;
+constexpr size_t kPairPartsBytes = (size_t)kPairParts * 64 * 64 * 4;
 
 // Accumulators of a wavefront: tile (i, j), register t of a lane is row 16 i + (lane & 15), column 16 j + 4 (lane >> 4) + t.
 template <int kW>
@@ -256,8 +261,17 @@ __global__ __launch_bounds__(kPairThreads, kW >= 6 ? 1 : 2) void pair_product(Pa
     constexpr uint32_t kPart = kPairPartBytes<kW>, kRing = kSlots * kPart;
     __shared__ PairRing<kW> smem;
     const PairJob p = job_of(jobs, blockIdx.x);
-    const int number = dealt_tile<(kW >= 6 ? 32 : 64)>(blockIdx.x - p.first, p.tiles());
+    constexpr bool kInParts = kW == kPairPartTile && !kFinal;
+    int number = dealt_tile<(kW >= 6 ? 32 : 64)>(blockIdx.x - p.first, p.tiles() * (kInParts ? p.splits : 1));
     if (number < 0) return;
+    int steps = __builtin_amdgcn_readfirstlane(p.steps), first_step = 0, part = 0;
+    if constexpr (kInParts) {
+        part = p.first_part + number;
+        const int split = number % p.splits;
+        number /= p.splits;
+        first_step = __builtin_amdgcn_readfirstlane((int)((int64_t)steps * split / p.splits));
+        steps = __builtin_amdgcn_readfirstlane((int)((int64_t)steps * (split + 1) / p.splits)) - first_step;
+    }
     int tm, tn;
     pair_tile_at(p, p.tiles_m, number, tm, tn);
     const int lane = threadIdx.x & 63;
@@ -275,14 +289,13 @@ __global__ __launch_bounds__(kPairThreads, kW >= 6 ? 1 : 2) void pair_product(Pa
         off[0][r] = (uint32_t)(min(first_m + f, p.m_frags - 1) - first_m) * (kPairFragment * 2u) + (uint32_t)lane * 16u;
         off[1][r] = (uint32_t)(min(first_n + f, p.n_frags - 1) - first_n) * (kPairFragment * 2u) + (uint32_t)lane * 16u;
     }
-    const char* const origin_a = tile_address<true>(p.A + pair_fragment(first_m, 0, p.m_frags));
-    const char* const origin_b = tile_address<true>(p.B + pair_fragment(first_n, 0, p.n_frags));
+    const char* const origin_a = tile_address<true>(p.A + pair_fragment(first_m, first_step, p.m_frags));
+    const char* const origin_b = tile_address<true>(p.B + pair_fragment(first_n, first_step, p.n_frags));
     // (assembly takes them in scalar registers, and the compiler may lose sight of their being the same in every lane)
     const int64_t step_bytes[2] = {pair_fragment(0, 1, __builtin_amdgcn_readfirstlane(p.m_frags)) * 2,
                                    pair_fragment(0, 1, __builtin_amdgcn_readfirstlane(p.n_frags)) * 2};
     // by type of part: where the next one to be requested is
     const char* from[4] = {origin_b + kPairPart * 2, origin_a, origin_b, origin_a + kPairPart * 2};
-    const int steps = __builtin_amdgcn_readfirstlane(p.steps);
     constexpr auto operand = [](int type) { return type == 0 || type == 2 ? 1 : 0; };
     const uint32_t my_lds = lds_base + (uint32_t)(kLoads * wave) * 1024u;
 
@@ -380,7 +393,34 @@ __global__ __launch_bounds__(kPairThreads, kW >= 6 ? 1 : 2) void pair_product(Pa
     for (int i = 0; i < kW; ++i)
 #pragma unroll
         for (int j = 0; j < kW; ++j) asm volatile("" : "+a"(acc[i][j]));
+    if constexpr (kInParts)
+        if (p.splits > 1) {
+            f32x4* const to = jobs.parts + (int64_t)(part * 4 + wave) * (kW * kW * 64) + lane;
+#pragma unroll
+            for (int i = 0; i < kW * kW; ++i) to[i * 64] = acc[i / kW][i % kW];
+            return;
+        }
     pair_epilogue<kW, kFinal>(p, acc, first_m + wm * kW, first_n + wn * kW, tm != tn);
+}
+
+// The sums of the parts, in order, and what is to become of them: a workgroup per tile.
+template <int kMax>
+__global__ __launch_bounds__(kPairThreads) void pair_join(PairJobList<kMax> jobs) {
+    constexpr int kW = kPairPartTile;
+    const PairJob p = job_of(jobs, blockIdx.x);
+    const int number = blockIdx.x - p.first;
+    if (number >= p.tiles()) return;
+    int tm, tn;
+    pair_tile_at(p, p.tiles_m, number, tm, tn);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    PairAccumulators<kW> acc;
+#pragma unroll
+    for (int i = 0; i < kW * kW; ++i) acc[i / kW][i % kW] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const f32x4* from = jobs.parts + (int64_t)((p.first_part + number * p.splits) * 4 + wave) * (kW * kW * 64) + lane;
+    for (int part = 0; part < p.splits; ++part, from += 4 * kW * kW * 64)
+#pragma unroll
+        for (int i = 0; i < kW * kW; ++i) acc[i / kW][i % kW] += from[i * 64];
+    store_pairs<kW>(p, acc, (tm * 2 + (wave >> 1)) * kW, (tn * 2 + (wave & 1)) * kW, tm != tn);
 }
 
 // The fewest microseconds a launch of the jobs is expected to take on tiles of 32 kW: what begins and ends it, its results at 4 TB/s, and per
@@ -399,64 +439,90 @@ constexpr PairTiming kPairTiming = kW == 8   ? PairTiming{8.0, 1.40, 9.0e-3, 256
                                    : kW == 6 ? PairTiming{6.0, 0.74, 5.06e-3, 256}
                                    : kW == 4 ? PairTiming{4.4, 0.36, 2.25e-3, 512}
                                              : PairTiming{3.5, 0.121, 0.86e-3, 512};
-template <int kW>
-inline void place_pair_jobs(PairJobs& jobs) {
+// Tiles and workgroups of the jobs with every reduction in `splits` parts.
+inline void place_pair_jobs(PairJobs& jobs, int kW, int splits = 1) {
     jobs.blocks = 0;
     for (int i = 0; i < jobs.n; ++i) {
         PairJob& p = jobs.job[i];
         p.tiles_m = ceil_div(p.m_frags, 2 * kW);
         p.tiles_n = ceil_div(p.n_frags, 2 * kW);
-        p.first = jobs.blocks;
-        jobs.blocks += ceil_div(p.tiles(), kNumXcd) * kNumXcd;
+        p.splits = splits;
+        p.first = p.first_part = jobs.blocks;
+        jobs.blocks += ceil_div(p.tiles() * splits, kNumXcd) * kNumXcd;
     }
 }
+// How the products of a launch are done: on which tiles, and in how many parts where few tiles have long reductions (the sums then take a
+// launch of their own).  256 x 256 over 4096, 20 us in one part: see kPairJoin.
+struct PairPlan {
+    int tile, splits;
+    double us;
+};
+constexpr double kPairJoin = 5.0;                // us that the launch of the sums takes, beside its bytes
 template <int kW>
-inline double pair_time(PairJobs& jobs) {
+inline double pair_time(PairJobs& jobs, int splits = 1) {
     constexpr PairTiming t = kPairTiming<kW>;
-    place_pair_jobs<kW>(jobs);
+    place_pair_jobs(jobs, kW, splits);
     double tiles = 0.0, tile_steps = 0.0, bytes = 0.0, longest = 0.0;
     for (int i = 0; i < jobs.n; ++i) {
         const PairJob& p = jobs.job[i];
-        tiles += p.tiles();
+        tiles += p.tiles() * splits;
         tile_steps += (double)p.tiles() * p.steps;
         bytes += (double)p.m_frags * p.n_frags * 1024.0 * (p.result == kPairs && !p.symmetric ? 2 : 1);
         longest = longest > p.steps ? longest : p.steps;
     }
     const double full = floor(tiles / t.slots), rest = tiles - full * t.slots;
     auto round = [&](double n) { return n > 0.0 ? (t.alone > n * t.share ? t.alone : n * t.share) : 0.0; };
-    const double steps = (full * round(t.slots) + round(rest)) * (tile_steps / tiles), least = longest * t.alone;
-    return t.fixed + bytes / 4.0e6 + (steps > least ? steps : least);
+    const double steps = (full * round(t.slots) + round(rest)) * (tile_steps / tiles), least = longest / splits * t.alone;
+    const double join = splits > 1 ? kPairJoin + tiles * 2.0 * 16384.0 / 4.0e6 : 0.0;
+    return t.fixed + bytes / 4.0e6 + join + (steps > least ? steps : least);
 }
-inline double pair_time(PairJobs& jobs, int* tile = nullptr) {
-    const double at[4] = {pair_time<2>(jobs), pair_time<4>(jobs), pair_time<6>(jobs), pair_time<8>(jobs)};
-    int best = 0;
-    for (int i = 1; i < 4; ++i)
-        if (at[i] < at[best]) best = i;
-    if (tile != nullptr) *tile = 2 * best + 2;
-    return at[best];
+inline PairPlan plan_pair_products(PairJobs& jobs) {
+    PairPlan best{2, 1, pair_time<2>(jobs)};
+    auto consider = [&](int tile, int splits, double us) {
+        if (us < best.us) best = PairPlan{tile, splits, us};
+    };
+    consider(4, 1, pair_time<4>(jobs));
+    consider(6, 1, pair_time<6>(jobs));
+    consider(8, 1, pair_time<8>(jobs));
+    if (jobs.parts == nullptr || jobs.job[0].result != kPairs) return best;
+    int steps = jobs.job[0].steps;
+    for (int i = 1; i < jobs.n; ++i) steps = steps < jobs.job[i].steps ? steps : jobs.job[i].steps;
+    for (int splits = 2; splits <= 32 && splits * 4 <= steps; splits *= 2) {
+        const double us = pair_time<kPairPartTile>(jobs, splits);
+        if (jobs.blocks > kPairParts) break;
+        consider(kPairPartTile, splits, us);
+    }
+    return best;
 }
 template <int kW, int kMax>
 inline void launch_pair_list(const PairJobs& jobs, hipStream_t s) {
     PairJobList<kMax> list{};
     list.n = jobs.n;
+    list.parts = jobs.parts;
+    int tiles = 0;
     for (int i = 0; i < jobs.n; ++i) list.job[i] = jobs.job[i];
     if (jobs.job[0].result != kPairs) pair_product<kW, true, kMax><<<(unsigned)jobs.blocks, kPairThreads, 0, s>>>(list);
     else pair_product<kW, false, kMax><<<(unsigned)jobs.blocks, kPairThreads, 0, s>>>(list);
+    if (jobs.job[0].splits == 1) return;
+    for (int i = 0; i < jobs.n; ++i) {
+        list.job[i].first = tiles;
+        tiles += list.job[i].tiles();
+    }
+    pair_join<kMax><<<(unsigned)tiles, kPairThreads, 0, s>>>(list);
 }
 template <int kW>
-inline void launch_pair_tiles(PairJobs& jobs, hipStream_t s) {
-    place_pair_jobs<kW>(jobs);
+inline void launch_pair_tiles(PairJobs& jobs, int splits, hipStream_t s) {
+    place_pair_jobs(jobs, kW, splits);
     if constexpr (kW <= 4)
         if (jobs.n <= kFewPairJobs) return launch_pair_list<kW, kFewPairJobs>(jobs, s);
     launch_pair_list<kW, kMaxPairJobs>(jobs, s);
 }
 inline void launch_pair_products(PairJobs& jobs, hipStream_t s) {
-    int tile;
-    pair_time(jobs, &tile);
-    if (tile == 8) launch_pair_tiles<8>(jobs, s);
-    else if (tile == 6) launch_pair_tiles<6>(jobs, s);
-    else if (tile == 4) launch_pair_tiles<4>(jobs, s);
-    else launch_pair_tiles<2>(jobs, s);
+    const PairPlan plan = plan_pair_products(jobs);
+    if (plan.tile == 8) launch_pair_tiles<8>(jobs, 1, s);
+    else if (plan.tile == 6) launch_pair_tiles<6>(jobs, 1, s);
+    else if (plan.tile == 4) launch_pair_tiles<4>(jobs, 1, s);
+    else launch_pair_tiles<2>(jobs, plan.splits, s);
 }
 
 }  // namespace pcm

@@ -226,8 +226,9 @@ PairJob symmetric_product(const f16* A, const f16* B, int m, int k, f16* C, floa
 // from m x m products and A goes on as A <- P A P, and at its end X <- Q X; all of them are symmetric.  In place of the two products over
 // the long side that a step costs this has three m x m ones (A P, (A P) P, P Q).
 template <class Launch>
-void iterate(const Task* tasks, TaskBuffers* buf, int n, int ns_steps, int segment, Launch launch) {
+void iterate(const Task* tasks, TaskBuffers* buf, int n, int ns_steps, int segment, f32x4* parts, Launch launch) {
     PairJobs jobs{};
+    jobs.parts = parts;
     auto each = [&](auto f) {
         for (int i = 0; i < n; ++i) f(tasks[i], buf[i], short_side(tasks[i].in.rows, tasks[i].in.cols), long_side(tasks[i].in.rows, tasks[i].in.cols));
     };
@@ -302,6 +303,7 @@ int run_group(Task* tasks, int n, int ns_steps, void* workspace, hipStream_t s) 
     TaskBuffers buf[kOrthGroup];
     list.n = n;
     Carver c(workspace);
+    f32x4* const sums = c.take<f32x4>(kPairPartsBytes / sizeof(f32x4));
     int parts = 0, tiles = 0;
     for (int i = 0; i < n; ++i) {
         UpdateMatrix& q = tasks[i].in;
@@ -329,11 +331,11 @@ int run_group(Task* tasks, int n, int ns_steps, void* workspace, hipStream_t s) 
         TaskBuffers b[kOrthGroup];
         for (int i = 0; i < n; ++i) b[i] = buf[i];
         double us = 0.0;
-        iterate(tasks, b, n, ns_steps, segment, [&](PairJobs& jobs) { us += pair_time(jobs); });
+        iterate(tasks, b, n, ns_steps, segment, sums, [&](PairJobs& jobs) { us += plan_pair_products(jobs).us; });
         return us;
     };
     const int segment = estimate(kSegment) < kSegmentGain * estimate(1) ? kSegment : 1;
-    iterate(tasks, buf, n, ns_steps, segment, [&](PairJobs& jobs) { launch_pair_products(jobs, s); });
+    iterate(tasks, buf, n, ns_steps, segment, sums, [&](PairJobs& jobs) { launch_pair_products(jobs, s); });
     return launch_status();
 }
 
@@ -360,7 +362,7 @@ size_t groups_bytes(int n, Shape shape) {
         first += group_length(first, n, shape, bytes);
         most = bytes > most ? bytes : most;
     }
-    return most;
+    return most + kPairPartsBytes;
 }
 
 bool misaligned(const void* p, unsigned by) { return (reinterpret_cast<uintptr_t>(p) & (by - 1)) != 0; }

@@ -33,7 +33,7 @@ std::map<const void*, std::string>& kernel_names() {   // by host stub; the libr
     return names;
 }
 std::string call;                                      // the call under way
-int failures = 0, launches = 0, calls = 0, products = 0;
+int failures = 0, launches = 0, calls = 0, products = 0, in_parts = 0;
 int fail_at = -1;                                      // the launch that fails, or -1
 bool check_bounds = false;
 hipError_t last_error = hipSuccess;
@@ -108,12 +108,35 @@ void look_at_products(const std::string& name, int kW, bool final, void** args, 
     const PairJobList<kMax>& list = *static_cast<PairJobList<kMax>*>(args[0]);
     if (list.n < 1 || list.n > kMax) return fail(kernel, "a list longer than its argument");
     int blocks = 0;
+    const int splits = list.job[0].splits;
     for (int i = 0; i < list.n; ++i) {
-        if (list.job[i].first != blocks) fail(kernel, "workgroups that do not follow one another");
-        blocks += (list.job[i].tiles() + 7) / 8 * 8;
-        look_at_job(list.job[i], kW, final);
+        const PairJob& p = list.job[i];
+        if (p.first != blocks || p.first_part != blocks) fail(kernel, "workgroups that do not follow one another");
+        if (p.splits != splits || splits < 1 || splits > p.steps || (splits > 1 && (kW != kPairPartTile || final))) fail(kernel, "parts that do not fit");
+        blocks += (p.tiles() * splits + 7) / 8 * 8;
+        look_at_job(p, kW, final);
+    }
+    if (splits > 1) {
+        if (blocks > kPairParts) fail(kernel, "more parts than their buffer has");
+        touches("parts", list.parts, (size_t)blocks * 64 * 64 * 4, true);
+        in_parts += list.n;
     }
     if ((int)grid.x != blocks) fail(kernel, "a grid that does not fit the jobs");
+}
+template <int kMax>
+void look_at_join(void** args, dim3 grid) {
+    const PairJobList<kMax>& list = *static_cast<PairJobList<kMax>*>(args[0]);
+    int tiles = 0;
+    for (int i = 0; i < list.n; ++i) {
+        const PairJob& p = list.job[i];
+        if (p.first != tiles) fail(kernel, "workgroups that do not follow one another");
+        tiles += p.tiles();
+        touches("parts", list.parts + (int64_t)p.first_part * 1024, (size_t)p.tiles() * p.splits * 64 * 64 * 4, false);
+        touches("C", p.C, pairs_bytes(p.m_frags, p.n_frags / 2), true);
+        if (p.Ct != nullptr && p.Ct != p.C) touches("C transposed", p.Ct, pairs_bytes(p.n_frags, p.m_frags / 2), true);
+        if (p.D != nullptr) touches("D", p.D, pairs_bytes(p.m_frags, p.n_frags / 2), false);
+    }
+    if ((int)grid.x != tiles) fail(kernel, "a grid that does not fit the jobs");
 }
 void look_at_matrices(bool squares, void** args, dim3 grid) {
     const UpdateMatrices& list = *static_cast<UpdateMatrices*>(args[0]);
@@ -164,6 +187,11 @@ void look_at_launch(const std::string& name, void** args, dim3 grid) {
         const bool final = name.compare(comma + 2, 4, "true") == 0;
         if (kMax == kFewPairJobs) look_at_products<kFewPairJobs>(name, kW, final, args, grid);
         else if (kMax == kMaxPairJobs) look_at_products<kMaxPairJobs>(name, kW, final, args, grid);
+        else fail(kernel, "an unknown list");
+    } else if (has("pair_join<")) {
+        const int kMax = number(name.find("pair_join<") + 10);
+        if (kMax == kFewPairJobs) look_at_join<kFewPairJobs>(args, grid);
+        else if (kMax == kMaxPairJobs) look_at_join<kMaxPairJobs>(args, grid);
         else fail(kernel, "an unknown list");
     } else if (has("update_squares")) {
         look_at_matrices(true, args, grid);
@@ -396,6 +424,7 @@ int main(int argc, char** argv) {
     if (what == "bounds") bounds();
     else if (what == "errors") errors();
     else return 2;
-    printf("%d calls, %d products, %d failures\n", calls, products, failures);
+    if (what == "bounds" && in_parts == 0) fail("products", "none was done in parts");
+    printf("%d calls, %d products, %d of them in parts, %d failures\n", calls, products, in_parts, failures);
     return failures == 0 ? 0 : 1;
 }
