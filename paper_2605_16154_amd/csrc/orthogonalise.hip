@@ -7,6 +7,7 @@
 // Launches: the squares of the matrix (in 64 bits, and the momentum where there is one), the matrix divided by its norm
 // in both orientations as pairs (pairs.h), then three products per step; the last one writes the result or the weights.
 // Matrices of a call share the launches as long as they are small.
+#include <algorithm>
 #include <utility>
 
 #include "gemm_pairs.h"
@@ -291,11 +292,12 @@ void iterate(const Task* tasks, TaskBuffers* buf, int n, int ns_steps, int segme
         go();
     }
 }
-// Longer segments save time where the long side is long or the matrix large; what is off in A in the directions that the matrix hardly has
-// grows by 3.4445^2 a step within a segment, where in X it grows by 3.4445: over three steps to 140 times 2^-22, over all five it spoils the
-// result.  In 64-bit arithmetic with rounded operands segments of three are as exact as fp32 products (0.4 to 2 times their error), and
-// a step at a time is better (0.2 to 0.6 times): so that is taken where it costs no more than a twentieth.
-constexpr int kSegment = 3;
+// Longer segments save time where the long side is long or the matrix large; but what is off in A in the directions that the matrix hardly
+// has grows by 3.4445^2 a step within a segment, where in X it grows by 3.4445.  Errors on matrices like gradients in relation to those of
+// fp32 products, segments of 1 / 2 / 3: short side 28 1.0 / 1.2 / 9.5, 63 1.0 / 1.5 / 5.6, 101 0.9 / 1.3 / 3.1, 195 0.7 / 1.1 / 2.1, 288 0.8 /
+// 1.4 / 1.3, 651 0.8 / 1.1 / 1.2, 1164 0.9 / 0.9 / 1.2 (all five steps in one spoil the result).  So segments of three are for short sides from
+// kLongSegmentSide on, where they save more than a twentieth.
+constexpr int kSegment = 3, kLongSegmentSide = 256;
 constexpr double kSegmentGain = 0.95;
 
 int run_group(Task* tasks, int n, int ns_steps, void* workspace, hipStream_t s) {
@@ -334,7 +336,9 @@ int run_group(Task* tasks, int n, int ns_steps, void* workspace, hipStream_t s) 
         iterate(tasks, b, n, ns_steps, segment, sums, [&](PairJobs& jobs) { us += plan_pair_products(jobs).us; });
         return us;
     };
-    const int segment = estimate(kSegment) < kSegmentGain * estimate(1) ? kSegment : 1;
+    int shortest = kMaxShortSide;
+    for (int i = 0; i < n; ++i) shortest = std::min(shortest, short_side(tasks[i].in.rows, tasks[i].in.cols));
+    const int segment = shortest >= kLongSegmentSide && estimate(kSegment) < kSegmentGain * estimate(1) ? kSegment : 1;
     iterate(tasks, buf, n, ns_steps, segment, sums, [&](PairJobs& jobs) { launch_pair_products(jobs, s); });
     return launch_status();
 }
