@@ -299,11 +299,18 @@ __global__ __launch_bounds__(kPairThreads, kW >= 6 ? 1 : 2) void pair_product(Pa
     constexpr auto operand = [](int type) { return type == 0 || type == 2 ? 1 : 0; };
     const uint32_t my_lds = lds_base + (uint32_t)(kLoads * wave) * 1024u;
 
+    // Small tiles have the registers for the sums of the two products with a lo by themselves: the sums of hi hi then round a third as often
+    // (short side 40 over 1505 fp32: errors 1.9 times those of fp32 products, so 1.1).
+    constexpr bool kApart = kW <= 4;
     PairAccumulators<kW> acc;
+    PairAccumulators<kApart ? kW : 1> low;
 #pragma unroll
     for (int i = 0; i < kW; ++i)
 #pragma unroll
-        for (int j = 0; j < kW; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < kW; ++j) {
+            acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if constexpr (kApart) low[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
 
     f16x8 set[4][kW];                                    // fragments, by type of part
     const uint32_t read_base[2] = {lds_base + (uint32_t)(wm * kW) * 1024u + (uint32_t)lane * 16u,
@@ -351,11 +358,15 @@ __global__ __launch_bounds__(kPairThreads, kW >= 6 ? 1 : 2) void pair_product(Pa
             constexpr int n = decltype(number)::value, i = n / kW, j = (i & 1) ? kW - 1 - n % kW : n % kW;
             // load l is issued at MFMA l * kMfmas / kTotal
             constexpr int l = (n * kTotal + kMfmas - 1) / kMfmas, type = (kType + l / kLoads) & 3;
+            f32x4& sum = [&]() -> f32x4& {
+                if constexpr (kApart && !(kA == 1 && kB == 2)) return low[i][j];
+                else return acc[i][j];
+            }();
             if constexpr (l < kTotal && l * kMfmas / kTotal == n) {
                 constexpr uint32_t to = (uint32_t)((kSlot + l / kLoads) % kSlots) * kPart + (l % kLoads) * 1024u;
-                mfma_pairs_and_load<to>(acc[i][j], set[kB][j], set[kA][i], from[type], off[operand(type)][l % kLoads], my_lds);
+                mfma_pairs_and_load<to>(sum, set[kB][j], set[kA][i], from[type], off[operand(type)][l % kLoads], my_lds);
             } else {
-                mfma_pairs(acc[i][j], set[kB][j], set[kA][i]);
+                mfma_pairs(sum, set[kB][j], set[kA][i]);
             }
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (l < kTotal && l * kMfmas / kTotal == n && l % kLoads == kLoads - 1) from[type] += step_bytes[operand(type)];
@@ -392,7 +403,13 @@ __global__ __launch_bounds__(kPairThreads, kW >= 6 ? 1 : 2) void pair_product(Pa
 #pragma unroll
     for (int i = 0; i < kW; ++i)
 #pragma unroll
-        for (int j = 0; j < kW; ++j) asm volatile("" : "+a"(acc[i][j]));
+        for (int j = 0; j < kW; ++j) {
+            asm volatile("" : "+a"(acc[i][j]));
+            if constexpr (kApart) {
+                asm volatile("" : "+a"(low[i][j]));
+                acc[i][j] += low[i][j];
+            }
+        }
     if constexpr (kInParts)
         if (p.splits > 1) {
             f32x4* const to = jobs.parts + (int64_t)(part * 4 + wave) * (kW * kW * 64) + lane;

@@ -294,9 +294,9 @@ void iterate(const Task* tasks, TaskBuffers* buf, int n, int ns_steps, int segme
 }
 // Longer segments save time where the long side is long or the matrix large; but what is off in A in the directions that the matrix hardly
 // has grows by 3.4445^2 a step within a segment, where in X it grows by 3.4445.  Errors on matrices like gradients in relation to those of
-// fp32 products, segments of 1 / 2 / 3: short side 28 1.0 / 1.2 / 9.5, 63 1.0 / 1.5 / 5.6, 101 0.9 / 1.3 / 3.1, 195 0.7 / 1.1 / 2.1, 288 0.8 /
-// 1.4 / 1.3, 651 0.8 / 1.1 / 1.2, 1164 0.9 / 0.9 / 1.2 (all five steps in one spoil the result).  So segments of three are for short sides from
-// kLongSegmentSide on, where they save more than a twentieth.
+// fp32 products, segments of 1 / 2 / 3: short side 28 0.6 / 0.7 / 7.3, 63 0.9 / 1.1 / 5.2, 101 0.7 / 1.0 / 2.5, 195 0.5 / 0.8 / 1.6, 288 0.6 /
+// 1.1 / 1.0, 651 0.5 / 0.7 / 0.8, 1164 0.5 / 0.6 / 0.7 (all five steps in one spoil the result).  So segments of three are for short sides from
+// kLongSegmentSide on, where they save more than a twentieth (64 x 11008 138 us a step at a time, 101 in segments of three).
 constexpr int kSegment = 3, kLongSegmentSide = 256;
 constexpr double kSegmentGain = 0.95;
 
