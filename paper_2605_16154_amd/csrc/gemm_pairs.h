@@ -440,22 +440,22 @@ __global__ __launch_bounds__(kPairThreads) void pair_join(PairJobList<kMax> jobs
     store_pairs<kW>(p, acc, (tm * 2 + (wave >> 1)) * kW, (tn * 2 + (wave & 1)) * kW, tm != tn);
 }
 
-// The fewest microseconds a launch of the jobs is expected to take on tiles of 32 kW: what begins and ends it, its results at 4 TB/s, and per
-// round of workgroups its steps.  A step of a workgroup takes `alone` where few run (the matrix pipe; kW = 2: loads and barriers) and each of
-// the chip's `share` where many do: at full load the power cap sets the clock, at 1.4 PFLOP/s of fp16 products (kW = 2: the path from L2 into
-// LDS, 70 GB/s per CU).  Measured against this, in us, tiles of 64 / 128 / 192 / 256: symmetric 256 over 1024 7.5 / 15.9 / 30.3 / 50.5
-// (estimated 7.6 / 16.1 / 29.8 / 53), 1024 over 1024 8.5 / 17.2 / 33 / 54 (8.7 / 17 / 31 / 54), 2048 over 2048 38 / 36 / 62 / 98 (43 / 32 /
-// 58 / 102), 4096 over 4096 244 / 199 / 155 / 211 (266 / 215 / 188 / 206); 1024 x 2816 over 1024 23.2 / 22.4 / 37 / 57 (29 / 23 / 36 / 59),
-// 4096 x 11008 over 4096 1131 / 803 / 781 / 761 (1315 / 888 / 925 / 894).
+// The microseconds a launch of the jobs is expected to take on tiles of 32 kW: what begins and ends it, its results at 4 TB/s, and per round of
+// workgroups its steps.  A step takes `alone` where few workgroups run (the matrix pipe; kW = 2: loads and barriers), `shared` for each of
+// those that a CU has more than one of, and `share` for each of the chip's where that is more: at full load the power cap sets the clock, at
+// 1.3 to 1.6 PFLOP/s of fp16 products (kW = 2: the path from L2 into LDS, 70 GB/s per CU).  Measured, in us, tiles of 64 / 128 / 192 / 256:
+// symmetric 256 over 1024 7.5 / 15.9 / 30 / 50 (estimated 7.4 / 19.5 / 30 / 62), 1024 over 1024 8.5 / 17.2 / 33 / 54 (8.3 / 20.4 / 31 / 63),
+// 2048 over 2048 38 / 36 / 62 / 98 (44 / 39 / 58 / 114), 4096 over 4096 255 / 202 / 176 / 220 (266 / 215 / 175 / 223); 1024 x 2816 over 1024 23 /
+// 22 / 37 / 57 (29 / 25 / 36 / 68), 4096 x 11008 over 4096 1170 / 877 / 850 / 790 (1315 / 888 / 864 / 813).
 struct PairTiming {
-    double fixed, alone, share;
+    double fixed, alone, shared, share;
     int slots;
 };
 template <int kW>
-constexpr PairTiming kPairTiming = kW == 8   ? PairTiming{8.0, 1.40, 9.0e-3, 256}
-                                   : kW == 6 ? PairTiming{6.0, 0.74, 5.06e-3, 256}
-                                   : kW == 4 ? PairTiming{4.4, 0.36, 2.25e-3, 512}
-                                             : PairTiming{3.5, 0.121, 0.86e-3, 512};
+constexpr PairTiming kPairTiming = kW == 8   ? PairTiming{14.0, 1.50, 1.50, 7.9e-3, 256}
+                                   : kW == 6 ? PairTiming{6.0, 0.74, 0.74, 4.7e-3, 256}
+                                   : kW == 4 ? PairTiming{4.4, 0.47, 0.36, 2.25e-3, 512}
+                                             : PairTiming{3.5, 0.121, 0.22, 0.86e-3, 512};
 // Tiles and workgroups of the jobs with every reduction in `splits` parts.
 inline void place_pair_jobs(PairJobs& jobs, int kW, int splits = 1) {
     jobs.blocks = 0;
@@ -488,7 +488,10 @@ inline double pair_time(PairJobs& jobs, int splits = 1) {
         longest = longest > p.steps ? longest : p.steps;
     }
     const double full = floor(tiles / t.slots), rest = tiles - full * t.slots;
-    auto round = [&](double n) { return n > 0.0 ? (t.alone > n * t.share ? t.alone : n * t.share) : 0.0; };
+    auto round = [&](double n) {
+        const double each = n > 256.0 ? ceil(n / 256.0) * t.shared : t.alone;
+        return n > 0.0 ? (each > n * t.share ? each : n * t.share) : 0.0;
+    };
     const double steps = (full * round(t.slots) + round(rest)) * (tile_steps / tiles), least = longest / splits * t.alone;
     const double join = splits > 1 ? kPairJoin + tiles * 2.0 * 16384.0 / 4.0e6 : 0.0;
     return t.fixed + bytes / 4.0e6 + join + (steps > least ? steps : least);
