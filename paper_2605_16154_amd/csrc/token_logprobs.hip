@@ -146,13 +146,16 @@ __device__ __forceinline__ void move_reference(RowSums& a, float to, float c) {
 enum Care : int { kFinite = 0, kAny = 1, kFar = 2 };
 template <bool kEntropy, int kCare>
 __device__ __forceinline__ void add_chunk(RowSums& a, const float (&z)[8], float c) {
+    float s = 0.f, t = 0.f;              // of the chunk: what a lane adds up one by one is then an eighth as long
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float x = kCare == kFar ? exponent(a, z[e], c) : __builtin_fmaf(z[e], c, -a.R);
-        const float p = __builtin_amdgcn_exp2f(x);
-        a.s += p;
-        if (kEntropy) a.t = __builtin_fmaf(p, kCare == kFinite ? x : fmaxf(x, -300.f), a.t);
+        const float p = __builtin_amdgcn_exp2f(x), y = kCare == kFinite ? x : fmaxf(x, -300.f);
+        s = e == 0 ? p : s + p;
+        if (kEntropy) t = e == 0 ? p * y : __builtin_fmaf(p, y, t);
     }
+    a.s += s;
+    if (kEntropy) a.t += t;
 }
 __device__ __forceinline__ float chunk_max(const float (&z)[8]) {
     return fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(z[0], z[1]), z[2]), z[3]), z[4]), z[5]), z[6]), z[7]);
