@@ -233,6 +233,9 @@ __device__ __forceinline__ PairJob job_of(const PairJobList<kMax>& jobs, int blo
 // 822 -> 783.)  One workgroup per CU for kW = 8 and 6, two for 4 and 2.
 template <int kW> constexpr int kPairSlots = kW == 6 ? 12 : kW == 2 ? 16 : 10;
 template <int kW> constexpr int kPairPeriod = kW == 6 ? 3 : kW == 2 ? 4 : 5;
+// What bounds it: with few workgroups the matrix pipe (256-wide tile, 192 MFMAs a step: 1.28 us, at 2.4 GHz every cycle); with all CUs at work the
+// board's power cap, which takes the clock to 1.9 GHz (symmetric 4096 over 4096 1.6 us a step on 136 CUs, the matrix pipes 72 to 80 % busy over whole
+// launches).  Without the epilogue 3 to 10 % less time, with all loads from the first step 3 to 8.
 template <int kW> constexpr uint32_t kPairPartBytes = 2u * kW * kPairPart * 2u;
 // Steps beyond the last one that a tile requests (and nobody reads): so far behind a matrix there has to be memory.
 constexpr int kPairStepsBeyond = 4;
@@ -267,10 +270,12 @@ __global__ __launch_bounds__(kPairThreads, kW >= 6 ? 1 : 2) void pair_product(Pa
     int steps = __builtin_amdgcn_readfirstlane(p.steps), first_step = 0, part = 0;
     if constexpr (kInParts) {
         part = p.first_part + number;
-        const int split = number % p.splits;
-        number /= p.splits;
-        first_step = __builtin_amdgcn_readfirstlane((int)((int64_t)steps * split / p.splits));
-        steps = __builtin_amdgcn_readfirstlane((int)((int64_t)steps * (split + 1) / p.splits)) - first_step;
+        if (p.splits > 1) {              // (up to 32 parts of up to 2^15 steps)
+            const int split = number % p.splits;
+            number /= p.splits;
+            first_step = __builtin_amdgcn_readfirstlane(steps * split / p.splits);
+            steps = __builtin_amdgcn_readfirstlane(steps * (split + 1) / p.splits) - first_step;
+        }
     }
     int tm, tn;
     pair_tile_at(p, p.tiles_m, number, tm, tn);
@@ -420,7 +425,8 @@ __global__ __launch_bounds__(kPairThreads, kW >= 6 ? 1 : 2) void pair_product(Pa
     pair_epilogue<kW, kFinal>(p, acc, first_m + wm * kW, first_n + wn * kW, tm != tn);
 }
 
-// The sums of the parts, in order, and what is to become of them: a workgroup per tile.
+// The sums of the parts, in order, and what is to become of them: a workgroup per tile.  Products with it, in one part / as planned: symmetric 64 over 2048
+// 11.0 / 9.0 us, over 11008 45 / 12.8, 256 over 4096 19.4 / 11.0, 512 over 11008 51 / 21.7.
 template <int kMax>
 __global__ __launch_bounds__(kPairThreads) void pair_join(PairJobList<kMax> jobs) {
     constexpr int kW = kPairPartTile;
@@ -434,7 +440,20 @@ __global__ __launch_bounds__(kPairThreads) void pair_join(PairJobList<kMax> jobs
 #pragma unroll
     for (int i = 0; i < kW * kW; ++i) acc[i / kW][i % kW] = f32x4{0.f, 0.f, 0.f, 0.f};
     const f32x4* from = jobs.parts + (int64_t)((p.first_part + number * p.splits) * 4 + wave) * (kW * kW * 64) + lane;
-    for (int part = 0; part < p.splits; ++part, from += 4 * kW * kW * 64)
+    constexpr int kStride = 4 * kW * kW * 64, kRead = 4;              // parts whose loads are under way together
+    int part = 0;
+    for (; part + kRead <= p.splits; part += kRead, from += kRead * kStride) {
+        f32x4 one[kRead][kW * kW];
+#pragma unroll
+        for (int r = 0; r < kRead; ++r)
+#pragma unroll
+            for (int i = 0; i < kW * kW; ++i) one[r][i] = from[r * kStride + i * 64];
+#pragma unroll
+        for (int r = 0; r < kRead; ++r)
+#pragma unroll
+            for (int i = 0; i < kW * kW; ++i) acc[i / kW][i % kW] += one[r][i];
+    }
+    for (; part < p.splits; ++part, from += kStride)
 #pragma unroll
         for (int i = 0; i < kW * kW; ++i) acc[i / kW][i % kW] += from[i * 64];
     store_pairs<kW>(p, acc, (tm * 2 + (wave >> 1)) * kW, (tn * 2 + (wave & 1)) * kW, tm != tn);
@@ -469,7 +488,7 @@ inline void place_pair_jobs(PairJobs& jobs, int kW, int splits = 1) {
     }
 }
 // How the products of a launch are done: on which tiles, and in how many parts where few tiles have long reductions (the sums then take a
-// launch of their own).  256 x 256 over 4096, 20 us in one part: see kPairJoin.
+// launch of their own, see pair_join).
 struct PairPlan {
     int tile, splits;
     double us;
