@@ -619,6 +619,18 @@ RowParts carve_parts(Carver& c, int64_t rows, int V, int top) {
     return p;
 }
 
+// A launch has fewer than 2^32 threads, at most kWide for a row: more rows take several launches (never of parts, which few rows have).
+constexpr int64_t kRowsPerLaunch = 1 << 23;
+Logits rows_from(Logits q, int64_t row, int64_t rows, int dtype) {
+    q.z = static_cast<const char*>(q.z) + row * q.ld * (dtype == PCM_F32 ? 4 : 2);
+    q.tokens = static_cast<const char*>(q.tokens) + row * (q.token_type == PCM_TOKEN_U8 ? 1 : q.token_type == PCM_TOKEN_I32 ? 4 : 8);
+    if (q.allowed != nullptr) q.allowed += row * q.allowed_ld;
+    q.rows = std::min(rows - row, kRowsPerLaunch);
+    return q;
+}
+template <class P>
+P* from(P* p, int64_t i) { return p == nullptr ? nullptr : p + i; }
+
 constexpr int64_t kMaxRows = 0x7fffffff;
 constexpr int kMaxVocabulary = 1 << 30;
 
@@ -666,12 +678,15 @@ PCM_API int pcm_token_logprobs(const void* logits, int64_t logits_ld, int dtype,
     if (!workspace_ok(workspace, workspace_bytes, pcm_token_logprobs_workspace_bytes(rows, V, top))) return PCM_EWORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const Logits q{logits, logits_ld, allowed, allowed_ld, tokens, token_type, rows, V, 1.f / temperature};
-    const LogprobsOut o{logp, lse, entropy, top, top_ids, top_logp};
     Carver c(workspace);
     const RowParts p = carve_parts(c, rows, V, top);
     StageTimer t(ST_TOKEN_LOGPROBS, s);
-    if (dtype == PCM_F32) launch_forward<float>(q, o, p, s);
-    else launch_forward<uint16_t>(q, o, p, s);
+    for (int64_t row = 0; row < rows; row += kRowsPerLaunch) {
+        const Logits some = rows_from(q, row, rows, dtype);
+        const LogprobsOut to{logp + row, lse + row, from(entropy, row), top, from(top_ids, row * top), from(top_logp, row * top)};
+        if (dtype == PCM_F32) launch_forward<float>(some, to, p, s);
+        else launch_forward<uint16_t>(some, to, p, s);
+    }
     return launch_status();
 }
 
@@ -688,10 +703,14 @@ PCM_API int pcm_token_logprobs_backward(const void* logits, int64_t logits_ld, i
     if (rc != PCM_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const Logits q{logits, logits_ld, allowed, allowed_ld, tokens, token_type, rows, V, 1.f / temperature};
-    const LogprobsGradient b{lse, dlogp, entropy, dentropy, dlogits, dlogits_ld};
     StageTimer t(ST_TOKEN_LOGPROBS_GRAD, s);
-    if (dtype == PCM_F32) launch_backward<float>(q, b, s);
-    else launch_backward<uint16_t>(q, b, s);
+    for (int64_t row = 0; row < rows; row += kRowsPerLaunch) {
+        const Logits some = rows_from(q, row, rows, dtype);
+        const LogprobsGradient b{lse + row, dlogp + row, from(entropy, row), from(dentropy, row),
+                                 static_cast<char*>(dlogits) + row * dlogits_ld * (dtype == PCM_F32 ? 4 : 2), dlogits_ld};
+        if (dtype == PCM_F32) launch_backward<float>(some, b, s);
+        else launch_backward<uint16_t>(some, b, s);
+    }
     return launch_status();
 }
 

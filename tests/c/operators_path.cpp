@@ -34,6 +34,7 @@ std::map<const void*, std::string>& kernel_names() {   // by host stub; the libr
 }
 std::string call;                                      // the call under way
 int failures = 0, launches = 0, calls = 0, products = 0, in_parts = 0;
+int64_t rows_seen = 0;                                 // of the logits of a call
 int fail_at = -1;                                      // the launch that fails, or -1
 bool check_bounds = false;
 hipError_t last_error = hipSuccess;
@@ -205,6 +206,7 @@ void look_at_launch(const std::string& name, void** args, dim3 grid) {
         look_at_logits(q, size);
         if (p.parts > 1) look_at_parts(q, o, p, !joins);
         if (joins || p.parts == 1) look_at_outputs(q, o);
+        if (!joins) rows_seen += q.rows;
         if ((int64_t)grid.x != q.rows * (joins ? 1 : p.parts)) fail(kernel, "a grid that does not fit the rows");
         if (!joins && (int64_t)p.parts * 2048 > q.V + 2048 && p.parts > 1) fail(kernel, "more parts than the row has");
     } else if (has("token_logprobs_narrow<")) {
@@ -212,6 +214,7 @@ void look_at_launch(const std::string& name, void** args, dim3 grid) {
         const int lanes = number(name.rfind(", ", name.find('>')) + 2);
         look_at_logits(q, size);
         look_at_outputs(q, *static_cast<LogprobsOut*>(args[1]));
+        rows_seen += q.rows;
         if (q.V > 16 * lanes) fail(kernel, "a row that its lanes do not hold");
         if ((int64_t)grid.x * (256 / lanes) < q.rows) fail(kernel, "a grid that does not fit the rows");
     } else if (has("token_logprobs_gradient<")) {
@@ -219,6 +222,7 @@ void look_at_launch(const std::string& name, void** args, dim3 grid) {
         const LogprobsGradient& b = *static_cast<LogprobsGradient*>(args[1]);
         const int lanes = number(name.rfind(", ", name.find('>')) + 2), parts = *static_cast<int*>(args[2]);
         look_at_logits(q, size);
+        rows_seen += q.rows;
         for (const float* p : {b.lse, b.dlogp, b.entropy, b.dentropy})
             if (p != nullptr) touches("a value per row", p, (size_t)q.rows * 4, false);
         touches_rows(b.dz == q.z ? "logits" : "the gradient", b.dz, q.rows, q.V, b.dz_ld, size, true);
@@ -256,7 +260,8 @@ hipError_t hipLaunchKernel(const void* stub, dim3 grid, dim3 block, void** args,
     if (check_bounds) {
         const std::string& name = kernel_names()[stub];
         kernel = name.c_str();
-        if (grid.x == 0 || grid.y != 1 || grid.z != 1 || block.x * block.y * block.z > 1024) fail(kernel, "an empty or too large grid");
+        if (grid.x == 0 || grid.y != 1 || grid.z != 1 || block.x * block.y * block.z > 1024 || (uint64_t)grid.x * block.x >> 32)
+            fail(kernel, "an empty or too large grid");
         spans.clear();
         look_at_launch(name, args, grid);
         check_overlaps();
@@ -282,6 +287,7 @@ void begin(const char* text) {
     call = text;
     regions.clear();
     launches = 0;
+    rows_seen = 0;
     last_error = hipSuccess;
     ++calls;
 }
@@ -392,6 +398,15 @@ void bounds() {
                     expect(backward(c, top == 0), PCM_OK);
                 }
         }
+    for (int64_t rows : {(int64_t)8388607, (int64_t)8388609, (int64_t)70000001, (int64_t)0x7fffffff})    // launches of less than 2^32 threads
+        for (int V : {1, 2, 300, 2000, 5000})
+            for (int top : {0, 1}) {
+                const RowsCall c{rows, V, top ? PCM_F32 : PCM_BF16, V % 3, V % 2 ? 2 : 1, top, true, top};
+                expect(forward(c), PCM_OK);
+                if (rows_seen != rows) fail("the call", "not every row once");
+                expect(backward(c, top == 0), PCM_OK);
+                if (rows_seen != rows) fail("the call", "not every row once");
+            }
     expect(forward({2, 1 << 30, PCM_BF16, PCM_TOKEN_I64, 1, 5, true, 0}), PCM_OK);
     expect(backward({2, 1 << 30, PCM_BF16, PCM_TOKEN_I64, 1, 5, true, 0}, false), PCM_OK);
     expect(forward({2, (1 << 30) + 1, PCM_BF16, PCM_TOKEN_I64, 1, 0, true, 0}), PCM_EUNSUPPORTED);
