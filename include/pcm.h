@@ -501,9 +501,12 @@ PCM_API int pcm_token_logprobs_backward(const void* logits, int64_t logits_ld, i
  * X_0 = G / |G|_F (taken transposed where G has more rows than columns; the result is transposed back).  Every singular value s
  * becomes a s + b s^3 + c s^5 per step: after five steps those above 0.002 |G|_F lie in [0.68, 1.21].
  * Products are carried to fp32 accuracy (operands as pairs of fp16 values, fp32 sums).
+ * (How they are done depends on the sizes of all matrices that share launches, so a matrix's last bits may depend on the others of its
+ * call; the same call gives the same bits.)
  *
  *   update    device [batch] matrices of rows x cols of dtype: rows update_ld >= cols values apart, matrices update_stride
- *   out       the same with out_ld, out_stride >= (rows - 1) out_ld + cols; may be the update itself
+ *   out       the same with out_ld, out_stride >= (rows - 1) out_ld + cols; may be the update itself,
+ *             with the same strides
  *   ns_steps  1 .. 10
  * A matrix of zeros gives zeros; one that holds a NaN or an infinity gives NaN throughout.
  * Limits: 1 <= rows, cols <= 2^20, the smaller of them <= 2^15.

@@ -274,6 +274,28 @@ def test_rows_beyond_32_bit_offsets():
     _check_backward(z, zd, tokens, rng.standard_normal(3), out=z)
 
 
+@pytest.mark.parametrize("top", (0, 2))
+def test_more_rows_than_a_launch_takes(top):
+    rows, V, tail = 2 ** 23 + 7, 4, 64
+    gen = torch.Generator("cuda").manual_seed(4)
+    z = torch.randn(rows, V, generator=gen, device="cuda")
+    tokens = torch.randint(0, V, (rows,), generator=gen, device="cuda", dtype=torch.uint8)
+    allowed = torch.rand(rows, V, generator=gen, device="cuda") < 0.8
+    pcm = _pcm()
+    whole = pcm.pcm_token_logprobs(z, tokens, allowed=allowed, top=top)
+    dlogp, dentropy = torch.randn(2, rows, generator=gen, device="cuda").unbind()
+    grad = pcm.pcm_token_logprobs_backward(z, tokens, whole["lse"], dlogp, whole["entropy"], dentropy, allowed=allowed)
+    for part in (slice(0, tail), slice(rows - tail, rows)):
+        zs, ts, ok = z[part].contiguous(), tokens[part].cpu(), allowed[part].cpu().numpy()
+        alone = _check_forward(zs, zs.double().cpu().numpy(), ts, ok, top=top)
+        for k, v in alone.items():
+            assert torch.equal(whole[k][part], v), k
+        got = _check_backward(zs, zs.double().cpu().numpy(), ts, dlogp[part].cpu().numpy(), dentropy[part].cpu().numpy(), ok)
+        if top == 0:                                   # (lse and entropy come from the same launch shape)
+            assert torch.equal(grad[part], got)
+    assert torch.isfinite(grad).all()
+
+
 def test_rows_do_not_depend_on_one_another_and_repeat_bit_for_bit():
     rng = np.random.default_rng(8)
     pcm = _pcm()
