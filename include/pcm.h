@@ -464,13 +464,14 @@ PCM_API int pcm_adamw_clip_step_ex(int n_tensors, const int64_t* numel, const fl
  *   tokens    device [rows] of token_type; a token >= V counts as V-1, a negative one marks a row without a token (logp 0)
  *   allowed   device u8, or NULL (all tokens): zero excludes a token, whatever its logit holds; allowed_ld = 0: [V], the same for
  *             every row, else rows of V values, allowed_ld >= V apart
- *   temperature  > 0, with a finite reciprocal
+ *   temperature  finite, at least 2^-126 (the least normal float)
  *   top       0 .. PCM_MAX_TOP_TOKENS
  *   logp, lse device f32 [rows];  entropy device f32 [rows] or NULL
  *   top_ids   device i32 [rows, top], top_logp device f32 [rows, top]; unused if top = 0
  * A row that allows nothing, or nothing but logits of -inf: lse -inf, entropy 0, logp -inf (an excluded token has logp -inf
- * in every row).  Where fewer than `top` tokens are allowed the rest is id -1 and logp -inf.  A NaN or +inf among the allowed logits
- * makes the row's lse, logp, entropy and top_logp NaN; a NaN is not among the alternatives.  Rows do not depend on one another.
+ * in every row).  Logits may be any finite values (lse and logp are infinite where they leave the range of fp32).  Where fewer than
+ * `top` tokens are allowed the rest is id -1 and logp -inf.  A NaN or +inf among the allowed logits makes the row's lse, logp, entropy
+ * and top_logp NaN; a NaN is not among the alternatives.  Rows do not depend on one another.
  * logits may be any rows of a larger matrix; they are only read.  rows = 0 is a valid call that does nothing.
  * Limits: rows < 2^31, 1 <= V <= 2^30.
  *

@@ -6,6 +6,25 @@ import numpy as np
 NS_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 
+def _row(z, ok, temperature):
+    """-> (ids of the allowed tokens, x - max x of them, log sum e^(x - max x), max x) of a row, x = z / temperature; the sum relative to
+    the largest logit, so that logits of any size leave it what it is.  The sum is NaN where there is none, -inf where it is empty."""
+    ids = np.flatnonzero(ok)
+    z = z[ids]
+    if np.isnan(z).any() or np.isposinf(z).any():
+        return ids, np.full(len(ids), np.nan), np.nan, np.nan
+    most = z.max() if len(ids) else -np.inf
+    if most == -np.inf:
+        return ids, np.full(len(ids), -np.inf), -np.inf, -np.inf
+    a = (z - most) / temperature
+    return ids, a, np.log(np.exp(a).sum()), most / temperature
+
+
+def _allowed(allowed, r, V):
+    ok = np.ones(V, bool) if allowed is None else np.asarray(allowed, bool)
+    return ok if ok.ndim == 1 else ok[r]
+
+
 def token_logprobs(logits, tokens, allowed=None, temperature=1.0, top=0):
     """-> dict(logp, lse, entropy [rows], top_ids, top_logp [rows, top]), row by row."""
     z = np.asarray(logits, dtype=np.float64)
@@ -13,32 +32,22 @@ def token_logprobs(logits, tokens, allowed=None, temperature=1.0, top=0):
     out = dict(logp=np.zeros(rows), lse=np.zeros(rows), entropy=np.zeros(rows), top_ids=np.full((rows, top), -1, np.int32),
                top_logp=np.full((rows, top), -np.inf))
     for r in range(rows):
-        ok = np.ones(V, bool) if allowed is None else np.asarray(allowed, bool)
-        ok = ok if ok.ndim == 1 else ok[r]
-        ids = np.flatnonzero(ok)
-        x = z[r, ids] / temperature
-        broken = np.isnan(x).any() or np.isposinf(x).any()
-        m = x.max() if len(x) else -np.inf
-        empty = not broken and m == -np.inf
-        if broken:
-            lse = entropy = np.nan
-        elif empty:
-            lse, entropy = -np.inf, 0.0
+        ok = _allowed(allowed, r, V)
+        ids, a, log_sum, most = _row(z[r], ok, temperature)
+        logp = np.full(V, -np.inf)
+        if log_sum == -np.inf:
+            out["lse"][r], out["entropy"][r] = -np.inf, 0.0
         else:
-            e = np.exp(x - m)
-            lse = m + np.log(e.sum())
-            p = e / e.sum()
-            live = p > 0
-            entropy = -(p[live] * (x[live] - lse)).sum()
-        out["lse"][r], out["entropy"][r] = lse, entropy
-        of = lambda j: -np.inf if empty else (np.nan if broken else z[r, j] / temperature - lse)
+            logp[ids] = a - log_sum
+            out["lse"][r] = most + log_sum
+            live = ~(logp[ids] == -np.inf)
+            out["entropy"][r] = -(np.exp(logp[ids][live]) * logp[ids][live]).sum()
         t = int(tokens[r])
         if t >= 0:
-            t = min(t, V - 1)
-            out["logp"][r] = of(t) if ok[t] else -np.inf
-        listed = [j for j in ids if not np.isnan(z[r, j])]
-        for k, j in enumerate(sorted(listed, key=lambda j: (-z[r, j], j))[:top]):
-            out["top_ids"][r, k], out["top_logp"][r, k] = j, of(j)
+            out["logp"][r] = logp[min(t, V - 1)]
+        listed = ids[~np.isnan(z[r, ids])]
+        best = listed[np.argsort(-z[r, listed], kind="stable")[:top]]
+        out["top_ids"][r, :len(best)], out["top_logp"][r, :len(best)] = best, logp[best]
     return out
 
 
@@ -46,15 +55,13 @@ def token_logprobs_gradient(logits, tokens, dlogp, dentropy=None, allowed=None, 
     """d logits of sum(dlogp * logp) + sum(dentropy * entropy)."""
     z = np.asarray(logits, dtype=np.float64)
     rows, V = z.shape
-    got = token_logprobs(logits, tokens, allowed, temperature)
     g = np.zeros((rows, V))
     for r in range(rows):
-        if not np.isfinite(got["lse"][r]):
+        ok = _allowed(allowed, r, V)
+        ids, a, log_sum, _ = _row(z[r], ok, temperature)
+        if not np.isfinite(log_sum):
             continue
-        ok = np.ones(V, bool) if allowed is None else np.asarray(allowed, bool)
-        ok = ok if ok.ndim == 1 else ok[r]
-        ids = np.flatnonzero(ok & (z[r] > -np.inf))
-        logp = z[r, ids] / temperature - got["lse"][r]
+        ids, logp = ids[a > -np.inf], a[a > -np.inf] - log_sum
         p = np.exp(logp)
         t = int(tokens[r])
         d = 0.0 if t < 0 else float(dlogp[r])
@@ -62,7 +69,7 @@ def token_logprobs_gradient(logits, tokens, dlogp, dentropy=None, allowed=None, 
         if t >= 0 and ok[min(t, V - 1)]:
             g[r, min(t, V - 1)] += d
         if dentropy is not None:
-            g[r, ids] -= float(dentropy[r]) * p * (logp + got["entropy"][r])
+            g[r, ids] -= float(dentropy[r]) * p * (logp - (p * logp).sum())
     return g / temperature
 
 

@@ -14,15 +14,13 @@ struct Logits {
     int token_type;
     int64_t rows;
     int V;
-    float inv_t;
+    float t, inv_t;              // the temperature
 };
 
-// What has been seen of a row: s = sum 2^a and t = sum 2^a a with a = z c - R.  r is the logit that R = r c was made from (-inf:
-// none yet); R is rounded, which takes nothing from the sums, as it is the same in all of them.  Logits beyond 1e38, where r c could
-// overflow, have R = 0 and a = (z - r) c.
+// What has been seen of a row: s = sum 2^a and t = sum 2^a a with a = (z - r) (log2 e) / temperature relative to a logit r (the lowest value: none yet).  The
+// difference comes first: it is zero for z = r, where a difference of products would be off by the rounding of one of them, which has no bound.
 struct RowSums {
-    float r, R, s, t;
-    __device__ bool far() const { return fabsf(r) > 1e38f && r != -__builtin_huge_valf(); }
+    float r, s, t;
 };
 struct LogprobsOut {
     float *logp, *lse, *entropy;     // entropy: or null

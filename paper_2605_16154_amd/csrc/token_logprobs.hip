@@ -2,8 +2,8 @@
 //
 // With x = logit / temperature over the allowed tokens of a row: lse = log sum e^x, log p(token) = x_token - lse,
 // entropy = lse - sum p x, and the `top` tokens of the largest logits (of equal ones the lower index).  One pass over the row:
-// every lane keeps s = sum 2^a and t = sum 2^a a with a = (x - r) log2 e, relative to a logit r that it has met, so that s is at
-// least one; r moves only when a logit is so far above it that s could overflow.  All sums are fp32.
+// every lane keeps s = sum 2^a and t = sum 2^a a with a = (logit - r) (log2 e) / temperature, relative to a logit r that it has met, so that s
+// is at least one whatever the size of the logits; r moves only when a logit is so far above it that s could overflow.  All sums are fp32.
 //
 // Bound by memory where there is much of it: a logit costs about nine instructions, one of them the exponential at a quarter of the rate, which
 // is 8 TB/s of bf16 logits.  (A running maximum that is exact would take two exponentials a logit or a pass of its own.)
@@ -20,6 +20,8 @@ namespace {
 
 constexpr int kTopMost = 64;                 // one list entry per lane
 constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+constexpr float kLowest = -3.402823466e38f;  // of the finite values
 
 __device__ inline float infinity() { return __builtin_huge_valf(); }
 __device__ inline int ceil_div_device(int a, int b) { return (int)(((int64_t)a + b - 1) / b); }
@@ -130,30 +132,26 @@ __device__ __forceinline__ void each_chunk(const T* row, const uint8_t* allowed,
 
 // How far above the reference a logit may be, in powers of two: 2^17 such terms still fit.
 constexpr float kHeadroom = 64.f;
+constexpr RowSums kNothing{kLowest, 0.f, 0.f};
+// Half the difference of two logits, which does not overflow, and c = 2 (log2 e) / temperature that goes with it.
+__device__ __forceinline__ float half_gap(float z, float r) { return __builtin_fmaf(z, 0.5f, -0.5f * r); }
+__device__ __forceinline__ float exponent_scale(const Logits& q) { return 2.f * q.inv_t * kLog2E; }
 // 0 * -inf would be NaN, and 2^-300 is zero
 __device__ __forceinline__ float times(float p, float a) { return p * fmaxf(a, -300.f); }
-__device__ __forceinline__ float exponent(const RowSums& a, float z, float c) { return a.far() ? (z - a.r) * c : __builtin_fmaf(z, c, -a.R); }
 
-// A logit far above the reference, or the first one, becomes the reference.
+// A logit far above the reference becomes the reference.
 __device__ __forceinline__ void move_reference(RowSums& a, float to, float c) {
-    RowSums b{to, 0.f, a.s, a.t};
-    b.R = b.far() ? 0.f : to * c;
-    if (a.r != -infinity()) {
-        const float d = a.far() || b.far() ? (a.r - to) * c : a.R - b.R, f = __builtin_amdgcn_exp2f(d);
-        b.t = f * (a.t + times(a.s, d));
-        b.s = f * a.s;
-    }
-    a = b;
+    const float d = half_gap(a.r, to) * c, f = __builtin_amdgcn_exp2f(d);
+    a = RowSums{to, f * a.s, f * (a.t + times(a.s, d))};
 }
-// How a chunk is added: kFinite every logit is finite, kAny also -inf (excluded tokens), kFar also beyond 1e38.
-enum Care : int { kFinite = 0, kAny = 1, kFar = 2 };
-template <bool kEntropy, int kCare>
+// kAny: also logits of -inf (excluded tokens), or so far below the reference that the exponent overflows.
+template <bool kEntropy, bool kAny>
 __device__ __forceinline__ void add_chunk(RowSums& a, const float (&z)[8], float c) {
     float s = 0.f, t = 0.f;              // of the chunk: what a lane adds up one by one is then an eighth as long
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float x = kCare == kFar ? exponent(a, z[e], c) : __builtin_fmaf(z[e], c, -a.R);
-        const float p = __builtin_amdgcn_exp2f(x), y = kCare == kFinite ? x : fmaxf(x, -300.f);
+        const float x = half_gap(z[e], a.r) * c;
+        const float p = __builtin_amdgcn_exp2f(x), y = kAny ? fmaxf(x, -300.f) : x;
         s = e == 0 ? p : s + p;
         if (kEntropy) t = e == 0 ? p * y : __builtin_fmaf(p, y, t);
     }
@@ -165,10 +163,13 @@ __device__ __forceinline__ float chunk_max(const float (&z)[8]) {
 }
 __device__ __forceinline__ RowSums join(RowSums a, RowSums b, float c) {
     if (a.r < b.r) { const RowSums x = a; a = b; b = x; }
-    if (a.r == -infinity()) return RowSums{a.r, a.R, a.s + b.s, a.t + b.t};        // zeros, or NaN
-    // b moves to a's reference; nothing is left of sums without one (but a NaN)
-    const float d = b.r == -infinity() ? -300.f : (a.far() || b.far() ? (b.r - a.r) * c : b.R - a.R), f = __builtin_amdgcn_exp2f(d);
-    return RowSums{a.r, a.R, a.s + f * b.s, a.t + f * (b.t + times(b.s, d))};
+    move_reference(b, a.r, c);
+    return RowSums{a.r, a.s + b.s, a.t + b.t};
+}
+__device__ __forceinline__ RowSums join_lanes(RowSums a, float c) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) a = join(a, RowSums{__shfl_xor(a.r, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)}, c);
+    return a;
 }
 
 // Selection of the largest logits.  A token is one 64-bit number, its logit as an integer of the same order above the complement of
@@ -226,37 +227,36 @@ __device__ __forceinline__ uint64_t merge_keys(uint64_t descending, uint64_t asc
 
 // A row's results, by one lane; and logp of a logit.
 struct RowResult {
-    float lse, entropy;
-    __device__ RowResult(const RowSums& a) {
+    __device__ RowResult(const RowSums& a, const Logits& q) {
         empty = a.s == 0.f;          // nothing allowed, or only logits of -inf
-        log2_s = __builtin_amdgcn_logf(a.s);
-        lse = empty ? -infinity() : kLn2 * (a.R + log2_s);
+        const float log2_s = __builtin_amdgcn_logf(a.s);
+        r = a.r;
+        scale = 2.f * q.inv_t;
+        log_s = kLn2 * log2_s;
+        lse = empty ? -infinity() : a.r / q.t + log_s;
         entropy = empty ? 0.f : kLn2 * (log2_s - a.t / a.s);
-        sums = a;
     }
-    __device__ float logp(float z, float c) const { return empty ? -infinity() : kLn2 * (exponent(sums, z, c) - log2_s); }
-    __device__ float lse_of(const Logits& q) const { return !empty && sums.far() ? sums.r * q.inv_t + kLn2 * log2_s : lse; }
+    __device__ float logp(float z) const { return empty ? -infinity() : __builtin_fmaf(half_gap(z, r), scale, -log_s); }
     bool empty;
-    float log2_s;
-    RowSums sums;
+    float r, scale, log_s, lse, entropy;
 };
 template <class T>
-__device__ __forceinline__ void store_row(const Logits& q, const LogprobsOut& o, int64_t row, const RowResult& res, float c) {
+__device__ __forceinline__ void store_row(const Logits& q, const LogprobsOut& o, int64_t row, const RowResult& res) {
     const int token = token_of(q, row);
     float logp = 0.f;
     if (token >= 0) {
         const bool in = q.allowed == nullptr || q.allowed[row * q.allowed_ld + token] != 0;
-        logp = in ? res.logp(to_float<T>(static_cast<const T*>(q.z)[row * q.ld + token]), c) : -infinity();
+        logp = in ? res.logp(to_float<T>(static_cast<const T*>(q.z)[row * q.ld + token])) : -infinity();
     }
     o.logp[row] = logp;
-    o.lse[row] = res.lse_of(q);
+    o.lse[row] = res.lse;
     if (o.entropy != nullptr) o.entropy[row] = res.entropy;
 }
-__device__ __forceinline__ void store_top(const LogprobsOut& o, int64_t row, uint64_t key, const RowResult& res, float c) {
+__device__ __forceinline__ void store_top(const LogprobsOut& o, int64_t row, uint64_t key, const RowResult& res) {
     const int lane = threadIdx.x & 63;
     if (lane >= o.top) return;
     o.top_ids[row * o.top + lane] = key != 0 ? key_token(key) : -1;
-    o.top_logp[row * o.top + lane] = key != 0 ? res.logp(key_logit(key), c) : -infinity();
+    o.top_logp[row * o.top + lane] = key != 0 ? res.logp(key_logit(key)) : -infinity();
 }
 
 // The largest chunk of every lane: its largest logit and where it is, the first of equal ones; j < 0: none yet.
@@ -353,39 +353,31 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_parts(Logits q, Logpr
     const T* z_row = static_cast<const T*>(q.z) + row * q.ld;
     const uint8_t* allowed = kMask ? q.allowed + row * q.allowed_ld : nullptr;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float c = q.inv_t * kLog2E, room = kHeadroom / c;
-    RowSums a{-infinity(), 0.f, 0.f, 0.f};
+    const float c = exponent_scale(q);
+    RowSums a = kNothing;
     Best best{-infinity(), -1};
-    int care = kMask ? kAny : kFinite;                   // of the whole wavefront
+    bool any = kMask;                                    // of the whole wavefront: logits may be -inf
     const int units = ceil_div_device(q.V, kThreads * 8), per_part = ceil_div_device(units, parts.parts);
     const int begin = min(q.V, part * per_part * kThreads * 8), end = min(q.V, begin + per_part * kThreads * 8);
     each_chunk<T, kMask, kThreads>(z_row, allowed, begin, end, q.V, threadIdx.x, [&](int j, const float (&z)[8], uint32_t ok) __attribute__((always_inline)) {
         const float most = chunk_max(z);
-        if (__any(most > a.r + room)) {
-            if (most > a.r + room) move_reference(a, most, c);
-            if (__any(a.far())) care = kFar;
-        }
+        const bool above = half_gap(most, a.r) * c > kHeadroom;
+        if (__any(above) && above) move_reference(a, most, c);
         if (kTop) best.look(j, most, z, ok);
-        if (care == kFinite) {
-            const float s = a.s, t = a.t;
-            add_chunk<kEntropy, kFinite>(a, z, c);
+        const float s = a.s, t = a.t;
+        if (!any) {
+            add_chunk<kEntropy, false>(a, z, c);
             if (kEntropy && __any(a.t != a.t)) {         // 0 * -inf: again, with care
                 a.s = s;
                 a.t = t;
-                care = kAny;
-                add_chunk<kEntropy, kAny>(a, z, c);
+                any = true;
+                add_chunk<kEntropy, true>(a, z, c);
             }
-        } else if (care == kAny) {
-            add_chunk<kEntropy, kAny>(a, z, c);
         } else {
-            add_chunk<kEntropy, kFar>(a, z, c);
+            add_chunk<kEntropy, true>(a, z, c);
         }
     });
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        const RowSums b{__shfl_xor(a.r, d, 64), __shfl_xor(a.R, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)};
-        a = join(a, b, c);
-    }
+    a = join_lanes(a, c);
     if (kWaves > 1 && lane == 0) wave_sums[wave] = a;
     uint64_t key = 0;
     if constexpr (kTop) {
@@ -401,9 +393,9 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_parts(Logits q, Logpr
         if (kTop && lane < o.top) parts.keys[(int64_t)blockIdx.x * o.top + lane] = key;
         return;
     }
-    const RowResult res(a);
-    if (lane == 0) store_row<T>(q, o, row, res, c);
-    if (kTop) store_top(o, row, key, res, c);
+    const RowResult res(a, q);
+    if (lane == 0) store_row<T>(q, o, row, res);
+    if (kTop) store_top(o, row, key, res);
 }
 
 // A workgroup per row: the parts of the row.
@@ -414,7 +406,7 @@ __global__ __launch_bounds__(kJoinThreads) void token_logprobs_join(Logits q, Lo
     __shared__ uint64_t lists[kWaves][64];
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float c = q.inv_t * kLog2E;
+    const float c = exponent_scale(q);
     uint64_t key = 0;
     if (o.top > 0) {
         const int n = parts.parts * o.top;
@@ -424,18 +416,14 @@ __global__ __launch_bounds__(kJoinThreads) void token_logprobs_join(Logits q, Lo
         __syncthreads();
     }
     if (wave != 0) return;
-    RowSums a{-infinity(), 0.f, 0.f, 0.f};
+    RowSums a = kNothing;
     for (int i = lane; i < parts.parts; i += 64) a = join(a, parts.sums[row * parts.parts + i], c);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        const RowSums b{__shfl_xor(a.r, d, 64), __shfl_xor(a.R, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)};
-        a = join(a, b, c);
-    }
-    const RowResult res(a);
-    if (lane == 0) store_row<T>(q, o, row, res, c);
+    a = join_lanes(a, c);
+    const RowResult res(a, q);
+    if (lane == 0) store_row<T>(q, o, row, res);
     if (o.top == 0) return;
     for (int w = 1; w < kWaves; ++w) key = merge_keys(key, lists[w][lane]);
-    store_top(o, row, key, res, c);
+    store_top(o, row, key, res);
 }
 
 // Rows of up to 16 kLanes logits: kLanes lanes per row, all of it in registers, and the sums relative to its largest logit.  43008 rows of 256 bf16:
@@ -460,24 +448,16 @@ __global__ __launch_bounds__(kNarrowThreads) void token_logprobs_narrow(Logits q
     const T* z_row = static_cast<const T*>(q.z) + row * q.ld;
     const uint8_t* allowed = kMask ? q.allowed + row * q.allowed_ld : nullptr;
     const int lane = threadIdx.x % kLanes;
-    const float c = q.inv_t * kLog2E;
+    const float c = exponent_scale(q);
     float z[2][8];
 #pragma unroll
     for (int h = 0; h < 2; ++h) load_chunk<T, kMask>(z_row, allowed, (h * kLanes + lane) * 8, q.V, z[h]);
-    RowSums a{-infinity(), 0.f, 0.f, 0.f};
-    const float most = lanes_max<kLanes>(fmaxf(chunk_max(z[0]), chunk_max(z[1])));
-    move_reference(a, most, c);
-    if (most == -infinity()) a.R = 0.f;
-    if (__any(a.far())) {
-        add_chunk<true, kFar>(a, z[0], c);
-        add_chunk<true, kFar>(a, z[1], c);
-    } else {
-        add_chunk<true, kAny>(a, z[0], c);
-        add_chunk<true, kAny>(a, z[1], c);
-    }
+    RowSums a{fmaxf(lanes_max<kLanes>(fmaxf(chunk_max(z[0]), chunk_max(z[1]))), kLowest), 0.f, 0.f};
+    add_chunk<true, true>(a, z[0], c);
+    add_chunk<true, true>(a, z[1], c);
     a.s = lanes_sum<kLanes>(a.s);
     a.t = lanes_sum<kLanes>(a.t);
-    if (lane == 0) store_row<T>(q, o, row, RowResult(a), c);
+    if (lane == 0) store_row<T>(q, o, row, RowResult(a, q));
 }
 
 template <class T>
@@ -637,14 +617,14 @@ P* from(P* p, int64_t i) { return p == nullptr ? nullptr : p + i; }
 
 constexpr int64_t kMaxRows = 0x7fffffff;
 constexpr int kMaxVocabulary = 1 << 30;
+constexpr float kLeastTemperature = 0x1p-126f;       // the least normal one: log2 e / temperature is finite
 
 // The checks that both directions share.
 int check_logits(const void* logits, int64_t ld, int dtype, const void* tokens, int token_type, const uint8_t* allowed, int64_t allowed_ld,
                  int64_t rows, int V, float temperature) {
     if (rows < 0 || V < 1 || ld < V || (dtype != PCM_F32 && dtype != PCM_BF16) ||
         (token_type != PCM_TOKEN_U8 && token_type != PCM_TOKEN_I32 && token_type != PCM_TOKEN_I64) ||
-        (allowed != nullptr && allowed_ld != 0 && allowed_ld < V) || !(temperature > 0.f) || !(1.f / temperature < __builtin_huge_valf()) ||
-        temperature == __builtin_huge_valf())
+        (allowed != nullptr && allowed_ld != 0 && allowed_ld < V) || !(temperature >= kLeastTemperature) || temperature == __builtin_huge_valf())
         return PCM_EINVAL;
     if (rows == 0) return PCM_OK;
     const uintptr_t token_size = token_type == PCM_TOKEN_U8 ? 1 : token_type == PCM_TOKEN_I32 ? 4 : 8;
@@ -681,7 +661,7 @@ PCM_API int pcm_token_logprobs(const void* logits, int64_t logits_ld, int dtype,
     if (rc != PCM_OK) return rc;
     if (!workspace_ok(workspace, workspace_bytes, pcm_token_logprobs_workspace_bytes(rows, V, top))) return PCM_EWORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const Logits q{logits, logits_ld, allowed, allowed_ld, tokens, token_type, rows, V, 1.f / temperature};
+    const Logits q{logits, logits_ld, allowed, allowed_ld, tokens, token_type, rows, V, temperature, 1.f / temperature};
     Carver c(workspace);
     const RowParts p = carve_parts(c, rows, V, top);
     StageTimer t(ST_TOKEN_LOGPROBS, s);
@@ -706,7 +686,7 @@ PCM_API int pcm_token_logprobs_backward(const void* logits, int64_t logits_ld, i
         return PCM_EINVAL;
     if (rc != PCM_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const Logits q{logits, logits_ld, allowed, allowed_ld, tokens, token_type, rows, V, 1.f / temperature};
+    const Logits q{logits, logits_ld, allowed, allowed_ld, tokens, token_type, rows, V, temperature, 1.f / temperature};
     StageTimer t(ST_TOKEN_LOGPROBS_GRAD, s);
     for (int64_t row = 0; row < rows; row += kRowsPerLaunch) {
         const Logits some = rows_from(q, row, rows, dtype);
