@@ -2,11 +2,13 @@
 //
 // With x = logit / temperature over the allowed tokens of a row: lse = log sum e^x, log p(token) = x_token - lse,
 // entropy = lse - sum p x, and the `top` tokens of the largest logits (of equal ones the lower index).  One pass over the row:
-// every lane keeps s = sum 2^a and t = sum 2^a a with a = (logit - r) (log2 e) / temperature, relative to a logit r that it has met, so that s
-// is at least one whatever the size of the logits; r moves only when a logit is so far above it that s could overflow.  All sums are fp32.
+// every lane keeps s = sum 2^a and t = sum 2^a a with a = (logit - r) (log2 e) / temperature relative to the largest logit r that it has met,
+// which moves once per chunk of eight logits at most; of two lanes' sums the larger logit stays.  So a <= 0 <= log s in the end: entropy
+// = log s - (t / s) ln 2 and -logp are sums of terms of one sign, and as exact for a row that is all but certain (relative to some other
+// logit both are differences of numbers that may be much larger).  All sums are fp32.
 //
-// Bound by memory where there is much of it: a logit costs about nine instructions, one of them the exponential at a quarter of the rate, which
-// is 8 TB/s of bf16 logits.  (A running maximum that is exact would take two exponentials a logit or a pass of its own.)
+// Bound by memory where there is much of it: a logit costs ten instructions and a chunk some ten more, one of them an exponential at a
+// quarter of the rate, which is 6.5 TB/s of bf16 logits.
 //
 // Gradient: d logit_j = ([j = token] d_logp - p_j (d_logp + d_entropy (log p_j + entropy))) / temperature, from lse and entropy as
 // the forward pass left them: every logit is read once and its gradient written once.
@@ -130,8 +132,6 @@ __device__ __forceinline__ void each_chunk(const T* row, const uint8_t* allowed,
     }
 }
 
-// How far above the reference a logit may be, in powers of two: 2^17 such terms still fit.
-constexpr float kHeadroom = 64.f;
 constexpr RowSums kNothing{kLowest, 0.f, 0.f};
 // Half the difference of two logits, which does not overflow, and c = 2 (log2 e) / temperature that goes with it.
 __device__ __forceinline__ float half_gap(float z, float r) { return __builtin_fmaf(z, 0.5f, -0.5f * r); }
@@ -139,7 +139,7 @@ __device__ __forceinline__ float exponent_scale(const Logits& q) { return 2.f * 
 // 0 * -inf would be NaN, and 2^-300 is zero
 __device__ __forceinline__ float times(float p, float a) { return p * fmaxf(a, -300.f); }
 
-// A logit far above the reference becomes the reference.
+// A logit above the reference becomes the reference.
 __device__ __forceinline__ void move_reference(RowSums& a, float to, float c) {
     const float d = half_gap(a.r, to) * c, f = __builtin_amdgcn_exp2f(d);
     a = RowSums{to, f * a.s, f * (a.t + times(a.s, d))};
@@ -361,8 +361,7 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_parts(Logits q, Logpr
     const int begin = min(q.V, part * per_part * kThreads * 8), end = min(q.V, begin + per_part * kThreads * 8);
     each_chunk<T, kMask, kThreads>(z_row, allowed, begin, end, q.V, threadIdx.x, [&](int j, const float (&z)[8], uint32_t ok) __attribute__((always_inline)) {
         const float most = chunk_max(z);
-        const bool above = half_gap(most, a.r) * c > kHeadroom;
-        if (__any(above) && above) move_reference(a, most, c);
+        move_reference(a, fmaxf(a.r, most), c);
         if (kTop) best.look(j, most, z, ok);
         const float s = a.s, t = a.t;
         if (!any) {
