@@ -477,8 +477,9 @@ PCM_API int pcm_adamw_clip_step_ex(int n_tensors, const int64_t* numel, const fl
  *
  * pcm_token_logprobs_backward -- the gradient of a loss in the logits, from its gradients in logp and entropy:
  *   d x_j = [j = token] dlogp - p_j (dlogp + dentropy (log p_j + entropy)),  dlogits = d x / temperature, 0 for excluded tokens
- *   and rows without a finite lse because nothing is allowed; a row without a token takes only the entropy's part.
- *   lse, entropy         device f32 [rows], as the forward call left them;  entropy NULL exactly if dentropy is
+ *   and in rows that allow nothing, or nothing but logits of -inf; a row without a token takes only the entropy's part.
+ *   lse, entropy         device f32 [rows], as the forward call left them;  entropy NULL exactly if dentropy is.  (Where |lse| is 1024
+ *                        or more, fp32 does not hold log sum well: such rows take the sum from the logits, which they then read twice)
  *   dlogp, dentropy      device f32 [rows];  dentropy NULL: no gradient through the entropy
  *   dlogits              device [rows] rows of V values of dtype, dlogits_ld >= V apart (values between rows are left as they
  *                        are); may be the logits themselves, with the same leading dimension

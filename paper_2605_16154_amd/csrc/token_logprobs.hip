@@ -11,7 +11,7 @@
 // quarter of the rate, which is 6.5 TB/s of bf16 logits.
 //
 // Gradient: d logit_j = ([j = token] d_logp - p_j (d_logp + d_entropy (log p_j + entropy))) / temperature, from lse and entropy as
-// the forward pass left them: every logit is read once and its gradient written once.
+// the forward pass left them: every logit is read once and its gradient written once.  (Rows whose lse is too large: see kLseCarries.)
 #include <algorithm>
 #include <type_traits>
 
@@ -101,9 +101,10 @@ __device__ inline uint32_t load_chunk(const T* row, const uint8_t* allowed, int 
 }
 // f(j, z, ok) for the chunks from `begin` to `end` that this thread of kStride has, the loads of kAhead chunks under way while as many
 // are worked on: with one at a time a wavefront waits for each (4096 rows of 65536 bf16 164 us).
+// start() is called once the first of them are under way: false ends it there.
 constexpr int kAhead = 2;
-template <class T, bool kMask, int kStride, class F>
-__device__ __forceinline__ void each_chunk(const T* row, const uint8_t* allowed, int begin, int end, int V, int lane, F f) {
+template <class T, bool kMask, int kStride, class Start, class F>
+__device__ __forceinline__ bool each_chunk(const T* row, const uint8_t* allowed, int begin, int end, int V, int lane, Start start, F f) {
     constexpr int kUnit = kStride * 8;
     const int rounds = max(0, min(end, V) - begin) / (kAhead * kUnit);           // of chunks that are whole in every lane
     int j = begin + lane * 8;
@@ -111,6 +112,7 @@ __device__ __forceinline__ void each_chunk(const T* row, const uint8_t* allowed,
         WholeChunk<T, kMask> now[kAhead], next[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) now[u].load(row, allowed, j + u * kUnit);
+        if (!start()) return false;
         for (int i = 0; i < rounds; ++i) {
             if (i + 1 < rounds)
 #pragma unroll
@@ -124,12 +126,15 @@ __device__ __forceinline__ void each_chunk(const T* row, const uint8_t* allowed,
             }
             j += kAhead * kUnit;
         }
+    } else if (!start()) {
+        return false;
     }
     for (int first = begin + rounds * kAhead * kUnit; first < end; first += kUnit, j += kUnit) {
         float z[8];
         const uint32_t ok = load_chunk<T, kMask>(row, allowed, j, V, z);
         f(j, z, ok);
     }
+    return true;
 }
 
 constexpr RowSums kNothing{kLowest, 0.f, 0.f};
@@ -166,9 +171,10 @@ __device__ __forceinline__ RowSums join(RowSums a, RowSums b, float c) {
     move_reference(b, a.r, c);
     return RowSums{a.r, a.s + b.s, a.t + b.t};
 }
+template <int kLanes = 64>
 __device__ __forceinline__ RowSums join_lanes(RowSums a, float c) {
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) a = join(a, RowSums{__shfl_xor(a.r, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)}, c);
+    for (int d = kLanes / 2; d > 0; d >>= 1) a = join(a, RowSums{__shfl_xor(a.r, d, 64), __shfl_xor(a.s, d, 64), __shfl_xor(a.t, d, 64)}, c);
     return a;
 }
 
@@ -359,7 +365,7 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_parts(Logits q, Logpr
     bool any = kMask;                                    // of the whole wavefront: logits may be -inf
     const int units = ceil_div_device(q.V, kThreads * 8), per_part = ceil_div_device(units, parts.parts);
     const int begin = min(q.V, part * per_part * kThreads * 8), end = min(q.V, begin + per_part * kThreads * 8);
-    each_chunk<T, kMask, kThreads>(z_row, allowed, begin, end, q.V, threadIdx.x, [&](int j, const float (&z)[8], uint32_t ok) __attribute__((always_inline)) {
+    each_chunk<T, kMask, kThreads>(z_row, allowed, begin, end, q.V, threadIdx.x, [] { return true; }, [&](int j, const float (&z)[8], uint32_t ok) __attribute__((always_inline)) {
         const float most = chunk_max(z);
         move_reference(a, fmaxf(a.r, most), c);
         if (kTop) best.look(j, most, z, ok);
@@ -486,47 +492,141 @@ __device__ inline void store_chunk<uint16_t>(uint16_t* row, int j, int V, const 
     }
 }
 
-// kLanes lanes per row, in chunks of eight logits; 256 / kLanes rows per workgroup, and a row in `parts` of them.  Bound by memory: 4096 rows of 131072
-// bf16 419 us, 1111 of 50021 fp32 with a mask 88 (5.1 and 5.0 TB/s read and written; a large copy has 4.8), 43008 of 256 bf16 10.
-constexpr int kGradientThreads = 256;
-template <class T, bool kMask, int kLanes>
-__global__ __launch_bounds__(kGradientThreads) void token_logprobs_gradient(Logits q, LogprobsGradient b, int parts) {
-    const int64_t row = (int64_t)(blockIdx.x / parts) * (kGradientThreads / kLanes) + threadIdx.x / kLanes;
-    const int part = blockIdx.x % parts;
-    if (row >= q.rows) return;
-    const T* z_row = static_cast<const T*>(q.z) + row * q.ld;
-    T* dz_row = static_cast<T*>(b.dz) + row * b.dz_ld;
-    const uint8_t* allowed = kMask ? q.allowed + row * q.allowed_ld : nullptr;
-    float lse = b.lse[row];
-    int token = token_of(q, row);
-    if (lse == -infinity()) {                            // nothing to choose from: every p is zero
-        lse = infinity();
-        token = -1;
+// What a row's lse no longer tells: from kLseCarries on it is rounded by 2^-15 and more, and so is every log p taken from it (at 10^10 nothing
+// is left of the log of the sum, and a token's own x / temperature may be hundreds above or below it).  Such rows, which training hardly
+// has, take their sums from the logits again (all rows of 4096 x 131072 bf16 such: 730 us instead of 419; 8 rows, which are then not
+// in parts, 46 instead of 6).
+constexpr float kLseCarries = 1024.f;
+__device__ __forceinline__ bool lse_carries(float lse) { return fabsf(lse) < kLseCarries; }          // (not where it is NaN)
+// What log p is relative to: log p = (z - r) / temperature - log_s.
+struct RowScale {
+    float r, log_s;
+};
+template <int kLanes>
+__device__ __forceinline__ RowScale scale_of(RowSums a, float c) {
+    a = join_lanes<kLanes < 64 ? kLanes : 64>(a, c);
+    if constexpr (kLanes > 64) {
+        __shared__ RowSums wave_sums[kLanes / 64];
+        if ((threadIdx.x & 63) == 0) wave_sums[threadIdx.x >> 6] = a;
+        __syncthreads();
+        a = kNothing;
+        for (int w = 0; w < kLanes / 64; ++w) a = join(a, wave_sums[w], c);
     }
-    const float dlogp = token < 0 ? 0.f : b.dlogp[row] * q.inv_t;
-    if (kMask && token >= 0 && allowed[token] == 0) token = -1;          // its own gradient is zero
-    float along = 0.f, scale = -dlogp;                   // g = p (scale + along a), a = log2 p
-    if (b.dentropy != nullptr) {
-        const float dh = b.dentropy[row] * q.inv_t;
-        along = -dh * kLn2;
-        scale -= dh * b.entropy[row];
+    return RowScale{a.r, a.s == 0.f ? -infinity() : kLn2 * __builtin_amdgcn_logf(a.s)};
+}
+__device__ __forceinline__ void add_moved(RowSums& a, const float (&z)[8], float c) {
+    move_reference(a, fmaxf(a.r, chunk_max(z)), c);
+    add_chunk<false, true>(a, z, c);
+}
+
+// The gradient of a row's logits, eight at a time.
+template <class T, bool kMask>
+struct RowGradient {
+    RowScale of;
+    int token, V;
+    float dlogp, along, scale, inv_t;
+    T* dz_row;
+    // (the values of a row are asked for before its logits, so as not to wait for those)
+    __device__ __forceinline__ RowGradient(const Logits& q, const LogprobsGradient& b, int64_t row) {
+        of = RowScale{0.f, b.lse[row]};
+        token = token_of(q, row);
+        V = q.V;
+        dz_row = static_cast<T*>(b.dz) + row * b.dz_ld;
+        inv_t = q.inv_t;
+        dlogp = token < 0 ? 0.f : b.dlogp[row] * q.inv_t;
+        if (kMask && token >= 0 && q.allowed[row * q.allowed_ld + token] == 0) token = -1;          // its own gradient is zero
+        along = 0.f;
+        scale = -dlogp;                                  // g = p (scale + along a), a = log2 sqrt p
+        if (b.dentropy != nullptr) {
+            const float dh = b.dentropy[row] * q.inv_t;
+            along = -2.f * dh * kLn2;
+            scale -= dh * b.entropy[row];
+        }
     }
-    const int units = ceil_div_device(q.V, kLanes * 8), per_part = ceil_div_device(units, parts);
-    const int begin = min(q.V, part * per_part * kLanes * 8), end = min(q.V, begin + per_part * kLanes * 8);
-    each_chunk<T, kMask, kLanes>(z_row, allowed, begin, end, q.V, threadIdx.x % kLanes, [&](int j, const float (&z)[8], uint32_t ok) __attribute__((always_inline)) {
+    __device__ __forceinline__ void relative_to(RowScale scale_of_row) {
+        of = scale_of_row;
+        if (of.log_s == -infinity()) {                   // nothing to choose from: every p is zero
+            of.log_s = infinity();
+            token = -1;
+        }
+    }
+    // kMoved: log p may be relative to a logit; with lse alone it is an instruction less.
+    template <bool kMoved>
+    __device__ __forceinline__ void store(int j, const float (&z)[8], uint32_t ok) const {
         float g[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float a = __builtin_fmaf(z[e], q.inv_t, -lse) * kLog2E;
-            const float p = __builtin_amdgcn_exp2f(a);
-            g[e] = kMask && !(ok >> e & 1) ? 0.f : p * __builtin_fmaf(along, fmaxf(a, -300.f), scale);
+            const float log_p = kMoved ? __builtin_fmaf(half_gap(z[e], of.r), 2.f * inv_t, -of.log_s) : __builtin_fmaf(z[e], inv_t, -of.log_s);
+            const float a = log_p * (0.5f * kLog2E);
+            const float root = __builtin_amdgcn_exp2f(a);            // (the instruction leaves no subnormal results, a product does)
+            g[e] = kMask && !(ok >> e & 1) ? 0.f : root * root * __builtin_fmaf(along, fmaxf(a, -150.f), scale);
         }
         if (token >= j && token < j + 8) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) g[e] += j + e == token ? dlogp : 0.f;
         }
-        store_chunk<T>(dz_row, j, q.V, g);
-    });
+        store_chunk<T>(dz_row, j, V, g);
+    }
+};
+
+// Rows of up to 16 kLanes logits: kLanes lanes per row, all of it in registers; 43008 rows of 256 bf16 9.3 us.  Wider ones (kLanes = 256): a workgroup
+// per row, or per part of one.  Bound by memory: 4096 rows of 131072 bf16 419 us, 1111 of 50021 fp32 with a mask 88 (5.1 and 5.0 TB/s read and
+// written; a large copy has 4.8).
+constexpr int kGradientThreads = 256;
+template <class T, bool kMask, int kLanes>
+__global__ __launch_bounds__(kGradientThreads) void token_logprobs_gradient(Logits q, LogprobsGradient b, int parts) {
+    const int64_t row = (int64_t)(blockIdx.x / parts) * (kGradientThreads / kLanes) + threadIdx.x / kLanes;
+    if (row >= q.rows) return;
+    const T* z_row = static_cast<const T*>(q.z) + row * q.ld;
+    const uint8_t* allowed = kMask ? q.allowed + row * q.allowed_ld : nullptr;
+    const int lane = threadIdx.x % kLanes;
+    const float c = exponent_scale(q);
+    RowGradient<T, kMask> gradient(q, b, row);
+    if constexpr (kLanes <= 64) {
+        float z[2][8];
+        uint32_t ok[2];
+        WholeChunk<T, kMask> whole[2];                   // both are asked for before the first is looked at
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if ((h * kLanes + lane) * 8 + 8 <= q.V) whole[h].load(z_row, allowed, (h * kLanes + lane) * 8);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int j = (h * kLanes + lane) * 8;
+            ok[h] = j + 8 <= q.V ? whole[h].get(z[h]) : load_chunk<T, kMask>(z_row, allowed, j, q.V, z[h]);
+        }
+        if (!__any(!lse_carries(gradient.of.log_s))) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) gradient.template store<false>((h * kLanes + lane) * 8, z[h], ok[h]);
+            return;
+        }
+        RowSums a = kNothing;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) add_moved(a, z[h], c);
+        const RowScale of = scale_of<kLanes>(a, c);
+        if (!lse_carries(gradient.of.log_s)) gradient.relative_to(of);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) gradient.template store<true>((h * kLanes + lane) * 8, z[h], ok[h]);
+    } else {
+        const int part = blockIdx.x % parts;
+        const int units = ceil_div_device(q.V, kLanes * 8), per_part = ceil_div_device(units, parts);
+        const int begin = min(q.V, part * per_part * kLanes * 8), end = min(q.V, begin + per_part * kLanes * 8);
+        auto store = [&](int j, const float (&z)[8], uint32_t ok) __attribute__((always_inline)) { gradient.template store<false>(j, z, ok); };
+        const bool done = each_chunk<T, kMask, kLanes>(z_row, allowed, begin, end, q.V, lane, [&]() __attribute__((always_inline)) { return lse_carries(gradient.of.log_s); }, store);
+        // Otherwise one workgroup has the row: its logits may become the gradient, which no other part may see.
+        if (done || part != 0) return;
+        RowSums a = kNothing;
+        for (int j = lane * 8; j < q.V; j += kLanes * 8) {
+            float z[8];
+            load_chunk<T, kMask>(z_row, allowed, j, q.V, z);
+            add_moved(a, z, c);
+        }
+        gradient.relative_to(scale_of<kLanes>(a, c));
+        for (int j = lane * 8; j < q.V; j += kLanes * 8) {
+            float z[8];
+            const uint32_t ok = load_chunk<T, kMask>(z_row, allowed, j, q.V, z);
+            gradient.template store<true>(j, z, ok);
+        }
+    }
 }
 
 // Lanes per row: a row of up to 1024 logits has 16 of them to a lane, longer ones go through workgroups of their own.
