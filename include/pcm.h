@@ -471,7 +471,8 @@ PCM_API int pcm_adamw_clip_step_ex(int n_tensors, const int64_t* numel, const fl
  * A row that allows nothing, or nothing but logits of -inf: lse -inf, entropy 0, logp -inf (an excluded token has logp -inf
  * in every row).  Logits may be any finite values (lse and logp are infinite where they leave the range of fp32).  Where fewer than
  * `top` tokens are allowed the rest is id -1 and logp -inf.  A NaN or +inf among the allowed logits makes the row's lse, logp, entropy
- * and top_logp NaN; a NaN is not among the alternatives.  Rows do not depend on one another.
+ * and top_logp NaN; a NaN is not among the alternatives.  A row's results do not depend on what other rows hold; their last bits may depend on
+ * how many there are (few long rows are summed in parts) and on whether alternatives are asked for.
  * logits may be any rows of a larger matrix; they are only read.  rows = 0 is a valid call that does nothing.
  * Limits: rows < 2^31, 1 <= V <= 2^30.
  *

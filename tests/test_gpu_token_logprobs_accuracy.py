@@ -74,3 +74,37 @@ def test_ordinary_rows(dtype, spread, rows, V):
         h = U * ((1 + E) * n + 2 * (E2 - E * E) + 2 * E + 2 * want["entropy"])
         assert rms(got["entropy"] - want["entropy"]) <= rms(h), rms(got["entropy"] - want["entropy"]) / U
         _signs(got)
+
+
+@pytest.mark.parametrize("rows,V,top", ((50, 256, 0), (50, 256, 4), (20, 3000, 0), (4, 60000, 3), (700, 9000, 2)))
+def test_a_row_does_not_depend_on_what_others_hold(rows, V, top):
+    """The same row among others of any kind, and at another place: the same bits.  Alone: the same but for its last ones."""
+    import paper_2605_16154_amd as pcm
+    gen = torch.Generator("cuda").manual_seed(V)
+    z = 2.0 * torch.randn((rows, V), generator=gen, device="cuda")
+    tokens = torch.randint(0, V, (rows,), generator=gen, device="cuda")
+    want = pcm.pcm_token_logprobs(z, tokens, top=top)
+    other = 1e30 * torch.randn((rows, V), generator=gen, device="cuda")
+    other[1::3] = float("nan")
+    other[2::3] = -float("inf")
+    d = torch.randn(rows, generator=gen, device="cuda")
+    grad = pcm.pcm_token_logprobs_backward(z, tokens, want["lse"], d, want["entropy"], d)
+    for keep, to in ((0, rows - 1), (rows - 1, 1), (rows // 2, rows // 2)):
+        x, t = other.clone(), tokens.clone()
+        x[to], t[to] = z[keep], tokens[keep]
+        got = pcm.pcm_token_logprobs(x, t, top=top)
+        for k in want:
+            assert torch.equal(got[k][to], want[k][keep]), k
+        dx = d.clone()
+        dx[to] = d[keep]
+        assert torch.equal(pcm.pcm_token_logprobs_backward(x, t, got["lse"], dx, got["entropy"], dx)[to], grad[keep])
+    alone = pcm.pcm_token_logprobs(z[3:4], tokens[3:4], top=top)
+    zd = z[3:4].double().cpu().numpy()
+    a = zd - zd.max()
+    p = np.exp(a) / np.exp(a).sum()
+    E, E2 = -(p * a).sum(), (p * a * a).sum()
+    d_s = 2 * (U * (V / (8 * (256 if V > 4096 else 64)) + 20) + 4 * U * (E + 1))
+    for k, tol in (("lse", d_s + 4 * U * 20), ("logp", d_s + 8 * U * 20), ("entropy", d_s * (2 + E) + 8 * U * E2)):
+        assert abs(alone[k].item() - want[k][3].item()) <= tol, k
+    if top:
+        assert torch.equal(alone["top_ids"][0], want["top_ids"][3])
