@@ -201,7 +201,9 @@ size_t task_bytes(int rows, int cols) {
     carve_task(c, rows, cols);
     return c.used();
 }
-// Matrices share launches while their buffers come to less than this (one alone may be larger).
+// Matrices share launches while their buffers come to less than this (one alone may be larger): a bound on the workspace, which time pays for.  1 MB
+// (one by one) / 64 MB / 256 MB / 1 GB: 8 of 256 x 1024 fp32 826 / 154 / 154 / 154 us, 8 of 1001 x 2815 1815 / 1815 / 1217 / 1115, 8 of 2048 x 5504
+// 7411 / 7411 / 7414 / 6131, 4 of 4096 x 11008 18.5 ms whatever it is.
 constexpr size_t kGroupBytes = (size_t)256 << 20;
 
 bool shape_ok(int rows, int cols) { return rows >= 1 && cols >= 1; }

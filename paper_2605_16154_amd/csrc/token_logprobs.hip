@@ -286,11 +286,13 @@ struct Best {
 // of every lane.  The lanes that have the `top` largest of those (of equal ones the lower chunk first) hold all that is asked for: a token of
 // another lane is behind the largest of each of them.  So their logits, `top` lanes of one in kThreads, are looked at again, and those not
 // below the last of the lanes' largest are sorted.  (Kept while passing over the logits, sorted lists take 40 us of 140 at 4096 x 65536.)
-// What it costs: 777 rows of 32003 fp32 none / 1 / 20 / 64 alternatives 25 / 29 / 31 / 38 us, with a mask of half the tokens 32 / 36 / 41 / 57.
+// What it costs: 777 rows of 32003 fp32 none / 1 / 20 / 64 alternatives 20 / 24 / 26 / 34 us, with a mask per row of half the tokens 25 / 30 / 35 / 50.
 template <int kThreads>
 struct TopScratch {
     uint64_t lists[kThreads / 64][64];
-    static constexpr int kRoom = 512;           // found so far when another round, of up to kThreads * 8, is begun without sorting them
+    // Found so far when another round, of up to kThreads * 8, is begun without sorting them.  64 / 512 / 2048: 4096 rows of 65536 bf16, 5 alternatives
+    // 108 / 109 / 117 us, 64 of them 201 / 200 / 192; rows that rise, where most of what is looked at is kept, 20 of them 118 / 122 / 137.
+    static constexpr int kRoom = 512;
     uint64_t found[kRoom + kThreads * 8];
     int lane_of[kTopMost];
     int lanes, n;
@@ -348,8 +350,8 @@ __device__ __forceinline__ uint64_t select_top(TopScratch<kThreads>& lds, const 
 }
 
 // A workgroup per part of a row (a wavefront for rows of up to kWaveRow), in chunks of eight logits per lane.  Measured: 4096 rows of 65536 bf16 with
-// the entropy 101 us (5.3 TB/s), with five alternatives 110; fp32 181 (5.9 TB/s).  8 rows of 131072 with eight alternatives, all latency: 8.5 us in 32
-// parts and 4.7 for the launch that joins them (69 in one part).
+// the entropy 100 us (5.4 TB/s), with five alternatives 109; fp32 178 (6.0 TB/s).  8 rows of 131072 with eight alternatives, all latency: 8.2 us in 32
+// parts and 5.1 for the launch that joins them (69 in one part).
 template <class T, bool kMask, bool kEntropy, bool kTop, int kThreads>
 __global__ __launch_bounds__(kThreads) void token_logprobs_parts(Logits q, LogprobsOut o, RowParts parts) {
     constexpr int kWaves = kThreads / 64;
@@ -432,7 +434,7 @@ __global__ __launch_bounds__(kJoinThreads) void token_logprobs_join(Logits q, Lo
 }
 
 // Rows of up to 16 kLanes logits: kLanes lanes per row, all of it in registers, and the sums relative to its largest logit.  43008 rows of 256 bf16:
-// 7.2 us (22 MB; as much latency as memory), where a workgroup per row takes 55.
+// 6.9 us (22 MB; as much latency as memory), where a workgroup per row takes 55.
 template <int kLanes>
 __device__ __forceinline__ float lanes_max(float x) {
 #pragma unroll
@@ -570,8 +572,8 @@ struct RowGradient {
 };
 
 // Rows of up to 16 kLanes logits: kLanes lanes per row, all of it in registers; 43008 rows of 256 bf16 9.3 us.  Wider ones (kLanes = 256): a workgroup
-// per row, or per part of one.  Bound by memory: 4096 rows of 131072 bf16 419 us, 1111 of 50021 fp32 with a mask 88 (5.1 and 5.0 TB/s read and
-// written; a large copy has 4.8).
+// per row, or per part of one.  Bound by memory: 4096 rows of 131072 bf16 419 us, 1111 of 50021 fp32 with a mask 86 (5.1 TB/s read and
+// written, both; a large copy has 4.8).
 constexpr int kGradientThreads = 256;
 template <class T, bool kMask, int kLanes>
 __global__ __launch_bounds__(kGradientThreads) void token_logprobs_gradient(Logits q, LogprobsGradient b, int parts) {
@@ -639,7 +641,8 @@ void with_lanes(int V, F f) {
     else if (V <= 512) f(std::integral_constant<int, 32>{});
     else f(std::integral_constant<int, 64>{});
 }
-// Parts of a row: as many as make `fill` workgroups of all rows, of two chunks per lane or more.  The pass over the logits is joined by another
+// Parts of a row: as many as make `fill` workgroups of all rows, of two chunks per lane or more (one / two / four at least, eight alternatives: 8 rows of
+// 131072 bf16 13.3 / 12.0 / 12.4 us, 8 of 32003 fp32 12.0 / 12.0 / 12.7; their gradients 3.3 / 3.3 / 3.9 and 3.6 / 3.6 / 4.3).  The pass over the logits is joined by another
 // launch, so it stays whole where rows fill the chip (workgroups 512 / 1024 / 2048 / 4096 at most, eight alternatives: 300 rows of 50021 bf16
 // 21.7 / 22.5 / 27.3 / 33.6 us, 777 of 32003 fp32 27.6 / 27.6 / 35.6 / 37.1).  The gradient has nothing to join, and short parts even out
 // (2048 / 4096 / 8192 / 16384: 1111 rows of 50021 fp32 106 / 97 / 88 / 93 us, 2500 of 30000 bf16 54 / 54 / 51 / 54).
