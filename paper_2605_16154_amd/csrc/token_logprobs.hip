@@ -644,8 +644,8 @@ void with_lanes(int V, F f) {
 // Parts of a row: as many as make `fill` workgroups of all rows, of two chunks per lane or more (one / two / four at least, eight alternatives: 8 rows of
 // 131072 bf16 13.3 / 12.0 / 12.4 us, 8 of 32003 fp32 12.0 / 12.0 / 12.7; their gradients 3.3 / 3.3 / 3.9 and 3.6 / 3.6 / 4.3).  The pass over the logits is joined by another
 // launch, so it stays whole where rows fill the chip (workgroups 512 / 1024 / 2048 / 4096 at most, eight alternatives: 300 rows of 50021 bf16
-// 21.7 / 22.5 / 27.3 / 33.6 us, 777 of 32003 fp32 27.6 / 27.6 / 35.6 / 37.1).  The gradient has nothing to join, and short parts even out
-// (2048 / 4096 / 8192 / 16384: 1111 rows of 50021 fp32 106 / 97 / 88 / 93 us, 2500 of 30000 bf16 54 / 54 / 51 / 54).
+// 18.1 / 19.3 / 22.7 / 28.1 us, 777 of 32003 fp32 24.5 / 24.5 / 30.6 / 31.7).  The gradient has nothing to join, and short parts even out
+// (2048 / 4096 / 8192 / 16384: 1111 rows of 50021 fp32 106 / 97 / 88 / 92 us, 2500 of 30000 bf16 57 / 57 / 52 / 58).
 constexpr int kForwardFill = 1024, kGradientFill = 8192, kWide = 256, kWaveRow = 4096;
 int row_parts(int64_t rows, int V, int fill) {
     if (V <= kWaveRow || rows < 1) return 1;
