@@ -172,9 +172,8 @@ def _round_states(x, field, random):
     fine = torch.floor(bits.int().view(torch.float32).double() * _power(16 - unit)).clamp(max=float(1 << 20)).long()
     code = torch.where(code >= 8, code, (fine + random) >> 16)
     if field == V_FIELD:
-        code = torch.where(bits > 0, code.clamp(min=1), code)
-    code = torch.where(top > 0, code, 0)
-    return code, top, sign
+        code = code.clamp(min=1)
+    return torch.where(bits > 0, code, 0), top, sign
 
 
 def _values(code, top, sign, field):
