@@ -537,6 +537,53 @@ PCM_API int pcm_muon_step(int n_tensors, const int* rows, const int* cols, const
                           double weight_decay, int ns_steps, int scale_rule, void* workspace, size_t workspace_bytes,
                           void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * pcm_adamw_many_step -- pcm_adamw_clip_step over all tensors of a model at once: any number of them, of any sizes and alignments, with
+ * gradients in fp32 or bf16 and moments in 32 or in 8 bits.  Norm, clipping and update as there, the norm over all tensors together.
+ *
+ * A plan is made once for the tensors (again when their addresses change) and holds what a step needs to find them; the moments are one
+ * flat block.  Both belong to the caller:
+ *   pcm_adamw_many_describe  fills a layout (host) from the sizes: the bytes of plan and state, and what the other calls need
+ *   pcm_adamw_many_plan      writes the plan to host memory of layout.plan_bytes bytes (8-byte aligned); the caller copies it to the device
+ *   state                    device, 16-byte aligned, layout.state_bytes bytes; zeros are the state before the first step.  Copying it out
+ *                            and back is a checkpoint
+ * With E = layout.elements, the sum of the tensors' sizes each rounded up to PCM_ADAMW_BLOCK, tensor i begins at the sum of those before it:
+ *   32 bits  float m[E], v[E]
+ *   8 bits   u8 m[E], v[E]; u8 exponent of m [E / PCM_ADAMW_BLOCK], of v [the same].  With T the exponent of a block (of PCM_ADAMW_BLOCK
+ *            elements) and f = 15 for m, 31 for v: a code c (of m the low seven bits, the eighth is the sign) is the value
+ *            (8 + c mod 8) 2^(T - f - 130 + c / 8) for c >= 8, else c 2^(T - f - 129); T = 255: NaN throughout.
+ *   What pads a tensor is zero.
+ * Moments in 8 bits are rounded to one of the two neighbouring codes so that their expectation is the value (T is the exponent that the largest of
+ * the block's rounded values has): element j takes bits 16 (j mod 2) .. + 15 of word (j mod 8) / 2 of Philox4x32-10(counter = (j / 8 low, high,
+ * step low, high), key = seed), for m and for v.  A v that is not zero keeps at least code 1; values below 2^-126 count as zero.  The weights
+ * are updated with the moments before they are rounded.
+ *
+ *   n_tensors, numel   numel[i] >= 0; at most 2^42 elements together
+ *   grads, grad_dtypes host arrays: device pointers and pcm_dtype of each;  weights host array of device pointers f32, updated in place
+ *   weights_bf16       NULL, or a host array of device pointers (entries may be NULL) that receive the new weights, rounded to nearest even
+ *   max_grad_norm      infinity: no clipping; without grad_norm_out the norm is then not formed and needs no workspace
+ *   seed               of the rounding of 8-bit moments
+ * Errors: PCM_EINVAL also where tensors of a plan that are written share memory with any other, for a layout that pcm_adamw_many_describe did
+ * not make and for hyper-parameters out of range; PCM_EWORKSPACE for a plan buffer that is too small.  Steps on the same state have to be ordered.
+ *
+ * pcm_adamw_many_states -- the values of 8-bit moments: m_out, v_out device [E] of dtype (bf16 holds them exactly).
+ * ------------------------------------------------------------------------------------------ */
+#define PCM_ADAMW_BLOCK 128
+typedef struct {
+    int64_t chunks, elements;
+    size_t plan_bytes, state_bytes;
+    int state_bits;
+} pcm_adamw_many_layout;
+PCM_API int pcm_adamw_many_describe(int n_tensors, const int64_t* numel, int state_bits, pcm_adamw_many_layout* layout);
+PCM_API int pcm_adamw_many_plan(int n_tensors, const int64_t* numel, const void* const* grads, const int* grad_dtypes,
+                                float* const* weights, void* const* weights_bf16, void* plan, size_t plan_bytes);
+PCM_API size_t pcm_adamw_many_step_workspace_bytes(const pcm_adamw_many_layout* layout);
+PCM_API int pcm_adamw_many_step(const void* plan, const pcm_adamw_many_layout* layout, void* state, int64_t step, double lr,
+                                double beta1, double beta2, double eps, double weight_decay, double max_grad_norm, uint64_t seed,
+                                float* grad_norm_out, void* workspace, size_t workspace_bytes, void* stream);
+PCM_API int pcm_adamw_many_states(const pcm_adamw_many_layout* layout, const void* state, int dtype, void* m_out, void* v_out,
+                                  void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -103,3 +103,94 @@ def muon_step(weights, grads, momentum, lr, momentum_coef=0.95, nesterov=True, w
         new_m.append(m)
         steps.append(o)
     return new_w, new_m, steps
+
+
+# ---- moments in 8 bits ---------------------------------------------------------------------------
+
+MOMENT_BLOCK = 128
+M_FIELD, V_FIELD = 15, 31            # largest exponent field of a code of m (with a sign) and of v
+
+
+def _philox_groups(groups, step, seed):
+    """Philox-4x32-10 of counters (group low, group high, step low, step high), as [groups, 8] numbers of 16 bits."""
+    low = np.uint64(0xFFFFFFFF)
+    g = np.asarray(groups, np.uint64)
+    c = [g & low, g >> np.uint64(32), np.full_like(g, step & 0xFFFFFFFF), np.full_like(g, step >> 32)]
+    k0, k1 = seed & 0xFFFFFFFF, seed >> 32
+    for _ in range(10):
+        p, q = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(q >> np.uint64(32)) ^ c[1] ^ np.uint64(k0), q & low, (p >> np.uint64(32)) ^ c[3] ^ np.uint64(k1), p & low]
+        k0, k1 = (k0 + 0x9E3779B9) & 0xFFFFFFFF, (k1 + 0xBB67AE85) & 0xFFFFFFFF
+    words = np.stack(c, axis=1)
+    return np.stack([words & np.uint64(0xFFFF), words >> np.uint64(16)], axis=2).reshape(len(g), 8).astype(np.int64)
+
+
+def moment_codes(x, random, field):
+    """-> (codes, block exponents) of fp32 values, whole blocks of them, with 16 random bits each; real arithmetic, value by value.
+
+    The two neighbours of a value among (8 + k) 2^e, k = 0 .. 7, e whole: the upper one where the part behind the point and random / 2^16
+    make one.  Below the block's reach the spacing stays what it is there."""
+    x = np.asarray(x, np.float32).reshape(-1, MOMENT_BLOCK)
+    u = np.asarray(random, np.int64).reshape(x.shape)
+    codes, tops = np.zeros(x.shape, np.uint8), np.zeros(len(x), np.uint8)
+    for b in range(len(x)):
+        a = np.abs(x[b].astype(np.float64))
+        if not np.all(np.isfinite(a)):
+            tops[b] = 255
+            continue
+        a[a < 2.0 ** -126] = 0.0
+        live = np.flatnonzero(a)
+        if len(live) == 0:
+            continue
+        exponent = np.frexp(a[live])[1] - 1
+        near = np.floor(a[live] / 2.0 ** (exponent - 3) + u[b, live] / 65536.0) * 2.0 ** (exponent - 3)
+        top = int((np.frexp(near)[1] - 1).max()) + 127
+        tops[b] = top
+        if top >= 255:
+            tops[b] = 255
+            continue
+        least = 2.0 ** (top - field - 129.0)
+        for i, value in zip(live, near):
+            if value < 8 * least:
+                k = int(np.floor((np.floor(a[i] / least * 65536.0) + u[b, i]) / 65536.0))
+            else:
+                e = int(np.frexp(value)[1]) - 1
+                k = 8 * (e + 127 - top + field) + int(round(value / 2.0 ** (e - 3))) - 8
+            codes[b, i] = max(k, 1) if field == V_FIELD else (k + 128 if k and np.signbit(x[b, i]) else k)
+    return codes.reshape(-1), tops
+
+
+def moment_values(codes, tops, field):
+    """The values that codes and block exponents stand for, in 64 bits."""
+    codes = np.asarray(codes, np.int64).reshape(-1, MOMENT_BLOCK)
+    top = np.asarray(tops, np.int64)[:, None]
+    c = codes if field == V_FIELD else codes & 127
+    x = np.where(c >= 8, (8.0 + c % 8) * 2.0 ** (top - field - 130.0 + c // 8), c * 2.0 ** (top - field - 129.0))
+    x = np.where(top == 255, np.nan, x)
+    return (x if field == V_FIELD else np.where(codes > 127, -x, x)).reshape(-1)
+
+
+def adamw_many_eight(weights, grads, state, step, seed, lr, beta1, beta2, eps, weight_decay, max_grad_norm):
+    """One step on moments in 8 bits, `state` = (m codes, v codes, m exponents, v exponents) of all tensors behind one another, each padded
+    to whole blocks.  Norm and factor in 64 bits, moments in 32 (each operation rounded), the update in 64.
+    -> (weights in 64 bits, state, norm)"""
+    f = np.float32
+    norm = np.sqrt(sum(float((np.asarray(g, np.float64) ** 2).sum()) for g in grads))
+    scale = f(1.0) if max_grad_norm is None else f(min(1.0, max_grad_norm / (norm + 1e-6)))
+    m_old = moment_values(state[0], state[2], M_FIELD).astype(f)
+    v_old = moment_values(state[1], state[3], V_FIELD).astype(f)
+    m, v, out, at = np.zeros_like(m_old), np.zeros_like(v_old), [], 0
+    for w, g in zip(weights, grads):
+        n = np.asarray(g).size
+        x = np.asarray(g, f).reshape(-1) * scale
+        part = slice(at, at + n)
+        m[part] = f(beta1) * m_old[part] + f(1.0 - beta1) * x
+        v[part] = f(beta2) * v_old[part] + f(1.0 - beta2) * (x * x)
+        mh = m[part].astype(np.float64) / (1.0 - beta1 ** step)
+        vh = v[part].astype(np.float64) / (1.0 - beta2 ** step)
+        out.append(np.asarray(w, np.float64).reshape(-1) * (1.0 - lr * weight_decay) - lr * mh / (np.sqrt(vh) + eps))
+        at += -(-n // MOMENT_BLOCK) * MOMENT_BLOCK
+    random = _philox_groups(np.arange(len(m) // 8), step, seed).reshape(-1)
+    mc, mt = moment_codes(m, random, M_FIELD)
+    vc, vt = moment_codes(v, random, V_FIELD)
+    return out, (mc, vc, mt, vt), norm

@@ -9,12 +9,16 @@ without the built library raises.
 from .binding import (  # noqa: F401
     PCM_BF16,
     PCM_F32,
+    AdamwManyPlan,
     PcmError,
     grpo_masked_actor_step,
     grpo_masked_actor_step_workspace_bytes,
     lib,
     library_path,
     pcm_adamw_clip_step,
+    pcm_adamw_many_plan,
+    pcm_adamw_many_states,
+    pcm_adamw_many_step,
     pcm_importance_weights,
     pcm_kept_phase_counts,
     pcm_label_phases,

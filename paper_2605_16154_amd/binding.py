@@ -35,6 +35,12 @@ class LossOptions(C.Structure):
                 ("packed_weights", C.c_void_p), ("dense_backward", C.c_int), ("grad_sumsq_out", C.c_void_p)]
 
 
+class AdamwManyLayout(C.Structure):
+    """pcm_adamw_many_layout of include/pcm.h."""
+    _fields_ = [("chunks", C.c_int64), ("elements", C.c_int64), ("plan_bytes", C.c_size_t), ("state_bytes", C.c_size_t),
+                ("state_bits", C.c_int)]
+
+
 def _sig(fn, res, args):
     fn.restype = res
     fn.argtypes = args
@@ -92,6 +98,12 @@ def lib() -> C.CDLL:
     _sig(L.pcm_muon_step, i32,
          [i32, C.POINTER(i32), C.POINTER(i32), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), f64, f64, i32,
           f64, i32, i32, vp, sz, vp])
+    layout = C.POINTER(AdamwManyLayout)
+    _sig(L.pcm_adamw_many_describe, i32, [i32, C.POINTER(i64), i32, layout])
+    _sig(L.pcm_adamw_many_plan, i32, [i32, C.POINTER(i64), C.POINTER(vp), C.POINTER(i32), C.POINTER(vp), C.POINTER(vp), vp, sz])
+    _sig(L.pcm_adamw_many_step_workspace_bytes, sz, [layout])
+    _sig(L.pcm_adamw_many_step, i32, [vp, layout, vp, i64, f64, f64, f64, f64, f64, f64, u64, vp, vp, sz, vp])
+    _sig(L.pcm_adamw_many_states, i32, [layout, vp, i32, vp, vp, vp])
     _sig(L.pcm_profile_enable, i32, [i32])
     _sig(L.pcm_profile_stage_count, i32, [])
     _sig(L.pcm_profile_stage_name, C.c_char_p, [i32])
@@ -668,6 +680,108 @@ def pcm_muon_step(grads, weights, momentum, lr: float = 0.02, momentum_coef: flo
         _check(lib().pcm_muon_step(*args, ws.data_ptr(), ws.numel(), stream), "pcm_muon_step")
     finally:
         _give_workspace(ws, dev, stream)
+
+
+def _on_current_device(device: torch.device, what: str) -> None:
+    """Launches go to the current device's stream, so the tensors have to be there."""
+    if device.index != torch._C._cuda_getDevice():
+        raise PcmError(f"{what}: tensors on {device}, which is not the current device")
+
+
+ADAMW_BLOCK = 128
+
+
+class AdamwManyPlan:
+    """What pcm_adamw_many_step works on: the tensors of a model (kept alive), where they are, and their moments.
+
+    `state` (uint8, on the device) holds the moments and nothing else does: a copy of it is a checkpoint.  `offsets[i]` is where tensor i begins
+    in the flat moments (pcm_adamw_many_states)."""
+
+    def __init__(self, grads, weights, weights_bf16, layout, table, state):
+        self.grads, self.weights, self.weights_bf16 = grads, weights, weights_bf16
+        self.layout, self.table, self.state = layout, table, state
+        self.offsets, at = [], 0
+        for w in weights:
+            self.offsets.append(at)
+            at += -(-w.numel() // ADAMW_BLOCK) * ADAMW_BLOCK
+
+    @property
+    def state_bits(self) -> int:
+        return self.layout.state_bits
+
+
+def pcm_adamw_many_plan(grads, weights, state_bits: int = 32, weights_bf16=None, state: Optional[torch.Tensor] = None) -> AdamwManyPlan:
+    """The plan of an AdamW step over lists of tensors: gradients float32 or bfloat16 (each its own), weights float32, moments in 32 or 8 bits.
+
+    `weights_bf16`, if given, is a list (entries may be None) of bf16 tensors that receive the new weights.  `state`: the moments to go on with
+    (uint8, `state` of an earlier plan of the same sizes), else zeros.  To be made again when a tensor's memory changes."""
+    n = len(grads)
+    if n == 0 or len(weights) != n or (weights_bf16 is not None and len(weights_bf16) != n):
+        raise PcmError("pcm_adamw_many_plan: lists must have equal length")
+    dev = weights[0].device
+    lowp = [None] * n if weights_bf16 is None else list(weights_bf16)
+    for g, w, b in zip(grads, weights, lowp):
+        if g.numel() != w.numel() or (b is not None and b.numel() != w.numel()):
+            raise PcmError("pcm_adamw_many_plan: gradient, weight and bf16 copy must have equal sizes")
+        if g.dtype not in DTYPES:
+            raise PcmError(f"grads must be float32 or bfloat16, got {g.dtype}")
+        if any(t is not None and t.device != dev for t in (g, w, b)):
+            raise PcmError("pcm_adamw_many_plan: all tensors must be on one device")
+    numel = (C.c_int64 * n)(*[w.numel() for w in weights])
+    layout = AdamwManyLayout()
+    _check(lib().pcm_adamw_many_describe(n, numel, state_bits, C.byref(layout)), "pcm_adamw_many_describe")
+    arr = lambda ts, dt, name: (C.c_void_p * n)(*[_ptr(t, dt, name) for t in ts])
+    table = torch.empty(layout.plan_bytes, dtype=torch.uint8)
+    _check(lib().pcm_adamw_many_plan(n, numel, arr(grads, None, "grads"), (C.c_int * n)(*[DTYPES[g.dtype] for g in grads]),
+                                     arr(weights, _F32, "weights"), arr(lowp, _BF16, "weights_bf16"), table.data_ptr(), table.numel()),
+           "pcm_adamw_many_plan")
+    if state is None:
+        state = torch.zeros(layout.state_bytes, dtype=torch.uint8, device=dev)
+    elif state.numel() != layout.state_bytes or state.device != dev:
+        raise PcmError(f"state must be {layout.state_bytes} bytes on {dev}")
+    _ptr(state, _U8, "state")
+    return AdamwManyPlan(list(grads), list(weights), lowp, layout, table.to(dev), state)
+
+
+def pcm_adamw_many_step(plan: AdamwManyPlan, step: int, lr: float = 1e-5, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                        weight_decay: float = 0.0, max_grad_norm: Optional[float] = 2.0, seed: int = 0,
+                        grad_norm_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Global-norm clipping + AdamW over the tensors of a plan (updated in place); -> grad norm f32[1].
+
+    max_grad_norm None: no clipping, and the norm only if `grad_norm_out` is given.  `seed` goes into the rounding of 8-bit moments."""
+    dev = plan.state.device
+    _on_current_device(dev, "pcm_adamw_many_step")
+    if max_grad_norm is not None and grad_norm_out is None:
+        grad_norm_out = torch.empty(1, dtype=_F32, device=dev)
+    entry, stream = lib().pcm_adamw_many_step, _stream()
+    head = (plan.table.data_ptr(), C.byref(plan.layout), plan.state.data_ptr(), step, lr, beta1, beta2, eps, weight_decay,
+            float("inf") if max_grad_norm is None else max_grad_norm, seed & 0xFFFFFFFFFFFFFFFF, _ptr(grad_norm_out, _F32, "grad_norm_out"))
+    if grad_norm_out is None:
+        _check(entry(*head, None, 0, stream), "pcm_adamw_many_step")
+        return None
+    ws = _take_workspace(lib().pcm_adamw_many_step_workspace_bytes(C.byref(plan.layout)), dev, stream)
+    try:
+        _check(entry(*head, ws.data_ptr(), ws.numel(), stream), "pcm_adamw_many_step")
+    finally:
+        _give_workspace(ws, dev, stream)
+    return grad_norm_out
+
+
+def pcm_adamw_many_states(plan: AdamwManyPlan, dtype: torch.dtype = torch.bfloat16) -> Tuple[torch.Tensor, torch.Tensor]:
+    """-> (m, v), flat, tensor i from plan.offsets[i] on.  Moments in 32 bits are the plan's own memory; those in 8 bits are read out as
+    bfloat16, which holds them exactly, or float32."""
+    E = plan.layout.elements
+    if plan.state_bits == 32:
+        m, v = plan.state.view(_F32).split(E) if E else (plan.state.view(_F32),) * 2
+        return m, v
+    if dtype not in DTYPES:
+        raise PcmError(f"dtype must be float32 or bfloat16, got {dtype}")
+    dev = plan.state.device
+    _on_current_device(dev, "pcm_adamw_many_states")
+    m, v = torch.empty((2, E), dtype=dtype, device=dev).unbind()
+    _check(lib().pcm_adamw_many_states(C.byref(plan.layout), plan.state.data_ptr(), DTYPES[dtype], m.data_ptr(), v.data_ptr(), _stream()),
+           "pcm_adamw_many_states")
+    return m, v
 
 
 def pcm_measure_mfma_rate(random_operands: bool = True, milliseconds: int = 100) -> Tuple[float, float]:

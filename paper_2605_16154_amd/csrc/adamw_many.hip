@@ -1,0 +1,462 @@
+// AdamW over all tensors of a model, states in 32 or in 8 bits.  Streaming work, bound by HBM:
+//
+//   pass 1  many_sumsq    fp64 partial sums of g^2 (only where the norm is asked for)
+//   pass 2  many_update   norm and clip factor from the partial sums; m, v, weights in place, bf16 copy
+//
+// The tensors are one list of chunks of up to 4096 elements in device memory, each with the addresses it needs, so hundreds of
+// tensors of any size are two launches, and a workgroup finds its work with one dependent load.
+//
+// States in 8 bits.  128 elements (a block) share an exponent E, that of the largest value; a code holds 3 bits behind the point and an
+// exponent field f up to F: m a sign and 4 bits (F = 15), v 5 bits (F = 31: v is a square, so both reach equally far down).  f = F is E; f = 0
+// holds the values below 2^(E - F + 1) at the spacing of f = 1, down to zero.  Values are rounded to one of their two neighbours with 16 random bits,
+// so that their expectation is the value: v moves by a thousandth of itself per step, a hundredth of the spacing, and rounding to nearest
+// would keep it where it is for good.  v > 0 never becomes 0, which would make the update m / eps.  The update itself takes m and v
+// before they are rounded.  All of it is integer arithmetic and fp32 without fused multiply-add: bits do not depend on the launch.
+#include "adamw_many.h"
+
+#include <cstdlib>
+
+#include "philox.h"
+
+namespace pcm {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPass = kThreads * 8;              // elements: eight neighbours a lane
+constexpr int kSumsqGrid = 1024, kUpdateGrid = 2048;
+constexpr int kSignField = 15, kSquareField = 31;
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+// tensors lie where the caller put them: 16 bytes at a time at whatever alignment their type has
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+
+// (a function per type: a template parameter would lose the alignment)
+#define PCM_STREAMED(type, name)                                                                                                  \
+    template <bool kStream>                                                                                                       \
+    __device__ inline auto load_##name(const type* p) { return kStream ? __builtin_nontemporal_load(p) : *p; }                    \
+    template <bool kStream>                                                                                                       \
+    __device__ inline void store_##name(type* p, type x) {                                                                        \
+        if (kStream) __builtin_nontemporal_store(x, p);                                                                           \
+        else *p = x;                                                                                                              \
+    }
+PCM_STREAMED(f32x4_any, four)
+PCM_STREAMED(u32x4_any, eight)
+PCM_STREAMED(u32x2, codes)
+#undef PCM_STREAMED
+
+// Eight fp32 values of which the first `n` exist; the others are 0.
+template <bool kStream>
+__device__ inline void load_floats(float (&x)[8], const float* p, int n) {
+    if (n >= 8) {
+        const f32x4 a = load_four<kStream>(reinterpret_cast<const f32x4_any*>(p)), b = load_four<kStream>(reinterpret_cast<const f32x4_any*>(p + 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[e + 4] = b[e]; }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = e < n ? p[e] : 0.f;
+    }
+}
+template <bool kStream>
+__device__ inline void store_floats(float* p, const float (&x)[8], int n) {
+    if (n >= 8) {
+        store_four<kStream>(reinterpret_cast<f32x4_any*>(p), f32x4_any{x[0], x[1], x[2], x[3]});
+        store_four<kStream>(reinterpret_cast<f32x4_any*>(p + 4), f32x4_any{x[4], x[5], x[6], x[7]});
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n) p[e] = x[e];
+    }
+}
+__device__ inline uint32_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+template <bool kStream>
+__device__ inline void load_gradient(float (&g)[8], const AdamwChunk& k, int i) {
+    const int n = k.count - i;
+    if (!k.grad_bf16) return load_floats<kStream>(g, static_cast<const float*>(k.grad) + i, n);
+    const uint16_t* p = static_cast<const uint16_t*>(k.grad) + i;
+    if (n >= 8) {
+        const u32x4 a = load_eight<kStream>(reinterpret_cast<const u32x4_any*>(p));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            g[2 * e] = __builtin_bit_cast(float, a[e] << 16);
+            g[2 * e + 1] = __builtin_bit_cast(float, a[e] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g[e] = e < n ? __builtin_bit_cast(float, (uint32_t)p[e] << 16) : 0.f;
+    }
+}
+__device__ inline void store_bf16(uint16_t* p, const float (&x)[8], int n) {
+    if (n >= 8) {
+        u32x4_any a;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[e] = bf16_bits(x[2 * e]) | bf16_bits(x[2 * e + 1]) << 16;
+        store_eight<false>(reinterpret_cast<u32x4_any*>(p), a);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n) p[e] = (uint16_t)bf16_bits(x[e]);
+    }
+}
+
+// Sum over the workgroup, in every thread; the same order whatever the values.
+__device__ inline double block_sum(double x) {
+    __shared__ double lds[kThreads / 64];
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+
+__global__ __launch_bounds__(kThreads) void many_sumsq(const AdamwChunk* chunks, int64_t n, double* partial) {
+    double acc[8] = {};
+    for (int64_t at = blockIdx.x; at < n; at += gridDim.x) {
+        const AdamwChunk k = chunks[at];
+#pragma unroll
+        for (int r = 0; r < kManyChunk / kPass; ++r) {
+            const int i = r * kPass + threadIdx.x * 8;
+            if (i >= k.count) continue;
+            float g[8];
+            load_gradient<false>(g, k, i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = __builtin_fma((double)g[e], (double)g[e], acc[e]);
+        }
+    }
+    const double total = block_sum(((acc[0] + acc[1]) + (acc[2] + acc[3])) + ((acc[4] + acc[5]) + (acc[6] + acc[7])));
+    if (threadIdx.x == 0) partial[blockIdx.x] = total;
+}
+
+// Largest value among the 16 lanes that hold a block.
+__device__ inline uint32_t block_max(uint32_t x) {
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x128, 0xf, 0xf, true));       // rotated by 8, 4, 2 and 1 lanes
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x124, 0xf, 0xf, true));
+    x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x122, 0xf, 0xf, true));
+    return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x121, 0xf, 0xf, true));
+}
+// A code without its sign, as a value.
+template <int kField>
+__device__ inline float value_of(uint32_t code, int top) {
+    const int field = max((int)(code >> 3), 1);
+    const float x = (float)(code >= 8 ? 8 + (code & 7) : code);
+    return top == 255 ? __builtin_nanf("") : ldexpf(x, field + top - kField - 130);
+}
+// Exponent of a block, from each lane's eight values (as bits without a sign) and their random bits.
+__device__ inline int exponent_of(const uint32_t (&bits)[8], const uint32_t (&random)[8]) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = max(most, bits[e] < 1u << 23 ? 0u : bits[e] + (random[e] << 4));
+    return (int)min(block_max(most) >> 23, 255u);
+}
+template <int kField>
+__device__ inline uint32_t code_of(uint32_t bits, uint32_t random, int top) {
+    const int code = (int)((bits + (random << 4)) >> 20) - ((top - kField) << 3);
+    // below 2^(top - kField + 1): multiples of 2^(top - kField - 2), of which 16 bits behind the point count
+    const uint32_t fine = ((uint32_t)ldexpf(__builtin_bit_cast(float, bits), 16 + 129 + kField - top) + random) >> 16;
+    const uint32_t c = code >= 8 ? (uint32_t)code : fine;
+    return bits < 1u << 23 ? 0u : c;
+}
+
+// Norm and clip factor; every workgroup forms them from the partial sums by itself.
+__device__ inline float clip_factor(const ManyStep& s) {
+    if (s.parts == 0) return 1.f;
+    double acc = 0.0;
+    for (int i = threadIdx.x; i < s.parts; i += kThreads) acc += s.partial[i];
+    const double norm = sqrt(block_sum(acc));
+    if (s.norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *s.norm_out = (float)norm;
+    return (float)fmin(1.0, s.max_norm / (norm + 1e-6));
+}
+
+template <int kBits, bool kStream>
+__global__ __launch_bounds__(kThreads) void many_update(ManyStep s) {
+    const float scale = clip_factor(s);
+    const AdamConst& c = s.c;
+    for (int64_t at = blockIdx.x; at < s.n; at += gridDim.x) {
+        const AdamwChunk k = s.chunks[kStream ? s.n - 1 - at : at];
+        const int blocks_end = (k.count + kManyBlock - 1) / kManyBlock * kManyBlock;
+#pragma unroll 1
+        for (int r = 0; r < kManyChunk / kPass; ++r) {
+            const int i = r * kPass + threadIdx.x * 8;
+            if (i >= blocks_end) break;                       // by whole blocks, so the lanes of a block stay together
+            const int n = k.count - i;
+            const int64_t j = k.at + i;
+            float g[8], w[8], m[8], v[8];
+            load_gradient<kStream>(g, k, i);
+            load_floats<kStream>(w, k.weight + i, n);
+            if constexpr (kBits == 32) {
+                float* const state = reinterpret_cast<float*>(s.state) + j;
+                load_floats<kStream>(m, state, 8);
+                load_floats<kStream>(v, state + s.elements, 8);
+            } else {
+                const uint8_t* const tops = reinterpret_cast<const uint8_t*>(s.state) + 2 * s.elements + j / kManyBlock;
+                const u32x2 mc = load_codes<kStream>(reinterpret_cast<const u32x2*>(s.state + j));
+                const u32x2 vc = load_codes<kStream>(reinterpret_cast<const u32x2*>(s.state + s.elements + j));
+                const int m_top = tops[0], v_top = tops[s.elements / kManyBlock];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t a = mc[e / 4] >> (e % 4 * 8) & 255, b = vc[e / 4] >> (e % 4 * 8) & 255;
+                    const float x = value_of<kSignField>(a & 127, m_top);
+                    m[e] = a > 127 ? -x : x;
+                    v[e] = value_of<kSquareField>(b, v_top);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = g[e] * scale;
+                m[e] = c.beta1 * m[e] + c.one_minus_beta1 * x;
+                v[e] = c.beta2 * v[e] + c.one_minus_beta2 * (x * x);
+                const float denom = sqrtf(v[e]) * c.inv_sqrt_bc2 + c.eps;
+                w[e] = w[e] * c.decay - c.step_size * (m[e] / denom);
+            }
+            store_floats<kStream>(k.weight + i, w, n);
+            if (k.lowp != nullptr) store_bf16(k.lowp + i, w, n);
+            if constexpr (kBits == 32) {
+                float* const state = reinterpret_cast<float*>(s.state) + j;
+                if (n < 8) {                                  // what pads a tensor stays zero
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e >= n) m[e] = v[e] = 0.f;
+                }
+                store_floats<kStream>(state, m, 8);
+                store_floats<kStream>(state + s.elements, v, 8);
+            } else {
+                const uint64_t group = (uint64_t)(j / 8);
+                const PhiloxWords bits = philox4x32((uint32_t)group, (uint32_t)(group >> 32), s.step[0], s.step[1], s.seed[0], s.seed[1]);
+                uint32_t random[8], mb[8], vb[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    random[e] = bits.w[e / 2] >> (e % 2 * 16) & 0xffffu;
+                    mb[e] = e < n ? __builtin_bit_cast(uint32_t, m[e]) & 0x7fffffffu : 0u;
+                    vb[e] = e < n ? __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu : 0u;
+                }
+                const int m_top = exponent_of(mb, random), v_top = exponent_of(vb, random);
+                u32x2 mc = {0, 0}, vc = {0, 0};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t a = code_of<kSignField>(mb[e], random[e], m_top), b = code_of<kSquareField>(vb[e], random[e], v_top);
+                    const uint32_t sign = a != 0 && __builtin_bit_cast(uint32_t, m[e]) >> 31 ? 128u : 0u;
+                    mc[e / 4] |= ((a & 127u) | sign) << (e % 4 * 8);
+                    vc[e / 4] |= (vb[e] < 1u << 23 ? 0u : min(max(b, 1u), 255u)) << (e % 4 * 8);
+                }
+                store_codes<kStream>(reinterpret_cast<u32x2*>(s.state + j), mc);
+                store_codes<kStream>(reinterpret_cast<u32x2*>(s.state + s.elements + j), vc);
+                if ((threadIdx.x & 15) == 0) {
+                    uint8_t* const tops = reinterpret_cast<uint8_t*>(s.state) + 2 * s.elements + j / kManyBlock;
+                    tops[0] = (uint8_t)m_top;
+                    tops[s.elements / kManyBlock] = (uint8_t)v_top;
+                }
+            }
+        }
+    }
+}
+
+// The values of 8-bit states: bf16 holds them exactly, as fp32 does (down to the least bf16 value, 2^-133).
+template <bool kBf16>
+__global__ __launch_bounds__(kThreads) void many_states(const uint8_t* state, int64_t elements, void* m_out, void* v_out) {
+    for (int64_t j = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 8; j < elements; j += (int64_t)gridDim.x * kPass) {
+        const uint8_t* const tops = state + 2 * elements + j / kManyBlock;
+        const u32x2 mc = *reinterpret_cast<const u32x2*>(state + j), vc = *reinterpret_cast<const u32x2*>(state + elements + j);
+        const int m_top = tops[0], v_top = tops[elements / kManyBlock];
+        float m[8], v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t a = mc[e / 4] >> (e % 4 * 8) & 255, b = vc[e / 4] >> (e % 4 * 8) & 255;
+            const float x = value_of<kSignField>(a & 127, m_top);
+            m[e] = a > 127 ? -x : x;
+            v[e] = value_of<kSquareField>(b, v_top);
+        }
+        if (kBf16) {
+            store_bf16(static_cast<uint16_t*>(m_out) + j, m, 8);
+            store_bf16(static_cast<uint16_t*>(v_out) + j, v, 8);
+        } else {
+            store_floats<false>(static_cast<float*>(m_out) + j, m, 8);
+            store_floats<false>(static_cast<float*>(v_out) + j, v, 8);
+        }
+    }
+}
+
+// ---- host side -----------------------------------------------------------------------------------
+
+constexpr int64_t kMostElements = (int64_t)1 << 42;
+
+bool layout_of(int n_tensors, const int64_t* numel, int state_bits, pcm_adamw_many_layout& out) {
+    if (n_tensors < 1 || numel == nullptr || (state_bits != 8 && state_bits != 32)) return false;
+    int64_t chunks = 0, elements = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        if (numel[i] < 0 || numel[i] > kMostElements) return false;
+        chunks += ceil_div64(numel[i], kManyChunk);
+        elements += ceil_div64(numel[i], kManyBlock) * kManyBlock;
+        if (elements > kMostElements) return false;
+    }
+    out.chunks = chunks;
+    out.elements = elements;
+    out.plan_bytes = (size_t)chunks * sizeof(AdamwChunk);
+    out.state_bytes = state_bits == 32 ? (size_t)elements * 8 : (size_t)elements * 2 + (size_t)(elements / kManyBlock) * 2;
+    out.state_bits = state_bits;
+    return true;
+}
+bool layout_ok(const pcm_adamw_many_layout* l) {
+    return l != nullptr && l->chunks >= 0 && l->elements >= 0 && l->elements <= kMostElements && l->elements % kManyBlock == 0 &&
+           l->chunks <= l->elements / kManyBlock && l->elements <= l->chunks * kManyChunk && (l->state_bits == 8 || l->state_bits == 32);
+}
+bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+int sumsq_grid(int64_t chunks) { return (int)(chunks < kSumsqGrid ? chunks : kSumsqGrid); }
+
+struct Extent {
+    uintptr_t begin, end;
+    bool written;
+};
+void sift(Extent* x, int64_t n, int64_t i) {
+    for (int64_t child; (child = 2 * i + 1) < n; i = child) {
+        if (child + 1 < n && x[child].begin < x[child + 1].begin) ++child;
+        if (x[i].begin >= x[child].begin) return;
+        const Extent t = x[i];
+        x[i] = x[child];
+        x[child] = t;
+    }
+}
+// Whether something that is written shares memory with anything else (sorted in place: nothing here may throw).
+bool share_memory(Extent* x, int64_t n) {
+    for (int64_t i = n / 2 - 1; i >= 0; --i) sift(x, n, i);
+    for (int64_t last = n - 1; last > 0; --last) {
+        const Extent t = x[0];
+        x[0] = x[last];
+        x[last] = t;
+        sift(x, last, 0);
+    }
+    uintptr_t end = 0, written_end = 0;               // of those that begin earlier
+    for (int64_t i = 0; i < n; ++i) {
+        if (x[i].begin < (x[i].written ? end : written_end)) return true;
+        if (x[i].end > end) end = x[i].end;
+        if (x[i].written && x[i].end > written_end) written_end = x[i].end;
+    }
+    return false;
+}
+
+// Parameters beyond which a step's arrays outgrow the 256 MB memory-side cache.
+constexpr int64_t kStreamElements = 20 << 20;
+
+}  // namespace
+}  // namespace pcm
+
+using namespace pcm;
+
+extern "C" {
+
+PCM_API int pcm_adamw_many_describe(int n_tensors, const int64_t* numel, int state_bits, pcm_adamw_many_layout* layout) {
+    pcm_adamw_many_layout l{};
+    if (layout == nullptr || !layout_of(n_tensors, numel, state_bits, l)) return PCM_EINVAL;
+    *layout = l;
+    return PCM_OK;
+}
+
+PCM_API int pcm_adamw_many_plan(int n_tensors, const int64_t* numel, const void* const* grads, const int* grad_dtypes,
+                                float* const* weights, void* const* weights_bf16, void* plan, size_t plan_bytes) {
+    pcm_adamw_many_layout l{};
+    if (!layout_of(n_tensors, numel, 32, l) || !grads || !grad_dtypes || !weights || !aligned(plan, 8)) return PCM_EINVAL;
+    if (plan_bytes < l.plan_bytes || (plan == nullptr && l.plan_bytes > 0)) return PCM_EWORKSPACE;
+    int64_t extents = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        if (grad_dtypes[i] != PCM_F32 && grad_dtypes[i] != PCM_BF16) return PCM_EINVAL;
+        if (numel[i] == 0) continue;
+        void* lowp = weights_bf16 ? weights_bf16[i] : nullptr;
+        if (!grads[i] || !weights[i] || !aligned(grads[i], grad_dtypes[i] == PCM_F32 ? 4 : 2) || !aligned(weights[i], 4) || !aligned(lowp, 2))
+            return PCM_EINVAL;
+        extents += lowp ? 3 : 2;
+    }
+    if (extents == 0) return PCM_OK;
+    Extent* const extent = static_cast<Extent*>(malloc((size_t)extents * sizeof(Extent)));
+    if (extent == nullptr) return PCM_EWORKSPACE;
+    int64_t n = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        if (numel[i] == 0) continue;
+        auto add = [&](const void* p, int64_t bytes, bool written) { extent[n++] = Extent{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, written}; };
+        add(grads[i], numel[i] * (grad_dtypes[i] == PCM_F32 ? 4 : 2), false);
+        add(weights[i], numel[i] * 4, true);
+        if (weights_bf16 && weights_bf16[i]) add(weights_bf16[i], numel[i] * 2, true);
+    }
+    const bool shared = share_memory(extent, n);
+    free(extent);
+    if (shared) return PCM_EINVAL;
+    AdamwChunk* to = static_cast<AdamwChunk*>(plan);
+    int64_t first = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        const bool half = grad_dtypes[i] == PCM_BF16;
+        for (int64_t at = 0; at < numel[i]; at += kManyChunk) {
+            const int64_t count = numel[i] - at < kManyChunk ? numel[i] - at : kManyChunk;
+            *to++ = AdamwChunk{static_cast<const char*>(grads[i]) + at * (half ? 2 : 4), weights[i] + at,
+                               weights_bf16 && weights_bf16[i] ? static_cast<uint16_t*>(weights_bf16[i]) + at : nullptr, first + at,
+                               (int32_t)count, half};
+        }
+        first += ceil_div64(numel[i], kManyBlock) * kManyBlock;
+    }
+    return PCM_OK;
+}
+
+PCM_API size_t pcm_adamw_many_step_workspace_bytes(const pcm_adamw_many_layout* layout) {
+    if (!layout_ok(layout)) return 0;
+    Carver c(nullptr);
+    c.take<double>(kSumsqGrid);
+    return c.used();
+}
+
+PCM_API int pcm_adamw_many_step(const void* plan, const pcm_adamw_many_layout* layout, void* state, int64_t step, double lr, double beta1,
+                                double beta2, double eps, double weight_decay, double max_grad_norm, uint64_t seed, float* grad_norm_out,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+    if (!layout_ok(layout) || !adam_arguments_ok(step, lr, beta1, beta2, eps, weight_decay, max_grad_norm) || !aligned(plan, 8) ||
+        !aligned(state, 16) || !aligned(grad_norm_out, 4))
+        return PCM_EINVAL;
+    if (layout->chunks > 0 && (!plan || !state)) return PCM_EINVAL;
+    const bool want_norm = max_grad_norm < __builtin_huge_val() || grad_norm_out != nullptr;
+    if (want_norm && !workspace_ok(workspace, workspace_bytes, pcm_adamw_many_step_workspace_bytes(layout))) return PCM_EWORKSPACE;
+    if (layout->chunks == 0 && grad_norm_out == nullptr) return PCM_OK;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    ManyStep a{};
+    a.chunks = static_cast<const AdamwChunk*>(plan);
+    a.n = layout->chunks;
+    a.state = static_cast<char*>(state);
+    a.elements = layout->elements;
+    a.max_norm = max_grad_norm;
+    a.norm_out = grad_norm_out;
+    a.c = adam_const(step, lr, beta1, beta2, eps, weight_decay);
+    a.step[0] = (uint32_t)step; a.step[1] = (uint32_t)((uint64_t)step >> 32);
+    a.seed[0] = (uint32_t)seed; a.seed[1] = (uint32_t)(seed >> 32);
+    if (want_norm) {
+        Carver c(workspace);
+        double* const partial = c.take<double>(kSumsqGrid);
+        a.partial = partial;
+        a.parts = a.n > 0 ? sumsq_grid(a.n) : 1;
+        StageTimer t(ST_OPT_NORM, s);
+        many_sumsq<<<(unsigned)a.parts, kThreads, 0, s>>>(a.chunks, a.n, partial);
+    }
+    StageTimer t(ST_OPT_ADAMW, s);
+    const unsigned grid = (unsigned)(a.n < 1 ? 1 : a.n < kUpdateGrid ? a.n : kUpdateGrid);
+    const bool past = a.elements > kStreamElements;
+    if (layout->state_bits == 32) {
+        if (past) many_update<32, true><<<grid, kThreads, 0, s>>>(a);
+        else many_update<32, false><<<grid, kThreads, 0, s>>>(a);
+    } else {
+        if (past) many_update<8, true><<<grid, kThreads, 0, s>>>(a);
+        else many_update<8, false><<<grid, kThreads, 0, s>>>(a);
+    }
+    return launch_status();
+}
+
+PCM_API int pcm_adamw_many_states(const pcm_adamw_many_layout* layout, const void* state, int dtype, void* m_out, void* v_out, void* stream) {
+    if (!layout_ok(layout) || layout->state_bits != 8 || (dtype != PCM_F32 && dtype != PCM_BF16) || !aligned(state, 16) ||
+        !aligned(m_out, dtype == PCM_F32 ? 4 : 2) || !aligned(v_out, dtype == PCM_F32 ? 4 : 2))
+        return PCM_EINVAL;
+    if (layout->elements == 0) return PCM_OK;
+    if (!state || !m_out || !v_out) return PCM_EINVAL;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    StageTimer t(ST_OPT_ADAMW, s);
+    const int64_t groups = ceil_div64(layout->elements, kPass);
+    const unsigned grid = (unsigned)(groups < 8192 ? groups : 8192);
+    if (dtype == PCM_BF16) many_states<true><<<grid, kThreads, 0, s>>>(static_cast<const uint8_t*>(state), layout->elements, m_out, v_out);
+    else many_states<false><<<grid, kThreads, 0, s>>>(static_cast<const uint8_t*>(state), layout->elements, m_out, v_out);
+    return launch_status();
+}
+
+}  // extern "C"

@@ -8,7 +8,7 @@
 //   pass 3  adamw_chunks   m, v, theta updated in place, low-precision copy written
 //
 // The tensors are addressed as one list of chunks, so the whole head is one launch per pass.
-#include "common.h"
+#include "adamw.h"
 
 namespace pcm {
 namespace {
@@ -115,14 +115,6 @@ __global__ __launch_bounds__(1024) void finish_norm(NormArgs p, NormResult* resu
     *result = r;
     if (p.norm_out) *p.norm_out = r.norm;
 }
-
-struct AdamConst {
-    float beta1, beta2, one_minus_beta1, one_minus_beta2;
-    float decay;            // 1 - lr * weight_decay
-    float step_size;        // lr / (1 - beta1^t)
-    float inv_sqrt_bc2;     // 1 / sqrt(1 - beta2^t)
-    float eps;
-};
 
 __device__ inline uint16_t to_bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
@@ -255,9 +247,7 @@ PCM_API int pcm_adamw_clip_step_ex(int n_tensors, const int64_t* numel, const fl
                                    void* stream) {
     if (reinterpret_cast<uintptr_t>(grad_sumsq) & 7u) return PCM_EINVAL;
     if (n_tensors < 1 || n_tensors > kMaxTensors || !numel || !grads || !weights || !m || !v) return PCM_EINVAL;
-    if (step < 1 || !(lr >= 0.0) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps > 0.0) ||
-        !(weight_decay >= 0.0) || !(max_grad_norm > 0.0))
-        return PCM_EINVAL;
+    if (!adam_arguments_ok(step, lr, beta1, beta2, eps, weight_decay, max_grad_norm)) return PCM_EINVAL;
     TensorList tl{};
     tl.n = n_tensors;
     int64_t chunks = 0, elements = 0;
@@ -280,13 +270,7 @@ PCM_API int pcm_adamw_clip_step_ex(int n_tensors, const int64_t* numel, const fl
     if (!workspace_ok(workspace, workspace_bytes, w.bytes)) return PCM_EWORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);
 
-    AdamConst c;
-    c.beta1 = (float)beta1; c.beta2 = (float)beta2;
-    c.one_minus_beta1 = (float)(1.0 - beta1); c.one_minus_beta2 = (float)(1.0 - beta2);
-    c.decay = (float)(1.0 - lr * weight_decay);
-    c.step_size = (float)(lr / (1.0 - pow(beta1, (double)step)));
-    c.inv_sqrt_bc2 = (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step)));
-    c.eps = (float)eps;
+    const AdamConst c = adam_const(step, lr, beta1, beta2, eps, weight_decay);
     const NormArgs norm = grad_sumsq != nullptr ? NormArgs{grad_sumsq, 1, max_grad_norm, 1e-6, grad_norm_out}
                                                 : NormArgs{w.partial, chunks, max_grad_norm, 1e-6, grad_norm_out};
     const bool own = norm.n <= kOwnNormPartials;
