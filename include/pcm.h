@@ -538,6 +538,52 @@ PCM_API int pcm_muon_step(int n_tensors, const int* rows, const int* cols, const
                           void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * pcm_linear_logprobs -- pcm_token_logprobs of the logits z = hidden weight, which are never in memory: softmax cross entropy over a large
+ * vocabulary (-logp is a row's), the old-policy pass and the scoring of a policy from its last hidden rows.
+ *
+ * With x_j = (hidden[r] . weight[:, j]) / temperature, j over the whole vocabulary:
+ *   lse = log sum_j e^(x_j);   logp = x_token - lse;   entropy = lse - sum_j p_j x_j with p_j = e^(x_j - lse).
+ * A row whose token is negative is left out (prompts, padding): its three results are 0, and what it holds is not met by any other.
+ * Products and sums are fp32 or better (PCM_F32: each value as two of 11 significand bits, products of their high and low parts without the last).
+ *
+ *   hidden    device [rows] rows of d values of dtype (PCM_F32 or PCM_BF16), hidden_ld >= d values apart
+ *   weight    device, of dtype: PCM_WEIGHT_IN_OUT d rows of V values, PCM_WEIGHT_OUT_IN V rows of d values, weight_ld apart.  bf16 weights are read
+ *             where they are if their address is a multiple of 16 bytes and weight_ld and the length of a row of 8 values, else by way of the workspace
+ *   tokens    device [rows] of token_type; a token >= V counts as V-1
+ *   temperature  finite, at least 2^-126
+ *   logp, lse device f32 [rows];  entropy device f32 [rows] or NULL
+ * A NaN or +inf among the logits makes the row's results NaN.  Last bits depend on how many rows there are.  rows = 0 is a valid call (of the
+ * gradient: dweight becomes zeros).
+ * Limits: 1 <= d <= 2^16, 1 <= V <= 2^22, rows <= 2^24.
+ * Workspace: the slots of the rows and 12 bytes per row and 64 columns, never a row of logits; of the weight, where it has to be copied,
+ * at most 256 MB or 256 columns.
+ *
+ * pcm_linear_logprobs_backward -- the gradient of a loss from its gradients in logp and entropy, as pcm_token_logprobs_backward:
+ *   dz_j = ([j = token] dlogp - p_j (dlogp + dentropy (log p_j + entropy))) / temperature;  dhidden = dz weight^T;  dweight = hidden^T dz.
+ * The logits are formed again, piece by piece of the vocabulary; of dz at most 1 GB or 256 columns are in memory at a time, in bf16 (PCM_BF16:
+ * each value is rounded once, 2^-9 of it; PCM_F32: pairs as above).
+ *   lse, entropy     device f32 [rows], as the forward call left them (log p carries the rounding of lse: 2^-24 |lse|);  entropy NULL exactly if dentropy is
+ *   dlogp, dentropy  device f32 [rows]; those of rows without a token are not looked at;  dentropy NULL: no gradient through the entropy
+ *   dhidden          device [rows] rows of d values of dtype, dhidden_ld apart, or NULL; zeros for rows without a token
+ *   dweight          device, layout of weight, dweight_ld apart, of dweight_dtype (PCM_F32, or PCM_BF16 for bf16 weights), or NULL.  The
+ *                    sum over all rows is formed in fp32 and rounded once.  accumulate != 0 (PCM_F32 only): it is added to what is there
+ * Not both NULL.  Values between rows are left as they are.
+ * ------------------------------------------------------------------------------------------ */
+typedef enum { PCM_WEIGHT_IN_OUT = 0, PCM_WEIGHT_OUT_IN = 1 } pcm_weight_layout;
+PCM_API size_t pcm_linear_logprobs_workspace_bytes(int64_t rows, int d, int V, int dtype, int weight_layout, const void* weight,
+                                                   int64_t weight_ld);
+PCM_API int pcm_linear_logprobs(const void* hidden, int64_t hidden_ld, const void* weight, int64_t weight_ld, int weight_layout, int dtype,
+                                const void* tokens, int token_type, int64_t rows, int d, int V, float temperature, float* logp,
+                                float* lse, float* entropy, void* workspace, size_t workspace_bytes, void* stream);
+PCM_API size_t pcm_linear_logprobs_backward_workspace_bytes(int64_t rows, int d, int V, int dtype, int weight_layout, const void* weight,
+                                                            int64_t weight_ld);
+PCM_API int pcm_linear_logprobs_backward(const void* hidden, int64_t hidden_ld, const void* weight, int64_t weight_ld, int weight_layout,
+                                         int dtype, const void* tokens, int token_type, int64_t rows, int d, int V, float temperature,
+                                         const float* lse, const float* dlogp, const float* entropy, const float* dentropy, void* dhidden,
+                                         int64_t dhidden_ld, void* dweight, int64_t dweight_ld, int dweight_dtype, int accumulate,
+                                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * pcm_adamw_many_step -- pcm_adamw_clip_step over all tensors of a model at once: any number of them, of any sizes and alignments, with
  * gradients in fp32 or bf16 and moments in 32 or in 8 bits.  Norm, clipping and update as there, the norm over all tensors together.
  *

@@ -194,3 +194,36 @@ def adamw_many_eight(weights, grads, state, step, seed, lr, beta1, beta2, eps, w
     mc, mt = moment_codes(m, random, M_FIELD)
     vc, vt = moment_codes(v, random, V_FIELD)
     return out, (mc, vc, mt, vt), norm
+
+
+# ---- log-probabilities through a projection ------------------------------------------------------------
+
+def linear_logprobs(hidden, weight, tokens, temperature=1.0):
+    """-> dict(logp, lse, entropy [rows]) of the logits hidden @ weight; zeros for rows without a token (whatever they hold)."""
+    hidden, weight = np.asarray(hidden, np.float64), np.asarray(weight, np.float64)
+    rows = len(hidden)
+    out = {k: np.zeros(rows) for k in ("logp", "lse", "entropy")}
+    live = np.flatnonzero(np.asarray(tokens) >= 0)
+    if len(live):
+        got = token_logprobs(hidden[live] @ weight, np.asarray(tokens)[live], temperature=temperature)
+        for k in out:
+            out[k][live] = got[k]
+    return out
+
+
+def linear_logits_gradient(hidden, weight, tokens, dlogp, dentropy=None, temperature=1.0):
+    """d of sum(dlogp * logp) + sum(dentropy * entropy) in hidden @ weight [rows, V]; zeros for rows without a token."""
+    hidden, weight = np.asarray(hidden, np.float64), np.asarray(weight, np.float64)
+    g = np.zeros((len(hidden), weight.shape[1]))
+    live = np.flatnonzero(np.asarray(tokens) >= 0)
+    if len(live):
+        g[live] = token_logprobs_gradient(hidden[live] @ weight, np.asarray(tokens)[live], np.asarray(dlogp)[live],
+                                          None if dentropy is None else np.asarray(dentropy)[live], temperature=temperature)
+    return g
+
+
+def linear_logprobs_gradient(hidden, weight, tokens, dlogp, dentropy=None, temperature=1.0):
+    """-> (d hidden, d weight)."""
+    g = linear_logits_gradient(hidden, weight, tokens, dlogp, dentropy, temperature)
+    h = np.where(np.asarray(tokens)[:, None] >= 0, np.asarray(hidden, np.float64), 0.0)
+    return g @ np.asarray(weight, np.float64).T, h.T @ g

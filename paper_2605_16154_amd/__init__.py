@@ -22,6 +22,8 @@ from .binding import (  # noqa: F401
     pcm_importance_weights,
     pcm_kept_phase_counts,
     pcm_label_phases,
+    pcm_linear_logprobs,
+    pcm_linear_logprobs_backward,
     pcm_measure_mfma_rate,
     pcm_muon_step,
     pcm_orthogonalise,

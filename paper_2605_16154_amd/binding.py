@@ -98,6 +98,11 @@ def lib() -> C.CDLL:
     _sig(L.pcm_muon_step, i32,
          [i32, C.POINTER(i32), C.POINTER(i32), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp), f64, f64, i32,
           f64, i32, i32, vp, sz, vp])
+    for name in ("pcm_linear_logprobs", "pcm_linear_logprobs_backward"):
+        _sig(getattr(L, name + "_workspace_bytes"), sz, [i64, i32, i32, i32, i32, vp, i64])
+    linear = [vp, i64, vp, i64, i32, i32, vp, i32, i64, i32, i32, f32]
+    _sig(L.pcm_linear_logprobs, i32, linear + [vp, vp, vp, vp, sz, vp])
+    _sig(L.pcm_linear_logprobs_backward, i32, linear + [vp, vp, vp, vp, vp, i64, vp, i64, i32, i32, vp, sz, vp])
     layout = C.POINTER(AdamwManyLayout)
     _sig(L.pcm_adamw_many_describe, i32, [i32, C.POINTER(i64), i32, layout])
     _sig(L.pcm_adamw_many_plan, i32, [i32, C.POINTER(i64), C.POINTER(vp), C.POINTER(i32), C.POINTER(vp), C.POINTER(vp), vp, sz])
@@ -612,6 +617,140 @@ def pcm_token_logprobs_backward(logits, tokens, lse, dlogp, entropy: Optional[to
         raise PcmError("out must have the shape and type of the logits")
     p_out, out_ld = _rows_ptr(out, "out")
     _check(entry(*args, *p, p_out, out_ld, _stream()), "pcm_token_logprobs_backward")
+    return out
+
+
+def _weight_ptr(t: torch.Tensor, name: str, layout: Optional[int] = None) -> Tuple[int, int, int]:
+    """Address, leading dimension and layout of a matrix [d, V]: 0 for d rows of V values, 1 for V rows of d values (a transposed view)."""
+    if not t.is_cuda:
+        raise PcmError(f"{name} must live in device memory")
+    (d, V), (by_row, by_column) = t.shape, t.stride()
+    if layout != 1 and (V == 1 or by_column == 1) and (d == 1 or by_row >= V):
+        return t.data_ptr(), by_row if d > 1 else V, 0
+    if layout != 0 and (d == 1 or by_row == 1) and (V == 1 or by_column >= d):
+        return t.data_ptr(), by_column if V > 1 else d, 1
+    raise PcmError(f"{name} must be a matrix or the transpose of one, with contiguous rows that do not overlap" if layout is None else
+                   f"{name} must have the layout of weight, with contiguous rows that do not overlap")
+
+
+def _linear_args(hidden, weight, tokens, temperature: float):
+    """The arguments that both directions of the log-probabilities through a projection begin with."""
+    dtype, token_type = DTYPES.get(hidden.dtype), TOKEN_TYPES.get(tokens.dtype)
+    if hidden.dim() != 2 or dtype is None:
+        raise PcmError("hidden must be [rows, d] of float32 or bfloat16")
+    rows, d = hidden.shape
+    if weight.dim() != 2 or weight.shape[0] != d or weight.dtype != hidden.dtype:
+        raise PcmError("weight must be [d, V] of the type of hidden")
+    V = weight.shape[1]
+    if d == 0 or V == 0:
+        raise PcmError("weight must not be empty")
+    if token_type is None or tokens.shape != (rows,):
+        raise PcmError("tokens must be [rows] of uint8, int32 or int64")
+    if not (hidden.device == weight.device == tokens.device):
+        raise PcmError("hidden, weight and tokens must be on one device")
+    p_hidden, ld = _rows_ptr(hidden, "hidden")
+    p_weight, weight_ld, layout = _weight_ptr(weight, "weight")
+    p_tokens, = _ptrs(_TOKENS, tokens)
+    _on_current_device(hidden.device, "hidden")
+    return (p_hidden, ld, p_weight, weight_ld, layout, dtype, p_tokens, token_type, rows, d, V, temperature), (rows, d, V, dtype, layout, p_weight,
+                                                                                                                weight_ld)
+
+
+def pcm_linear_logprobs(hidden, weight, tokens, temperature: float = 1.0, want_entropy: bool = True,
+                        out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """-> dict(logp f32[rows], lse f32[rows], and as asked entropy f32[rows]) of the logits hidden @ weight / temperature, which are not kept.
+
+    hidden [rows, d], float32 or bfloat16, with contiguous rows (a view of a wider matrix will do); weight [d, V] of the same type, or the
+    transposed view of a matrix [V, d]; tokens [rows] uint8, int32 or int64, negative where a row has none: its results are 0.  `out` may carry
+    preallocated tensors."""
+    entry = lib().pcm_linear_logprobs
+    args, sizes = _linear_args(hidden, weight, tokens, temperature)
+    rows, dev = args[8], hidden.device
+    names = ("logp", "lse", "entropy") if want_entropy else ("logp", "lse")
+    if out is None:
+        out = dict(zip(names, torch.empty((len(names), rows), dtype=_F32, device=dev).unbind()))
+    p = []
+    for name in names:
+        t = out.get(name)
+        if t is None:
+            out[name] = t = torch.empty(rows, dtype=_F32, device=dev)
+        elif tuple(t.shape) != (rows,):
+            raise PcmError(f"out[{name!r}] has shape {tuple(t.shape)}, expected {(rows,)}")
+        p.append(_ptr(t, _F32, name))
+    if not want_entropy:
+        p.append(None)
+    if rows == 0:
+        _check(entry(*args, *p, None, 0, _stream()), "pcm_linear_logprobs")
+        return out
+    need = lib().pcm_linear_logprobs_workspace_bytes(*sizes)
+    if need == 0:
+        raise PcmError("pcm_linear_logprobs: unsupported shape or argument")
+    stream = _stream()
+    ws = _take_workspace(need, dev, stream)
+    try:
+        _check(entry(*args, *p, ws.data_ptr(), ws.numel(), stream), "pcm_linear_logprobs")
+    finally:
+        _give_workspace(ws, dev, stream)
+    return out
+
+
+def pcm_linear_logprobs_backward(hidden, weight, tokens, lse, dlogp, entropy: Optional[torch.Tensor] = None,
+                                 dentropy: Optional[torch.Tensor] = None, temperature: float = 1.0, want_dhidden: bool = True,
+                                 want_dweight: bool = True, dweight_dtype: Optional[torch.dtype] = None, accumulate: bool = False,
+                                 out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """-> dict(dhidden [rows, d], dweight [d, V], as asked), from dlogp f32[rows] and, if the loss has a part in the entropy, dentropy f32[rows]
+    with the entropy of the forward call; lse as the forward call returned it.
+
+    dweight has the type of weight (or dweight_dtype: float32 also for bfloat16 weights) and its layout.  `out` may carry preallocated tensors;
+    with accumulate the gradient is added to out["dweight"] (float32)."""
+    entry = lib().pcm_linear_logprobs_backward
+    args, sizes = _linear_args(hidden, weight, tokens, temperature)
+    rows, d, V, dev, layout = args[8], args[9], args[10], hidden.device, args[4]
+    if dentropy is None:
+        entropy = None
+    elif entropy is None:
+        raise PcmError("a gradient in the entropy needs the entropy")
+    p = _ptrs(_ROW_GRADS, lse, dlogp, entropy, dentropy)
+    for t in (lse, dlogp) if dentropy is None else (lse, dlogp, entropy, dentropy):
+        if t.shape != (rows,):
+            raise PcmError("lse, dlogp, entropy and dentropy must be [rows]")
+    out = {} if out is None else out
+    p_dh = p_dw = None
+    dh_ld, dw_ld, dw_type = d, 0, PCM_F32
+    if want_dhidden:
+        t = out.get("dhidden")
+        if t is None:
+            out["dhidden"] = t = torch.empty((rows, d), dtype=hidden.dtype, device=dev)
+        elif t.shape != (rows, d) or t.dtype != hidden.dtype:
+            raise PcmError("out['dhidden'] must have the shape and type of hidden")
+        p_dh, dh_ld = _rows_ptr(t, "dhidden")
+    if want_dweight:
+        t = out.get("dweight")
+        if t is None:
+            if accumulate:
+                raise PcmError("accumulate needs out['dweight']")
+            dt = weight.dtype if dweight_dtype is None else dweight_dtype
+            t = torch.empty((V, d), dtype=dt, device=dev).t() if layout else torch.empty((d, V), dtype=dt, device=dev)
+            out["dweight"] = t
+        elif t.shape != (d, V) or (dweight_dtype is not None and t.dtype != dweight_dtype):
+            raise PcmError("out['dweight'] must have the shape of weight and the type asked for")
+        if t.dtype not in DTYPES:
+            raise PcmError(f"dweight must be float32 or bfloat16, got {t.dtype}")
+        p_dw, dw_ld, _ = _weight_ptr(t, "dweight", layout)
+        dw_type = DTYPES[t.dtype]
+    tail = (p_dh, dh_ld, p_dw, dw_ld, dw_type, int(accumulate))
+    if rows == 0:
+        _check(entry(*args, *p, *tail, None, 0, _stream()), "pcm_linear_logprobs_backward")
+        return out
+    need = lib().pcm_linear_logprobs_backward_workspace_bytes(*sizes)
+    if need == 0:
+        raise PcmError("pcm_linear_logprobs_backward: unsupported shape or argument")
+    stream = _stream()
+    ws = _take_workspace(need, dev, stream)
+    try:
+        _check(entry(*args, *p, *tail, ws.data_ptr(), ws.numel(), stream), "pcm_linear_logprobs_backward")
+    finally:
+        _give_workspace(ws, dev, stream)
     return out
 
 

@@ -19,7 +19,8 @@ OBJ_DIR = os.path.join(PKG, "_build")
 
 SOURCES = ["runtime.hip", "score.hip", "keep_probs.hip", "sample.hip", "gather.hip",
            "actor_f32.hip", "actor_f32_direct.hip", "actor_bf16.hip", "actor_api.hip", "optimizer.hip", "labeler.hip",
-           "token_logprobs.hip", "orthogonalise.hip", "adamw_many.hip"]
+           "token_logprobs.hip", "orthogonalise.hip", "adamw_many.hip", "linear_logprobs.hip",
+           "linear_gradient.hip"]
 MEASURE_SOURCES = ["measure/mfma_rate.hip"]
 # the fp64 tails of the selection stage and the moments that are rounded to 8 bits are specified without fused multiply-add
 NO_CONTRACT = {"score.hip", "keep_probs.hip", "adamw_many.hip"}

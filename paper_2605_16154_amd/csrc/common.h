@@ -65,6 +65,8 @@ enum Stage : int {
     ST_TOKEN_LOGPROBS_GRAD,
     ST_ORTH_PREPARE,
     ST_ORTH_PRODUCTS,
+    ST_LINEAR_LOGPROBS,
+    ST_LINEAR_LOGPROBS_GRAD,
     ST_COUNT
 };
 

@@ -71,6 +71,7 @@ template <int kW, int kSlots = kRingSlots> constexpr int kRingBytes = kSlots * k
 template <int kW> constexpr int kWaveStageBytes = kRingBytes<kW> / 4;
 
 struct GemmProblem {
+    static constexpr bool kBoundedB = false, kHalves = false;   // see BoundedProblem
     const bf16* A;    // M x K1 operand, leading dimension lda (layout given by the kernel's template arguments)
     const bf16* B;    // N x K1 operand, leading dimension ldb
     const bf16* A2;   // optional second reduction segment (same M, N, layouts and leading dimensions), K2 columns;
@@ -102,6 +103,19 @@ struct GemmProblem {
     int cut;
 };
 enum Cut : int { kCutNone = 0, kCutHead = 1, kCutTail = 2 };
+
+// A product whose B operand lies in the caller's memory as it is: rows and reduction index of B end anywhere (in whole 16-byte pieces;
+// pointer and leading dimension multiples of 16 bytes), and what lies beyond reads as zero or, within a row's pitch or the next row, as what
+// is there.  So columns n >= N_real of the result hold anything, and the A operand has to be zero for k >= K_real up to the next multiple of 64.
+// M, N, K1 as above, rounded up.
+// kThirds: operands are fp16 matrices, pairs hi + lo of 22 significand bits each; three reduction segments of K1 add up
+// hi hi, hi lo and lo hi (A2, B2; A3, B3).
+template <bool kThirds>
+struct BoundedProblem : GemmProblem {
+    static constexpr bool kBoundedB = true, kHalves = kThirds;
+    int N_real, K_real;
+    const bf16 *A3, *B3;
+};
 enum RowsRole : int { kRowsUnused = 0, kRowsAreM = 1, kRowsAreK = 2 };
 
 // Accumulators of a wavefront: kW x kW tiles of 16 x 16.  Tile (i, j), register t of a lane is
@@ -203,24 +217,46 @@ __device__ inline void direct_load_16B(const char* base, uint32_t lane_offset, u
                  : "s"(lds_addr), "v"(lane_offset), "s"(base)
                  : "memory");
 }
+// The same through a buffer descriptor: lanes whose offset is not below its number of bytes bring in zeros.
+__device__ inline u32x4 buffer_of(const char* base, uint32_t bytes) {
+    const uint64_t at = (uint64_t)(uintptr_t)base;
+    return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, bytes, 0x00020000u};      // raw, 32-bit data format
+}
+__device__ inline void direct_load_16B(u32x4 buffer, uint32_t lane_offset, uint32_t lds_addr) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(lds_addr), "v"(lane_offset), "s"(buffer)
+                 : "memory");
+}
 // acc += B fragment x A fragment.  Inline assembly so that the accumulators stay in the accumulation registers: through
 // the builtin the register allocator moves them back and forth.  Operands of the next MFMAs come from LDS reads (the
 // compiler waits for those before it passes the registers on), never from a vector instruction right before.
+template <bool kHalves = false>
 __device__ __forceinline__ void mfma_16x16x32(f32x4& acc, bf16x8 b, bf16x8 a) {
-    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(b), "v"(a));
+    if constexpr (kHalves) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(b), "v"(a));
+    else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(b), "v"(a));
 }
 // The same around direct_load_16B to lds_addr + kLdsOffset: a load into LDS may not follow the write of m0 directly,
 // and the MFMA is the instruction in between.
-template <uint32_t kLdsOffset>
+#define PCM_MFMA_AND_LOAD(type, load, base)                                                                  \
+    asm volatile("s_add_u32 m0, %1, %2\n\t"                                                                  \
+                 "v_mfma_f32_16x16x32_" type " %0, %3, %4, %0\n\t" load                                       \
+                 : "+a"(acc)                                                                                  \
+                 : "s"(lds_addr), "n"(kLdsOffset), "v"(b), "v"(a), "v"(lane_offset), "s"(base)                \
+                 : "memory", "scc")
+template <uint32_t kLdsOffset, bool kHalves = false>
 __device__ __forceinline__ void mfma_16x16x32_and_load(f32x4& acc, bf16x8 b, bf16x8 a, const char* base, uint32_t lane_offset,
                                                        uint32_t lds_addr) {
-    asm volatile("s_add_u32 m0, %1, %2\n\t"
-                 "v_mfma_f32_16x16x32_bf16 %0, %3, %4, %0\n\t"
-                 "global_load_lds_dwordx4 %5, %6"
-                 : "+a"(acc)
-                 : "s"(lds_addr), "n"(kLdsOffset), "v"(b), "v"(a), "v"(lane_offset), "s"(base)
-                 : "memory", "scc");
+    if constexpr (kHalves) PCM_MFMA_AND_LOAD("f16", "global_load_lds_dwordx4 %5, %6", base);
+    else PCM_MFMA_AND_LOAD("bf16", "global_load_lds_dwordx4 %5, %6", base);
 }
+template <uint32_t kLdsOffset, bool kHalves = false>
+__device__ __forceinline__ void mfma_16x16x32_and_load(f32x4& acc, bf16x8 b, bf16x8 a, u32x4 buffer, uint32_t lane_offset,
+                                                       uint32_t lds_addr) {
+    if constexpr (kHalves) PCM_MFMA_AND_LOAD("f16", "buffer_load_dwordx4 %5, %6, 0 offen lds", buffer);
+    else PCM_MFMA_AND_LOAD("bf16", "buffer_load_dwordx4 %5, %6, 0 offen lds", buffer);
+}
+#undef PCM_MFMA_AND_LOAD
 // Direct loads retire in issue order, so waiting until at most `newest` remain outstanding
 // guarantees that all older ones have landed.
 template <int kNewest>
@@ -279,13 +315,14 @@ struct OperandRing {
 };
 
 // The work of workgroup `block` of a product; smem: the kernel's LDS.  kShared: one of several products of a launch.
-template <int kLayA, int kLayB, bool kShared, class Epilogue, int kW, int kSlots>
-__device__ __forceinline__ void gemm_tile(const GemmProblem& p, const Epilogue& epi, int block, OperandRing<kW, kSlots>& smem) {
+template <int kLayA, int kLayB, bool kShared, class Problem, class Epilogue, int kW, int kSlots>
+__device__ __forceinline__ void gemm_tile(const Problem& p, const Epilogue& epi, int block, OperandRing<kW, kSlots>& smem) {
     constexpr int TM = kTile<kW>, TN = kTile<kW>;
     constexpr uint32_t kTileBytes = TM * kTileK * 2;             // one operand tile
     constexpr int kLoadsPerTile = kW;                            // wave-wide loads per wavefront per tile
     constexpr int kSmemBytes = kRingBytes<kW, kSlots>;
     constexpr int kAhead = kSlots / 2;                           // steps requested ahead of the one being multiplied
+    constexpr bool kHalves = Problem::kHalves, kBoundedB = Problem::kBoundedB;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // wave-uniform, kept in a scalar register
@@ -310,7 +347,7 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, const Epilogue& 
     if (!tile_of_workgroup<kW>(block % n_tiles, n_tiles, live_m, tiles_n, tm, tn)) return;   // before any barrier
     const int m0 = tm * TM, n0 = n_first + tn * TN;
     // reduction range of this workgroup, in 64-wide steps over the concatenation of both segments
-    const int steps1 = k1 / kTileK, steps_all = steps1 + p.K2 / kTileK;
+    const int steps1 = k1 / kTileK, steps_all = kHalves ? 3 * steps1 : steps1 + p.K2 / kTileK;
     const int per_split = (steps_all + p.splits - 1) / p.splits;
     const int step_begin = split * per_split;
     const int step_end = min(steps_all, step_begin + per_split);
@@ -333,7 +370,7 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, const Epilogue& 
     // operand 0 = A rows m0.., operand 1 = B rows n0..  Per-lane offsets do not depend on the step; the
     // tile origin is a wave-uniform pointer that walks along k.
     uint32_t lane_off[2][4], load_stride[2];
-    const char* seg_origin[2][2];          // [operand][segment]: this tile's bytes at k = 0 of the segment
+    const char* seg_origin[2][kHalves ? 3 : 2];   // [operand][segment]: this tile's bytes at k = 0 of the segment
     uint32_t k_step_bytes[2];              // distance between consecutive steps
 #pragma unroll
     for (int operand = 0; operand < 2; ++operand) {
@@ -370,8 +407,37 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, const Epilogue& 
         }
     }
     auto tile_origin = [&](int operand, int step) {
+        if constexpr (kHalves) {
+            const int seg = step < steps1 ? 0 : step < 2 * steps1 ? 1 : 2;
+            return (seg == 0 ? seg_origin[operand][0] : seg == 1 ? seg_origin[operand][1] : seg_origin[operand][2]) +
+                   (int64_t)(step - seg * steps1) * (int64_t)k_step_bytes[operand];
+        }
         const bool seg1 = step < steps1;
         return seg_origin[operand][seg1 ? 0 : 1] + (int64_t)(seg1 ? step : step - steps1) * (int64_t)k_step_bytes[operand];
+    };
+    if constexpr (kHalves) {
+        seg_origin[0][2] = seg_origin[0][0] + (reinterpret_cast<const char*>(p.A3) - reinterpret_cast<const char*>(p.A));
+        seg_origin[1][2] = seg_origin[1][0] + (reinterpret_cast<const char*>(p.B3) - reinterpret_cast<const char*>(p.B));
+    }
+    // Bounded B: bytes from a tile's origin that are there, in every step but the one in which the reduction index ends, and in that one.
+    // [rows][K]: the rows that are there, the last of them up to the end of K; [K][rows]: 64 k-rows, or those that are there, the last up to its end.
+    uint32_t bytes_b = 0, bytes_b_end = 0;
+    int step_of_end = 0x7fffffff;
+    if constexpr (kBoundedB) {
+        const int rows = min(TN, p.N_real - n0), end = (p.K_real - 1) / kTileK, k_left = p.K_real - end * kTileK;
+        const uint32_t ld = (uint32_t)p.ldb;
+        if (kLayB == kRowsByK) {
+            bytes_b = (uint32_t)rows * ld * 2u;
+            bytes_b_end = ((uint32_t)(rows - 1) * ld + (uint32_t)k_left) * 2u;
+        } else {
+            bytes_b = ((uint32_t)(kTileK - 1) * ld + (uint32_t)rows) * 2u;
+            bytes_b_end = ((uint32_t)(k_left - 1) * ld + (uint32_t)rows) * 2u;
+        }
+        step_of_end = end;
+    }
+    auto bytes_at = [&](int step) {
+        if constexpr (kHalves) step = step < steps1 ? step : step < 2 * steps1 ? step - steps1 : step - 2 * steps1;
+        return step == step_of_end ? bytes_b_end : bytes_b;
     };
     // `slot` is the byte offset of a ring slot
     auto load_ctx_at = [&](int operand, uint32_t slot, const char* origin) {
@@ -389,8 +455,11 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, const Epilogue& 
     auto issue_tile = [&](int operand, uint32_t slot, int step) {
         const LoadCtx c = load_ctx(operand, slot, step);
 #pragma unroll
-        for (uint32_t r = 0; r < (uint32_t)kLoadsPerTile; ++r)
-            direct_load_16B(c.base, c.off[load_variant(operand == 0 ? kLayA : kLayB, r)] + r * c.stride, c.dst + r * 1024u);
+        for (uint32_t r = 0; r < (uint32_t)kLoadsPerTile; ++r) {
+            const uint32_t off = c.off[load_variant(operand == 0 ? kLayA : kLayB, r)] + r * c.stride;
+            if (kBoundedB && operand == 1) direct_load_16B(buffer_of(c.base, bytes_at(step)), off, c.dst + r * 1024u);
+            else direct_load_16B(c.base, off, c.dst + r * 1024u);
+        }
     };
 
     Accumulators<kW> acc;
@@ -475,7 +544,9 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, const Epilogue& 
         // instructions always share one operand fragment.
         // refilled: the operand whose tile is refilled meanwhile, c: from and to where; rd_a, rd_b: bases of the fragments of
         // the next slice.
+        uint32_t bytes_now = 0;      // bounded B: of the tile that origin_b names
         auto slice = [&](int set, auto refilled, const LoadCtx& c, uint32_t rd_a, uint32_t rd_b, auto hook) {
+            const u32x4 buffer = kBoundedB && decltype(refilled)::value == 1 ? buffer_of(c.base, bytes_now) : u32x4{0, 0, 0, 0};
             uint32_t tr_at = rd_a;       // [K][rows]: address of the fragment being read
             s16x4 tr_lo = {0, 0, 0, 0};  // [K][rows]: its first half
             auto transposed = [&](int n) { return is_a(n) ? kLayA == kKByRows : kLayB == kKByRows; };
@@ -495,12 +566,14 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, const Epilogue& 
                 constexpr int g = decltype(row)::value;
                 constexpr int j0 = (g & 1) ? kW - 1 : 0;
                 constexpr int layout = decltype(refilled)::value == 0 ? kLayA : kLayB;
-                mfma_16x16x32_and_load<g * 1024u>(acc[g][j0], fb[set][j0], fa[set][g], c.base,
-                                                  c.off[load_variant(layout, g)] + g * c.stride, c.dst);
+                const uint32_t off = c.off[load_variant(layout, g)] + g * c.stride;
+                if constexpr (kBoundedB && decltype(refilled)::value == 1)
+                    mfma_16x16x32_and_load<g * 1024u, kHalves>(acc[g][j0], fb[set][j0], fa[set][g], buffer, off, c.dst);
+                else mfma_16x16x32_and_load<g * 1024u, kHalves>(acc[g][j0], fb[set][j0], fa[set][g], c.base, off, c.dst);
 #pragma unroll
                 for (int jj = 1; jj < kW; ++jj) {
                     const int j = (g & 1) ? kW - 1 - jj : jj;
-                    mfma_16x16x32(acc[g][j], fb[set][j], fa[set][g]);
+                    mfma_16x16x32<kHalves>(acc[g][j], fb[set][j], fa[set][g]);
                     __builtin_amdgcn_sched_barrier(0);
                     if (kW == kLargeTile) {
                         // read n of the next slice: [rows][K] in gap jj, [K][rows] in halves in gaps jj and jj + 1 with the
@@ -533,6 +606,7 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, const Epilogue& 
         // segment is used.
         const char* origin_a = tile_origin(0, min(step_begin + kAhead, last));
         const char* origin_b = tile_origin(1, min(step_begin + kAhead - 1, last));
+        if constexpr (kBoundedB) bytes_now = bytes_at(min(step_begin + kAhead - 1, last));
         uint32_t sa = 0, sb = next_slot(sa), refill_a = (kSlots - 1) * kTileBytes, na = next_slot(sb), nb = next_slot(na);
         uint32_t rd_a = base_a[1] + sa, rd_b = base_b[1] + sb, stride_now = 0;
         // In six pieces of two or three scalar instructions; the A origin only after the last load from it.
@@ -548,6 +622,9 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& p, const Epilogue& 
                 origin += stride_now;
             } else {
                 origin = at == steps1 ? seg_origin[operand][1] : origin;
+                if constexpr (kHalves) origin = at == 2 * steps1 ? seg_origin[operand][2] : origin;
+                if constexpr (kBoundedB)
+                    if (operand == 1) bytes_now = bytes_at(min(at, last));
             }
         };
         auto between_b = [&](int piece) {
@@ -1057,6 +1134,13 @@ inline int tile_for(int64_t M, int64_t N, int splits) {
 // 79.8, 1344 of 1024 -> 1024 39.4 / 39.6 / 42.0, 512 of 3072 -> 1536 145.7 / 145.4 / 150.7.
 constexpr int kDeepSteps = 9;
 inline int steps_per_part(const GemmProblem& p) { return ceil_div((p.K1 + p.K2) / kTileK, p.splits); }
+
+// Bounded products: one launch on tiles of kW.
+template <class Problem, class Epilogue, int kLayA, int kLayB, int kW, int kSlots>
+__global__ __launch_bounds__(kGemmThreads, kW == kLargeTile || kSlots > kRingSlots ? 1 : 2) void gemm_bounded(Problem p, Epilogue epi) {
+    __shared__ OperandRing<kW, kSlots> smem;
+    gemm_tile<kLayA, kLayB, false>(p, epi, blockIdx.x, smem);
+}
 
 template <int kLayA = kRowsByK, int kLayB = kRowsByK, int kW = kLargeTile, class Epilogue>
 inline void launch_gemm_tile(const GemmProblem& p, const Epilogue& epi, hipStream_t s) {

@@ -1,0 +1,413 @@
+// Gradient of the log-probabilities through a vocabulary projection, in the hidden rows and in the projection.
+//
+// Piece by piece of the vocabulary:
+//   z = h W of the piece; the epilogue makes dz of it (log p = z / temperature - lse is known) and writes that, the only matrix of rows x vocabulary
+//       there is, in bf16 (fp32: as a pair of fp16)
+//   dhidden += dz W^T, over the piece
+//   dW of the piece = h^T dz, over all rows at once, so that it is written once and rounded once
+// Six operations per row, value of a row and token, all on the matrix cores.
+#include "linear_logprobs.h"
+
+namespace pcm {
+namespace {
+
+typedef _Float16 f16;
+typedef __attribute__((ext_vector_type(4))) f16 f16x4;
+
+// ---- dz -------------------------------------------------------------------------------------------
+
+struct LogitGradient {
+    const SlotGradient* of;
+    const int32_t* token;
+    const float *h_unit, *w_unit;        // fp32, or null
+    float c;                             // log2 e / temperature
+    int first, columns;                  // of the vocabulary in this piece
+    // dz of the 16-column tile j of a wavefront's block, four neighbours of one row; G, at: the row's, `at` its token's place in the block
+    __device__ __forceinline__ f32x4 operator()(f32x4 z, float unit, const SlotGradient& G, int at, int column, bool whole, int col0) const {
+        f32x4 r;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const float a = __builtin_fmaf(z[t] * unit, c, -G.lse2);
+            const float p = __builtin_amdgcn_exp2f(a);
+            // (where p is 0 log p may be -inf, which is not to become a NaN)
+            r[t] = -p * __builtin_fmaf(G.h, __builtin_fmaf(a < -150.f ? -150.f : a, kLn2, G.entropy), G.g);
+            if (at == column + t) r[t] += G.g;
+            if (!whole && col0 + column + t >= columns) r[t] = 0.f;
+        }
+        return r;
+    }
+};
+
+// dz as bf16.  Rows behind the last slot (token -1) become zeros.
+struct EpiLogitGradient {
+    LogitGradient gradient;
+    bf16* dz;
+    int64_t ld;
+    template <int kW>
+    __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* lds) const {
+        constexpr int RW = kWaveRows<kW>, kStride = RW * 2 + 16;
+        char* st = wave_stage(tc, lds);
+        const int col0 = tc.col0(), quarter = tc.lane >> 4;
+        const bool whole = col0 + RW <= gradient.columns;
+#pragma unroll
+        for (int i = 0; i < kW; ++i) {
+            const int row = tc.row0() + i * 16 + (tc.lane & 15);
+            const SlotGradient G = gradient.of[row];
+            const int token = gradient.token[row], at = token - gradient.first - col0;
+            stage_tile_row<kW>(st, kStride, tc.lane, i * 16 + (tc.lane & 15), [&](int j) {
+                const f32x4 r = gradient(acc[i][j], 1.f, G, at, j * 16 + quarter * 4, whole, col0);
+                return token < 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : r;
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_wave_barrier();
+        copy_rows_out<RW, RW * 2>(st, kStride, reinterpret_cast<char*>(dz + (int64_t)tc.row0() * ld + col0), ld * 2, RW, tc.lane);
+    }
+};
+// dz 2^z_shift as hi + lo of fp16.
+struct EpiLogitGradientPairs {
+    LogitGradient gradient;
+    f16 *hi, *lo;
+    int64_t ld;
+    template <int kW>
+    __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* lds) const {
+        constexpr int RW = kWaveRows<kW>, kStride = RW * 4 + 16;
+        char* st = wave_stage(tc, lds);
+        const int col0 = tc.col0(), quarter = tc.lane >> 4;
+        const bool whole = col0 + RW <= gradient.columns;
+        const float w_unit = *gradient.w_unit;
+#pragma unroll
+        for (int half = 0; half < RW / 64; ++half) {       // 64 rows per pass
+#pragma unroll
+            for (int ii = 0; ii < 4; ++ii) {
+                const int i = half * 4 + ii, row = tc.row0() + i * 16 + (tc.lane & 15);
+                const SlotGradient G = gradient.of[row];
+                const int token = gradient.token[row], at = token - gradient.first - col0;
+                const float unit = gradient.h_unit[row] * w_unit;
+                char* to = st + (ii * 16 + (tc.lane & 15)) * kStride;
+#pragma unroll
+                for (int j = 0; j < kW; ++j) {
+                    f32x4 r = gradient(acc[i][j], unit, G, at, j * 16 + quarter * 4, whole, col0);
+                    f16x4 h, l;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const float x = token < 0 ? 0.f : r[t];
+                        h[t] = (f16)x;
+                        l[t] = (f16)(x - (float)h[t]);
+                    }
+                    char* at_j = to + (j * 16 + 4 * quarter) * 2;
+                    *reinterpret_cast<f16x4*>(at_j) = h;
+                    *reinterpret_cast<f16x4*>(at_j + RW * 2) = l;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            __builtin_amdgcn_wave_barrier();
+            const int64_t at = (int64_t)(tc.row0() + half * 64) * ld + col0;
+            copy_rows_out<64, RW * 2>(st, kStride, reinterpret_cast<char*>(hi + at), ld * 2, 64, tc.lane);
+            copy_rows_out<64, RW * 2>(st + RW * 2, kStride, reinterpret_cast<char*>(lo + at), ld * 2, 64, tc.lane);
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+};
+
+// ---- results --------------------------------------------------------------------------------------
+
+__device__ inline uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+
+// What a product over all rows is to be multiplied by: 2^(most - 14) for pairs.
+__device__ inline float weight_gradient_unit(const int32_t* most) { return most == nullptr || *most <= -(1 << 20) ? 1.f : ldexpf(1.f, *most - 14); }
+
+// acc into rows and columns of a matrix that end anywhere, at any alignment of its type, through LDS so that whole lines leave.
+template <class T>
+struct EpiStoreAnywhere {
+    T* C;
+    int64_t ldc;
+    int rows, cols;
+    const int32_t* most;                 // or null
+    int accumulate;                      // T = float
+    template <int kW>
+    __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* lds) const {
+        constexpr int RW = kWaveRows<kW>, kStride = RW * 4 + 16;
+        char* st = wave_stage(tc, lds);
+        const int col0 = tc.col0(), n_cols = min(RW, cols - col0);
+        const float unit = weight_gradient_unit(most);
+        if (n_cols <= 0) return;
+#pragma unroll
+        for (int i = 0; i < RW / 32; ++i) {                // 32 rows per pass
+#pragma unroll
+            for (int ii = 0; ii < 2; ++ii)
+#pragma unroll
+                for (int j = 0; j < kW; ++j)
+                    *reinterpret_cast<f32x4*>(st + (ii * 16 + (tc.lane & 15)) * kStride + (j * 16 + 4 * (tc.lane >> 4)) * 4) = acc[2 * i + ii][j];
+            __builtin_amdgcn_wave_barrier();
+            const int row0 = tc.row0() + i * 32, n_rows = min(32, rows - row0);
+            constexpr int kPer = 4, kLanes = RW / kPer;     // columns of a lane; lanes of a row
+            const int c = tc.lane % kLanes * kPer;
+            for (int r = tc.lane / kLanes; r < n_rows; r += 64 / kLanes) {
+                f32x4 x = *reinterpret_cast<const f32x4*>(st + r * kStride + c * 4);
+                x *= unit;
+                T* const to = C + (int64_t)(row0 + r) * ldc + col0 + c;
+                if constexpr (sizeof(T) == 4) {
+                    typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+                    if (c + kPer <= n_cols) {
+                        if (accumulate) x += *reinterpret_cast<const f32x4_any*>(to);
+                        *reinterpret_cast<f32x4_any*>(to) = x;
+                    } else {
+                        for (int e = 0; e < kPer; ++e)
+                            if (c + e < n_cols) to[e] = accumulate ? to[e] + x[e] : x[e];
+                    }
+                } else {
+                    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+                    typedef u32x2 __attribute__((aligned(2))) u32x2_any;
+                    const bf16x4 y = to_bf16x4(x[0], x[1], x[2], x[3]);
+                    if (c + kPer <= n_cols) *reinterpret_cast<u32x2_any*>(to) = __builtin_bit_cast(u32x2, y);
+                    else
+                        for (int e = 0; e < kPer; ++e)
+                            if (c + e < n_cols) to[e] = bf16_bits(x[e]);
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+};
+
+// Sums of the parts of a product, [parts][rows of ld], to a matrix of any type; `slot_of`: row r is row slot_of[r] of the parts, or zeros.
+struct PartSum {
+    const float* parts;
+    int64_t part, ld;
+    int n;
+    const int32_t* slot_of;              // or null
+    const int32_t *z_shift, *most;       // fp32, or null: powers of two of the rows, of the whole
+    const float* w_unit;                 // with z_shift
+    int rows, cols, accumulate;
+};
+template <class T>
+__global__ __launch_bounds__(256) void linear_sum_parts(PartSum q, T* out, int64_t ld) {
+    const int row = blockIdx.y * 65535 + blockIdx.z, i = (blockIdx.x * 256 + threadIdx.x) * 4;
+    if (row >= q.rows || i >= q.cols) return;
+    const int slot = q.slot_of != nullptr ? q.slot_of[row] : row;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    if (slot >= 0) {
+        const float* from = q.parts + (int64_t)slot * q.ld + i;
+        for (int p = 0; p < q.n; ++p, from += q.part) x += *reinterpret_cast<const f32x4*>(from);
+        if (q.z_shift != nullptr) x *= ldexpf(*q.w_unit, -q.z_shift[slot]);
+        x *= weight_gradient_unit(q.most);
+    }
+    T* const to = out + (int64_t)row * ld + i;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (i + e >= q.cols) break;
+        if constexpr (sizeof(T) == 4) to[e] = q.accumulate ? to[e] + x[e] : x[e];
+        else to[e] = bf16_bits(x[e]);
+    }
+}
+void sum_parts(const PartSum& q, void* out, int64_t ld, int dtype, hipStream_t s) {
+    const dim3 grid((unsigned)ceil_div(q.cols, 1024), (unsigned)ceil_div(q.rows, 65535), (unsigned)std::min(q.rows, 65535));
+    if (dtype == PCM_F32) linear_sum_parts<float><<<grid, 256, 0, s>>>(q, static_cast<float*>(out), ld);
+    else linear_sum_parts<uint16_t><<<grid, 256, 0, s>>>(q, static_cast<uint16_t*>(out), ld);
+}
+
+// ---- host side --------------------------------------------------------------------------------------
+
+// Parts of a reduction of `steps`: as many as fill the chip with tiles of kW, of eight steps or more.
+int parts_for(int64_t tiles, int steps, int resident) {
+    if (tiles >= resident) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({resident / tiles, steps / 8, 32}));
+}
+struct ProductPlan {
+    int kW, parts;
+    ProductPlan() : kW(kSmallTile), parts(1) {}
+    ProductPlan(int M, int N, int steps) {
+        kW = tile_for(M, N, 1);
+        const int64_t tiles = (int64_t)(M / (32 * kW)) * (N / (32 * kW));
+        parts = parts_for(tiles, steps, kW == kLargeTile ? 256 : 512);
+    }
+};
+
+struct BackwardPlan {
+    int columns;                     // of a piece
+    int64_t z_ld;
+    Slots slots;
+    SlotGradients grads;
+    WeightCopy copy;
+    half_bits *z, *z_low;            // [padded, z_ld]
+    int z_tile;
+    ProductPlan dh, dw;
+    float *dh_parts, *dw_parts;
+    int dh_ld, dw_rows, dw_ld;       // of a part
+    size_t bytes;
+};
+// `dw_direct`: whole products go straight to dweight.
+BackwardPlan plan_backward(void* workspace, int rows, const WeightSource& src) {
+    Carver c(workspace);
+    BackwardPlan b{};
+    b.slots = carve_slots(c, rows, src.d, src.dtype);
+    b.grads = carve_gradients(c, b.slots, src.dtype);
+    const int width = src.dtype == PCM_F32 ? 4 : 2;
+    // at most 1 GB of dz
+    int64_t columns = ((int64_t)1 << 30) / ((int64_t)b.slots.padded * width) / kTileN * kTileN;
+    if (!src.in_place) columns = std::min<int64_t>(columns, copy_columns(src));
+    b.columns = (int)std::min<int64_t>(std::max<int64_t>(columns, kTileN), round_up(src.V, kTileN));
+    b.copy = carve_weight(c, src, b.columns);
+    b.z_ld = b.columns;
+    const size_t z = (size_t)b.slots.padded * (size_t)b.z_ld + kTileM;
+    b.z = c.take<half_bits>(z);
+    if (src.dtype == PCM_F32) b.z_low = c.take<half_bits>(z);
+    b.z_tile = rows <= 128 ? kSmallTile : tile_for(b.slots.padded, b.columns, 1);
+    b.dh_ld = round_up(src.d, kTileN);
+    b.dh = ProductPlan(b.slots.padded, b.dh_ld, b.columns / kTileK * (width / 2));
+    b.dh_parts = c.take<float>((size_t)b.dh.parts * b.slots.padded * b.dh_ld);
+    const int d256 = round_up(src.d, kTileM);
+    b.dw_rows = src.layout == PCM_WEIGHT_OUT_IN ? b.columns : d256;
+    b.dw_ld = src.layout == PCM_WEIGHT_OUT_IN ? d256 : b.columns;
+    b.dw = ProductPlan(b.dw_rows, b.dw_ld, b.slots.padded / kTileK * (width / 2));
+    if (b.dw.parts > 1) b.dw_parts = c.take<float>((size_t)b.dw.parts * b.dw_rows * b.dw_ld);
+    b.bytes = c.used();
+    return b;
+}
+
+struct BackwardOut {
+    void* dh;
+    int64_t dh_ld;
+    void* dw;
+    int64_t dw_ld;
+    int dw_dtype, accumulate;
+};
+
+template <bool kThirds>
+void logit_gradient(const BackwardPlan& b, const WeightSource& src, const WeightOperand& w, int rows, int first, int columns, float c, hipStream_t s) {
+    BoundedProblem<kThirds> p = slot_product<kThirds>(b.slots, kRowsAreM);
+    p.M = rows <= 128 ? 128 : b.slots.padded;
+    set_a(p, b.slots.h, b.slots.h_low, b.slots.d64);
+    const LogitGradient gradient{b.grads.of, b.slots.token, kThirds ? b.slots.h_unit : nullptr, kThirds ? b.copy.unit : nullptr, c, first, columns};
+    auto launch = [&](const auto& epi) {
+        if (src.layout == PCM_WEIGHT_OUT_IN) {
+            set_b<kRowsByK>(p, w.w, w.low, w.ld, columns, src.d);
+            launch_slot_product<kThirds, kRowsByK, kRowsByK>(p, b.z_tile, epi, s);
+        } else {
+            set_b<kKByRows>(p, w.w, w.low, w.ld, columns, src.d);
+            launch_slot_product<kThirds, kRowsByK, kKByRows>(p, b.z_tile, epi, s);
+        }
+    };
+    if constexpr (kThirds) launch(EpiLogitGradientPairs{gradient, reinterpret_cast<f16*>(b.z), reinterpret_cast<f16*>(b.z_low), b.z_ld});
+    else launch(EpiLogitGradient{gradient, reinterpret_cast<bf16*>(b.z), b.z_ld});
+}
+
+template <bool kThirds>
+void hidden_gradient(const BackwardPlan& b, const WeightSource& src, const WeightOperand& w, int columns, bool add, hipStream_t s) {
+    BoundedProblem<kThirds> p = slot_product<kThirds>(b.slots, kRowsAreM);
+    p.M = b.slots.padded;
+    p.splits = b.dh.parts;
+    set_a(p, b.z, b.z_low, b.z_ld);
+    const EpiStoreF32 epi{b.dh_parts, b.dh_ld, (int64_t)b.slots.padded * b.dh_ld, add, nullptr, FinalPanel{}};
+    if (src.layout == PCM_WEIGHT_OUT_IN) {
+        set_b<kKByRows>(p, w.w, w.low, w.ld, src.d, columns);
+        launch_slot_product<kThirds, kRowsByK, kKByRows>(p, b.dh.kW, epi, s);
+    } else {
+        set_b<kRowsByK>(p, w.w, w.low, w.ld, src.d, columns);
+        launch_slot_product<kThirds, kRowsByK, kRowsByK>(p, b.dh.kW, epi, s);
+    }
+}
+
+template <bool kThirds>
+void weight_gradient(const BackwardPlan& b, const WeightSource& src, int first, int columns, const BackwardOut& out, hipStream_t s) {
+    BoundedProblem<kThirds> p = slot_product<kThirds>(b.slots, kRowsAreK);
+    const bool by_token = src.layout == PCM_WEIGHT_OUT_IN;
+    const half_bits *h = kThirds ? b.grads.w_h : b.slots.h, *h_low = kThirds ? b.grads.w_h_low : nullptr;
+    p.splits = b.dw.parts;
+    // (both operands are of this call's scratch, whole tiles of them: the bounds are those of the scratch)
+    if (by_token) {
+        set_a(p, b.z, b.z_low, b.z_ld);
+        set_b<kKByRows>(p, h, h_low, b.slots.d64, src.d, b.slots.padded);
+        p.M = round_up(columns, kTileM);
+    } else {
+        set_a(p, h, h_low, b.slots.d64);
+        set_b<kKByRows>(p, b.z, b.z_low, b.z_ld, columns, b.slots.padded);
+        p.M = round_up(src.d, kTileM);
+    }
+    const int rows = by_token ? columns : src.d, cols = by_token ? src.d : columns;
+    const int64_t at = by_token ? first * out.dw_ld : first;
+    const int32_t* most = kThirds ? b.slots.most : nullptr;
+    if (b.dw.parts > 1) {
+        const EpiStoreF32 epi{b.dw_parts, b.dw_ld, (int64_t)b.dw_rows * b.dw_ld, 0, nullptr, FinalPanel{}};
+        launch_slot_product<kThirds, kKByRows, kKByRows>(p, b.dw.kW, epi, s);
+        const PartSum q{b.dw_parts, (int64_t)b.dw_rows * b.dw_ld, b.dw_ld, b.dw.parts, nullptr, nullptr, most, nullptr, rows, cols, out.accumulate};
+        sum_parts(q, static_cast<char*>(out.dw) + at * (out.dw_dtype == PCM_F32 ? 4 : 2), out.dw_ld, out.dw_dtype, s);
+    } else if (out.dw_dtype == PCM_F32) {
+        const EpiStoreAnywhere<float> epi{static_cast<float*>(out.dw) + at, out.dw_ld, rows, cols, most, out.accumulate};
+        launch_slot_product<kThirds, kKByRows, kKByRows>(p, b.dw.kW, epi, s);
+    } else if constexpr (!kThirds) {
+        const EpiStoreAnywhere<uint16_t> epi{static_cast<uint16_t*>(out.dw) + at, out.dw_ld, rows, cols, nullptr, 0};
+        launch_slot_product<kThirds, kKByRows, kKByRows>(p, b.dw.kW, epi, s);
+    }
+}
+
+template <bool kThirds>
+void backward(const BackwardPlan& b, const WeightSource& src, int rows, float c, const BackwardOut& out, hipStream_t s) {
+    for (int first = 0; first < src.V; first += b.columns) {
+        const int columns = std::min(b.columns, src.V - first);
+        const WeightOperand w = weight_piece(src, b.copy, first, columns, s);
+        logit_gradient<kThirds>(b, src, w, rows, first, columns, c, s);
+        if (out.dh != nullptr) hidden_gradient<kThirds>(b, src, w, columns, first > 0, s);
+        if (out.dw != nullptr) weight_gradient<kThirds>(b, src, first, columns, out, s);
+    }
+    if (out.dh == nullptr) return;
+    const PartSum q{b.dh_parts, (int64_t)b.slots.padded * b.dh_ld, b.dh_ld, b.dh.parts, b.slots.slot_of, kThirds ? b.grads.z_shift : nullptr, nullptr,
+                    kThirds ? b.copy.unit : nullptr, rows, src.d, 0};
+    sum_parts(q, out.dh, out.dh_ld, src.dtype, s);
+}
+
+}  // namespace
+}  // namespace pcm
+
+using namespace pcm;
+
+extern "C" {
+
+PCM_API size_t pcm_linear_logprobs_backward_workspace_bytes(int64_t rows, int d, int V, int dtype, int weight_layout, const void* weight,
+                                                            int64_t weight_ld) {
+    const void* const fine = reinterpret_cast<const void*>((uintptr_t)256);
+    if (rows < 1 || check_linear(fine, d, weight, weight_ld, weight_layout, dtype, fine, PCM_TOKEN_U8, rows, d, V, 1.f) != PCM_OK) return 0;
+    return plan_backward(nullptr, (int)rows, weight_source(weight, weight_ld, dtype, weight_layout, d, V)).bytes;
+}
+
+PCM_API int pcm_linear_logprobs_backward(const void* hidden, int64_t hidden_ld, const void* weight, int64_t weight_ld, int weight_layout,
+                                         int dtype, const void* tokens, int token_type, int64_t rows, int d, int V, float temperature,
+                                         const float* lse, const float* dlogp, const float* entropy, const float* dentropy, void* dhidden,
+                                         int64_t dhidden_ld, void* dweight, int64_t dweight_ld, int dweight_dtype, int accumulate,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = check_linear(hidden, hidden_ld, weight, weight_ld, weight_layout, dtype, tokens, token_type, rows, d, V, temperature);
+    if (rc == PCM_EINVAL || (entropy == nullptr) != (dentropy == nullptr) || (!dhidden && !dweight)) return PCM_EINVAL;
+    auto off = [](const void* p, int size) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(size - 1)) != 0; };
+    if (dhidden && (dhidden_ld < d || off(dhidden, dtype == PCM_F32 ? 4 : 2))) return PCM_EINVAL;
+    if (dweight && (dweight_ld < (weight_layout == PCM_WEIGHT_OUT_IN ? d : V) ||
+                    (dweight_dtype != PCM_F32 && (dweight_dtype != PCM_BF16 || dtype != PCM_BF16 || accumulate)) ||
+                    off(dweight, dweight_dtype == PCM_F32 ? 4 : 2)))
+        return PCM_EINVAL;
+    if (rows > 0 && (!lse || !dlogp || off(lse, 4) || off(dlogp, 4) || off(entropy, 4) || off(dentropy, 4))) return PCM_EINVAL;
+    if (rc != PCM_OK) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (rows == 0) {
+        if (!dweight || accumulate) return PCM_OK;
+        const bool by_token = weight_layout == PCM_WEIGHT_OUT_IN;
+        const PartSum none{nullptr, 0, 0, 0, nullptr, nullptr, nullptr, nullptr, by_token ? V : d, by_token ? d : V, 0};
+        sum_parts(none, dweight, dweight_ld, dweight_dtype, s);
+        return launch_status();
+    }
+    const WeightSource src = weight_source(weight, weight_ld, dtype, weight_layout, d, V);
+    BackwardPlan b = plan_backward(workspace, (int)rows, src);
+    if (!workspace_ok(workspace, workspace_bytes, b.bytes)) return PCM_EWORKSPACE;
+    const LinearRows in{hidden, hidden_ld, tokens, token_type, (int)rows, d, V};
+    const float inv_t = 1.f / temperature, c = inv_t * kLog2E;
+    b.grads.lse = lse; b.grads.dlogp = dlogp; b.grads.entropy = entropy; b.grads.dentropy = dentropy;
+    b.grads.inv_t = inv_t;
+    const BackwardOut out{dhidden, dhidden_ld, dweight, dweight_ld, dweight_dtype, accumulate};
+    StageTimer t(ST_LINEAR_LOGPROBS_GRAD, s);
+    gather_slots(in, b.slots, &b.grads, dtype, s);
+    prepare_weight(src, b.copy, s);
+    if (dtype == PCM_F32) backward<true>(b, src, (int)rows, c, out, s);
+    else backward<false>(b, src, (int)rows, c, out, s);
+    return launch_status();
+}
+
+}  // extern "C"

@@ -1,0 +1,733 @@
+// Log-probabilities of tokens through a vocabulary projection, without the logits.
+//
+//   slots      rows with a token -> slots (linear_logprobs.h), hidden rows gathered
+//   products   z = h W on the matrix cores; the epilogue turns a wavefront's block of logits into three numbers per row: largest logit, sum of
+//              2^a and of 2^a a, a = (z - largest) log2 e / temperature; the token's logit is written down where it passes by
+//   join       the blocks of a row -> log-sum-exp, log p, entropy
+// Up to 16 rows the projection is streamed once past rows in registers (few_rows), bound by its bytes.
+#include "linear_logprobs.h"
+
+#include <type_traits>
+
+namespace pcm {
+namespace {
+
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+typedef _Float16 f16;
+
+// ---- slots ---------------------------------------------------------------------------------------
+
+__device__ inline int token_at(const LinearRows& in, int row) {          // -1: none
+    int64_t t;
+    if (in.token_type == PCM_TOKEN_U8) t = static_cast<const uint8_t*>(in.tokens)[row];
+    else if (in.token_type == PCM_TOKEN_I32) t = static_cast<const int32_t*>(in.tokens)[row];
+    else t = static_cast<const int64_t*>(in.tokens)[row];
+    return t < 0 ? -1 : t >= in.V ? in.V - 1 : (int)t;
+}
+
+__device__ inline int block_count(int x) {                               // over 256 threads, in every thread
+    __shared__ int lds[4];
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return lds[0] + lds[1] + lds[2] + lds[3];
+}
+
+__global__ __launch_bounds__(256) void linear_counts(LinearRows in, int32_t* counts) {
+    int n = 0;
+    for (int i = threadIdx.x; i < kCountRows; i += 256) {
+        const int row = blockIdx.x * kCountRows + i;
+        n += row < in.rows && token_at(in, row) >= 0;
+    }
+    n = block_count(n);
+    if (threadIdx.x == 0) counts[blockIdx.x] = n;
+}
+
+// 1024 rows a workgroup, four neighbours a thread.  Where its rows begin among the slots it counts itself, from the tokens or, for long
+// lists, from the counts of the launch before.
+__global__ __launch_bounds__(256) void linear_slots(LinearRows in, Slots slots) {
+    int before = 0;
+    if (slots.counts != nullptr) {
+        for (int b = threadIdx.x; b < (int)blockIdx.x; b += 256) before += slots.counts[b];
+    } else {
+        for (int row = threadIdx.x; row < (int)blockIdx.x * kCountRows; row += 256) before += token_at(in, row) >= 0;
+    }
+    before = block_count(before);
+    const int first = blockIdx.x * kCountRows + threadIdx.x * 4;
+    int token[4], mine = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        token[e] = first + e < in.rows ? token_at(in, first + e) : -1;
+        mine += token[e] >= 0;
+    }
+    int upto = mine;                                                     // inclusive over the wavefront
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int x = __shfl_up(upto, off, 64);
+        if ((int)(threadIdx.x & 63) >= off) upto += x;
+    }
+    __shared__ int wave_total[4];
+    if ((threadIdx.x & 63) == 63) wave_total[threadIdx.x >> 6] = upto;
+    __syncthreads();
+    int slot = before + upto - mine;
+    for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) slot += wave_total[w];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (first + e < in.rows) slots.slot_of[first + e] = token[e] >= 0 ? slot : -1;
+        if (token[e] >= 0) slots.token[slot++] = token[e];
+    }
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 255) {
+        *slots.live = slot;
+        *slots.most = -(1 << 20);
+    }
+}
+
+// Exponent e with 2^e <= x < 2^(e + 1); x > 0 and finite.
+__device__ inline int exponent_of(float x) { return ilogbf(x); }
+__device__ inline float finite_abs(float x) {
+    x = fabsf(x);
+    return x < __builtin_huge_valf() ? x : 0.f;       // not for infinities and NaN
+}
+__device__ inline float wave_max(float x) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor(x, off, 64));
+    return x;
+}
+// The power of two that brings values below 2^(exponent + 1) below 2^15.
+__device__ inline int shift_for(int exponent) { return min(126, max(-126, 14 - exponent)); }
+__device__ inline half_bits high_part(float x) { return __builtin_bit_cast(half_bits, (f16)x); }
+__device__ inline half_bits low_part(float x) { return __builtin_bit_cast(half_bits, (f16)(x - (float)(f16)x)); }
+
+// Up to eight neighbouring 16-bit values; zeros behind the first n.
+__device__ inline u32x4 load_8(const half_bits* p, int n) {
+    if (n >= 8) return *reinterpret_cast<const u32x4_any*>(p);
+    u32x4 x = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < n) x[e / 2] |= (uint32_t)p[e] << (e % 2 * 16);
+    return x;
+}
+
+// A wavefront per row: bf16 rows are copied, fp32 rows become pairs.  256 more take the slots behind the last one.
+constexpr int kGatherRows = 16;                       // per workgroup
+template <class T>
+__global__ __launch_bounds__(256) void linear_gather(LinearRows in, Slots slots, SlotGradients grads) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int live = *slots.live;
+    int most = -(1 << 20);
+    for (int r = wave; r < kGatherRows; r += 4) {
+        const int row = blockIdx.x * kGatherRows + r;
+        if (row >= in.rows) {
+            const int slot = live + row - in.rows;
+            if (slot >= min(slots.padded, (live + 255) / 256 * 256)) break;
+            for (int i = lane * 8; i < slots.d64; i += 512) {
+                *reinterpret_cast<u32x4*>(slots.h + (int64_t)slot * slots.d64 + i) = u32x4{0, 0, 0, 0};
+                if (sizeof(T) == 4) *reinterpret_cast<u32x4*>(slots.h_low + (int64_t)slot * slots.d64 + i) = u32x4{0, 0, 0, 0};
+            }
+            if (lane == 0) {
+                slots.token[slot] = -1;
+                if (sizeof(T) == 4) slots.h_unit[slot] = 1.f;
+                if (grads.of != nullptr) grads.of[slot] = SlotGradient{0.f, 0.f, 0.f, 0.f};
+                if (sizeof(T) == 4 && grads.of != nullptr) grads.z_shift[slot] = 0;
+            }
+            continue;
+        }
+        const int slot = slots.slot_of[row];
+        if (slot < 0) continue;
+        const T* const from = static_cast<const T*>(in.hidden) + row * in.ld;
+        const int64_t to = (int64_t)slot * slots.d64;
+        float largest = 0.f;
+        if constexpr (sizeof(T) == 2) {
+            for (int i = lane * 8; i < slots.d64; i += 512) *reinterpret_cast<u32x4*>(slots.h + to + i) = load_8(from + i, in.d - i);
+        } else {
+            for (int i = lane; i < in.d; i += 64) largest = fmaxf(largest, finite_abs(from[i]));
+            largest = wave_max(largest);
+            const int shift = largest > 0.f ? shift_for(exponent_of(largest)) : 0;
+            for (int i = lane; i < slots.d64; i += 64) {
+                const float x = i < in.d ? ldexpf(from[i], shift) : 0.f;
+                slots.h[to + i] = high_part(x);
+                slots.h_low[to + i] = low_part(x);
+            }
+            if (lane == 0) slots.h_unit[slot] = ldexpf(1.f, -shift);
+        }
+        if (grads.of != nullptr) {
+            SlotGradient of;
+            of.g = grads.dlogp[row] * grads.inv_t;
+            of.h = grads.dentropy != nullptr ? grads.dentropy[row] * grads.inv_t : 0.f;
+            of.lse2 = grads.lse[row] * kLog2E;
+            of.entropy = grads.dentropy != nullptr ? grads.entropy[row] : 0.f;
+            if constexpr (sizeof(T) == 4) {
+                // |p (log p + entropy)| is at most the larger of 1 / e and the entropy
+                const float bound = fabsf(of.g) + fabsf(of.h) * (0.5f + fabsf(of.entropy));
+                const int shift = bound > 0.f && bound < __builtin_huge_valf() ? shift_for(exponent_of(bound)) : 0;
+                of.g = ldexpf(of.g, shift);
+                of.h = ldexpf(of.h, shift);
+                if (lane == 0) grads.z_shift[slot] = shift;
+                if (bound > 0.f && largest > 0.f) most = max(most, exponent_of(largest) - shift);
+            }
+            if (lane == 0) grads.of[slot] = of;
+        }
+    }
+    if (sizeof(T) == 4 && grads.of != nullptr) {
+        __shared__ int lds[4];
+        if (lane == 0) lds[wave] = most;
+        __syncthreads();
+        most = max(max(lds[0], lds[1]), max(lds[2], lds[3]));
+        if (threadIdx.x == 0 && most > -(1 << 20)) atomicMax(slots.most, most);
+    }
+}
+
+// h 2^(14 - most - z_shift) as pairs: dz 2^z_shift times it adds up over rows of any sizes.
+__global__ __launch_bounds__(256) void linear_weigh(LinearRows in, Slots slots, SlotGradients grads) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int live = *slots.live, most = *slots.most;
+    for (int r = wave; r < kGatherRows; r += 4) {
+        const int row = blockIdx.x * kGatherRows + r;
+        if (row >= in.rows) {
+            const int slot = live + row - in.rows;
+            if (slot >= min(slots.padded, (live + 255) / 256 * 256)) break;
+            for (int i = lane * 8; i < slots.d64; i += 512) {
+                *reinterpret_cast<u32x4*>(grads.w_h + (int64_t)slot * slots.d64 + i) = u32x4{0, 0, 0, 0};
+                *reinterpret_cast<u32x4*>(grads.w_h_low + (int64_t)slot * slots.d64 + i) = u32x4{0, 0, 0, 0};
+            }
+            continue;
+        }
+        const int slot = slots.slot_of[row];
+        if (slot < 0) continue;
+        const float* const from = static_cast<const float*>(in.hidden) + row * in.ld;
+        const int64_t to = (int64_t)slot * slots.d64;
+        const int shift = max(-300, 14 - most - grads.z_shift[slot]);
+        for (int i = lane; i < slots.d64; i += 64) {
+            const float x = i < in.d ? ldexpf(from[i], shift) : 0.f;
+            grads.w_h[to + i] = high_part(x);
+            grads.w_h_low[to + i] = low_part(x);
+        }
+    }
+}
+
+// ---- weights that have to be copied ----------------------------------------------------------------
+
+__global__ __launch_bounds__(256) void linear_absmax(const float* w, int64_t ld, int rows, int cols, float* parts) {
+    float most = 0.f;
+    for (int row = blockIdx.x; row < rows; row += gridDim.x)
+        for (int i = threadIdx.x; i < cols; i += 256) most = fmaxf(most, finite_abs(w[row * ld + i]));
+    most = wave_max(most);
+    __shared__ float lds[4];
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) parts[blockIdx.x] = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+}
+__global__ __launch_bounds__(kAbsmaxParts) void linear_unit(const float* parts, int n, float* unit) {
+    float most = wave_max(threadIdx.x < (unsigned)n ? parts[threadIdx.x] : 0.f);
+    __shared__ float lds[kAbsmaxParts / 64];
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = most;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 0; w < kAbsmaxParts / 64; ++w) most = fmaxf(most, lds[w]);
+    *unit = most > 0.f ? ldexpf(1.f, -shift_for(exponent_of(most))) : 1.f;
+}
+// rows x cols of the source to rows of ld_to, zeros behind cols; a workgroup takes 2048 values of a row.
+template <class T>
+__global__ __launch_bounds__(256) void linear_copy(const T* w, int64_t ld, int rows, int cols, half_bits* to, half_bits* low, int64_t ld_to,
+                                                   const float* unit) {
+    const int row = blockIdx.y * 65535 + blockIdx.z;
+    const int i = blockIdx.x * 2048 + threadIdx.x * 8;
+    if (row >= rows || i >= ld_to) return;
+    const T* const from = w + row * ld + i;
+    const int n = cols - i;
+    half_bits* const out = to + row * ld_to + i;
+    if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<u32x4*>(out) = load_8(from, n);
+    } else {
+        const float scale = 1.f / *unit;                  // a power of two
+        u32x4 hi = {0, 0, 0, 0}, lo = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = e < n ? from[e] * scale : 0.f;
+            hi[e / 2] |= (uint32_t)high_part(x) << (e % 2 * 16);
+            lo[e / 2] |= (uint32_t)low_part(x) << (e % 2 * 16);
+        }
+        *reinterpret_cast<u32x4*>(out) = hi;
+        *reinterpret_cast<u32x4*>(low + row * ld_to + i) = lo;
+    }
+}
+
+// ---- statistics of blocks of logits ------------------------------------------------------------------
+
+// Of the parts of each slot: [parts][ld].  A part that saw nothing has the sum 0.
+struct PartSums {
+    float *most, *sum, *moment;          // largest z; sum 2^a; sum 2^a a, a = (z - most) c
+    int64_t ld;
+    int parts;
+};
+struct RowSums {
+    float m, s, t;
+};
+__device__ inline void merge(RowSums& a, const RowSums& b, float c) {
+    if (b.s == 0.f) return;
+    if (a.s == 0.f) { a = b; return; }
+    const float m = fmaxf(a.m, b.m), da = fmaxf((a.m - m) * c, -1e30f), db = fmaxf((b.m - m) * c, -1e30f);
+    const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
+    a.t = ea * (a.t + a.s * da) + eb * (b.t + b.s * db);
+    a.s = a.s * ea + b.s * eb;
+    a.m = m;
+}
+// (z - m) c for a logit that is not above m; -150 stands for all that is as good as nothing.  NaN where z is.
+__device__ inline void add_exponent(float a, float& s, float& t) {
+    const float e = __builtin_amdgcn_exp2f(a);
+    s += e;
+    t = __builtin_fmaf(e, fmaxf(a, -150.f), t);
+}
+
+struct EpiRowStats {
+    PartSums out;
+    float* token_z;                      // [padded]
+    const int32_t* token;
+    const float *h_unit, *w_unit;        // fp32, or null
+    float c;                             // log2 e / temperature
+    int first, columns;                  // of the vocabulary in this piece
+    int first_part;
+    template <int kW>
+    __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char*) const {
+        constexpr int RW = kWaveRows<kW>;
+        const int col0 = tc.col0(), part = first_part + col0 / RW;
+        if (col0 >= columns) return;                       // no part of its own
+        const bool whole = col0 + RW <= columns;
+        const int quarter = tc.lane >> 4;
+        const float w_scale = w_unit != nullptr ? *w_unit : 1.f;
+#pragma unroll
+        for (int i = 0; i < kW; ++i) {
+            const int row = tc.row0() + i * 16 + (tc.lane & 15);
+            const float unit = h_unit != nullptr ? h_unit[row] * w_scale : 1.f;
+            const int at = token[row] - first - col0;      // of the token in this block
+            float z[kW][4], m = -__builtin_huge_valf();
+#pragma unroll
+            for (int j = 0; j < kW; ++j)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    z[j][t] = acc[i][j][t] * unit;
+                    if (!whole && col0 + j * 16 + quarter * 4 + t >= columns) z[j][t] = -__builtin_huge_valf();
+                    m = fmaxf(m, z[j][t]);
+                }
+            if (__any(at >= 0 && at < RW)) {
+#pragma unroll
+                for (int j = 0; j < kW; ++j)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        if (at == j * 16 + quarter * 4 + t) token_z[row] = z[j][t];
+            }
+            m = fmaxf(m, __shfl_xor(m, 16, 64));
+            m = fmaxf(m, __shfl_xor(m, 32, 64));
+            float s = 0.f, moment = 0.f;
+#pragma unroll
+            for (int j = 0; j < kW; ++j) {
+                float sj = 0.f, tj = 0.f;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) add_exponent((z[j][t] - m) * c, sj, tj);
+                s += sj;
+                moment += tj;
+            }
+            s += __shfl_xor(s, 16, 64);
+            s += __shfl_xor(s, 32, 64);
+            moment += __shfl_xor(moment, 16, 64);
+            moment += __shfl_xor(moment, 32, 64);
+            float* const to = quarter == 0 ? out.most : quarter == 1 ? out.sum : out.moment;
+            if (quarter < 3) to[part * out.ld + row] = quarter == 0 ? m : quarter == 1 ? s : moment;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+};
+
+struct RowResults {
+    float *logp, *lse, *entropy;
+};
+// Results of a row from its parts: kRows rows a workgroup, the other threads parts of them.
+template <int kRows>
+__global__ __launch_bounds__(256) void linear_join(LinearRows in, const int32_t* slot_of, PartSums parts, const float* token_z, float inv_t,
+                                                   RowResults out) {
+    constexpr int kParts = 256 / kRows;
+    __shared__ RowSums lds[kParts][kRows];
+    const int r = threadIdx.x % kRows, k = threadIdx.x / kRows;
+    const int row = blockIdx.x * kRows + r;
+    const float c = inv_t * kLog2E;
+    int slot = -1;
+    if (row < in.rows) slot = slot_of != nullptr ? slot_of[row] : token_at(in, row) >= 0 ? row : -1;
+    RowSums a = {0.f, 0.f, 0.f};
+    if (slot >= 0) {
+#pragma unroll 4
+        for (int p = k; p < parts.parts; p += kParts) {
+            const int64_t at = p * parts.ld + slot;
+            merge(a, RowSums{parts.most[at], parts.sum[at], parts.moment[at]}, c);
+        }
+    }
+    lds[k][r] = a;
+#pragma unroll
+    for (int step = kParts / 2; step > 0; step >>= 1) {
+        __syncthreads();
+        if (k < step) {
+            merge(a, lds[k + step][r], c);
+            lds[k][r] = a;
+        }
+    }
+    if (k != 0 || row >= in.rows) return;
+    float logp = 0.f, lse = 0.f, entropy = 0.f;
+    if (slot >= 0) {
+        const float log_s = logf(a.s);
+        lse = __builtin_fmaf(a.m, inv_t, log_s);
+        logp = (token_z[slot] - a.m) * inv_t - log_s;
+        entropy = log_s - kLn2 * (a.t / a.s);
+        if (!(a.s < __builtin_huge_valf())) lse = logp = entropy = __builtin_nanf("");
+    }
+    out.logp[row] = logp;
+    out.lse[row] = lse;
+    if (out.entropy != nullptr) out.entropy[row] = entropy;
+}
+
+// ---- few rows --------------------------------------------------------------------------------------
+
+// The part of the projection that a lane brings in as 16 bytes, zeros where it ends.
+template <class T>
+__device__ inline u32x4 load_16B(const T* p, int n) {
+    if constexpr (sizeof(T) == 2) {
+        return load_8(p, n);
+    } else {
+        typedef u32x4 __attribute__((aligned(4))) u32x4_floats;
+        if (n >= 4) return *reinterpret_cast<const u32x4_floats*>(p);
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < n) x[e] = p[e];
+        return __builtin_bit_cast(u32x4, x);
+    }
+}
+
+// z of up to 16 rows and a block of the vocabulary.  The four wavefronts of a workgroup take every fourth slice of the reduction index, their sums
+// are added in LDS.  A slice is 4 lane groups x kE values of k (kE = 16 bytes of them).
+//   [V][d]: a lane brings in kE values of k of one column and is its fragment; four fragments of 16 columns share one of the hidden rows.
+//   [d][V]: a lane brings in kE columns at kE values of k and has the fragments of kE columns, bf16 after exchanging halves between pairs of rows.
+template <class T, int kLayout>
+__global__ __launch_bounds__(256) void few_rows(LinearRows in, const T* w, int64_t ld, PartSums out, float* token_z, float c) {
+    constexpr int kE = 16 / sizeof(T), kSlice = 4 * kE;
+    constexpr int kTiles = kLayout == PCM_WEIGHT_OUT_IN ? 4 : kE, kLoads = kLayout == PCM_WEIGHT_OUT_IN ? 4 : kE;
+    constexpr int kColumns = kTiles * 16;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane >> 4, at = lane & 15;
+    const int n0 = blockIdx.x * kColumns;
+    f32x4 acc[kTiles];
+#pragma unroll
+    for (int j = 0; j < kTiles; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // (lanes of rows that are not there take the last one's values along)
+    const T* const h_row = static_cast<const T*>(in.hidden) + min(at, in.rows - 1) * in.ld;
+    const bool has_row = at < in.rows;
+    auto slice = [&](int k0, auto inside) __attribute__((always_inline)) {
+        constexpr bool kInside = decltype(inside)::value;          // all of it is there
+        const int k = k0 + group * kE;
+        u32x4 piece[kLoads];
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) {
+            const int v = n0 + (kLayout == PCM_WEIGHT_OUT_IN ? q * 16 + at : at * kE), row = kLayout == PCM_WEIGHT_OUT_IN ? v : k + q;
+            const T* const from = w + row * ld + (kLayout == PCM_WEIGHT_OUT_IN ? k : v);
+            piece[q] = u32x4{0, 0, 0, 0};
+            if (kInside) piece[q] = load_16B(from, kE);
+            else if (kLayout == PCM_WEIGHT_OUT_IN ? v < in.V && k < in.d : v < in.V && row < in.d) piece[q] = load_16B(from, kLayout == PCM_WEIGHT_OUT_IN ? in.d - k : in.V - v);
+        }
+        u32x4 h = {0, 0, 0, 0};
+        if (kInside) h = load_16B(h_row + k, kE);
+        else if (k < in.d) h = load_16B(h_row + k, in.d - k);
+        if constexpr (sizeof(T) == 2) {
+            const bf16x8 hf = __builtin_bit_cast(bf16x8, h);
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j) {
+                u32x4 f;
+                if (kLayout == PCM_WEIGHT_OUT_IN) f = piece[j];
+                else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)                  // column j of rows 2 q and 2 q + 1
+                        f[q] = __builtin_amdgcn_perm(piece[2 * q + 1][j / 2], piece[2 * q][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+                }
+                acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), hf, acc[j], 0, 0, 0);
+            }
+        } else {
+            const f32x4 hf = __builtin_bit_cast(f32x4, h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j) {
+                    const f32x4 f = __builtin_bit_cast(f32x4, piece[kLayout == PCM_WEIGHT_OUT_IN ? j : e]);
+                    acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[kLayout == PCM_WEIGHT_OUT_IN ? e : j], hf[e], acc[j], 0, 0, 0);
+                }
+        }
+    };
+    int k0 = wave * kSlice;
+    if (n0 + kColumns <= in.V) {
+#pragma unroll 2
+        for (; k0 + kSlice <= in.d; k0 += 4 * kSlice) slice(k0, std::true_type{});
+    }
+    for (; k0 < in.d; k0 += 4 * kSlice) slice(k0, std::false_type{});
+    __shared__ f32x4 sums[4][kTiles][64];
+#pragma unroll
+    for (int j = 0; j < kTiles; ++j) sums[wave][j][lane] = acc[j];
+    __syncthreads();
+    // a lane has row `at` and, of tile j, columns 4 group + t of 16
+    constexpr int kMine = kTiles / 4;
+    const int token = has_row ? token_at(in, at) : -1;
+    float z[kMine][4], m = -__builtin_huge_valf();
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int j = wave * kMine + i;
+        const f32x4 total = (sums[0][j][lane] + sums[1][j][lane]) + (sums[2][j][lane] + sums[3][j][lane]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int column = group * 4 + t, v = n0 + (kLayout == PCM_WEIGHT_OUT_IN ? j * 16 + column : column * kE + j);
+            z[i][t] = v < in.V ? total[t] : -__builtin_huge_valf();
+            m = fmaxf(m, z[i][t]);
+            if (v == token) token_z[at] = z[i][t];
+        }
+    }
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    float s = 0.f, t = 0.f;
+    if (n0 < in.V && m > -__builtin_huge_valf()) {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) add_exponent((z[i][e] - m) * c, s, t);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s += z[i][e] == -__builtin_huge_valf() ? 0.f : z[i][e];       // NaN stays NaN
+    }
+    s += __shfl_xor(s, 16, 64);
+    s += __shfl_xor(s, 32, 64);
+    t += __shfl_xor(t, 16, 64);
+    t += __shfl_xor(t, 32, 64);
+    __shared__ RowSums part[4][16];
+    if (group == 0) part[wave][at] = RowSums{m, s, t};
+    __syncthreads();
+    if (threadIdx.x >= 16 || !has_row) return;
+    RowSums a = part[0][at];
+    for (int q = 1; q < 4; ++q) merge(a, part[q][at], c);
+    out.most[blockIdx.x * out.ld + at] = a.m;
+    out.sum[blockIdx.x * out.ld + at] = a.s;
+    out.moment[blockIdx.x * out.ld + at] = a.t;
+}
+
+int few_columns(int dtype, int layout) { return layout == PCM_WEIGHT_OUT_IN || dtype == PCM_F32 ? 64 : 128; }
+template <class T>
+void launch_few(const LinearRows& in, const void* w, int64_t ld, int layout, const PartSums& parts, float* token_z, float c, hipStream_t s) {
+    const T* const p = static_cast<const T*>(w);
+    if (layout == PCM_WEIGHT_OUT_IN) few_rows<T, PCM_WEIGHT_OUT_IN><<<(unsigned)parts.parts, 256, 0, s>>>(in, p, ld, parts, token_z, c);
+    else few_rows<T, PCM_WEIGHT_IN_OUT><<<(unsigned)parts.parts, 256, 0, s>>>(in, p, ld, parts, token_z, c);
+}
+
+// ---- the forward call --------------------------------------------------------------------------------
+
+PartSums carve_parts(Carver& c, int64_t ld, int parts) {
+    PartSums p{};
+    p.ld = ld;
+    p.parts = parts;
+    p.most = c.take<float>((size_t)(ld * parts));
+    p.sum = c.take<float>((size_t)(ld * parts));
+    p.moment = c.take<float>((size_t)(ld * parts));
+    return p;
+}
+struct ForwardPlan {
+    bool few;
+    int tile, columns;               // of the products: kW, columns of a piece
+    Slots slots;
+    WeightCopy copy;
+    PartSums parts;
+    float* token_z;
+    size_t bytes;
+};
+ForwardPlan plan_forward(void* workspace, int rows, const WeightSource& src) {
+    Carver c(workspace);
+    ForwardPlan f{};
+    f.few = rows <= kFewRows;
+    if (f.few) {
+        f.parts = carve_parts(c, kFewRows, ceil_div(src.V, few_columns(src.dtype, src.layout)));
+        f.token_z = c.take<float>(kFewRows);
+    } else {
+        f.slots = carve_slots(c, rows, src.d, src.dtype);
+        f.columns = src.in_place ? src.V : copy_columns(src);
+        f.copy = carve_weight(c, src, f.columns);
+        f.tile = rows <= 128 ? kSmallTile : tile_for(f.slots.padded, round_up(std::min(f.columns, src.V), kTileN), 1);
+        // (pieces are multiples of 256 columns, so only the last one ends inside a wavefront's block)
+        f.parts = carve_parts(c, f.slots.padded, ceil_div(src.V, 16 * f.tile));
+        f.token_z = c.take<float>((size_t)f.slots.padded);
+    }
+    f.bytes = c.used();
+    return f;
+}
+
+template <bool kThirds>
+void forward_products(const ForwardPlan& f, const WeightSource& src, int rows, float c, hipStream_t s) {
+    for (int first = 0; first < src.V; first += f.columns) {
+        const int columns = std::min(f.columns, src.V - first);
+        const WeightOperand w = weight_piece(src, f.copy, first, columns, s);
+        BoundedProblem<kThirds> p = slot_product<kThirds>(f.slots, kRowsAreM);
+        p.M = rows <= 128 ? 128 : f.slots.padded;
+        set_a(p, f.slots.h, f.slots.h_low, f.slots.d64);
+        const EpiRowStats epi{f.parts, f.token_z, f.slots.token, kThirds ? f.slots.h_unit : nullptr, kThirds ? f.copy.unit : nullptr, c, first,
+                              columns, first / (16 * f.tile)};
+        if (src.layout == PCM_WEIGHT_OUT_IN) {
+            set_b<kRowsByK>(p, w.w, w.low, w.ld, columns, src.d);
+            launch_slot_product<kThirds, kRowsByK, kRowsByK>(p, f.tile, epi, s);
+        } else {
+            set_b<kKByRows>(p, w.w, w.low, w.ld, columns, src.d);
+            launch_slot_product<kThirds, kRowsByK, kKByRows>(p, f.tile, epi, s);
+        }
+    }
+}
+
+}  // namespace
+
+// ---- shared ------------------------------------------------------------------------------------------
+
+Slots carve_slots(Carver& c, int rows, int d, int dtype) {
+    Slots q{};
+    q.padded = round_up(rows, kTileM);
+    q.d64 = round_up(d, kTileK);
+    q.live = c.take<int32_t>(1);
+    q.most = c.take<int32_t>(1);
+    q.slot_of = c.take<int32_t>((size_t)rows);
+    q.token = c.take<int32_t>((size_t)q.padded);
+    // (a tile of the product over rows reads up to 255 columns past a row)
+    const size_t h = (size_t)q.padded * q.d64 + kTileM;
+    q.h = c.take<half_bits>(h);
+    if (dtype == PCM_F32) {
+        q.h_low = c.take<half_bits>(h);
+        q.h_unit = c.take<float>((size_t)q.padded);
+    }
+    if (rows > 4 * kCountRows) q.counts = c.take<int32_t>((size_t)ceil_div(rows, kCountRows));
+    return q;
+}
+SlotGradients carve_gradients(Carver& c, const Slots& slots, int dtype) {
+    SlotGradients g{};
+    g.of = c.take<SlotGradient>((size_t)slots.padded);
+    if (dtype == PCM_F32) {
+        const size_t h = (size_t)slots.padded * slots.d64 + kTileM;
+        g.z_shift = c.take<int32_t>((size_t)slots.padded);
+        g.w_h = c.take<half_bits>(h);
+        g.w_h_low = c.take<half_bits>(h);
+    }
+    return g;
+}
+void gather_slots(const LinearRows& in, const Slots& slots, const SlotGradients* grads, int dtype, hipStream_t s) {
+    const unsigned lists = (unsigned)ceil_div(in.rows, kCountRows), blocks = (unsigned)ceil_div(in.rows + kTileM, kGatherRows);
+    if (slots.counts != nullptr) linear_counts<<<lists, 256, 0, s>>>(in, slots.counts);
+    linear_slots<<<lists, 256, 0, s>>>(in, slots);
+    const SlotGradients g = grads != nullptr ? *grads : SlotGradients{};
+    if (dtype == PCM_F32) {
+        linear_gather<float><<<blocks, 256, 0, s>>>(in, slots, g);
+        if (grads != nullptr) linear_weigh<<<blocks, 256, 0, s>>>(in, slots, g);
+    } else {
+        linear_gather<half_bits><<<blocks, 256, 0, s>>>(in, slots, g);
+    }
+}
+
+WeightSource weight_source(const void* w, int64_t ld, int dtype, int layout, int d, int V) {
+    const int length = layout == PCM_WEIGHT_OUT_IN ? d : V;
+    return WeightSource{w, ld, dtype, layout, d, V,
+                        dtype == PCM_BF16 && (reinterpret_cast<uintptr_t>(w) & 15u) == 0 && ld % 8 == 0 && length % 8 == 0};
+}
+// Pieces of at most 256 MB, in whole tiles.
+int copy_columns(const WeightSource& src) {
+    const int64_t most = (int64_t)(256 << 20) / (round_up(src.d, kTileM) * (src.dtype == PCM_F32 ? 4 : 2)) / kTileN * kTileN;
+    return (int)std::min<int64_t>(std::max<int64_t>(most, kTileN), round_up(src.V, kTileN));
+}
+WeightCopy carve_weight(Carver& c, const WeightSource& src, int columns) {
+    WeightCopy q{};
+    if (src.in_place) return q;
+    q.columns = round_up(columns, kTileN);
+    const int rows = src.layout == PCM_WEIGHT_OUT_IN ? q.columns : round_up(src.d, kTileM);
+    q.ld = src.layout == PCM_WEIGHT_OUT_IN ? round_up(src.d, kTileK) : q.columns;
+    q.w = c.take<half_bits>((size_t)rows * q.ld);
+    if (src.dtype == PCM_F32) {
+        q.low = c.take<half_bits>((size_t)rows * q.ld);
+        q.absmax = c.take<float>(kAbsmaxParts);
+        q.unit = c.take<float>(1);
+    }
+    return q;
+}
+void prepare_weight(const WeightSource& src, const WeightCopy& copy, hipStream_t s) {
+    if (src.dtype != PCM_F32) return;
+    const int rows = src.layout == PCM_WEIGHT_OUT_IN ? src.V : src.d, cols = src.layout == PCM_WEIGHT_OUT_IN ? src.d : src.V;
+    const int parts = std::min(rows, kAbsmaxParts);
+    linear_absmax<<<(unsigned)parts, 256, 0, s>>>(static_cast<const float*>(src.w), src.ld, rows, cols, copy.absmax);
+    linear_unit<<<1, kAbsmaxParts, 0, s>>>(copy.absmax, parts, copy.unit);
+}
+WeightOperand weight_piece(const WeightSource& src, const WeightCopy& copy, int first, int columns, hipStream_t s) {
+    const int64_t at = src.layout == PCM_WEIGHT_OUT_IN ? first * src.ld : first;
+    if (src.in_place) return WeightOperand{static_cast<const half_bits*>(src.w) + at, nullptr, src.ld};
+    // everything that a bounded product asks for: its rows and its reduction index end with the copy's values
+    const int rows = src.layout == PCM_WEIGHT_OUT_IN ? columns : src.d, cols = src.layout == PCM_WEIGHT_OUT_IN ? src.d : columns;
+    const dim3 grid((unsigned)ceil_div((int)copy.ld, 2048), (unsigned)ceil_div(rows, 65535), (unsigned)std::min(rows, 65535));
+    if (src.dtype == PCM_F32) linear_copy<float><<<grid, 256, 0, s>>>(static_cast<const float*>(src.w) + at, src.ld, rows, cols, copy.w, copy.low, copy.ld, copy.unit);
+    else linear_copy<half_bits><<<grid, 256, 0, s>>>(static_cast<const half_bits*>(src.w) + at, src.ld, rows, cols, copy.w, nullptr, copy.ld, nullptr);
+    return WeightOperand{copy.w, copy.low, copy.ld};
+}
+
+int check_linear(const void* hidden, int64_t hidden_ld, const void* weight, int64_t weight_ld, int layout, int dtype, const void* tokens,
+                 int token_type, int64_t rows, int d, int V, float temperature) {
+    if (rows < 0 || d < 1 || V < 1 || hidden_ld < d || (layout != PCM_WEIGHT_IN_OUT && layout != PCM_WEIGHT_OUT_IN) ||
+        weight_ld < (layout == PCM_WEIGHT_OUT_IN ? d : V) || (dtype != PCM_F32 && dtype != PCM_BF16) ||
+        (token_type != PCM_TOKEN_U8 && token_type != PCM_TOKEN_I32 && token_type != PCM_TOKEN_I64) || !(temperature >= 0x1p-126f) ||
+        temperature == __builtin_huge_valf())
+        return PCM_EINVAL;
+    if (rows == 0) return PCM_OK;
+    const uintptr_t value = dtype == PCM_F32 ? 3 : 1, token = token_type == PCM_TOKEN_U8 ? 0 : token_type == PCM_TOKEN_I32 ? 3 : 7;
+    if (!hidden || !weight || !tokens || (reinterpret_cast<uintptr_t>(hidden) & value) != 0 || (reinterpret_cast<uintptr_t>(weight) & value) != 0 ||
+        (reinterpret_cast<uintptr_t>(tokens) & token) != 0)
+        return PCM_EINVAL;
+    return rows > (1 << 24) || d > (1 << 16) || V > (1 << 22) || weight_ld > (1 << 24) ? PCM_EUNSUPPORTED : PCM_OK;
+}
+
+}  // namespace pcm
+
+using namespace pcm;
+
+extern "C" {
+
+PCM_API size_t pcm_linear_logprobs_workspace_bytes(int64_t rows, int d, int V, int dtype, int weight_layout, const void* weight,
+                                                   int64_t weight_ld) {
+    // (the addresses that are not given are taken to be fine)
+    const void* const fine = reinterpret_cast<const void*>((uintptr_t)256);
+    if (rows < 1 || check_linear(fine, d, weight, weight_ld, weight_layout, dtype, fine, PCM_TOKEN_U8, rows, d, V, 1.f) != PCM_OK) return 0;
+    return plan_forward(nullptr, (int)rows, weight_source(weight, weight_ld, dtype, weight_layout, d, V)).bytes;
+}
+
+PCM_API int pcm_linear_logprobs(const void* hidden, int64_t hidden_ld, const void* weight, int64_t weight_ld, int weight_layout, int dtype,
+                                const void* tokens, int token_type, int64_t rows, int d, int V, float temperature, float* logp, float* lse,
+                                float* entropy, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = check_linear(hidden, hidden_ld, weight, weight_ld, weight_layout, dtype, tokens, token_type, rows, d, V, temperature);
+    if (rc == PCM_EINVAL) return rc;
+    if (rows == 0) return PCM_OK;
+    auto misaligned = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; };
+    if (!logp || !lse || misaligned(logp) || misaligned(lse) || misaligned(entropy)) return PCM_EINVAL;
+    if (rc != PCM_OK) return rc;
+    const WeightSource src = weight_source(weight, weight_ld, dtype, weight_layout, d, V);
+    const ForwardPlan f = plan_forward(workspace, (int)rows, src);
+    if (!workspace_ok(workspace, workspace_bytes, f.bytes)) return PCM_EWORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const LinearRows in{hidden, hidden_ld, tokens, token_type, (int)rows, d, V};
+    const float inv_t = 1.f / temperature, c = inv_t * kLog2E;
+    const RowResults out{logp, lse, entropy};
+    StageTimer t(ST_LINEAR_LOGPROBS, s);
+    if (f.few) {
+        if (dtype == PCM_F32) launch_few<float>(in, weight, weight_ld, weight_layout, f.parts, f.token_z, c, s);
+        else launch_few<half_bits>(in, weight, weight_ld, weight_layout, f.parts, f.token_z, c, s);
+        linear_join<1><<<(unsigned)rows, 256, 0, s>>>(in, nullptr, f.parts, f.token_z, inv_t, out);
+        return launch_status();
+    }
+    gather_slots(in, f.slots, nullptr, dtype, s);
+    prepare_weight(src, f.copy, s);
+    if (dtype == PCM_F32) forward_products<true>(f, src, (int)rows, c, s);
+    else forward_products<false>(f, src, (int)rows, c, s);
+    linear_join<16><<<(unsigned)ceil_div((int)rows, 16), 256, 0, s>>>(in, f.slots.slot_of, f.parts, f.token_z, inv_t, out);
+    return launch_status();
+}
+
+}  // extern "C"

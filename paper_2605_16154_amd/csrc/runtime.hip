@@ -15,7 +15,7 @@ const char* const kStageNames[ST_COUNT] = {
     "gemm_dWg_dWu",    "gemm_dX",          "reduce",         "f32_forward", "f32_loss",
     "f32_backward",    "opt_grad_norm",    "opt_adamw",
     "label_phases",    "live_rows",        "token_logprobs", "token_logprobs_grad",
-    "orth_prepare",    "orth_products"};
+    "orth_prepare",    "orth_products",   "linear_logprobs", "linear_logprobs_grad"};
 
 struct Pending {
     int stage;
