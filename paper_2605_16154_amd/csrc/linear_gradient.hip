@@ -16,52 +16,70 @@ typedef __attribute__((ext_vector_type(4))) f16 f16x4;
 
 // ---- dz -------------------------------------------------------------------------------------------
 
+// Vector instructions that no product runs beside: 10 issue slots per logit (the accumulator's move, log p, exponential, factor, product, rounding and
+// the way through LDS).
 struct LogitGradient {
     const SlotGradient* of;
     const int32_t* token;
-    const float *h_unit, *w_unit;        // fp32, or null
+    const float *h_unit, *w_unit;        // fp32, or null: powers of two
     float c;                             // log2 e / temperature
     int first, columns;                  // of the vocabulary in this piece
-    // dz of the 16-column tile j of a wavefront's block, four neighbours of one row; G, at: the row's, `at` its token's place in the block
-    __device__ __forceinline__ f32x4 operator()(f32x4 z, float unit, const SlotGradient& G, int at, int column, bool whole, int col0) const {
-        f32x4 r;
+    // dz of rows 16 i + (lane & 15) of a wavefront's block: store(local row, tile column j, four neighbours).  Rows behind the last slot
+    // are zeros times W with a gradient of zero.
+    template <bool kWhole, int kW, class F>
+    __device__ __forceinline__ void row(const TileCoord<kW>& tc, const Accumulators<kW>& acc, int i, int col0, F store) const {
+        constexpr int RW = kWaveRows<kW>;
+        const int quarter = tc.lane >> 4, slot = tc.row0() + i * 16 + (tc.lane & 15);
+        const SlotGradient G = of[slot];
+        const int at = token[slot] - first - col0;         // of the token in this block
+        const float scale = h_unit != nullptr ? c * (h_unit[slot] * *w_unit) : c;
+        const float along = G.h * kLn2, rest = __builtin_fmaf(G.h, G.entropy, G.g);
+        f32x4 r[kW];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const float a = __builtin_fmaf(z[t] * unit, c, -G.lse2);
-            const float p = __builtin_amdgcn_exp2f(a);
-            // (where p is 0 log p may be -inf, which is not to become a NaN)
-            r[t] = -p * __builtin_fmaf(G.h, __builtin_fmaf(a < -150.f ? -150.f : a, kLn2, G.entropy), G.g);
-            if (at == column + t) r[t] += G.g;
-            if (!whole && col0 + column + t >= columns) r[t] = 0.f;
+        for (int j = 0; j < kW; ++j)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const float a = __builtin_fmaf(acc[i][j][t], scale, -G.lse2);
+                // (where p is 0 log p may be -inf, which is not to become a NaN)
+                const float x = -__builtin_amdgcn_exp2f(a) * __builtin_fmaf(along, fmaxf(a, -150.f), rest);
+                r[j][t] = kWhole || col0 + j * 16 + quarter * 4 + t < columns ? x : 0.f;
+            }
+        if (__any(at >= 0 && at < RW)) {
+#pragma unroll
+            for (int j = 0; j < kW; ++j)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) r[j][t] += at == j * 16 + quarter * 4 + t ? G.g : 0.f;
         }
-        return r;
+#pragma unroll
+        for (int j = 0; j < kW; ++j) store(j, r[j]);
+        __builtin_amdgcn_sched_barrier(0);
     }
 };
 
-// dz as bf16.  Rows behind the last slot (token -1) become zeros.
+// dz as bf16.
 struct EpiLogitGradient {
     LogitGradient gradient;
     bf16* dz;
     int64_t ld;
-    template <int kW>
-    __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* lds) const {
+    template <bool kWhole, int kW>
+    __device__ __forceinline__ void rows(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* st) const {
         constexpr int RW = kWaveRows<kW>, kStride = RW * 2 + 16;
-        char* st = wave_stage(tc, lds);
-        const int col0 = tc.col0(), quarter = tc.lane >> 4;
-        const bool whole = col0 + RW <= gradient.columns;
+        const int col0 = tc.col0();
 #pragma unroll
         for (int i = 0; i < kW; ++i) {
-            const int row = tc.row0() + i * 16 + (tc.lane & 15);
-            const SlotGradient G = gradient.of[row];
-            const int token = gradient.token[row], at = token - gradient.first - col0;
-            stage_tile_row<kW>(st, kStride, tc.lane, i * 16 + (tc.lane & 15), [&](int j) {
-                const f32x4 r = gradient(acc[i][j], 1.f, G, at, j * 16 + quarter * 4, whole, col0);
-                return token < 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : r;
+            char* const to = st + (i * 16 + (tc.lane & 15)) * kStride + 4 * (tc.lane >> 4) * 2;
+            gradient.row<kWhole>(tc, acc, i, col0, [&](int j, const f32x4& r) __attribute__((always_inline)) {
+                *reinterpret_cast<bf16x4*>(to + j * 32) = to_bf16x4(r[0], r[1], r[2], r[3]);
             });
-            __builtin_amdgcn_sched_barrier(0);
         }
         __builtin_amdgcn_wave_barrier();
         copy_rows_out<RW, RW * 2>(st, kStride, reinterpret_cast<char*>(dz + (int64_t)tc.row0() * ld + col0), ld * 2, RW, tc.lane);
+    }
+    template <int kW>
+    __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* lds) const {
+        char* st = wave_stage(tc, lds);
+        if (tc.col0() + kWaveRows<kW> <= gradient.columns) rows<true>(tc, acc, st);
+        else rows<false>(tc, acc, st);
     }
 };
 // dz 2^z_shift as hi + lo of fp16.
@@ -69,37 +87,25 @@ struct EpiLogitGradientPairs {
     LogitGradient gradient;
     f16 *hi, *lo;
     int64_t ld;
-    template <int kW>
-    __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* lds) const {
+    template <bool kWhole, int kW>
+    __device__ __forceinline__ void rows(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* st) const {
         constexpr int RW = kWaveRows<kW>, kStride = RW * 4 + 16;
-        char* st = wave_stage(tc, lds);
-        const int col0 = tc.col0(), quarter = tc.lane >> 4;
-        const bool whole = col0 + RW <= gradient.columns;
-        const float w_unit = *gradient.w_unit;
+        const int col0 = tc.col0();
 #pragma unroll
         for (int half = 0; half < RW / 64; ++half) {       // 64 rows per pass
 #pragma unroll
             for (int ii = 0; ii < 4; ++ii) {
-                const int i = half * 4 + ii, row = tc.row0() + i * 16 + (tc.lane & 15);
-                const SlotGradient G = gradient.of[row];
-                const int token = gradient.token[row], at = token - gradient.first - col0;
-                const float unit = gradient.h_unit[row] * w_unit;
-                char* to = st + (ii * 16 + (tc.lane & 15)) * kStride;
-#pragma unroll
-                for (int j = 0; j < kW; ++j) {
-                    f32x4 r = gradient(acc[i][j], unit, G, at, j * 16 + quarter * 4, whole, col0);
+                char* const to = st + (ii * 16 + (tc.lane & 15)) * kStride + 4 * (tc.lane >> 4) * 2;
+                gradient.row<kWhole>(tc, acc, half * 4 + ii, col0, [&](int j, const f32x4& r) __attribute__((always_inline)) {
                     f16x4 h, l;
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
-                        const float x = token < 0 ? 0.f : r[t];
-                        h[t] = (f16)x;
-                        l[t] = (f16)(x - (float)h[t]);
+                        h[t] = (f16)r[t];
+                        l[t] = (f16)(r[t] - (float)h[t]);
                     }
-                    char* at_j = to + (j * 16 + 4 * quarter) * 2;
-                    *reinterpret_cast<f16x4*>(at_j) = h;
-                    *reinterpret_cast<f16x4*>(at_j + RW * 2) = l;
-                }
-                __builtin_amdgcn_sched_barrier(0);
+                    *reinterpret_cast<f16x4*>(to + j * 32) = h;
+                    *reinterpret_cast<f16x4*>(to + j * 32 + RW * 2) = l;
+                });
             }
             __builtin_amdgcn_wave_barrier();
             const int64_t at = (int64_t)(tc.row0() + half * 64) * ld + col0;
@@ -107,6 +113,12 @@ struct EpiLogitGradientPairs {
             copy_rows_out<64, RW * 2>(st + RW * 2, kStride, reinterpret_cast<char*>(lo + at), ld * 2, 64, tc.lane);
             __builtin_amdgcn_wave_barrier();
         }
+    }
+    template <int kW>
+    __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* lds) const {
+        char* st = wave_stage(tc, lds);
+        if (tc.col0() + kWaveRows<kW> <= gradient.columns) rows<true>(tc, acc, st);
+        else rows<false>(tc, acc, st);
     }
 };
 
@@ -132,6 +144,13 @@ struct EpiStoreAnywhere {
         const int col0 = tc.col0(), n_cols = min(RW, cols - col0);
         const float unit = weight_gradient_unit(most);
         if (n_cols <= 0) return;
+        if constexpr (sizeof(T) == 2) {
+            if (n_cols == RW && ((reinterpret_cast<uintptr_t>(C) | (uintptr_t)(ldc * 2)) & 15u) == 0) {      // 16 bytes a lane
+                const EpiStoreBf16 store{reinterpret_cast<bf16*>(C), ldc, rows};
+                store(tc, acc, lds);
+                return;
+            }
+        }
 #pragma unroll
         for (int i = 0; i < RW / 32; ++i) {                // 32 rows per pass
 #pragma unroll
@@ -209,18 +228,25 @@ void sum_parts(const PartSum& q, void* out, int64_t ld, int dtype, hipStream_t s
 
 // ---- host side --------------------------------------------------------------------------------------
 
-// Parts of a reduction of `steps`: as many as fill the chip with tiles of kW, of eight steps or more.
-int parts_for(int64_t tiles, int steps, int resident) {
-    if (tiles >= resident) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({resident / tiles, steps / 8, 32}));
-}
+// Tile and parts of the reduction of a product of M x N whose reduction takes `steps`, by an estimate: rounds of workgroups over 256 CUs times
+// the steps of a part (0.94 us with the large tile, 0.46 with the small one, see tile_for; ten steps more for the start and the epilogue), and
+// the parts, written and read, at 4.8 TB/s.
 struct ProductPlan {
     int kW, parts;
     ProductPlan() : kW(kSmallTile), parts(1) {}
     ProductPlan(int M, int N, int steps) {
-        kW = tile_for(M, N, 1);
-        const int64_t tiles = (int64_t)(M / (32 * kW)) * (N / (32 * kW));
-        parts = parts_for(tiles, steps, kW == kLargeTile ? 256 : 512);
+        double best = 1e30;
+        for (const int tile : {kLargeTile, kSmallTile})
+            for (int n = 1; n <= 16 && (n == 1 || steps / n >= 8); ++n) {
+                const int64_t groups = (int64_t)ceil_div(M, 32 * tile) * ceil_div(N, 32 * tile) * n;
+                const double round = (tile == kLargeTile ? 0.94 : 0.46) * (ceil_div(steps, n) + 10);
+                const double cost = (double)((groups + 255) / 256) * round + (n == 1 ? 0.0 : 2.0 * n * M * N * 4.0 / 4.8e6 + 3.0);
+                if (cost < best) {
+                    best = cost;
+                    kW = tile;
+                    parts = n;
+                }
+            }
     }
 };
 

@@ -13,6 +13,7 @@ namespace pcm {
 namespace {
 
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
 typedef _Float16 f16;
 
 // ---- slots ---------------------------------------------------------------------------------------
@@ -45,6 +46,7 @@ __global__ __launch_bounds__(256) void linear_counts(LinearRows in, int32_t* cou
     if (threadIdx.x == 0) counts[blockIdx.x] = n;
 }
 
+constexpr int kNoExponent = -(1 << 20);
 // 1024 rows a workgroup, four neighbours a thread.  Where its rows begin among the slots it counts itself, from the tokens or, for long
 // lists, from the counts of the launch before.
 __global__ __launch_bounds__(256) void linear_slots(LinearRows in, Slots slots) {
@@ -80,7 +82,7 @@ __global__ __launch_bounds__(256) void linear_slots(LinearRows in, Slots slots) 
     }
     if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 255) {
         *slots.live = slot;
-        *slots.most = -(1 << 20);
+        *slots.most = kNoExponent;
     }
 }
 
@@ -100,8 +102,8 @@ __device__ inline int shift_for(int exponent) { return min(126, max(-126, 14 - e
 __device__ inline half_bits high_part(float x) { return __builtin_bit_cast(half_bits, (f16)x); }
 __device__ inline half_bits low_part(float x) { return __builtin_bit_cast(half_bits, (f16)(x - (float)(f16)x)); }
 
-// Up to eight neighbouring 16-bit values; zeros behind the first n.
-__device__ inline u32x4 load_8(const half_bits* p, int n) {
+// 16 bytes at any address of their type; zeros behind the first n values.
+__device__ inline u32x4 load_16B(const half_bits* p, int n) {
     if (n >= 8) return *reinterpret_cast<const u32x4_any*>(p);
     u32x4 x = {0, 0, 0, 0};
 #pragma unroll
@@ -109,110 +111,151 @@ __device__ inline u32x4 load_8(const half_bits* p, int n) {
         if (e < n) x[e / 2] |= (uint32_t)p[e] << (e % 2 * 16);
     return x;
 }
+__device__ inline f32x4 load_4(const float* p, int n) {
+    if (n >= 4) return *reinterpret_cast<const f32x4_any*>(p);
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < n) x[e] = p[e];
+    return x;
+}
+__device__ inline u32x4 load_16B(const float* p, int n) { return __builtin_bit_cast(u32x4, load_4(p, n)); }
+
+// Eight fp32 values times a power of two as pairs.
+template <class F>
+__device__ inline void store_pairs(half_bits* hi, half_bits* lo, F value) {
+    u32x4 h = {0, 0, 0, 0}, l = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float x = value(e);
+        h[e / 2] |= (uint32_t)high_part(x) << (e % 2 * 16);
+        l[e / 2] |= (uint32_t)low_part(x) << (e % 2 * 16);
+    }
+    *reinterpret_cast<u32x4*>(hi) = h;
+    *reinterpret_cast<u32x4*>(lo) = l;
+}
+// A row of d values times 2^shift as pairs, zeros up to d64, by a wavefront.
+__device__ inline void pair_row(const float* from, int d, int shift, half_bits* hi, half_bits* lo, int d64, int lane) {
+    for (int i = lane * 8; i < d64; i += 512) {
+        const f32x4 a = load_4(from + i, d - i), b = load_4(from + i + 4, d - i - 4);
+        store_pairs(hi + i, lo + i, [&](int e) { return ldexpf(e < 4 ? a[e] : b[e - 4], shift); });
+    }
+}
+__device__ inline void zero_row(half_bits* to, int d64, int lane) {
+    for (int i = lane * 8; i < d64; i += 512) *reinterpret_cast<u32x4*>(to + i) = u32x4{0, 0, 0, 0};
+}
 
 // A wavefront per row: bf16 rows are copied, fp32 rows become pairs.  256 more take the slots behind the last one.
-constexpr int kGatherRows = 16;                       // per workgroup
-template <class T>
+// kList: the launch that lists the slots is part of this one, each workgroup counting the tokens before its rows (short lists; 256 rows of 256 bf16 take
+// 5 us so instead of 8 in two launches).
+constexpr int kGatherRows = 4;                        // per workgroup
+template <class T, bool kList>
 __global__ __launch_bounds__(256) void linear_gather(LinearRows in, Slots slots, SlotGradients grads) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int live = *slots.live;
-    int most = -(1 << 20);
-    for (int r = wave; r < kGatherRows; r += 4) {
-        const int row = blockIdx.x * kGatherRows + r;
-        if (row >= in.rows) {
-            const int slot = live + row - in.rows;
-            if (slot >= min(slots.padded, (live + 255) / 256 * 256)) break;
-            for (int i = lane * 8; i < slots.d64; i += 512) {
-                *reinterpret_cast<u32x4*>(slots.h + (int64_t)slot * slots.d64 + i) = u32x4{0, 0, 0, 0};
-                if (sizeof(T) == 4) *reinterpret_cast<u32x4*>(slots.h_low + (int64_t)slot * slots.d64 + i) = u32x4{0, 0, 0, 0};
-            }
-            if (lane == 0) {
-                slots.token[slot] = -1;
-                if (sizeof(T) == 4) slots.h_unit[slot] = 1.f;
-                if (grads.of != nullptr) grads.of[slot] = SlotGradient{0.f, 0.f, 0.f, 0.f};
-                if (sizeof(T) == 4 && grads.of != nullptr) grads.z_shift[slot] = 0;
-            }
-            continue;
-        }
-        const int slot = slots.slot_of[row];
-        if (slot < 0) continue;
-        const T* const from = static_cast<const T*>(in.hidden) + row * in.ld;
-        const int64_t to = (int64_t)slot * slots.d64;
-        float largest = 0.f;
-        if constexpr (sizeof(T) == 2) {
-            for (int i = lane * 8; i < slots.d64; i += 512) *reinterpret_cast<u32x4*>(slots.h + to + i) = load_8(from + i, in.d - i);
-        } else {
-            for (int i = lane; i < in.d; i += 64) largest = fmaxf(largest, finite_abs(from[i]));
-            largest = wave_max(largest);
-            const int shift = largest > 0.f ? shift_for(exponent_of(largest)) : 0;
-            for (int i = lane; i < slots.d64; i += 64) {
-                const float x = i < in.d ? ldexpf(from[i], shift) : 0.f;
-                slots.h[to + i] = high_part(x);
-                slots.h_low[to + i] = low_part(x);
-            }
-            if (lane == 0) slots.h_unit[slot] = ldexpf(1.f, -shift);
-        }
-        if (grads.of != nullptr) {
-            SlotGradient of;
-            of.g = grads.dlogp[row] * grads.inv_t;
-            of.h = grads.dentropy != nullptr ? grads.dentropy[row] * grads.inv_t : 0.f;
-            of.lse2 = grads.lse[row] * kLog2E;
-            of.entropy = grads.dentropy != nullptr ? grads.entropy[row] : 0.f;
-            if constexpr (sizeof(T) == 4) {
-                // |p (log p + entropy)| is at most the larger of 1 / e and the entropy
-                const float bound = fabsf(of.g) + fabsf(of.h) * (0.5f + fabsf(of.entropy));
-                const int shift = bound > 0.f && bound < __builtin_huge_valf() ? shift_for(exponent_of(bound)) : 0;
-                of.g = ldexpf(of.g, shift);
-                of.h = ldexpf(of.h, shift);
-                if (lane == 0) grads.z_shift[slot] = shift;
-                if (bound > 0.f && largest > 0.f) most = max(most, exponent_of(largest) - shift);
-            }
-            if (lane == 0) grads.of[slot] = of;
+    const int first = blockIdx.x * kGatherRows, row = first + wave;
+    int before = 0, token = -1;
+    if (kList) {
+        for (int i = threadIdx.x; i < min(first, in.rows); i += 256) before += token_at(in, i) >= 0;
+        before = block_count(before);
+        for (int w = 0; w < kGatherRows; ++w) {
+            const int t = first + w < in.rows ? token_at(in, first + w) : -1;
+            if (w == wave) token = t;
+            if (w < wave) before += t >= 0;
         }
     }
-    if (sizeof(T) == 4 && grads.of != nullptr) {
-        __shared__ int lds[4];
-        if (lane == 0) lds[wave] = most;
-        __syncthreads();
-        most = max(max(lds[0], lds[1]), max(lds[2], lds[3]));
-        if (threadIdx.x == 0 && most > -(1 << 20)) atomicMax(slots.most, most);
+    if (row >= in.rows) {
+        // (a workgroup on the border has counted the rows before its own, so `before` is all of them)
+        const int live = kList ? before : *slots.live, slot = live + row - in.rows;
+        if (kList && row == in.rows && lane == 0) *slots.live = live;
+        if (slot >= min(slots.padded, (live + 255) / 256 * 256)) return;
+        zero_row(slots.h + (int64_t)slot * slots.d64, slots.d64, lane);
+        if (sizeof(T) == 4) zero_row(slots.h_low + (int64_t)slot * slots.d64, slots.d64, lane);
+        if (lane == 0) {
+            slots.token[slot] = -1;
+            if (sizeof(T) == 4) slots.h_unit[slot] = 1.f;
+            if (grads.of != nullptr) grads.of[slot] = SlotGradient{0.f, 0.f, 0.f, 0.f};
+            if (sizeof(T) == 4 && grads.of != nullptr) grads.z_shift[slot] = 0;
+        }
+        return;
     }
+    int slot;
+    if (kList) {
+        slot = token >= 0 ? before : -1;
+        if (lane == 0) {
+            slots.slot_of[row] = slot;
+            if (slot >= 0) slots.token[slot] = token;
+        }
+    } else {
+        slot = slots.slot_of[row];
+    }
+    if (slot < 0) return;
+    const T* const from = static_cast<const T*>(in.hidden) + row * in.ld;
+    const int64_t to = (int64_t)slot * slots.d64;
+    float largest = 0.f;
+    if constexpr (sizeof(T) == 2) {
+        for (int i = lane * 8; i < slots.d64; i += 512) *reinterpret_cast<u32x4*>(slots.h + to + i) = load_16B(from + i, in.d - i);
+    } else {
+        for (int i = lane * 4; i < in.d; i += 256) {
+            const f32x4 x = load_4(from + i, in.d - i);
+            largest = fmaxf(fmaxf(largest, fmaxf(finite_abs(x[0]), finite_abs(x[1]))), fmaxf(finite_abs(x[2]), finite_abs(x[3])));
+        }
+        largest = wave_max(largest);
+        const int shift = largest > 0.f ? shift_for(exponent_of(largest)) : 0;
+        pair_row(from, in.d, shift, slots.h + to, slots.h_low + to, slots.d64, lane);
+        if (lane == 0) slots.h_unit[slot] = ldexpf(1.f, -shift);
+    }
+    if (grads.of == nullptr || lane != 0) return;
+    SlotGradient of;
+    of.g = grads.dlogp[row] * grads.inv_t;
+    of.h = grads.dentropy != nullptr ? grads.dentropy[row] * grads.inv_t : 0.f;
+    of.lse2 = grads.lse[row] * kLog2E;
+    of.entropy = grads.dentropy != nullptr ? grads.entropy[row] : 0.f;
+    if constexpr (sizeof(T) == 4) {
+        // |p (log p + entropy)| is at most the larger of 1 / e and the entropy
+        const float bound = fabsf(of.g) + fabsf(of.h) * (0.5f + fabsf(of.entropy));
+        const int shift = bound > 0.f && bound < __builtin_huge_valf() ? shift_for(exponent_of(bound)) : 0;
+        of.g = ldexpf(of.g, shift);
+        of.h = ldexpf(of.h, shift);
+        grads.z_shift[slot] = shift;
+        // (the largest of whole numbers: their order does not matter)
+        if (bound > 0.f && largest > 0.f) atomicMax(slots.most, exponent_of(largest) - shift);
+    }
+    grads.of[slot] = of;
 }
 
 // h 2^(14 - most - z_shift) as pairs: dz 2^z_shift times it adds up over rows of any sizes.
 __global__ __launch_bounds__(256) void linear_weigh(LinearRows in, Slots slots, SlotGradients grads) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, row = blockIdx.x * kGatherRows + (int)(threadIdx.x >> 6);
     const int live = *slots.live, most = *slots.most;
-    for (int r = wave; r < kGatherRows; r += 4) {
-        const int row = blockIdx.x * kGatherRows + r;
-        if (row >= in.rows) {
-            const int slot = live + row - in.rows;
-            if (slot >= min(slots.padded, (live + 255) / 256 * 256)) break;
-            for (int i = lane * 8; i < slots.d64; i += 512) {
-                *reinterpret_cast<u32x4*>(grads.w_h + (int64_t)slot * slots.d64 + i) = u32x4{0, 0, 0, 0};
-                *reinterpret_cast<u32x4*>(grads.w_h_low + (int64_t)slot * slots.d64 + i) = u32x4{0, 0, 0, 0};
-            }
-            continue;
-        }
-        const int slot = slots.slot_of[row];
-        if (slot < 0) continue;
-        const float* const from = static_cast<const float*>(in.hidden) + row * in.ld;
-        const int64_t to = (int64_t)slot * slots.d64;
-        const int shift = max(-300, 14 - most - grads.z_shift[slot]);
-        for (int i = lane; i < slots.d64; i += 64) {
-            const float x = i < in.d ? ldexpf(from[i], shift) : 0.f;
-            grads.w_h[to + i] = high_part(x);
-            grads.w_h_low[to + i] = low_part(x);
-        }
+    if (row >= in.rows) {
+        const int slot = live + row - in.rows;
+        if (slot >= min(slots.padded, (live + 255) / 256 * 256)) return;
+        zero_row(grads.w_h + (int64_t)slot * slots.d64, slots.d64, lane);
+        zero_row(grads.w_h_low + (int64_t)slot * slots.d64, slots.d64, lane);
+        return;
     }
+    const int slot = slots.slot_of[row];
+    if (slot < 0) return;
+    const int64_t to = (int64_t)slot * slots.d64;
+    pair_row(static_cast<const float*>(in.hidden) + row * in.ld, in.d, max(-300, 14 - most - grads.z_shift[slot]), grads.w_h + to, grads.w_h_low + to,
+             slots.d64, lane);
 }
 
 // ---- weights that have to be copied ----------------------------------------------------------------
 
+// 4096 values of a row at a time.
 __global__ __launch_bounds__(256) void linear_absmax(const float* w, int64_t ld, int rows, int cols, float* parts) {
+    const int per_row = (cols + 4095) / 4096;
     float most = 0.f;
-    for (int row = blockIdx.x; row < rows; row += gridDim.x)
-        for (int i = threadIdx.x; i < cols; i += 256) most = fmaxf(most, finite_abs(w[row * ld + i]));
+    for (int64_t at = blockIdx.x; at < (int64_t)rows * per_row; at += gridDim.x) {
+        const int row = (int)(at / per_row), i = (int)(at % per_row) * 4096 + threadIdx.x * 4;
+        f32x4 x[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[q] = i + q * 1024 < cols ? load_4(w + row * ld + i + q * 1024, cols - i - q * 1024) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            most = fmaxf(fmaxf(most, fmaxf(finite_abs(x[q][0]), finite_abs(x[q][1]))), fmaxf(finite_abs(x[q][2]), finite_abs(x[q][3])));
+    }
     most = wave_max(most);
     __shared__ float lds[4];
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = most;
@@ -239,31 +282,24 @@ __global__ __launch_bounds__(256) void linear_copy(const T* w, int64_t ld, int r
     const int n = cols - i;
     half_bits* const out = to + row * ld_to + i;
     if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<u32x4*>(out) = load_8(from, n);
+        *reinterpret_cast<u32x4*>(out) = load_16B(from, n);
     } else {
         const float scale = 1.f / *unit;                  // a power of two
-        u32x4 hi = {0, 0, 0, 0}, lo = {0, 0, 0, 0};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = e < n ? from[e] * scale : 0.f;
-            hi[e / 2] |= (uint32_t)high_part(x) << (e % 2 * 16);
-            lo[e / 2] |= (uint32_t)low_part(x) << (e % 2 * 16);
-        }
-        *reinterpret_cast<u32x4*>(out) = hi;
-        *reinterpret_cast<u32x4*>(low + row * ld_to + i) = lo;
+        const f32x4 a = load_4(from, n), b = load_4(from + 4, n - 4);
+        store_pairs(out, low + row * ld_to + i, [&](int e) { return (e < 4 ? a[e] : b[e - 4]) * scale; });
     }
 }
 
 // ---- statistics of blocks of logits ------------------------------------------------------------------
 
-// Of the parts of each slot: [parts][ld].  A part that saw nothing has the sum 0.
-struct PartSums {
-    float *most, *sum, *moment;          // largest z; sum 2^a; sum 2^a a, a = (z - most) c
-    int64_t ld;
-    int parts;
-};
+// What a part of a row's logits comes to: the largest z; sum 2^a; sum 2^a a, a = (z - largest) c.  A part that saw nothing has the sum 0.
 struct RowSums {
     float m, s, t;
+};
+struct PartSums {
+    f32x4* of;                           // [parts][ld], the fourth value unused
+    int64_t ld;
+    int parts;
 };
 __device__ inline void merge(RowSums& a, const RowSums& b, float c) {
     if (b.s == 0.f) return;
@@ -274,67 +310,85 @@ __device__ inline void merge(RowSums& a, const RowSums& b, float c) {
     a.s = a.s * ea + b.s * eb;
     a.m = m;
 }
-// (z - m) c for a logit that is not above m; -150 stands for all that is as good as nothing.  NaN where z is.
-__device__ inline void add_exponent(float a, float& s, float& t) {
-    const float e = __builtin_amdgcn_exp2f(a);
-    s += e;
-    t = __builtin_fmaf(e, fmaxf(a, -150.f), t);
+// The sums of `kN` x 4 logits relative to m; -150 stands for what is as good as nothing (a is -inf where z is, or is that far below m).
+template <int kN, class F>
+__device__ __forceinline__ RowSums sums_of(float m, float c, F z) {
+    RowSums r{m, 0.f, 0.f};
+    auto add = [&](auto floor) __attribute__((always_inline)) {
+        r.s = r.t = 0.f;
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+            float s = 0.f, t = 0.f;                        // four terms before they are added to the others
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float a = (z(j, e) - m) * c, x = __builtin_amdgcn_exp2f(a);
+                s += x;
+                t = __builtin_fmaf(x, decltype(floor)::value ? fmaxf(a, -150.f) : a, t);
+            }
+            r.s += s;
+            r.t += t;
+        }
+    };
+    add(std::false_type{});
+    if (__any(!(r.t > -__builtin_huge_valf()))) add(std::true_type{});
+    return r;
 }
 
+// The logits of a tile, a wavefront's block of which is a part of its rows.  Vector instructions that no product runs beside: 10 issue
+// slots per logit (the accumulator's move, the maximum, difference, product, exponential, sum and moment).
 struct EpiRowStats {
     PartSums out;
     float* token_z;                      // [padded]
     const int32_t* token;
-    const float *h_unit, *w_unit;        // fp32, or null
+    const float *h_unit, *w_unit;        // fp32, or null: powers of two
     float c;                             // log2 e / temperature
     int first, columns;                  // of the vocabulary in this piece
     int first_part;
     template <int kW>
     __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char*) const {
         constexpr int RW = kWaveRows<kW>;
-        const int col0 = tc.col0(), part = first_part + col0 / RW;
+        const int col0 = tc.col0();
         if (col0 >= columns) return;                       // no part of its own
-        const bool whole = col0 + RW <= columns;
-        const int quarter = tc.lane >> 4;
+        if (col0 + RW <= columns) rows<true>(tc, acc, col0);
+        else rows<false>(tc, acc, col0);
+    }
+    template <bool kWhole, int kW>
+    __device__ __forceinline__ void rows(const TileCoord<kW>& tc, const Accumulators<kW>& acc, int col0) const {
+        constexpr int RW = kWaveRows<kW>;
+        const int quarter = tc.lane >> 4, row0 = tc.row0() + (tc.lane & 15);
         const float w_scale = w_unit != nullptr ? *w_unit : 1.f;
+        int at[kW];                                        // of the token in this block
+        float unit[kW];
 #pragma unroll
         for (int i = 0; i < kW; ++i) {
-            const int row = tc.row0() + i * 16 + (tc.lane & 15);
-            const float unit = h_unit != nullptr ? h_unit[row] * w_scale : 1.f;
-            const int at = token[row] - first - col0;      // of the token in this block
-            float z[kW][4], m = -__builtin_huge_valf();
+            at[i] = token[row0 + i * 16] - first - col0;
+            unit[i] = h_unit != nullptr ? h_unit[row0 + i * 16] * w_scale : 1.f;
+        }
+#pragma unroll
+        for (int i = 0; i < kW; ++i) {
+            auto z = [&](int j, int t) __attribute__((always_inline)) {
+                return kWhole || col0 + j * 16 + quarter * 4 + t < columns ? acc[i][j][t] : -__builtin_huge_valf();
+            };
+            float m = -__builtin_huge_valf();
 #pragma unroll
             for (int j = 0; j < kW; ++j)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    z[j][t] = acc[i][j][t] * unit;
-                    if (!whole && col0 + j * 16 + quarter * 4 + t >= columns) z[j][t] = -__builtin_huge_valf();
-                    m = fmaxf(m, z[j][t]);
-                }
-            if (__any(at >= 0 && at < RW)) {
+                for (int t = 0; t < 4; ++t) m = fmaxf(m, z(j, t));
+            if (__any(at[i] >= 0 && at[i] < RW)) {
 #pragma unroll
                 for (int j = 0; j < kW; ++j)
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
-                        if (at == j * 16 + quarter * 4 + t) token_z[row] = z[j][t];
+                        if (at[i] == j * 16 + quarter * 4 + t) token_z[row0 + i * 16] = acc[i][j][t] * unit[i];
             }
             m = fmaxf(m, __shfl_xor(m, 16, 64));
             m = fmaxf(m, __shfl_xor(m, 32, 64));
-            float s = 0.f, moment = 0.f;
-#pragma unroll
-            for (int j = 0; j < kW; ++j) {
-                float sj = 0.f, tj = 0.f;
-#pragma unroll
-                for (int t = 0; t < 4; ++t) add_exponent((z[j][t] - m) * c, sj, tj);
-                s += sj;
-                moment += tj;
-            }
-            s += __shfl_xor(s, 16, 64);
-            s += __shfl_xor(s, 32, 64);
-            moment += __shfl_xor(moment, 16, 64);
-            moment += __shfl_xor(moment, 32, 64);
-            float* const to = quarter == 0 ? out.most : quarter == 1 ? out.sum : out.moment;
-            if (quarter < 3) to[part * out.ld + row] = quarter == 0 ? m : quarter == 1 ? s : moment;
+            RowSums r = sums_of<kW>(m, c * unit[i], z);
+            r.s += __shfl_xor(r.s, 16, 64);
+            r.s += __shfl_xor(r.s, 32, 64);
+            r.t += __shfl_xor(r.t, 16, 64);
+            r.t += __shfl_xor(r.t, 32, 64);
+            if (quarter == 0) out.of[(first_part + col0 / RW) * out.ld + row0 + i * 16] = f32x4{m * unit[i], r.s, r.t, 0.f};
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -358,8 +412,8 @@ __global__ __launch_bounds__(256) void linear_join(LinearRows in, const int32_t*
     if (slot >= 0) {
 #pragma unroll 4
         for (int p = k; p < parts.parts; p += kParts) {
-            const int64_t at = p * parts.ld + slot;
-            merge(a, RowSums{parts.most[at], parts.sum[at], parts.moment[at]}, c);
+            const f32x4 b = parts.of[p * parts.ld + slot];
+            merge(a, RowSums{b[0], b[1], b[2]}, c);
         }
     }
     lds[k][r] = a;
@@ -387,22 +441,6 @@ __global__ __launch_bounds__(256) void linear_join(LinearRows in, const int32_t*
 
 // ---- few rows --------------------------------------------------------------------------------------
 
-// The part of the projection that a lane brings in as 16 bytes, zeros where it ends.
-template <class T>
-__device__ inline u32x4 load_16B(const T* p, int n) {
-    if constexpr (sizeof(T) == 2) {
-        return load_8(p, n);
-    } else {
-        typedef u32x4 __attribute__((aligned(4))) u32x4_floats;
-        if (n >= 4) return *reinterpret_cast<const u32x4_floats*>(p);
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < n) x[e] = p[e];
-        return __builtin_bit_cast(u32x4, x);
-    }
-}
-
 // z of up to 16 rows and a block of the vocabulary.  The four wavefronts of a workgroup take every fourth slice of the reduction index, their sums
 // are added in LDS.  A slice is 4 lane groups x kE values of k (kE = 16 bytes of them).
 //   [V][d]: a lane brings in kE values of k of one column and is its fragment; four fragments of 16 columns share one of the hidden rows.
@@ -420,51 +458,77 @@ __global__ __launch_bounds__(256) void few_rows(LinearRows in, const T* w, int64
     // (lanes of rows that are not there take the last one's values along)
     const T* const h_row = static_cast<const T*>(in.hidden) + min(at, in.rows - 1) * in.ld;
     const bool has_row = at < in.rows;
-    auto slice = [&](int k0, auto inside) __attribute__((always_inline)) {
-        constexpr bool kInside = decltype(inside)::value;          // all of it is there
+    // [d][V]: where the vocabulary ends lanes move back to its last kE columns and count those that are their own.
+    const bool moves = kLayout == PCM_WEIGHT_IN_OUT && in.V >= kE;
+    auto first_column = [&](int lane_of_16) { return moves ? min(n0 + lane_of_16 * kE, in.V - kE) : n0 + lane_of_16 * kE; };
+    struct Slice {
+        u32x4 w[kLoads], h;
+    };
+    // whole slices of k (rows of [V][d] behind the last one are the last one again)
+    auto load = [&](Slice& x, int k0) __attribute__((always_inline)) {
         const int k = k0 + group * kE;
-        u32x4 piece[kLoads];
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q)
+            x.w[q] = load_16B(kLayout == PCM_WEIGHT_OUT_IN ? w + min(n0 + q * 16 + at, in.V - 1) * ld + k : w + (k + q) * ld + first_column(at), kE);
+        x.h = load_16B(h_row + k, kE);
+    };
+    auto load_edge = [&](Slice& x, int k0) __attribute__((always_inline)) {
+        const int k = k0 + group * kE;
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
-            const int v = n0 + (kLayout == PCM_WEIGHT_OUT_IN ? q * 16 + at : at * kE), row = kLayout == PCM_WEIGHT_OUT_IN ? v : k + q;
-            const T* const from = w + row * ld + (kLayout == PCM_WEIGHT_OUT_IN ? k : v);
-            piece[q] = u32x4{0, 0, 0, 0};
-            if (kInside) piece[q] = load_16B(from, kE);
-            else if (kLayout == PCM_WEIGHT_OUT_IN ? v < in.V && k < in.d : v < in.V && row < in.d) piece[q] = load_16B(from, kLayout == PCM_WEIGHT_OUT_IN ? in.d - k : in.V - v);
+            const int v = kLayout == PCM_WEIGHT_OUT_IN ? n0 + q * 16 + at : first_column(at), row = kLayout == PCM_WEIGHT_OUT_IN ? k : k + q;
+            x.w[q] = u32x4{0, 0, 0, 0};
+            if (v < in.V && row < in.d) x.w[q] = kLayout == PCM_WEIGHT_OUT_IN ? load_16B(w + v * ld + k, in.d - k) : load_16B(w + row * ld + v, in.V - v);
         }
-        u32x4 h = {0, 0, 0, 0};
-        if (kInside) h = load_16B(h_row + k, kE);
-        else if (k < in.d) h = load_16B(h_row + k, in.d - k);
+        x.h = u32x4{0, 0, 0, 0};
+        if (k < in.d) x.h = load_16B(h_row + k, in.d - k);
+    };
+    auto multiply = [&](const Slice& x) __attribute__((always_inline)) {
         if constexpr (sizeof(T) == 2) {
-            const bf16x8 hf = __builtin_bit_cast(bf16x8, h);
+            const bf16x8 hf = __builtin_bit_cast(bf16x8, x.h);
 #pragma unroll
             for (int j = 0; j < kTiles; ++j) {
                 u32x4 f;
-                if (kLayout == PCM_WEIGHT_OUT_IN) f = piece[j];
+                if constexpr (kLayout == PCM_WEIGHT_OUT_IN) f = x.w[j];
                 else {
 #pragma unroll
                     for (int q = 0; q < 4; ++q)                  // column j of rows 2 q and 2 q + 1
-                        f[q] = __builtin_amdgcn_perm(piece[2 * q + 1][j / 2], piece[2 * q][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+                        f[q] = __builtin_amdgcn_perm(x.w[2 * q + 1][j / 2], x.w[2 * q][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
                 }
                 acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), hf, acc[j], 0, 0, 0);
             }
         } else {
-            const f32x4 hf = __builtin_bit_cast(f32x4, h);
+            const f32x4 hf = __builtin_bit_cast(f32x4, x.h);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int j = 0; j < kTiles; ++j) {
-                    const f32x4 f = __builtin_bit_cast(f32x4, piece[kLayout == PCM_WEIGHT_OUT_IN ? j : e]);
+                    const f32x4 f = __builtin_bit_cast(f32x4, x.w[kLayout == PCM_WEIGHT_OUT_IN ? j : e]);
                     acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[kLayout == PCM_WEIGHT_OUT_IN ? e : j], hf[e], acc[j], 0, 0, 0);
                 }
         }
     };
-    int k0 = wave * kSlice;
-    if (n0 + kColumns <= in.V) {
-#pragma unroll 2
-        for (; k0 + kSlice <= in.d; k0 += 4 * kSlice) slice(k0, std::true_type{});
+    // Whole slices: kAhead are under way while one is multiplied (past the end the last one again).
+    constexpr int kAhead = kLoads > 4 ? 2 : 4, kStride = 4 * kSlice;
+    int done = 0;
+    if ((kLayout == PCM_WEIGHT_OUT_IN || moves) && wave * kSlice + kSlice <= in.d) {
+        const int n = (in.d - kSlice - wave * kSlice) / kStride + 1;
+        Slice x[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) load(x[i], wave * kSlice + min(i, n - 1) * kStride);
+        for (; done < n; done += kAhead)
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (done + i < n) multiply(x[i]);
+                load(x[i], wave * kSlice + min(done + i + kAhead, n - 1) * kStride);
+            }
+        done = n;
     }
-    for (; k0 < in.d; k0 += 4 * kSlice) slice(k0, std::false_type{});
+    for (int k0 = wave * kSlice + done * kStride; k0 < in.d; k0 += kStride) {
+        Slice x;
+        load_edge(x, k0);
+        multiply(x);
+    }
     __shared__ f32x4 sums[4][kTiles][64];
 #pragma unroll
     for (int j = 0; j < kTiles; ++j) sums[wave][j][lane] = acc[j];
@@ -479,39 +543,35 @@ __global__ __launch_bounds__(256) void few_rows(LinearRows in, const T* w, int64
         const f32x4 total = (sums[0][j][lane] + sums[1][j][lane]) + (sums[2][j][lane] + sums[3][j][lane]);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const int column = group * 4 + t, v = n0 + (kLayout == PCM_WEIGHT_OUT_IN ? j * 16 + column : column * kE + j);
-            z[i][t] = v < in.V ? total[t] : -__builtin_huge_valf();
+            const int column = group * 4 + t, v = kLayout == PCM_WEIGHT_OUT_IN ? n0 + j * 16 + column : first_column(column) + j;
+            const bool own = v < in.V && (kLayout == PCM_WEIGHT_OUT_IN || v >= n0 + column * kE);
+            z[i][t] = own ? total[t] : -__builtin_huge_valf();
             m = fmaxf(m, z[i][t]);
-            if (v == token) token_z[at] = z[i][t];
+            if (own && v == token) token_z[at] = z[i][t];
         }
     }
     m = fmaxf(m, __shfl_xor(m, 16, 64));
     m = fmaxf(m, __shfl_xor(m, 32, 64));
-    float s = 0.f, t = 0.f;
-    if (n0 < in.V && m > -__builtin_huge_valf()) {
-#pragma unroll
-        for (int i = 0; i < kMine; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) add_exponent((z[i][e] - m) * c, s, t);
+    RowSums r{m, 0.f, 0.f};
+    if (m > -__builtin_huge_valf()) {
+        r = sums_of<kMine>(m, c, [&](int i, int e) __attribute__((always_inline)) { return z[i][e]; });
     } else {
 #pragma unroll
         for (int i = 0; i < kMine; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s += z[i][e] == -__builtin_huge_valf() ? 0.f : z[i][e];       // NaN stays NaN
+            for (int e = 0; e < 4; ++e) r.s += z[i][e] == -__builtin_huge_valf() ? 0.f : z[i][e];       // nothing, or NaN
     }
-    s += __shfl_xor(s, 16, 64);
-    s += __shfl_xor(s, 32, 64);
-    t += __shfl_xor(t, 16, 64);
-    t += __shfl_xor(t, 32, 64);
+    r.s += __shfl_xor(r.s, 16, 64);
+    r.s += __shfl_xor(r.s, 32, 64);
+    r.t += __shfl_xor(r.t, 16, 64);
+    r.t += __shfl_xor(r.t, 32, 64);
     __shared__ RowSums part[4][16];
-    if (group == 0) part[wave][at] = RowSums{m, s, t};
+    if (group == 0) part[wave][at] = r;
     __syncthreads();
     if (threadIdx.x >= 16 || !has_row) return;
     RowSums a = part[0][at];
     for (int q = 1; q < 4; ++q) merge(a, part[q][at], c);
-    out.most[blockIdx.x * out.ld + at] = a.m;
-    out.sum[blockIdx.x * out.ld + at] = a.s;
-    out.moment[blockIdx.x * out.ld + at] = a.t;
+    out.of[blockIdx.x * out.ld + at] = f32x4{a.m, a.s, a.t, 0.f};
 }
 
 int few_columns(int dtype, int layout) { return layout == PCM_WEIGHT_OUT_IN || dtype == PCM_F32 ? 64 : 128; }
@@ -528,9 +588,7 @@ PartSums carve_parts(Carver& c, int64_t ld, int parts) {
     PartSums p{};
     p.ld = ld;
     p.parts = parts;
-    p.most = c.take<float>((size_t)(ld * parts));
-    p.sum = c.take<float>((size_t)(ld * parts));
-    p.moment = c.take<float>((size_t)(ld * parts));
+    p.of = c.take<f32x4>((size_t)(ld * parts));
     return p;
 }
 struct ForwardPlan {
@@ -617,14 +675,20 @@ SlotGradients carve_gradients(Carver& c, const Slots& slots, int dtype) {
 }
 void gather_slots(const LinearRows& in, const Slots& slots, const SlotGradients* grads, int dtype, hipStream_t s) {
     const unsigned lists = (unsigned)ceil_div(in.rows, kCountRows), blocks = (unsigned)ceil_div(in.rows + kTileM, kGatherRows);
-    if (slots.counts != nullptr) linear_counts<<<lists, 256, 0, s>>>(in, slots.counts);
-    linear_slots<<<lists, 256, 0, s>>>(in, slots);
     const SlotGradients g = grads != nullptr ? *grads : SlotGradients{};
+    // (the exponent that fp32 gradients gather begins with the list)
+    const bool own_list = slots.counts == nullptr && !(dtype == PCM_F32 && grads != nullptr);
+    if (!own_list) {
+        if (slots.counts != nullptr) linear_counts<<<lists, 256, 0, s>>>(in, slots.counts);
+        linear_slots<<<lists, 256, 0, s>>>(in, slots);
+    }
     if (dtype == PCM_F32) {
-        linear_gather<float><<<blocks, 256, 0, s>>>(in, slots, g);
+        if (own_list) linear_gather<float, true><<<blocks, 256, 0, s>>>(in, slots, g);
+        else linear_gather<float, false><<<blocks, 256, 0, s>>>(in, slots, g);
         if (grads != nullptr) linear_weigh<<<blocks, 256, 0, s>>>(in, slots, g);
     } else {
-        linear_gather<half_bits><<<blocks, 256, 0, s>>>(in, slots, g);
+        if (own_list) linear_gather<half_bits, true><<<blocks, 256, 0, s>>>(in, slots, g);
+        else linear_gather<half_bits, false><<<blocks, 256, 0, s>>>(in, slots, g);
     }
 }
 
@@ -655,7 +719,7 @@ WeightCopy carve_weight(Carver& c, const WeightSource& src, int columns) {
 void prepare_weight(const WeightSource& src, const WeightCopy& copy, hipStream_t s) {
     if (src.dtype != PCM_F32) return;
     const int rows = src.layout == PCM_WEIGHT_OUT_IN ? src.V : src.d, cols = src.layout == PCM_WEIGHT_OUT_IN ? src.d : src.V;
-    const int parts = std::min(rows, kAbsmaxParts);
+    const int parts = (int)std::min<int64_t>((int64_t)rows * ceil_div(cols, 4096), kAbsmaxParts);
     linear_absmax<<<(unsigned)parts, 256, 0, s>>>(static_cast<const float*>(src.w), src.ld, rows, cols, copy.absmax);
     linear_unit<<<1, kAbsmaxParts, 0, s>>>(copy.absmax, parts, copy.unit);
 }
@@ -726,7 +790,7 @@ PCM_API int pcm_linear_logprobs(const void* hidden, int64_t hidden_ld, const voi
     prepare_weight(src, f.copy, s);
     if (dtype == PCM_F32) forward_products<true>(f, src, (int)rows, c, s);
     else forward_products<false>(f, src, (int)rows, c, s);
-    linear_join<16><<<(unsigned)ceil_div((int)rows, 16), 256, 0, s>>>(in, f.slots.slot_of, f.parts, f.token_z, inv_t, out);
+    linear_join<4><<<(unsigned)ceil_div((int)rows, 4), 256, 0, s>>>(in, f.slots.slot_of, f.parts, f.token_z, inv_t, out);
     return launch_status();
 }
 
