@@ -24,31 +24,52 @@ struct LogitGradient {
     const float *h_unit, *w_unit;        // fp32, or null: powers of two
     float c;                             // log2 e / temperature
     int first, columns;                  // of the vocabulary in this piece
-    // dz of rows 16 i + (lane & 15) of a wavefront's block: store(local row, tile column j, four neighbours).  Rows behind the last slot
-    // are zeros times W with a gradient of zero.
+    // What is to be known of rows 16 i + (lane & 15) of a wavefront's block, asked for all at once.
+    struct Row {
+        float scale, lse2, along, rest, g;
+        int at;                          // of the token in this block
+    };
+    template <int kW>
+    __device__ __forceinline__ void load(Row (&row)[kW], const TileCoord<kW>& tc) const {
+        const float w_scale = w_unit != nullptr ? *w_unit : 1.f;
+        SlotGradient G[kW];
+        float unit[kW];
+#pragma unroll
+        for (int i = 0; i < kW; ++i) {
+            const int slot = tc.row0() + i * 16 + (tc.lane & 15);
+            G[i] = of[slot];
+            row[i].at = token[slot] - first - tc.col0();
+            unit[i] = h_unit != nullptr ? h_unit[slot] : 1.f;
+        }
+#pragma unroll
+        for (int i = 0; i < kW; ++i) {
+            row[i].scale = c * (unit[i] * w_scale);
+            row[i].lse2 = G[i].lse2;
+            row[i].along = G[i].h * kLn2;
+            row[i].rest = __builtin_fmaf(G[i].h, G[i].entropy, G[i].g);
+            row[i].g = G[i].g;
+        }
+    }
+    // dz of a row: store(tile column j, four neighbours).  Rows behind the last slot are zeros times W with a gradient of zero.
     template <bool kWhole, int kW, class F>
-    __device__ __forceinline__ void row(const TileCoord<kW>& tc, const Accumulators<kW>& acc, int i, int col0, F store) const {
+    __device__ __forceinline__ void row(const Row& q, const TileCoord<kW>& tc, const Accumulators<kW>& acc, int i, F store) const {
         constexpr int RW = kWaveRows<kW>;
-        const int quarter = tc.lane >> 4, slot = tc.row0() + i * 16 + (tc.lane & 15);
-        const SlotGradient G = of[slot];
-        const int at = token[slot] - first - col0;         // of the token in this block
-        const float scale = h_unit != nullptr ? c * (h_unit[slot] * *w_unit) : c;
-        const float along = G.h * kLn2, rest = __builtin_fmaf(G.h, G.entropy, G.g);
+        const int quarter = tc.lane >> 4;
         f32x4 r[kW];
 #pragma unroll
         for (int j = 0; j < kW; ++j)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const float a = __builtin_fmaf(acc[i][j][t], scale, -G.lse2);
+                const float a = __builtin_fmaf(accumulator(acc[i][j][t]), q.scale, -q.lse2);
                 // (where p is 0 log p may be -inf, which is not to become a NaN)
-                const float x = -__builtin_amdgcn_exp2f(a) * __builtin_fmaf(along, fmaxf(a, -150.f), rest);
-                r[j][t] = kWhole || col0 + j * 16 + quarter * 4 + t < columns ? x : 0.f;
+                const float x = -__builtin_amdgcn_exp2f(a) * __builtin_fmaf(q.along, fmaxf(a, -150.f), q.rest);
+                r[j][t] = kWhole || tc.col0() + j * 16 + quarter * 4 + t < columns ? x : 0.f;
             }
-        if (__any(at >= 0 && at < RW)) {
+        if (__any(q.at >= 0 && q.at < RW)) {
 #pragma unroll
             for (int j = 0; j < kW; ++j)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) r[j][t] += at == j * 16 + quarter * 4 + t ? G.g : 0.f;
+                for (int t = 0; t < 4; ++t) r[j][t] += q.at == j * 16 + quarter * 4 + t ? q.g : 0.f;
         }
 #pragma unroll
         for (int j = 0; j < kW; ++j) store(j, r[j]);
@@ -64,11 +85,13 @@ struct EpiLogitGradient {
     template <bool kWhole, int kW>
     __device__ __forceinline__ void rows(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* st) const {
         constexpr int RW = kWaveRows<kW>, kStride = RW * 2 + 16;
+        LogitGradient::Row row[kW];
+        gradient.load(row, tc);
         const int col0 = tc.col0();
 #pragma unroll
         for (int i = 0; i < kW; ++i) {
             char* const to = st + (i * 16 + (tc.lane & 15)) * kStride + 4 * (tc.lane >> 4) * 2;
-            gradient.row<kWhole>(tc, acc, i, col0, [&](int j, const f32x4& r) __attribute__((always_inline)) {
+            gradient.row<kWhole>(row[i], tc, acc, i, [&](int j, const f32x4& r) __attribute__((always_inline)) {
                 *reinterpret_cast<bf16x4*>(to + j * 32) = to_bf16x4(r[0], r[1], r[2], r[3]);
             });
         }
@@ -90,13 +113,15 @@ struct EpiLogitGradientPairs {
     template <bool kWhole, int kW>
     __device__ __forceinline__ void rows(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* st) const {
         constexpr int RW = kWaveRows<kW>, kStride = RW * 4 + 16;
+        LogitGradient::Row row[kW];
+        gradient.load(row, tc);
         const int col0 = tc.col0();
 #pragma unroll
         for (int half = 0; half < RW / 64; ++half) {       // 64 rows per pass
 #pragma unroll
             for (int ii = 0; ii < 4; ++ii) {
                 char* const to = st + (ii * 16 + (tc.lane & 15)) * kStride + 4 * (tc.lane >> 4) * 2;
-                gradient.row<kWhole>(tc, acc, half * 4 + ii, col0, [&](int j, const f32x4& r) __attribute__((always_inline)) {
+                gradient.row<kWhole>(row[half * 4 + ii], tc, acc, half * 4 + ii, [&](int j, const f32x4& r) __attribute__((always_inline)) {
                     f16x4 h, l;
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
@@ -131,26 +156,49 @@ __device__ inline float weight_gradient_unit(const int32_t* most) { return most 
 
 // acc into rows and columns of a matrix that end anywhere, at any alignment of its type, through LDS so that whole lines leave.
 template <class T>
-struct EpiStoreAnywhere {
-    T* C;
+struct EpiStoreAnywhere;
+template <>
+struct EpiStoreAnywhere<uint16_t> {                        // bf16
+    uint16_t* C;
+    int64_t ldc;
+    int rows, cols;
+    template <int kW>
+    __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* lds) const {
+        constexpr int RW = kWaveRows<kW>, kStride = RW * 2 + 16;
+        char* st = wave_stage(tc, lds);
+        const int row0 = tc.row0(), col0 = tc.col0(), n_rows = min(RW, rows - row0), n_cols = min(RW, cols - col0);
+        if (n_rows <= 0 || n_cols <= 0) return;
+#pragma unroll
+        for (int i = 0; i < kW; ++i) {
+            stage_tile_row<kW>(st, kStride, tc.lane, i * 16 + (tc.lane & 15), [&](int j) { return acc[i][j]; });
+            __builtin_amdgcn_sched_barrier(0);             // one tile row's conversions at a time
+        }
+        __builtin_amdgcn_wave_barrier();
+        uint16_t* const to = C + (int64_t)row0 * ldc + col0;
+        if (n_cols == RW && ((reinterpret_cast<uintptr_t>(C) | (uintptr_t)(ldc * 2)) & 15u) == 0) {
+            copy_rows_out<RW, RW * 2>(st, kStride, reinterpret_cast<char*>(to), ldc * 2, n_rows, tc.lane);
+            return;
+        }
+        for (int r = 0; r < n_rows; ++r)
+            for (int c = tc.lane; c < n_cols; c += 64) to[r * ldc + c] = *reinterpret_cast<const uint16_t*>(st + r * kStride + c * 2);
+    }
+};
+template <>
+struct EpiStoreAnywhere<float> {
+    float* C;
     int64_t ldc;
     int rows, cols;
     const int32_t* most;                 // or null
-    int accumulate;                      // T = float
+    int accumulate;                      // added to what is there
     template <int kW>
     __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* lds) const {
+        typedef f32x4 __attribute__((aligned(4))) f32x4_any;
         constexpr int RW = kWaveRows<kW>, kStride = RW * 4 + 16;
+        constexpr int kLanes = RW / 4;                     // of a row, four columns each
         char* st = wave_stage(tc, lds);
-        const int col0 = tc.col0(), n_cols = min(RW, cols - col0);
+        const int col0 = tc.col0(), n_cols = min(RW, cols - col0), c = tc.lane % kLanes * 4;
         const float unit = weight_gradient_unit(most);
         if (n_cols <= 0) return;
-        if constexpr (sizeof(T) == 2) {
-            if (n_cols == RW && ((reinterpret_cast<uintptr_t>(C) | (uintptr_t)(ldc * 2)) & 15u) == 0) {      // 16 bytes a lane
-                const EpiStoreBf16 store{reinterpret_cast<bf16*>(C), ldc, rows};
-                store(tc, acc, lds);
-                return;
-            }
-        }
 #pragma unroll
         for (int i = 0; i < RW / 32; ++i) {                // 32 rows per pass
 #pragma unroll
@@ -160,29 +208,16 @@ struct EpiStoreAnywhere {
                     *reinterpret_cast<f32x4*>(st + (ii * 16 + (tc.lane & 15)) * kStride + (j * 16 + 4 * (tc.lane >> 4)) * 4) = acc[2 * i + ii][j];
             __builtin_amdgcn_wave_barrier();
             const int row0 = tc.row0() + i * 32, n_rows = min(32, rows - row0);
-            constexpr int kPer = 4, kLanes = RW / kPer;     // columns of a lane; lanes of a row
-            const int c = tc.lane % kLanes * kPer;
             for (int r = tc.lane / kLanes; r < n_rows; r += 64 / kLanes) {
                 f32x4 x = *reinterpret_cast<const f32x4*>(st + r * kStride + c * 4);
                 x *= unit;
-                T* const to = C + (int64_t)(row0 + r) * ldc + col0 + c;
-                if constexpr (sizeof(T) == 4) {
-                    typedef f32x4 __attribute__((aligned(4))) f32x4_any;
-                    if (c + kPer <= n_cols) {
-                        if (accumulate) x += *reinterpret_cast<const f32x4_any*>(to);
-                        *reinterpret_cast<f32x4_any*>(to) = x;
-                    } else {
-                        for (int e = 0; e < kPer; ++e)
-                            if (c + e < n_cols) to[e] = accumulate ? to[e] + x[e] : x[e];
-                    }
+                float* const to = C + (int64_t)(row0 + r) * ldc + col0 + c;
+                if (c + 4 <= n_cols) {
+                    if (accumulate) x += *reinterpret_cast<const f32x4_any*>(to);
+                    *reinterpret_cast<f32x4_any*>(to) = x;
                 } else {
-                    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-                    typedef u32x2 __attribute__((aligned(2))) u32x2_any;
-                    const bf16x4 y = to_bf16x4(x[0], x[1], x[2], x[3]);
-                    if (c + kPer <= n_cols) *reinterpret_cast<u32x2_any*>(to) = __builtin_bit_cast(u32x2, y);
-                    else
-                        for (int e = 0; e < kPer; ++e)
-                            if (c + e < n_cols) to[e] = bf16_bits(x[e]);
+                    for (int e = 0; e < 4; ++e)
+                        if (c + e < n_cols) to[e] = accumulate ? to[e] + x[e] : x[e];
                 }
             }
             __builtin_amdgcn_wave_barrier();
@@ -363,7 +398,7 @@ void weight_gradient(const BackwardPlan& b, const WeightSource& src, int first, 
         const EpiStoreAnywhere<float> epi{static_cast<float*>(out.dw) + at, out.dw_ld, rows, cols, most, out.accumulate};
         launch_slot_product<kThirds, kKByRows, kKByRows>(p, b.dw.kW, epi, s);
     } else if constexpr (!kThirds) {
-        const EpiStoreAnywhere<uint16_t> epi{static_cast<uint16_t*>(out.dw) + at, out.dw_ld, rows, cols, nullptr, 0};
+        const EpiStoreAnywhere<uint16_t> epi{static_cast<uint16_t*>(out.dw) + at, out.dw_ld, rows, cols};
         launch_slot_product<kThirds, kKByRows, kKByRows>(p, b.dw.kW, epi, s);
     }
 }

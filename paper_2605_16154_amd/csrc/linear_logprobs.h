@@ -87,6 +87,14 @@ WeightOperand weight_piece(const WeightSource& src, const WeightCopy& copy, int 
 int check_linear(const void* hidden, int64_t hidden_ld, const void* weight, int64_t weight_ld, int layout, int dtype, const void* tokens,
                  int token_type, int64_t rows, int d, int V, float temperature);
 
+// An accumulator's value, moved where it is asked for: left to itself the compiler moves all 256 of a lane ahead of the first branch of an
+// epilogue, and from there to scratch memory.
+__device__ __forceinline__ float accumulator(float x) {
+    float r;
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(r) : "a"(x));
+    return r;
+}
+
 // A product of all slots (M, or the reduction index) with whatever B is.
 template <bool kThirds>
 inline BoundedProblem<kThirds> slot_product(const Slots& slots, int rows_role) {

@@ -301,41 +301,43 @@ struct PartSums {
     int64_t ld;
     int parts;
 };
-__device__ inline void merge(RowSums& a, const RowSums& b, float c) {
-    if (b.s == 0.f) return;
-    if (a.s == 0.f) { a = b; return; }
-    const float m = fmaxf(a.m, b.m), da = fmaxf((a.m - m) * c, -1e30f), db = fmaxf((b.m - m) * c, -1e30f);
-    const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
-    a.t = ea * (a.t + a.s * da) + eb * (b.t + b.s * db);
+__device__ __forceinline__ void merge(RowSums& a, const RowSums& b, float c) {
+    const float m = fmaxf(a.s == 0.f ? b.m : a.m, b.s == 0.f ? a.m : b.m);
+    const float da = fmaxf((a.m - m) * c, -1e30f), db = fmaxf((b.m - m) * c, -1e30f);
+    const float ea = a.s == 0.f ? 0.f : __builtin_amdgcn_exp2f(da), eb = b.s == 0.f ? 0.f : __builtin_amdgcn_exp2f(db);
+    a.t = ea * __builtin_fmaf(a.s, da, a.t) + eb * __builtin_fmaf(b.s, db, b.t);
     a.s = a.s * ea + b.s * eb;
     a.m = m;
 }
-// The sums of `kN` x 4 logits relative to m; -150 stands for what is as good as nothing (a is -inf where z is, or is that far below m).
+// The sums of kN x 4 logits relative to m; -150 stands for what is as good as nothing (a is -inf where z is, or is that far below m).
 template <int kN, class F>
 __device__ __forceinline__ RowSums sums_of(float m, float c, F z) {
     RowSums r{m, 0.f, 0.f};
-    auto add = [&](auto floor) __attribute__((always_inline)) {
-        r.s = r.t = 0.f;
 #pragma unroll
-        for (int j = 0; j < kN; ++j) {
-            float s = 0.f, t = 0.f;                        // four terms before they are added to the others
+    for (int j = 0; j < kN; ++j) {
+        float s = 0.f, t = 0.f;                            // four terms before they are added to the others
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float a = (z(j, e) - m) * c, x = __builtin_amdgcn_exp2f(a);
-                s += x;
-                t = __builtin_fmaf(x, decltype(floor)::value ? fmaxf(a, -150.f) : a, t);
-            }
-            r.s += s;
-            r.t += t;
+        for (int e = 0; e < 4; ++e) {
+            const float a = (z(j, e) - m) * c, x = __builtin_amdgcn_exp2f(a);
+            s += x;
+            t = __builtin_fmaf(x, fmaxf(a, -150.f), t);
         }
-    };
-    add(std::false_type{});
-    if (__any(!(r.t > -__builtin_huge_valf()))) add(std::true_type{});
+        r.s += s;
+        r.t += t;
+    }
     return r;
 }
 
-// The logits of a tile, a wavefront's block of which is a part of its rows.  Vector instructions that no product runs beside: 10 issue
-// slots per logit (the accumulator's move, the maximum, difference, product, exponential, sum and moment).
+// The largest of three, NaN aside (fmaxf would first quieten each operand, an instruction more).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// The logits of a tile, a wavefront's block of which is a part of its rows.  Vector instructions that no product runs beside: 11.5 issue
+// slots per logit (the accumulator moved twice, half a maximum, difference, product, exponential, sum, moment and its guard).  A lane has a quarter of 16 neighbours' rows
+// to itself; the quarters meet at the end, all rows together, so that the exchanges wait for one another only there.
 struct EpiRowStats {
     PartSums out;
     float* token_z;                      // [padded]
@@ -364,33 +366,40 @@ struct EpiRowStats {
             at[i] = token[row0 + i * 16] - first - col0;
             unit[i] = h_unit != nullptr ? h_unit[row0 + i * 16] * w_scale : 1.f;
         }
+        RowSums r[kW];
 #pragma unroll
         for (int i = 0; i < kW; ++i) {
             auto z = [&](int j, int t) __attribute__((always_inline)) {
-                return kWhole || col0 + j * 16 + quarter * 4 + t < columns ? acc[i][j][t] : -__builtin_huge_valf();
+                const float x = accumulator(acc[i][j][t]);
+                return kWhole || col0 + j * 16 + quarter * 4 + t < columns ? x : -__builtin_huge_valf();
             };
             float m = -__builtin_huge_valf();
 #pragma unroll
-            for (int j = 0; j < kW; ++j)
-#pragma unroll
-                for (int t = 0; t < 4; ++t) m = fmaxf(m, z(j, t));
+            for (int j = 0; j < kW; ++j) {
+                m = max3(z(j, 0), z(j, 1), m);
+                m = max3(z(j, 2), z(j, 3), m);
+            }
+            r[i] = sums_of<kW>(m, c * unit[i], z);
+            if (!kWhole && m == -__builtin_huge_valf()) r[i].s = r[i].t = 0.f;       // no column of this lane's
+            r[i].m = m * unit[i];
             if (__any(at[i] >= 0 && at[i] < RW)) {
+                float x = 0.f;
 #pragma unroll
                 for (int j = 0; j < kW; ++j)
 #pragma unroll
-                    for (int t = 0; t < 4; ++t)
-                        if (at[i] == j * 16 + quarter * 4 + t) token_z[row0 + i * 16] = acc[i][j][t] * unit[i];
+                    for (int t = 0; t < 4; ++t) x = at[i] == j * 16 + quarter * 4 + t ? z(j, t) : x;
+                if (at[i] >= 0 && at[i] < RW && at[i] % 16 / 4 == quarter) token_z[row0 + i * 16] = x * unit[i];
             }
-            m = fmaxf(m, __shfl_xor(m, 16, 64));
-            m = fmaxf(m, __shfl_xor(m, 32, 64));
-            RowSums r = sums_of<kW>(m, c * unit[i], z);
-            r.s += __shfl_xor(r.s, 16, 64);
-            r.s += __shfl_xor(r.s, 32, 64);
-            r.t += __shfl_xor(r.t, 16, 64);
-            r.t += __shfl_xor(r.t, 32, 64);
-            if (quarter == 0) out.of[(first_part + col0 / RW) * out.ld + row0 + i * 16] = f32x4{m * unit[i], r.s, r.t, 0.f};
             __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int off = 16; off <= 32; off *= 2)
+#pragma unroll
+            for (int i = 0; i < kW; ++i)
+                merge(r[i], RowSums{__shfl_xor(r[i].m, off, 64), __shfl_xor(r[i].s, off, 64), __shfl_xor(r[i].t, off, 64)}, c);
+#pragma unroll
+        for (int i = 0; i < kW; ++i)
+            if (quarter == i % 4) out.of[(first_part + col0 / RW) * out.ld + row0 + i * 16] = f32x4{r[i].m, r[i].s, r[i].t, 0.f};
     }
 };
 
