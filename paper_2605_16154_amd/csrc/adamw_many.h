@@ -6,7 +6,7 @@
 namespace pcm {
 
 constexpr int kManyBlock = PCM_ADAMW_BLOCK;      // elements that share an exponent
-constexpr int kManyChunk = 4096;                 // elements of a chunk: what a workgroup takes at a time
+constexpr int kManyChunk = 2048;                 // elements of a chunk: what a workgroup takes at a time, eight a lane
 
 // A piece of one tensor: the plan is a list of these.
 struct AdamwChunk {

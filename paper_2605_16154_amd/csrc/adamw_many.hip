@@ -3,7 +3,7 @@
 //   pass 1  many_sumsq    fp64 partial sums of g^2 (only where the norm is asked for)
 //   pass 2  many_update   norm and clip factor from the partial sums; m, v, weights in place, bf16 copy
 //
-// The tensors are one list of chunks of up to 4096 elements in device memory, each with the addresses it needs, so hundreds of
+// The tensors are one list of chunks of up to 2048 elements in device memory, each with the addresses it needs, so hundreds of
 // tensors of any size are two launches, and a workgroup finds its work with one dependent load.
 //
 // States in 8 bits.  128 elements (a block) share an exponent E, that of the largest value; a code holds 3 bits behind the point and an
@@ -22,82 +22,142 @@ namespace pcm {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPass = kThreads * 8;              // elements: eight neighbours a lane
+static_assert(kManyChunk == kThreads * 8, "eight elements a lane");
 constexpr int kSumsqGrid = 1024, kUpdateGrid = 2048;
 constexpr int kSignField = 15, kSquareField = 31;
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-// tensors lie where the caller put them: 16 bytes at a time at whatever alignment their type has
-typedef f32x4 __attribute__((aligned(4))) f32x4_any;
-typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+// Tensors lie where the caller put them: 16 bytes at a time at whatever alignment their type has.  Their addresses come out of memory, so it has
+// to be said that they are global ones.
+#define PCM_GLOBAL __attribute__((address_space(1)))
+typedef PCM_GLOBAL f32x4 __attribute__((aligned(4))) four_floats;
+typedef PCM_GLOBAL u32x4 __attribute__((aligned(2))) eight_halves;
+typedef PCM_GLOBAL u32x2 __attribute__((aligned(2))) four_halves;
+typedef PCM_GLOBAL u32x2 eight_codes;
+typedef PCM_GLOBAL float global_float;
+typedef PCM_GLOBAL uint16_t global_half;
 
 // (a function per type: a template parameter would lose the alignment)
-#define PCM_STREAMED(type, name)                                                                                                  \
-    template <bool kStream>                                                                                                       \
-    __device__ inline auto load_##name(const type* p) { return kStream ? __builtin_nontemporal_load(p) : *p; }                    \
-    template <bool kStream>                                                                                                       \
-    __device__ inline void store_##name(type* p, type x) {                                                                        \
-        if (kStream) __builtin_nontemporal_store(x, p);                                                                           \
-        else *p = x;                                                                                                              \
+#define PCM_STREAMED(type, value, name)                                                                             \
+    template <bool kStream>                                                                                         \
+    __device__ __forceinline__ value load_##name(const type* p) { return kStream ? __builtin_nontemporal_load(p) : *p; } \
+    template <bool kStream>                                                                                         \
+    __device__ __forceinline__ void store_##name(type* p, value x) {                                                \
+        if (kStream) __builtin_nontemporal_store(x, p);                                                             \
+        else *p = x;                                                                                                \
     }
-PCM_STREAMED(f32x4_any, four)
-PCM_STREAMED(u32x4_any, eight)
-PCM_STREAMED(u32x2, codes)
+PCM_STREAMED(four_floats, f32x4, floats)
+PCM_STREAMED(eight_halves, u32x4, halves)
+PCM_STREAMED(four_halves, u32x2, few_halves)
+PCM_STREAMED(eight_codes, u32x2, codes)
 #undef PCM_STREAMED
 
-// Eight fp32 values of which the first `n` exist; the others are 0.
-template <bool kStream>
-__device__ inline void load_floats(float (&x)[8], const float* p, int n) {
-    if (n >= 8) {
-        const f32x4 a = load_four<kStream>(reinterpret_cast<const f32x4_any*>(p)), b = load_four<kStream>(reinterpret_cast<const f32x4_any*>(p + 4));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[e + 4] = b[e]; }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = e < n ? p[e] : 0.f;
-    }
-}
-template <bool kStream>
-__device__ inline void store_floats(float* p, const float (&x)[8], int n) {
-    if (n >= 8) {
-        store_four<kStream>(reinterpret_cast<f32x4_any*>(p), f32x4_any{x[0], x[1], x[2], x[3]});
-        store_four<kStream>(reinterpret_cast<f32x4_any*>(p + 4), f32x4_any{x[4], x[5], x[6], x[7]});
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) p[e] = x[e];
-    }
-}
 __device__ inline uint32_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
-template <bool kStream>
-__device__ inline void load_gradient(float (&g)[8], const AdamwChunk& k, int i) {
-    const int n = k.count - i;
-    if (!k.grad_bf16) return load_floats<kStream>(g, static_cast<const float*>(k.grad) + i, n);
-    const uint16_t* p = static_cast<const uint16_t*>(k.grad) + i;
-    if (n >= 8) {
-        const u32x4 a = load_eight<kStream>(reinterpret_cast<const u32x4_any*>(p));
+__device__ inline float low_half(uint32_t x) { return __builtin_bit_cast(float, x << 16); }
+__device__ inline float high_half(uint32_t x) { return __builtin_bit_cast(float, x & 0xffff0000u); }
+
+// Where a lane's eight elements of a chunk are: two fours.  States in 8 bits keep them together, 16 lanes to a block; else fours of neighbouring lanes are
+// neighbours, which every access takes as whole lines.
+template <bool kTogether>
+__device__ inline int four_at(int h) { return kTogether ? threadIdx.x * 8 + h * 4 : h * (kManyChunk / 2) + threadIdx.x * 4; }
+
+// A lane's gradients of a chunk as they come: fp32, or bf16 in the first half.
+template <bool kTogether, bool kStream>
+struct Gradients {
+    f32x4 x[2];
+    __device__ __forceinline__ void load(const AdamwChunk& k) {
+        if (k.grad_bf16) {
+            const global_half* p = (const global_half*)k.grad;
+            u32x4 both = {0, 0, 0, 0};
+            if (k.count == kManyChunk) {
+                if (kTogether) both = load_halves<kStream>((const eight_halves*)(p + four_at<true>(0)));
+                else {
+                    const u32x2 a = load_few_halves<kStream>((const four_halves*)(p + four_at<false>(0)));
+                    const u32x2 b = load_few_halves<kStream>((const four_halves*)(p + four_at<false>(1)));
+                    both = u32x4{a[0], a[1], b[0], b[1]};
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int i = four_at<kTogether>(e / 4) + e % 4;
+                    if (i < k.count) both[e / 2] |= (uint32_t)p[i] << (e % 2 * 16);
+                }
+            }
+            x[0] = __builtin_bit_cast(f32x4, both);
+        } else {
+            const global_float* p = (const global_float*)k.grad;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int i = four_at<kTogether>(h);
+                x[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (k.count == kManyChunk) x[h] = load_floats<kStream>((const four_floats*)(p + i));
+                else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (i + e < k.count) x[h][e] = p[i + e];
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void get(float (&g)[8], const AdamwChunk& k) const {
+        const u32x4 both = __builtin_bit_cast(u32x4, x[0]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            g[2 * e] = __builtin_bit_cast(float, a[e] << 16);
-            g[2 * e + 1] = __builtin_bit_cast(float, a[e] & 0xffff0000u);
+            g[2 * e] = k.grad_bf16 ? low_half(both[e]) : x[e / 2][e % 2 * 2];
+            g[2 * e + 1] = k.grad_bf16 ? high_half(both[e]) : x[e / 2][e % 2 * 2 + 1];
+        }
+    }
+};
+// Eight fp32 values at two fours of a matrix; those from `count` on are left alone, and 0.
+template <bool kTogether, bool kStream>
+__device__ __forceinline__ void load_eight(f32x4 (&x)[2], const float* from, int count) {
+    const global_float* p = (const global_float*)from;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = four_at<kTogether>(h);
+        x[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (count == kManyChunk) x[h] = load_floats<kStream>((const four_floats*)(p + i));
+        else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e < count) x[h][e] = p[i + e];
+        }
+    }
+}
+template <bool kTogether, bool kStream>
+__device__ __forceinline__ void store_eight(float* to, const float (&x)[8], int count) {
+    global_float* p = (global_float*)to;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = four_at<kTogether>(h);
+        if (count == kManyChunk) store_floats<kStream>((four_floats*)(p + i), f32x4{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]});
+        else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e < count) p[i + e] = x[4 * h + e];
+        }
+    }
+}
+template <bool kTogether>
+__device__ __forceinline__ void store_bf16(uint16_t* to, const float (&x)[8], int count) {
+    global_half* p = (global_half*)to;
+    u32x4 a;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) a[e] = bf16_bits(x[2 * e]) | bf16_bits(x[2 * e + 1]) << 16;
+    if (count == kManyChunk) {
+        if (kTogether) store_halves<false>((eight_halves*)(p + four_at<true>(0)), a);
+        else {
+            store_few_halves<false>((four_halves*)(p + four_at<false>(0)), u32x2{a[0], a[1]});
+            store_few_halves<false>((four_halves*)(p + four_at<false>(1)), u32x2{a[2], a[3]});
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = e < n ? __builtin_bit_cast(float, (uint32_t)p[e] << 16) : 0.f;
-    }
-}
-__device__ inline void store_bf16(uint16_t* p, const float (&x)[8], int n) {
-    if (n >= 8) {
-        u32x4_any a;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) a[e] = bf16_bits(x[2 * e]) | bf16_bits(x[2 * e + 1]) << 16;
-        store_eight<false>(reinterpret_cast<u32x4_any*>(p), a);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) p[e] = (uint16_t)bf16_bits(x[e]);
+        for (int e = 0; e < 8; ++e) {
+            const int i = four_at<kTogether>(e / 4) + e % 4;
+            if (i < count) p[i] = (uint16_t)(a[e / 2] >> (e % 2 * 16));
+        }
     }
 }
 
@@ -113,17 +173,31 @@ __device__ inline double block_sum(double x) {
 
 __global__ __launch_bounds__(kThreads) void many_sumsq(const AdamwChunk* chunks, int64_t n, double* partial) {
     double acc[8] = {};
-    for (int64_t at = blockIdx.x; at < n; at += gridDim.x) {
-        const AdamwChunk k = chunks[at];
+    auto add = [&](const AdamwChunk& k, const Gradients<false, false>& x) __attribute__((always_inline)) {
+        float g[8];
+        x.get(g, k);
 #pragma unroll
-        for (int r = 0; r < kManyChunk / kPass; ++r) {
-            const int i = r * kPass + threadIdx.x * 8;
-            if (i >= k.count) continue;
-            float g[8];
-            load_gradient<false>(g, k, i);
+        for (int e = 0; e < 8; ++e) acc[e] = __builtin_fma((double)g[e], (double)g[e], acc[e]);
+    };
+    // four chunks under way
+    constexpr int kAhead = 4;
+    int64_t at = blockIdx.x;
+    for (; at + (int64_t)(kAhead - 1) * gridDim.x < n; at += (int64_t)kAhead * gridDim.x) {
+        AdamwChunk k[kAhead];
+        Gradients<false, false> x[kAhead];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] = __builtin_fma((double)g[e], (double)g[e], acc[e]);
+        for (int q = 0; q < kAhead; ++q) {
+            k[q] = chunks[at + (int64_t)q * gridDim.x];
+            x[q].load(k[q]);
         }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) add(k[q], x[q]);
+    }
+    for (; at < n; at += gridDim.x) {
+        const AdamwChunk k = chunks[at];
+        Gradients<false, false> x;
+        x.load(k);
+        add(k, x);
     }
     const double total = block_sum(((acc[0] + acc[1]) + (acc[2] + acc[3])) + ((acc[4] + acc[5]) + (acc[6] + acc[7])));
     if (threadIdx.x == 0) partial[blockIdx.x] = total;
@@ -169,93 +243,132 @@ __device__ inline float clip_factor(const ManyStep& s) {
     return (float)fmin(1.0, s.max_norm / (norm + 1e-6));
 }
 
+// What a lane takes up of a chunk.
+template <int kBits, bool kStream>
+struct Eight;
+template <bool kStream>
+struct Eight<32, kStream> {
+    AdamwChunk k;
+    Gradients<false, kStream> g;
+    f32x4 w[2], m[2], v[2];
+    __device__ __forceinline__ void load(const ManyStep& s, int64_t chunk) {
+        k = s.chunks[chunk];
+        const float* const state = reinterpret_cast<const float*>(s.state) + k.at;
+        g.load(k);
+        load_eight<false, kStream>(w, k.weight, k.count);
+        load_eight<false, kStream>(m, state, k.count);
+        load_eight<false, kStream>(v, state + s.elements, k.count);
+    }
+    __device__ __forceinline__ void get(float (&mm)[8], float (&vv)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { mm[e] = m[e / 4][e % 4]; vv[e] = v[e / 4][e % 4]; }
+    }
+    __device__ __forceinline__ void put(const ManyStep& s, const float (&mm)[8], const float (&vv)[8]) const {
+        float* const state = reinterpret_cast<float*>(s.state) + k.at;
+        store_eight<false, kStream>(state, mm, k.count);
+        store_eight<false, kStream>(state + s.elements, vv, k.count);
+    }
+};
+template <bool kStream>
+struct Eight<8, kStream> {
+    AdamwChunk k;
+    Gradients<true, kStream> g;
+    f32x4 w[2];
+    u32x2 m, v;
+    int m_top, v_top;
+    __device__ __forceinline__ bool in_block() const { return (int)threadIdx.x * 8 < (k.count + kManyBlock - 1) / kManyBlock * kManyBlock; }
+    __device__ __forceinline__ void load(const ManyStep& s, int64_t chunk) {
+        k = s.chunks[chunk];
+        g.load(k);
+        // (a line of weights is two loads of a lane's neighbours: the second finds it in the cache)
+        load_eight<true, false>(w, k.weight, k.count);
+        m = v = u32x2{0, 0};
+        m_top = v_top = 0;
+        if (!in_block()) return;
+        const int64_t j = k.at + threadIdx.x * 8;
+        const PCM_GLOBAL uint8_t* const state = (const PCM_GLOBAL uint8_t*)s.state;
+        const PCM_GLOBAL uint8_t* const tops = state + 2 * s.elements + j / kManyBlock;
+        m = load_codes<kStream>((const eight_codes*)(state + j));
+        v = load_codes<kStream>((const eight_codes*)(state + s.elements + j));
+        m_top = tops[0];
+        v_top = tops[s.elements / kManyBlock];
+    }
+    __device__ __forceinline__ void get(float (&mm)[8], float (&vv)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t a = m[e / 4] >> (e % 4 * 8) & 255, b = v[e / 4] >> (e % 4 * 8) & 255;
+            const float x = value_of<kSignField>(a & 127, m_top);
+            mm[e] = a > 127 ? -x : x;
+            vv[e] = value_of<kSquareField>(b, v_top);
+        }
+    }
+    __device__ __forceinline__ void put(const ManyStep& s, const float (&mm)[8], const float (&vv)[8]) const {
+        if (!in_block()) return;                              // by whole blocks, so the lanes of a block stay together
+        const int64_t j = k.at + threadIdx.x * 8;
+        const int n = k.count - (int)threadIdx.x * 8;
+        const uint64_t group = (uint64_t)(j / 8);
+        const PhiloxWords bits = philox4x32((uint32_t)group, (uint32_t)(group >> 32), s.step[0], s.step[1], s.seed[0], s.seed[1]);
+        uint32_t random[8], mb[8], vb[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            random[e] = bits.w[e / 2] >> (e % 2 * 16) & 0xffffu;
+            mb[e] = e < n ? __builtin_bit_cast(uint32_t, mm[e]) & 0x7fffffffu : 0u;
+            vb[e] = e < n ? __builtin_bit_cast(uint32_t, vv[e]) & 0x7fffffffu : 0u;
+        }
+        const int m_new = exponent_of(mb, random), v_new = exponent_of(vb, random);
+        u32x2 mc = {0, 0}, vc = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t a = code_of<kSignField>(mb[e], random[e], m_new), b = code_of<kSquareField>(vb[e], random[e], v_new);
+            const uint32_t sign = a != 0 && __builtin_bit_cast(uint32_t, mm[e]) >> 31 ? 128u : 0u;
+            mc[e / 4] |= ((a & 127u) | sign) << (e % 4 * 8);
+            vc[e / 4] |= (vb[e] < 1u << 23 ? 0u : min(max(b, 1u), 255u)) << (e % 4 * 8);
+        }
+        PCM_GLOBAL uint8_t* const state = (PCM_GLOBAL uint8_t*)s.state;
+        store_codes<kStream>((eight_codes*)(state + j), mc);
+        store_codes<kStream>((eight_codes*)(state + s.elements + j), vc);
+        if ((threadIdx.x & 15) == 0) {
+            PCM_GLOBAL uint8_t* const tops = state + 2 * s.elements + j / kManyBlock;
+            tops[0] = (uint8_t)m_new;
+            tops[s.elements / kManyBlock] = (uint8_t)v_new;
+        }
+    }
+};
+
+// A workgroup takes every gridDim-th chunk, the next one's values under way while one is worked on; the first one's while the norm is formed.
 template <int kBits, bool kStream>
 __global__ __launch_bounds__(kThreads) void many_update(ManyStep s) {
-    const float scale = clip_factor(s);
+    constexpr bool kTogether = kBits == 8;
     const AdamConst& c = s.c;
-    for (int64_t at = blockIdx.x; at < s.n; at += gridDim.x) {
-        const AdamwChunk k = s.chunks[kStream ? s.n - 1 - at : at];
-        const int blocks_end = (k.count + kManyBlock - 1) / kManyBlock * kManyBlock;
-#pragma unroll 1
-        for (int r = 0; r < kManyChunk / kPass; ++r) {
-            const int i = r * kPass + threadIdx.x * 8;
-            if (i >= blocks_end) break;                       // by whole blocks, so the lanes of a block stay together
-            const int n = k.count - i;
-            const int64_t j = k.at + i;
-            float g[8], w[8], m[8], v[8];
-            load_gradient<kStream>(g, k, i);
-            load_floats<kStream>(w, k.weight + i, n);
-            if constexpr (kBits == 32) {
-                float* const state = reinterpret_cast<float*>(s.state) + j;
-                load_floats<kStream>(m, state, 8);
-                load_floats<kStream>(v, state + s.elements, 8);
-            } else {
-                const uint8_t* const tops = reinterpret_cast<const uint8_t*>(s.state) + 2 * s.elements + j / kManyBlock;
-                const u32x2 mc = load_codes<kStream>(reinterpret_cast<const u32x2*>(s.state + j));
-                const u32x2 vc = load_codes<kStream>(reinterpret_cast<const u32x2*>(s.state + s.elements + j));
-                const int m_top = tops[0], v_top = tops[s.elements / kManyBlock];
+    int64_t at = blockIdx.x;
+    auto chunk = [&](int64_t i) { return kStream ? s.n - 1 - i : i; };
+    Eight<kBits, kStream> x;
+    if (at < s.n) x.load(s, chunk(at));
+    const float scale = clip_factor(s);
+    for (; at < s.n; at += gridDim.x) {
+        const Eight<kBits, kStream> now = x;
+        if (at + gridDim.x < s.n) x.load(s, chunk(at + gridDim.x));
+        float g[8], w[8], m[8], v[8];
+        now.g.get(g, now.k);
+        now.get(m, v);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t a = mc[e / 4] >> (e % 4 * 8) & 255, b = vc[e / 4] >> (e % 4 * 8) & 255;
-                    const float x = value_of<kSignField>(a & 127, m_top);
-                    m[e] = a > 127 ? -x : x;
-                    v[e] = value_of<kSquareField>(b, v_top);
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float x = g[e] * scale;
-                m[e] = c.beta1 * m[e] + c.one_minus_beta1 * x;
-                v[e] = c.beta2 * v[e] + c.one_minus_beta2 * (x * x);
-                const float denom = sqrtf(v[e]) * c.inv_sqrt_bc2 + c.eps;
-                w[e] = w[e] * c.decay - c.step_size * (m[e] / denom);
-            }
-            store_floats<kStream>(k.weight + i, w, n);
-            if (k.lowp != nullptr) store_bf16(k.lowp + i, w, n);
-            if constexpr (kBits == 32) {
-                float* const state = reinterpret_cast<float*>(s.state) + j;
-                if (n < 8) {                                  // what pads a tensor stays zero
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (e >= n) m[e] = v[e] = 0.f;
-                }
-                store_floats<kStream>(state, m, 8);
-                store_floats<kStream>(state + s.elements, v, 8);
-            } else {
-                const uint64_t group = (uint64_t)(j / 8);
-                const PhiloxWords bits = philox4x32((uint32_t)group, (uint32_t)(group >> 32), s.step[0], s.step[1], s.seed[0], s.seed[1]);
-                uint32_t random[8], mb[8], vb[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    random[e] = bits.w[e / 2] >> (e % 2 * 16) & 0xffffu;
-                    mb[e] = e < n ? __builtin_bit_cast(uint32_t, m[e]) & 0x7fffffffu : 0u;
-                    vb[e] = e < n ? __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu : 0u;
-                }
-                const int m_top = exponent_of(mb, random), v_top = exponent_of(vb, random);
-                u32x2 mc = {0, 0}, vc = {0, 0};
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t a = code_of<kSignField>(mb[e], random[e], m_top), b = code_of<kSquareField>(vb[e], random[e], v_top);
-                    const uint32_t sign = a != 0 && __builtin_bit_cast(uint32_t, m[e]) >> 31 ? 128u : 0u;
-                    mc[e / 4] |= ((a & 127u) | sign) << (e % 4 * 8);
-                    vc[e / 4] |= (vb[e] < 1u << 23 ? 0u : min(max(b, 1u), 255u)) << (e % 4 * 8);
-                }
-                store_codes<kStream>(reinterpret_cast<u32x2*>(s.state + j), mc);
-                store_codes<kStream>(reinterpret_cast<u32x2*>(s.state + s.elements + j), vc);
-                if ((threadIdx.x & 15) == 0) {
-                    uint8_t* const tops = reinterpret_cast<uint8_t*>(s.state) + 2 * s.elements + j / kManyBlock;
-                    tops[0] = (uint8_t)m_top;
-                    tops[s.elements / kManyBlock] = (uint8_t)v_top;
-                }
-            }
+        for (int e = 0; e < 8; ++e) {
+            const float y = g[e] * scale;
+            m[e] = c.beta1 * m[e] + c.one_minus_beta1 * y;
+            v[e] = c.beta2 * v[e] + c.one_minus_beta2 * (y * y);
+            const float denom = sqrtf(v[e]) * c.inv_sqrt_bc2 + c.eps;
+            w[e] = now.w[e / 4][e % 4] * c.decay - c.step_size * (m[e] / denom);
         }
+        store_eight<kTogether, kStream && !kTogether>(now.k.weight, w, now.k.count);
+        if (now.k.lowp != nullptr) store_bf16<kTogether>(now.k.lowp, w, now.k.count);
+        now.put(s, m, v);
     }
 }
 
 // The values of 8-bit states: bf16 holds them exactly, as fp32 does (down to the least bf16 value, 2^-133).
 template <bool kBf16>
 __global__ __launch_bounds__(kThreads) void many_states(const uint8_t* state, int64_t elements, void* m_out, void* v_out) {
-    for (int64_t j = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 8; j < elements; j += (int64_t)gridDim.x * kPass) {
+    for (int64_t j = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 8; j < elements; j += (int64_t)gridDim.x * kManyChunk) {
         const uint8_t* const tops = state + 2 * elements + j / kManyBlock;
         const u32x2 mc = *reinterpret_cast<const u32x2*>(state + j), vc = *reinterpret_cast<const u32x2*>(state + elements + j);
         const int m_top = tops[0], v_top = tops[elements / kManyBlock];
@@ -267,13 +380,20 @@ __global__ __launch_bounds__(kThreads) void many_states(const uint8_t* state, in
             m[e] = a > 127 ? -x : x;
             v[e] = value_of<kSquareField>(b, v_top);
         }
-        if (kBf16) {
-            store_bf16(static_cast<uint16_t*>(m_out) + j, m, 8);
-            store_bf16(static_cast<uint16_t*>(v_out) + j, v, 8);
-        } else {
-            store_floats<false>(static_cast<float*>(m_out) + j, m, 8);
-            store_floats<false>(static_cast<float*>(v_out) + j, v, 8);
-        }
+        auto write = [&](void* out, const float (&x)[8]) {
+            if (kBf16) {
+                u32x4 a;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) a[e] = bf16_bits(x[2 * e]) | bf16_bits(x[2 * e + 1]) << 16;
+                store_halves<false>((eight_halves*)(static_cast<uint16_t*>(out) + j), a);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    store_floats<false>((four_floats*)(static_cast<float*>(out) + j + 4 * h), f32x4{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]});
+            }
+        };
+        write(m_out, m);
+        write(v_out, v);
     }
 }
 
@@ -452,7 +572,7 @@ PCM_API int pcm_adamw_many_states(const pcm_adamw_many_layout* layout, const voi
     if (!state || !m_out || !v_out) return PCM_EINVAL;
     hipStream_t s = static_cast<hipStream_t>(stream);
     StageTimer t(ST_OPT_ADAMW, s);
-    const int64_t groups = ceil_div64(layout->elements, kPass);
+    const int64_t groups = ceil_div64(layout->elements, kManyChunk);
     const unsigned grid = (unsigned)(groups < 8192 ? groups : 8192);
     if (dtype == PCM_BF16) many_states<true><<<grid, kThreads, 0, s>>>(static_cast<const uint8_t*>(state), layout->elements, m_out, v_out);
     else many_states<false><<<grid, kThreads, 0, s>>>(static_cast<const uint8_t*>(state), layout->elements, m_out, v_out);

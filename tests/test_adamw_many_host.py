@@ -13,6 +13,7 @@ LIB = os.path.join(ROOT, "paper_2605_16154_amd", "libpcm.so")
 OK, EINVAL, EWORKSPACE = 0, -1, -2
 vp, i32, i64, u64, f64, sz = C.c_void_p, C.c_int, C.c_int64, C.c_uint64, C.c_double, C.c_size_t
 A = 1 << 30                                  # an address that is only looked at
+CHUNK = 2048                                 # elements of a chunk of a plan
 
 
 class Layout(C.Structure):
@@ -57,7 +58,7 @@ def test_layout(cdll, numel):
     for bits, per_block in ((32, 128 * 8), (8, 128 * 2 + 2)):
         rc, layout = _describe(cdll, numel, bits)
         assert (rc, layout.elements, layout.state_bytes, layout.state_bits) == (OK, 128 * blocks, per_block * blocks, bits)
-        assert layout.chunks == sum(-(-n // 4096) for n in numel) and layout.plan_bytes == 40 * layout.chunks
+        assert layout.chunks == sum(-(-n // CHUNK) for n in numel) and layout.plan_bytes == 40 * layout.chunks
         assert cdll.pcm_adamw_many_step_workspace_bytes(C.byref(layout)) == 8192
 
 
@@ -71,10 +72,10 @@ def test_plan_holds_every_element_once(cdll):
     assert len(chunks) == layout.chunks
     at, k = 0, 0
     for n, d, g, w, b in zip(numel, dtypes, grads, weights, lowp):
-        for first in range(0, n, 4096):
+        for first in range(0, n, CHUNK):
             c = chunks[k]
             assert (c["g"], c["w"], c["b"]) == (g + first * (2 if d else 4), w + first * 4, b + first * 2 if b else 0)
-            assert (c["at"], c["count"], c["half"]) == (at + first, min(4096, n - first), d)
+            assert (c["at"], c["count"], c["half"]) == (at + first, min(CHUNK, n - first), d)
             k += 1
         at += -(-n // 128) * 128
     assert at == layout.elements
