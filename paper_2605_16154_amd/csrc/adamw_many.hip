@@ -14,6 +14,7 @@
 // before they are rounded.  All of it is integer arithmetic and fp32 without fused multiply-add: bits do not depend on the launch.
 #include "adamw_many.h"
 
+#include <algorithm>
 #include <cstdlib>
 
 #include "philox.h"
@@ -23,7 +24,9 @@ namespace {
 
 constexpr int kThreads = 256;
 static_assert(kManyChunk == kThreads * 8, "eight elements a lane");
-constexpr int kSumsqGrid = 1024, kUpdateGrid = 2048;
+// Workgroups of the two passes.  Update of 341 M parameters in 32 / 203 M in 8 bits by 2048 / 1280 (five to a CU) / 1024 of them: 1910 / 1873 / 1880 and
+// 713 / 705 / 715 us.
+constexpr int kSumsqGrid = 1024, kUpdateGrid = 1280;
 constexpr int kSignField = 15, kSquareField = 31;
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -63,8 +66,8 @@ __device__ inline float high_half(uint32_t x) { return __builtin_bit_cast(float,
 template <bool kTogether>
 __device__ inline int four_at(int h) { return kTogether ? threadIdx.x * 8 + h * 4 : h * (kManyChunk / 2) + threadIdx.x * 4; }
 
-// A lane's gradients of a chunk as they come: fp32, or bf16 in the first half.
-template <bool kTogether, bool kStream>
+// A lane's gradients of a chunk as they come: fp32, or bf16 in the first half (kHalvesTogether: those are eight neighbours).
+template <bool kTogether, bool kStream, bool kHalvesTogether = kTogether>
 struct Gradients {
     f32x4 x[2];
     __device__ __forceinline__ void load(const AdamwChunk& k) {
@@ -72,7 +75,7 @@ struct Gradients {
             const global_half* p = (const global_half*)k.grad;
             u32x4 both = {0, 0, 0, 0};
             if (k.count == kManyChunk) {
-                if (kTogether) both = load_halves<kStream>((const eight_halves*)(p + four_at<true>(0)));
+                if (kHalvesTogether) both = load_halves<kStream>((const eight_halves*)(p + four_at<true>(0)));
                 else {
                     const u32x2 a = load_few_halves<kStream>((const four_halves*)(p + four_at<false>(0)));
                     const u32x2 b = load_few_halves<kStream>((const four_halves*)(p + four_at<false>(1)));
@@ -81,7 +84,7 @@ struct Gradients {
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int i = four_at<kTogether>(e / 4) + e % 4;
+                    const int i = four_at<kHalvesTogether>(e / 4) + e % 4;
                     if (i < k.count) both[e / 2] |= (uint32_t)p[i] << (e % 2 * 16);
                 }
             }
@@ -173,7 +176,7 @@ __device__ inline double block_sum(double x) {
 
 __global__ __launch_bounds__(kThreads) void many_sumsq(const AdamwChunk* chunks, int64_t n, double* partial) {
     double acc[8] = {};
-    auto add = [&](const AdamwChunk& k, const Gradients<false, false>& x) __attribute__((always_inline)) {
+    auto add = [&](const AdamwChunk& k, const Gradients<false, false, true>& x) __attribute__((always_inline)) {
         float g[8];
         x.get(g, k);
 #pragma unroll
@@ -184,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void many_sumsq(const AdamwChunk* chunks,
     int64_t at = blockIdx.x;
     for (; at + (int64_t)(kAhead - 1) * gridDim.x < n; at += (int64_t)kAhead * gridDim.x) {
         AdamwChunk k[kAhead];
-        Gradients<false, false> x[kAhead];
+        Gradients<false, false, true> x[kAhead];
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
             k[q] = chunks[at + (int64_t)q * gridDim.x];
@@ -195,7 +198,7 @@ __global__ __launch_bounds__(kThreads) void many_sumsq(const AdamwChunk* chunks,
     }
     for (; at < n; at += gridDim.x) {
         const AdamwChunk k = chunks[at];
-        Gradients<false, false> x;
+        Gradients<false, false, true> x;
         x.load(k);
         add(k, x);
     }
@@ -210,38 +213,98 @@ __device__ inline uint32_t block_max(uint32_t x) {
     x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x122, 0xf, 0xf, true));
     return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x121, 0xf, 0xf, true));
 }
-// A code without its sign, as a value.
+// Codes of eight values of a block whose exponent is `top`, without their signs, as values.  A code is the upper bits of an fp32 number whose exponent
+// begins at top - kField: an addition and a shift; below f = 1 with the implicit one put in and taken away again.  Blocks whose values do not fit
+// into that (close to the least numbers, or NaN) are rare and go the long way: the lanes of a wavefront together.
 template <int kField>
-__device__ inline float value_of(uint32_t code, int top) {
-    const int field = max((int)(code >> 3), 1);
-    const float x = (float)(code >= 8 ? 8 + (code & 7) : code);
-    return top == 255 ? __builtin_nanf("") : ldexpf(x, field + top - kField - 130);
+__device__ __forceinline__ void values_of(float (&x)[8], const uint32_t (&code)[8], int top) {
+    if (!__any(top == 255 || (top > 0 && top <= kField))) {
+        const uint32_t base = (uint32_t)(top - kField) << 3;
+        const float one = __builtin_bit_cast(float, (8 + base) << 20);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bool fine = code[e] < 8;
+            x[e] = __builtin_bit_cast(float, ((fine ? code[e] + 8 : code[e]) + base) << 20) - (fine ? one : 0.f);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float v = ldexpf((float)(code[e] >= 8 ? 8 + (code[e] & 7) : code[e]), max((int)(code[e] >> 3), 1) + top - kField - 130);
+            x[e] = top == 255 ? __builtin_nanf("") : v;
+        }
+    }
 }
-// Exponent of a block, from each lane's eight values (as bits without a sign) and their random bits.
-__device__ inline int exponent_of(const uint32_t (&bits)[8], const uint32_t (&random)[8]) {
+// Exponent of a block, from each lane's eight values (as bits without a sign) and their random bits (times 16).
+__device__ __forceinline__ int exponent_of(const uint32_t (&bits)[8], const uint32_t (&random)[8]) {
     uint32_t most = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) most = max(most, bits[e] < 1u << 23 ? 0u : bits[e] + (random[e] << 4));
-    return (int)min(block_max(most) >> 23, 255u);
+    for (int e = 0; e < 8; ++e) most = max(most, bits[e] + random[e]);
+    most = block_max(most);
+    // zeros and what is below the normal numbers count as nothing, which matters where there is nothing else
+    if (__any(most < 3u << 23)) {
+        most = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = max(most, bits[e] < 1u << 23 ? 0u : bits[e] + random[e]);
+        most = block_max(most);
+    }
+    return (int)min(most >> 23, 255u);
 }
+// Codes of eight values, without signs.
 template <int kField>
-__device__ inline uint32_t code_of(uint32_t bits, uint32_t random, int top) {
-    const int code = (int)((bits + (random << 4)) >> 20) - ((top - kField) << 3);
+__device__ __forceinline__ void codes_of(uint32_t (&code)[8], const uint32_t (&bits)[8], const uint32_t (&random)[8], int top) {
+    const int base = (top - kField) << 3;
+    bool fine = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int c = (int)((bits[e] + random[e]) >> 20) - base;
+        fine |= c < 8 && bits[e] >= 1u << 23;
+        code[e] = bits[e] < 1u << 23 ? 0u : (uint32_t)c;
+    }
     // below 2^(top - kField + 1): multiples of 2^(top - kField - 2), of which 16 bits behind the point count
-    const uint32_t fine = ((uint32_t)ldexpf(__builtin_bit_cast(float, bits), 16 + 129 + kField - top) + random) >> 16;
-    const uint32_t c = code >= 8 ? (uint32_t)code : fine;
-    return bits < 1u << 23 ? 0u : c;
+    if (!__any(fine)) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (bits[e] < 1u << 23 || (int)code[e] >= 8) continue;
+        code[e] = ((uint32_t)ldexpf(__builtin_bit_cast(float, bits[e]), 16 + 129 + kField - top) + (random[e] >> 4)) >> 16;
+        if (kField == kSquareField) code[e] = max(code[e], 1u);
+    }
+}
+__device__ __forceinline__ void split_codes(uint32_t (&code)[8], u32x2 x) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) code[e] = x[e / 4] >> (e % 4 * 8) & 255;
+}
+// m and v of eight elements.
+__device__ __forceinline__ void moments_of(float (&m)[8], float (&v)[8], u32x2 mc, u32x2 vc, int m_top, int v_top) {
+    uint32_t a[8], b[8], mag[8];
+    split_codes(a, mc);
+    split_codes(b, vc);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mag[e] = a[e] & 127;
+    values_of<kSignField>(m, mag, m_top);
+    values_of<kSquareField>(v, b, v_top);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m[e] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, m[e]) | (a[e] & 128) << 24);
 }
 
-// Norm and clip factor; every workgroup forms them from the partial sums by itself.
-__device__ inline float clip_factor(const ManyStep& s) {
-    if (s.parts == 0) return 1.f;
-    double acc = 0.0;
-    for (int i = threadIdx.x; i < s.parts; i += kThreads) acc += s.partial[i];
-    const double norm = sqrt(block_sum(acc));
-    if (s.norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *s.norm_out = (float)norm;
-    return (float)fmin(1.0, s.max_norm / (norm + 1e-6));
-}
+// Norm and clip factor; every workgroup forms them from the partial sums by itself.  They are asked for before anything else.
+struct ClipFactor {
+    static constexpr int kEach = kSumsqGrid / kThreads;
+    double part[kEach];
+    __device__ __forceinline__ void load(const ManyStep& s) {
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            const int i = q * kThreads + threadIdx.x;
+            part[q] = i < s.parts ? s.partial[i] : 0.0;
+        }
+    }
+    __device__ __forceinline__ float get(const ManyStep& s) const {
+        if (s.parts == 0) return 1.f;
+        const double norm = sqrt(block_sum((part[0] + part[1]) + (part[2] + part[3])));
+        if (s.norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *s.norm_out = (float)norm;
+        return (float)fmin(1.0, s.max_norm / (norm + 1e-6));
+    }
+};
+static_assert(ClipFactor::kEach == 4, "");
 
 // What a lane takes up of a chunk.
 template <int kBits, bool kStream>
@@ -293,36 +356,36 @@ struct Eight<8, kStream> {
         m_top = tops[0];
         v_top = tops[s.elements / kManyBlock];
     }
-    __device__ __forceinline__ void get(float (&mm)[8], float (&vv)[8]) const {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t a = m[e / 4] >> (e % 4 * 8) & 255, b = v[e / 4] >> (e % 4 * 8) & 255;
-            const float x = value_of<kSignField>(a & 127, m_top);
-            mm[e] = a > 127 ? -x : x;
-            vv[e] = value_of<kSquareField>(b, v_top);
-        }
-    }
+    __device__ __forceinline__ void get(float (&mm)[8], float (&vv)[8]) const { moments_of(mm, vv, m, v, m_top, v_top); }
     __device__ __forceinline__ void put(const ManyStep& s, const float (&mm)[8], const float (&vv)[8]) const {
         if (!in_block()) return;                              // by whole blocks, so the lanes of a block stay together
         const int64_t j = k.at + threadIdx.x * 8;
         const int n = k.count - (int)threadIdx.x * 8;
         const uint64_t group = (uint64_t)(j / 8);
         const PhiloxWords bits = philox4x32((uint32_t)group, (uint32_t)(group >> 32), s.step[0], s.step[1], s.seed[0], s.seed[1]);
-        uint32_t random[8], mb[8], vb[8];
+        uint32_t random[8], mb[8], vb[8], a[8], b[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            random[e] = bits.w[e / 2] >> (e % 2 * 16) & 0xffffu;
-            mb[e] = e < n ? __builtin_bit_cast(uint32_t, mm[e]) & 0x7fffffffu : 0u;
-            vb[e] = e < n ? __builtin_bit_cast(uint32_t, vv[e]) & 0x7fffffffu : 0u;
+            random[e] = (e % 2 ? bits.w[e / 2] >> 12 : bits.w[e / 2] << 4) & 0xffff0u;
+            mb[e] = __builtin_bit_cast(uint32_t, mm[e]) & 0x7fffffffu;
+            vb[e] = __builtin_bit_cast(uint32_t, vv[e]) & 0x7fffffffu;
+        }
+        if (__any(n < 8)) {                                   // what pads a tensor
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                mb[e] = e < n ? mb[e] : 0u;
+                vb[e] = e < n ? vb[e] : 0u;
+            }
         }
         const int m_new = exponent_of(mb, random), v_new = exponent_of(vb, random);
+        codes_of<kSignField>(a, mb, random, m_new);
+        codes_of<kSquareField>(b, vb, random, v_new);
         u32x2 mc = {0, 0}, vc = {0, 0};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint32_t a = code_of<kSignField>(mb[e], random[e], m_new), b = code_of<kSquareField>(vb[e], random[e], v_new);
-            const uint32_t sign = a != 0 && __builtin_bit_cast(uint32_t, mm[e]) >> 31 ? 128u : 0u;
-            mc[e / 4] |= ((a & 127u) | sign) << (e % 4 * 8);
-            vc[e / 4] |= (vb[e] < 1u << 23 ? 0u : min(max(b, 1u), 255u)) << (e % 4 * 8);
+            const uint32_t sign = a[e] != 0 ? __builtin_bit_cast(uint32_t, mm[e]) >> 24 & 128u : 0u;
+            mc[e / 4] |= ((a[e] & 127u) | sign) << (e % 4 * 8);
+            vc[e / 4] |= (b[e] & 255u) << (e % 4 * 8);
         }
         PCM_GLOBAL uint8_t* const state = (PCM_GLOBAL uint8_t*)s.state;
         store_codes<kStream>((eight_codes*)(state + j), mc);
@@ -337,14 +400,16 @@ struct Eight<8, kStream> {
 
 // A workgroup takes every gridDim-th chunk, the next one's values under way while one is worked on; the first one's while the norm is formed.
 template <int kBits, bool kStream>
-__global__ __launch_bounds__(kThreads) void many_update(ManyStep s) {
+__global__ __launch_bounds__(kThreads, 5) void many_update(ManyStep s) {
     constexpr bool kTogether = kBits == 8;
     const AdamConst& c = s.c;
     int64_t at = blockIdx.x;
     auto chunk = [&](int64_t i) { return kStream ? s.n - 1 - i : i; };
+    ClipFactor clip;
+    clip.load(s);
     Eight<kBits, kStream> x;
     if (at < s.n) x.load(s, chunk(at));
-    const float scale = clip_factor(s);
+    const float scale = clip.get(s);
     for (; at < s.n; at += gridDim.x) {
         const Eight<kBits, kStream> now = x;
         if (at + gridDim.x < s.n) x.load(s, chunk(at + gridDim.x));
@@ -356,8 +421,10 @@ __global__ __launch_bounds__(kThreads) void many_update(ManyStep s) {
             const float y = g[e] * scale;
             m[e] = c.beta1 * m[e] + c.one_minus_beta1 * y;
             v[e] = c.beta2 * v[e] + c.one_minus_beta2 * (y * y);
-            const float denom = sqrtf(v[e]) * c.inv_sqrt_bc2 + c.eps;
-            w[e] = now.w[e / 4][e % 4] * c.decay - c.step_size * (m[e] / denom);
+            // (8 bits: root and reciprocal of the hardware, 1 ulp each: with the exact ones 203 M parameters take 7 % longer)
+            const float root = kBits == 8 ? __builtin_amdgcn_sqrtf(v[e]) : sqrtf(v[e]);
+            const float denom = root * c.inv_sqrt_bc2 + c.eps;
+            w[e] = now.w[e / 4][e % 4] * c.decay - c.step_size * (kBits == 8 ? m[e] * __builtin_amdgcn_rcpf(denom) : m[e] / denom);
         }
         store_eight<kTogether, kStream && !kTogether>(now.k.weight, w, now.k.count);
         if (now.k.lowp != nullptr) store_bf16<kTogether>(now.k.lowp, w, now.k.count);
@@ -373,13 +440,7 @@ __global__ __launch_bounds__(kThreads) void many_states(const uint8_t* state, in
         const u32x2 mc = *reinterpret_cast<const u32x2*>(state + j), vc = *reinterpret_cast<const u32x2*>(state + elements + j);
         const int m_top = tops[0], v_top = tops[elements / kManyBlock];
         float m[8], v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t a = mc[e / 4] >> (e % 4 * 8) & 255, b = vc[e / 4] >> (e % 4 * 8) & 255;
-            const float x = value_of<kSignField>(a & 127, m_top);
-            m[e] = a > 127 ? -x : x;
-            v[e] = value_of<kSquareField>(b, v_top);
-        }
+        moments_of(m, v, mc, vc, m_top, v_top);
         auto write = [&](void* out, const float (&x)[8]) {
             if (kBf16) {
                 u32x4 a;
@@ -422,7 +483,7 @@ bool layout_ok(const pcm_adamw_many_layout* l) {
            l->chunks <= l->elements / kManyBlock && l->elements <= l->chunks * kManyChunk && (l->state_bits == 8 || l->state_bits == 32);
 }
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-int sumsq_grid(int64_t chunks) { return (int)(chunks < kSumsqGrid ? chunks : kSumsqGrid); }
+int sumsq_grid(int64_t chunks) { return (int)std::min<int64_t>(kSumsqGrid, chunks); }
 
 struct Extent {
     uintptr_t begin, end;
