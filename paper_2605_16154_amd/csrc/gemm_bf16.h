@@ -115,7 +115,23 @@ struct BoundedProblem : GemmProblem {
     static constexpr bool kBoundedB = true, kHalves = kThirds;
     int N_real, K_real;
     const bf16 *A3, *B3;
+    // > 0: the product is done in as many parts, splits at most, as suit the rows that are there (parts_for; what a part costs beside its steps)
+    int part_cost, part_steps;       // part_steps: the steps that this goes by
 };
+// Parts of a reduction of `steps` for `tiles` tiles: the fewest steps in a row over all rounds of 256 workgroups, ten more for the start
+// and end of each, and what the parts cost when they are written and added up: part_cost each and six for the launch.
+__host__ __device__ inline int parts_for(int tiles, int steps, int most, int part_cost) {
+    int best = 1, least = 0x7fffffff;
+    if (tiles > 2048) return 1;                          // eight rounds and more even out
+    for (int n = 1; n <= most; ++n) {
+        const int rounds = (tiles * n + 255) / 256, cost = rounds * ((steps + n - 1) / n + 10) + (n > 1 ? n * part_cost + 6 : 0);
+        if (cost < least) {
+            least = cost;
+            best = n;
+        }
+    }
+    return best;
+}
 enum RowsRole : int { kRowsUnused = 0, kRowsAreM = 1, kRowsAreK = 2 };
 
 // Accumulators of a wavefront: kW x kW tiles of 16 x 16.  Tile (i, j), register t of a lane is
@@ -126,7 +142,8 @@ using Accumulators = f32x4[kW][kW];
 template <int kW>
 struct TileCoord {
     int m0, n0, wm, wn, lane;
-    int split;   // which part of a split reduction this workgroup computed
+    int split;   // which part of a split reduction this workgroup computed, of how many
+    int splits;
     __device__ int row0() const { return m0 + wm * kWaveRows<kW>; }
     __device__ int col0() const { return n0 + wn * kWaveRows<kW>; }
 };
@@ -329,9 +346,11 @@ __device__ __forceinline__ void gemm_tile(const Problem& p, const Epilogue& epi,
     const int wm = wave >> 1, wn = wave & 1;
     const int tiles_m = p.M / TM;
     int tiles_n = p.N / TN, n_first = 0;
-    const int n_tiles = tiles_m * tiles_n;
-    const int split = block / n_tiles;
-    if (kShared && split >= p.splits) return;                    // their workgroups come in multiples of eight
+    int n_tiles = tiles_m * tiles_n;
+    int split = block / n_tiles, splits = p.splits;
+    bool chosen = false;                                         // the parts are chosen below
+    if constexpr (kBoundedB) chosen = p.part_cost > 0;
+    if (kShared && !chosen && split >= p.splits) return;         // their workgroups come in multiples of eight
     int k1 = p.K1, live_m = tiles_m;
     if (p.kept != nullptr) {
         const int rows = p.live_rows();
@@ -343,12 +362,21 @@ __device__ __forceinline__ void gemm_tile(const Problem& p, const Epilogue& epi,
         n_first = p.cut == kCutTail ? p.N - columns * kTileN : 0;
         tiles_n = (p.cut == kCutTail ? columns : p.N / kTileN - columns) * (kTileN / TN);
     }
+    if constexpr (kBoundedB) {
+        if (p.part_cost > 0) {
+            const int live_tiles = live_m * tiles_n;
+            splits = parts_for(live_tiles, p.part_steps, p.splits, p.part_cost);
+            n_tiles = (live_tiles + kNumXcd - 1) / kNumXcd * kNumXcd;
+            if (n_tiles == 0 || block >= n_tiles * splits) return;
+            split = block / n_tiles;
+        }
+    }
     int tm, tn;
     if (!tile_of_workgroup<kW>(block % n_tiles, n_tiles, live_m, tiles_n, tm, tn)) return;   // before any barrier
     const int m0 = tm * TM, n0 = n_first + tn * TN;
     // reduction range of this workgroup, in 64-wide steps over the concatenation of both segments
     const int steps1 = k1 / kTileK, steps_all = kHalves ? 3 * steps1 : steps1 + p.K2 / kTileK;
-    const int per_split = (steps_all + p.splits - 1) / p.splits;
+    const int per_split = (steps_all + splits - 1) / splits;
     const int step_begin = split * per_split;
     const int step_end = min(steps_all, step_begin + per_split);
 
@@ -648,7 +676,7 @@ __device__ __forceinline__ void gemm_tile(const Problem& p, const Epilogue& epi,
     }
 
     if (p.skip_if_empty && step_begin >= step_end && !runs_when_empty(epi, 0)) return;   // nothing to add (uniform over the workgroup)
-    const TileCoord<kW> tc{m0, n0, wm, wn, lane, split};
+    const TileCoord<kW> tc{m0, n0, wm, wn, lane, split, splits};
     epi(tc, acc, reinterpret_cast<char*>(smem.data));
 }
 

@@ -28,8 +28,10 @@ struct SlotGradient {
 };
 struct Slots {
     int32_t* live;                   // [1]: how many slots hold a row
+    int32_t* parts;                  // [1]: backward: in how many parts the product for dhidden was done
     int32_t* most;                   // [1]: fp32, backward: the largest exponent of h 2^-z_shift
     int32_t* slot_of;                // [rows]: -1 for a row without a token
+    int32_t* row_of;                 // [padded]: of the slots below live
     int32_t* token;                  // [padded]: in 0 .. V - 1; -1 from live up to the next multiple of 256
     half_bits *h, *h_low;            // [padded, d64]: the hidden rows, zeros behind d and from live up to the next multiple of 256
     float* h_unit;                   // fp32: [padded]: what a row of the pairs is to be multiplied by
@@ -43,6 +45,8 @@ struct SlotGradients {
     // fp32
     int32_t* z_shift;                // [padded]: a row of dz is held times 2^z_shift
     half_bits *w_h, *w_h_low;        // [padded, d64]: h 2^(14 - most - z_shift): what dz is multiplied with for dW
+    void* dh;                        // [rows], dh_ld apart, or null: rows without a token are made zeros
+    int64_t dh_ld;
 };
 
 constexpr int kCountRows = 1024;
@@ -127,12 +131,54 @@ inline void set_b(BoundedProblem<kThirds>& p, const half_bits* b, const half_bit
     p.N = N_real;                        // to whole tiles by the launch
     p.K1 = round_up(K_real, kTileK);
 }
-template <bool kThirds, int kLayA, int kLayB, class Epilogue>
-inline void launch_slot_product(BoundedProblem<kThirds> p, int kW, const Epilogue& epi, hipStream_t s) {
-    p.N = round_up(p.N, 32 * kW);
-    const unsigned grid = (unsigned)(p.M / (32 * kW)) * (unsigned)(p.N / (32 * kW)) * (unsigned)p.splits;
-    if (kW == kLargeTile) gemm_bounded<BoundedProblem<kThirds>, Epilogue, kLayA, kLayB, kLargeTile, kRingSlots><<<grid, kGemmThreads, 0, s>>>(p, epi);
-    else gemm_bounded<BoundedProblem<kThirds>, Epilogue, kLayA, kLayB, kSmallTile, kRingSlots><<<grid, kGemmThreads, 0, s>>>(p, epi);
+// A product with its epilogue, ready to be launched.
+template <bool kThirds, int kLayoutA, int kLayoutB, class E>
+struct SlotProduct {
+    using Problem = BoundedProblem<kThirds>;
+    using Epilogue = E;
+    static constexpr int kLayA = kLayoutA, kLayB = kLayoutB;
+    Problem p;
+    E epi;
+    int kW;
+    unsigned grid;
+    SlotProduct(Problem problem, int tile, const E& e) : p(problem), epi(e), kW(tile) {
+        p.N = round_up(p.N, 32 * kW);
+        const int tiles_n = p.N / (32 * kW), tiles = p.M / (32 * kW) * tiles_n;
+        grid = (unsigned)tiles * (unsigned)p.splits;
+        if (p.splits == 1) p.part_cost = 0;
+        if (p.part_cost == 0) return;
+        grid = (unsigned)round_up(tiles, kNumXcd);         // the most that any number of rows takes
+        for (int live = std::min(p.M / (32 * kW), 2048 / tiles_n + 1); live > 0; --live) {
+            const int n = live * tiles_n;
+            grid = std::max(grid, (unsigned)(round_up(n, kNumXcd) * parts_for(n, p.part_steps, p.splits, p.part_cost)));
+        }
+    }
+    int steps() const { return p.K1 / kTileK * (kThirds ? 3 : 1) / p.splits; }
+    void launch(hipStream_t s) const {
+        if (kW == kLargeTile) gemm_bounded<Problem, E, kLayA, kLayB, kLargeTile, kRingSlots><<<grid, kGemmThreads, 0, s>>>(p, epi);
+        else if (grid <= 256 && steps() >= kDeepSteps) gemm_bounded<Problem, E, kLayA, kLayB, kSmallTile, kDeepRingSlots><<<grid, kGemmThreads, 0, s>>>(p, epi);   // as launch_gemm_tile
+        else gemm_bounded<Problem, E, kLayA, kLayB, kSmallTile, kRingSlots><<<grid, kGemmThreads, 0, s>>>(p, epi);
+    }
+};
+// Two products that depend on the same launches, on small tiles, as one launch where each leaves CUs idle (a launch of its own takes as long to
+// begin and end as a few steps).
+template <class A, class B>
+__global__ __launch_bounds__(kGemmThreads, 2) void gemm_bounded_pair(typename A::Problem p, typename A::Epilogue e, int first, typename B::Problem q,
+                                                                    typename B::Epilogue f) {
+    __shared__ OperandRing<kSmallTile, kRingSlots> smem;
+    const int block = blockIdx.x;
+    if (block < first) gemm_tile<A::kLayA, A::kLayB, true>(p, e, block, smem);
+    else gemm_tile<B::kLayA, B::kLayB, true>(q, f, block - first, smem);
+}
+template <class A, class B>
+inline void launch_pair(const A& a, const B& b, hipStream_t s) {
+    const int first = round_up((int)a.grid, kNumXcd);
+    if (a.kW != kSmallTile || b.kW != kSmallTile || first + b.grid > 512) {
+        a.launch(s);
+        b.launch(s);
+        return;
+    }
+    gemm_bounded_pair<A, B><<<first + b.grid, kGemmThreads, 0, s>>>(a.p, a.epi, first, b.p, b.epi);
 }
 
 }  // namespace pcm

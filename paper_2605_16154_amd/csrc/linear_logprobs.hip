@@ -78,7 +78,10 @@ __global__ __launch_bounds__(256) void linear_slots(LinearRows in, Slots slots) 
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         if (first + e < in.rows) slots.slot_of[first + e] = token[e] >= 0 ? slot : -1;
-        if (token[e] >= 0) slots.token[slot++] = token[e];
+        if (token[e] >= 0) {
+            slots.row_of[slot] = first + e;
+            slots.token[slot++] = token[e];
+        }
     }
     if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 255) {
         *slots.live = slot;
@@ -183,12 +186,20 @@ __global__ __launch_bounds__(256) void linear_gather(LinearRows in, Slots slots,
         slot = token >= 0 ? before : -1;
         if (lane == 0) {
             slots.slot_of[row] = slot;
-            if (slot >= 0) slots.token[slot] = token;
+            if (slot >= 0) {
+                slots.token[slot] = token;
+                slots.row_of[slot] = row;
+            }
         }
     } else {
         slot = slots.slot_of[row];
     }
-    if (slot < 0) return;
+    if (slot < 0) {
+        if (grads.dh == nullptr) return;
+        T* const dh = static_cast<T*>(grads.dh) + row * grads.dh_ld;
+        for (int i = lane; i < in.d; i += 64) dh[i] = 0;
+        return;
+    }
     const T* const from = static_cast<const T*>(in.hidden) + row * in.ld;
     const int64_t to = (int64_t)slot * slots.d64;
     float largest = 0.f;
@@ -614,7 +625,7 @@ ForwardPlan plan_forward(void* workspace, int rows, const WeightSource& src) {
     ForwardPlan f{};
     f.few = rows <= kFewRows;
     if (f.few) {
-        f.parts = carve_parts(c, kFewRows, ceil_div(src.V, few_columns(src.dtype, src.layout)));
+        f.parts = carve_parts(c, rows, ceil_div(src.V, few_columns(src.dtype, src.layout)));
         f.token_z = c.take<float>(kFewRows);
     } else {
         f.slots = carve_slots(c, rows, src.d, src.dtype);
@@ -641,10 +652,10 @@ void forward_products(const ForwardPlan& f, const WeightSource& src, int rows, f
                               columns, first / (16 * f.tile)};
         if (src.layout == PCM_WEIGHT_OUT_IN) {
             set_b<kRowsByK>(p, w.w, w.low, w.ld, columns, src.d);
-            launch_slot_product<kThirds, kRowsByK, kRowsByK>(p, f.tile, epi, s);
+            SlotProduct<kThirds, kRowsByK, kRowsByK, EpiRowStats>(p, f.tile, epi).launch(s);
         } else {
             set_b<kKByRows>(p, w.w, w.low, w.ld, columns, src.d);
-            launch_slot_product<kThirds, kRowsByK, kKByRows>(p, f.tile, epi, s);
+            SlotProduct<kThirds, kRowsByK, kKByRows, EpiRowStats>(p, f.tile, epi).launch(s);
         }
     }
 }
@@ -658,8 +669,10 @@ Slots carve_slots(Carver& c, int rows, int d, int dtype) {
     q.padded = round_up(rows, kTileM);
     q.d64 = round_up(d, kTileK);
     q.live = c.take<int32_t>(1);
+    q.parts = c.take<int32_t>(1);
     q.most = c.take<int32_t>(1);
     q.slot_of = c.take<int32_t>((size_t)rows);
+    q.row_of = c.take<int32_t>((size_t)q.padded);
     q.token = c.take<int32_t>((size_t)q.padded);
     // (a tile of the product over rows reads up to 255 columns past a row)
     const size_t h = (size_t)q.padded * q.d64 + kTileM;
