@@ -555,7 +555,7 @@ PCM_API int pcm_muon_step(int n_tensors, const int* rows, const int* cols, const
  * A NaN or +inf among the logits makes the row's results NaN.  Last bits depend on how many rows there are.  rows = 0 is a valid call (of the
  * gradient: dweight becomes zeros).
  * Limits: 1 <= d <= 2^16, 1 <= V <= 2^22, rows <= 2^24.
- * Workspace: the slots of the rows and 12 bytes per row and 64 columns, never a row of logits; of the weight, where it has to be copied,
+ * Workspace: the slots of the rows and 16 bytes per row and 64 or 128 columns, never the logits; of the weight, where it has to be copied,
  * at most 256 MB or 256 columns.
  *
  * pcm_linear_logprobs_backward -- the gradient of a loss from its gradients in logp and entropy, as pcm_token_logprobs_backward:

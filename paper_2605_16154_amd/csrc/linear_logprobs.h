@@ -148,8 +148,9 @@ struct SlotProduct {
         if (p.splits == 1) p.part_cost = 0;
         if (p.part_cost == 0) return;
         grid = (unsigned)round_up(tiles, kNumXcd);         // the most that any number of rows takes
-        for (int live = std::min(p.M / (32 * kW), 2048 / tiles_n + 1); live > 0; --live) {
-            const int n = live * tiles_n;
+        const int each = kTileM / (32 * kW) * tiles_n;     // of 256 rows
+        for (int live = std::min(p.M / kTileM, 2048 / each + 1); live > 0; --live) {
+            const int n = live * each;
             grid = std::max(grid, (unsigned)(round_up(n, kNumXcd) * parts_for(n, p.part_steps, p.splits, p.part_cost)));
         }
     }

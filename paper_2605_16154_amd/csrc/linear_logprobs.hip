@@ -5,7 +5,7 @@
 //              2^a and of 2^a a, a = (z - largest) log2 e / temperature; the token's logit is written down where it passes by
 //   join       the blocks of a row -> log-sum-exp, log p, entropy
 // Up to 16 rows the projection is streamed once past rows in registers (few_rows), bound by its bytes.
-#include "linear_logprobs.h"
+#include "linear_epilogues.h"
 
 #include <type_traits>
 
@@ -14,7 +14,6 @@ namespace {
 
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;
 typedef f32x4 __attribute__((aligned(4))) f32x4_any;
-typedef _Float16 f16;
 
 // ---- slots ---------------------------------------------------------------------------------------
 
@@ -301,122 +300,8 @@ __global__ __launch_bounds__(256) void linear_copy(const T* w, int64_t ld, int r
     }
 }
 
-// ---- statistics of blocks of logits ------------------------------------------------------------------
+// ---- joining the parts -------------------------------------------------------------------------------
 
-// What a part of a row's logits comes to: the largest z; sum 2^a; sum 2^a a, a = (z - largest) c.  A part that saw nothing has the sum 0.
-struct RowSums {
-    float m, s, t;
-};
-struct PartSums {
-    f32x4* of;                           // [parts][ld], the fourth value unused
-    int64_t ld;
-    int parts;
-};
-__device__ __forceinline__ void merge(RowSums& a, const RowSums& b, float c) {
-    const float m = fmaxf(a.s == 0.f ? b.m : a.m, b.s == 0.f ? a.m : b.m);
-    const float da = fmaxf((a.m - m) * c, -1e30f), db = fmaxf((b.m - m) * c, -1e30f);
-    const float ea = a.s == 0.f ? 0.f : __builtin_amdgcn_exp2f(da), eb = b.s == 0.f ? 0.f : __builtin_amdgcn_exp2f(db);
-    a.t = ea * __builtin_fmaf(a.s, da, a.t) + eb * __builtin_fmaf(b.s, db, b.t);
-    a.s = a.s * ea + b.s * eb;
-    a.m = m;
-}
-// The sums of kN x 4 logits relative to m; -150 stands for what is as good as nothing (a is -inf where z is, or is that far below m).
-template <int kN, class F>
-__device__ __forceinline__ RowSums sums_of(float m, float c, F z) {
-    RowSums r{m, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < kN; ++j) {
-        float s = 0.f, t = 0.f;                            // four terms before they are added to the others
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float a = (z(j, e) - m) * c, x = __builtin_amdgcn_exp2f(a);
-            s += x;
-            t = __builtin_fmaf(x, fmaxf(a, -150.f), t);
-        }
-        r.s += s;
-        r.t += t;
-    }
-    return r;
-}
-
-// The largest of three, NaN aside (fmaxf would first quieten each operand, an instruction more).
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
-
-// The logits of a tile, a wavefront's block of which is a part of its rows.  Vector instructions that no product runs beside: 11.5 issue
-// slots per logit (the accumulator moved twice, half a maximum, difference, product, exponential, sum, moment and its guard).  A lane has a quarter of 16 neighbours' rows
-// to itself; the quarters meet at the end, all rows together, so that the exchanges wait for one another only there.
-struct EpiRowStats {
-    PartSums out;
-    float* token_z;                      // [padded]
-    const int32_t* token;
-    const float *h_unit, *w_unit;        // fp32, or null: powers of two
-    float c;                             // log2 e / temperature
-    int first, columns;                  // of the vocabulary in this piece
-    int first_part;
-    template <int kW>
-    __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char*) const {
-        constexpr int RW = kWaveRows<kW>;
-        const int col0 = tc.col0();
-        if (col0 >= columns) return;                       // no part of its own
-        if (col0 + RW <= columns) rows<true>(tc, acc, col0);
-        else rows<false>(tc, acc, col0);
-    }
-    template <bool kWhole, int kW>
-    __device__ __forceinline__ void rows(const TileCoord<kW>& tc, const Accumulators<kW>& acc, int col0) const {
-        constexpr int RW = kWaveRows<kW>;
-        const int quarter = tc.lane >> 4, row0 = tc.row0() + (tc.lane & 15);
-        const float w_scale = w_unit != nullptr ? *w_unit : 1.f;
-        int at[kW];                                        // of the token in this block
-        float unit[kW];
-#pragma unroll
-        for (int i = 0; i < kW; ++i) {
-            at[i] = token[row0 + i * 16] - first - col0;
-            unit[i] = h_unit != nullptr ? h_unit[row0 + i * 16] * w_scale : 1.f;
-        }
-        RowSums r[kW];
-#pragma unroll
-        for (int i = 0; i < kW; ++i) {
-            auto z = [&](int j, int t) __attribute__((always_inline)) {
-                const float x = accumulator(acc[i][j][t]);
-                return kWhole || col0 + j * 16 + quarter * 4 + t < columns ? x : -__builtin_huge_valf();
-            };
-            float m = -__builtin_huge_valf();
-#pragma unroll
-            for (int j = 0; j < kW; ++j) {
-                m = max3(z(j, 0), z(j, 1), m);
-                m = max3(z(j, 2), z(j, 3), m);
-            }
-            r[i] = sums_of<kW>(m, c * unit[i], z);
-            if (!kWhole && m == -__builtin_huge_valf()) r[i].s = r[i].t = 0.f;       // no column of this lane's
-            r[i].m = m * unit[i];
-            if (__any(at[i] >= 0 && at[i] < RW)) {
-                float x = 0.f;
-#pragma unroll
-                for (int j = 0; j < kW; ++j)
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) x = at[i] == j * 16 + quarter * 4 + t ? z(j, t) : x;
-                if (at[i] >= 0 && at[i] < RW && at[i] % 16 / 4 == quarter) token_z[row0 + i * 16] = x * unit[i];
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (int off = 16; off <= 32; off *= 2)
-#pragma unroll
-            for (int i = 0; i < kW; ++i)
-                merge(r[i], RowSums{__shfl_xor(r[i].m, off, 64), __shfl_xor(r[i].s, off, 64), __shfl_xor(r[i].t, off, 64)}, c);
-#pragma unroll
-        for (int i = 0; i < kW; ++i)
-            if (quarter == i % 4) out.of[(first_part + col0 / RW) * out.ld + row0 + i * 16] = f32x4{r[i].m, r[i].s, r[i].t, 0.f};
-    }
-};
-
-struct RowResults {
-    float *logp, *lse, *entropy;
-};
 // Results of a row from its parts: kRows rows a workgroup, the other threads parts of them.
 template <int kRows>
 __global__ __launch_bounds__(256) void linear_join(LinearRows in, const int32_t* slot_of, PartSums parts, const float* token_z, float inv_t,
@@ -630,6 +515,8 @@ ForwardPlan plan_forward(void* workspace, int rows, const WeightSource& src) {
     } else {
         f.slots = carve_slots(c, rows, src.d, src.dtype);
         f.columns = src.in_place ? src.V : copy_columns(src);
+        // (a launch has fewer than 2^32 threads: 2^22 small tiles leave room)
+        f.columns = (int)std::min<int64_t>(f.columns, std::max<int64_t>(kTileN, ((int64_t)1 << 36) / f.slots.padded / kTileN * kTileN));
         f.copy = carve_weight(c, src, f.columns);
         f.tile = rows <= 128 ? kSmallTile : tile_for(f.slots.padded, round_up(std::min(f.columns, src.V), kTileN), 1);
         // (pieces are multiples of 256 columns, so only the last one ends inside a wavefront's block)
