@@ -13,7 +13,8 @@
  *
  * and, to complete the actor update, pcm_adamw_clip_step applies the gradients (App. D).
  * Around it, for policies over any vocabulary and as an optimizer for matrices: pcm_token_logprobs and its gradient,
- * pcm_orthogonalise and pcm_muon_step.
+ * pcm_orthogonalise and pcm_muon_step; for a policy's last layer and its whole set of parameters: pcm_linear_logprobs and its gradient,
+ * pcm_adamw_many_step.
  *
  * Conventions common to every entry point
  *   - Return value: PCM_OK or a negative pcm_status.  Nothing throws, aborts or prints.
@@ -548,7 +549,7 @@ PCM_API int pcm_muon_step(int n_tensors, const int* rows, const int* cols, const
  *
  *   hidden    device [rows] rows of d values of dtype (PCM_F32 or PCM_BF16), hidden_ld >= d values apart
  *   weight    device, of dtype: PCM_WEIGHT_IN_OUT d rows of V values, PCM_WEIGHT_OUT_IN V rows of d values, weight_ld apart.  bf16 weights are read
- *             where they are if their address is a multiple of 16 bytes and weight_ld and the length of a row of 8 values, else by way of the workspace
+ *             where they are if their address is a multiple of 16 bytes and weight_ld (below 2^23) and the length of a row of 8 values, else by way of the workspace
  *   tokens    device [rows] of token_type; a token >= V counts as V-1
  *   temperature  finite, at least 2^-126
  *   logp, lse device f32 [rows];  entropy device f32 [rows] or NULL
@@ -567,7 +568,7 @@ PCM_API int pcm_muon_step(int n_tensors, const int* rows, const int* cols, const
  *   dhidden          device [rows] rows of d values of dtype, dhidden_ld apart, or NULL; zeros for rows without a token
  *   dweight          device, layout of weight, dweight_ld apart, of dweight_dtype (PCM_F32, or PCM_BF16 for bf16 weights), or NULL.  The
  *                    sum over all rows is formed in fp32 and rounded once.  accumulate != 0 (PCM_F32 only): it is added to what is there
- * Not both NULL.  Values between rows are left as they are.
+ * Not both NULL.  Values between rows are left as they are.  Results may not share memory with what is read.
  * ------------------------------------------------------------------------------------------ */
 typedef enum { PCM_WEIGHT_IN_OUT = 0, PCM_WEIGHT_OUT_IN = 1 } pcm_weight_layout;
 PCM_API size_t pcm_linear_logprobs_workspace_bytes(int64_t rows, int d, int V, int dtype, int weight_layout, const void* weight,

@@ -216,7 +216,7 @@ template <bool kThirds>
 void backward(const BackwardPlan& b, const WeightSource& src, int rows, float c, const BackwardOut& out, hipStream_t s) {
     for (int first = 0; first < src.V; first += b.columns) {
         const int columns = std::min(b.columns, src.V - first);
-        const WeightOperand w = weight_piece(src, b.copy, first, columns, s);
+        const WeightOperand w = weight_operand(src, b.copy, first, columns, s);
         if (src.layout == PCM_WEIGHT_OUT_IN) {
             logit_gradient<kThirds, kRowsByK>(b, src, w, rows, first, columns, c, s);
             piece_gradients<kThirds, kKByRows>(b, src, w, first, columns, out, s);
@@ -283,8 +283,7 @@ PCM_API int pcm_linear_logprobs_backward(const void* hidden, int64_t hidden_ld, 
     b.grads.dh_ld = dhidden_ld;
     const BackwardOut out{dhidden, dhidden_ld, dweight, dweight_ld, dweight_dtype, accumulate};
     StageTimer t(ST_LINEAR_LOGPROBS_GRAD, s);
-    gather_slots(in, b.slots, &b.grads, dtype, s);
-    prepare_weight(src, b.copy, s);
+    prepare_operands(in, b.slots, &b.grads, src, b.copy, b.columns, s);
     if (dtype == PCM_F32) backward<true>(b, src, (int)rows, c, out, s);
     else backward<false>(b, src, (int)rows, c, out, s);
     return launch_status();

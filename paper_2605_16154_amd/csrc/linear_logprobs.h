@@ -44,13 +44,19 @@ struct SlotGradients {
     SlotGradient* of;                // [padded]
     // fp32
     int32_t* z_shift;                // [padded]: a row of dz is held times 2^z_shift
+    int32_t* exponent;               // [padded]: of h 2^-z_shift (short lists only, else the largest is gathered in slots.most)
     half_bits *w_h, *w_h_low;        // [padded, d64]: h 2^(14 - most - z_shift): what dz is multiplied with for dW
     void* dh;                        // [rows], dh_ld apart, or null: rows without a token are made zeros
     int64_t dh_ld;
 };
 
 constexpr int kCountRows = 1024;
-constexpr int kFewRows = 16;         // rows up to which the projection streams past them instead of being multiplied in tiles
+// Rows that the projection streams past, 16 at a time, instead of being multiplied in tiles.  Calls with rows in bf16, streamed / in tiles: 16 rows of
+// 1024 -> 32003 21 / 43 us ([d, V]) and 21 / 26 ([V, d]), of 4096 -> 65536 100 / 115 and 122 / 140.  fp32 rows in tiles need the weight as pairs first, so more
+// of them stream: 64 of 1024 -> 32003 66 / 106 ([d, V]) and 91 / 104 ([V, d]), 100 104 / 106 and 152 / 103; 64 of 4096 -> 65536 451 / 1004 and
+// 653 / 1095, 100 745 / 1006 and 1078 / 1093.
+constexpr int kFewRows = 16;
+inline int few_rows_most(int dtype, int layout) { return dtype != PCM_F32 ? kFewRows : layout == 1 ? 64 : 96; }
 constexpr int kAbsmaxParts = 1024;
 constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -64,9 +70,41 @@ struct WeightSource {
 struct WeightCopy {
     half_bits *w, *low;
     int64_t ld;
-    float* absmax;                   // fp32: [kAbsmaxParts]
+    float* absmax;                   // fp32: [absmax_parts]
+    int absmax_parts;
     float* unit;                     // fp32: [1]: what the pairs are to be multiplied by
     int columns;
+};
+// Rows of a matrix by workgroups of 256: 2^lanes neighbours of `each` values in a row, the other threads rows; a row in `chunks`.
+struct RowSplit {
+    int lanes, chunks, blocks;
+    RowSplit() = default;
+    RowSplit(int rows, int64_t cols, int each) {
+        lanes = 0;
+        while (lanes < 8 && ((int64_t)each << lanes) < cols) ++lanes;
+        chunks = (int)((cols + ((int64_t)each << lanes) - 1) / ((int64_t)each << lanes));
+        blocks = ((rows + (256 >> lanes) - 1) >> (8 - lanes)) * chunks;
+    }
+};
+// The largest size of a value of the weight, part by part.
+struct WeightAbsmax {
+    const float* w;
+    int64_t ld;
+    int rows, cols, parts;
+    RowSplit split;
+    float* out;
+};
+// A piece of the weight to its copy, zeros behind its columns up to ld_to.
+struct WeightPiece {
+    const void* w;
+    int64_t ld;
+    int rows, cols;
+    half_bits *to, *low;
+    int64_t ld_to;
+    RowSplit split;
+    const float* absmax;             // fp32
+    int absmax_parts;
+    float* unit;
 };
 // A piece of the columns of the vocabulary as an operand.
 struct WeightOperand {
@@ -78,14 +116,15 @@ inline int round_up(int x, int to) { return (x + to - 1) / to * to; }
 
 Slots carve_slots(Carver& c, int rows, int d, int dtype);
 SlotGradients carve_gradients(Carver& c, const Slots& slots, int dtype);
-// Rows to slots; hidden rows, and what reaches them, to the slots' matrices.
-void gather_slots(const LinearRows& in, const Slots& slots, const SlotGradients* grads, int dtype, hipStream_t s);
 WeightSource weight_source(const void* w, int64_t ld, int dtype, int layout, int d, int V);
 // columns: of the pieces that the caller works in.
 WeightCopy carve_weight(Carver& c, const WeightSource& src, int columns);
 int copy_columns(const WeightSource& src);               // of a piece that is copied
-void prepare_weight(const WeightSource& src, const WeightCopy& copy, hipStream_t s);     // once per call
-WeightOperand weight_piece(const WeightSource& src, const WeightCopy& copy, int first, int columns, hipStream_t s);
+// Rows to slots; hidden rows, and what reaches them, to the slots' matrices; the first `columns` of the weight to their copy, if it needs one.
+void prepare_operands(const LinearRows& in, const Slots& slots, const SlotGradients* grads, const WeightSource& src, const WeightCopy& copy, int columns,
+                      hipStream_t s);
+// The operand of a piece, copied if it has to be and is not the first one.
+WeightOperand weight_operand(const WeightSource& src, const WeightCopy& copy, int first, int columns, hipStream_t s);
 
 // What both entry points ask of their common arguments.
 int check_linear(const void* hidden, int64_t hidden_ld, const void* weight, int64_t weight_ld, int layout, int dtype, const void* tokens,

@@ -4,7 +4,7 @@
 //   products   z = h W on the matrix cores; the epilogue turns a wavefront's block of logits into three numbers per row: largest logit, sum of
 //              2^a and of 2^a a, a = (z - largest) log2 e / temperature; the token's logit is written down where it passes by
 //   join       the blocks of a row -> log-sum-exp, log p, entropy
-// Up to 16 rows the projection is streamed once past rows in registers (few_rows), bound by its bytes.
+// Few rows (few_rows_most) have the projection streamed past them, 16 in the registers of a wavefront, bound by its bytes.
 #include "linear_epilogues.h"
 
 #include <type_traits>
@@ -46,15 +46,10 @@ __global__ __launch_bounds__(256) void linear_counts(LinearRows in, int32_t* cou
 }
 
 constexpr int kNoExponent = -(1 << 20);
-// 1024 rows a workgroup, four neighbours a thread.  Where its rows begin among the slots it counts itself, from the tokens or, for long
-// lists, from the counts of the launch before.
+// Long lists: 1024 rows a workgroup, four neighbours a thread; where its rows begin among the slots it adds up from the counts of the launch before.
 __global__ __launch_bounds__(256) void linear_slots(LinearRows in, Slots slots) {
     int before = 0;
-    if (slots.counts != nullptr) {
-        for (int b = threadIdx.x; b < (int)blockIdx.x; b += 256) before += slots.counts[b];
-    } else {
-        for (int row = threadIdx.x; row < (int)blockIdx.x * kCountRows; row += 256) before += token_at(in, row) >= 0;
-    }
+    for (int b = threadIdx.x; b < (int)blockIdx.x; b += 256) before += slots.counts[b];
     before = block_count(before);
     const int first = blockIdx.x * kCountRows + threadIdx.x * 4;
     int token[4], mine = 0;
@@ -98,6 +93,14 @@ __device__ inline float wave_max(float x) {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor(x, off, 64));
     return x;
+}
+__device__ inline float block_max(float x) {          // over 256 threads, in every thread
+    __shared__ float lds[4];
+    x = wave_max(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
 }
 // The power of two that brings values below 2^(exponent + 1) below 2^15.
 __device__ inline int shift_for(int exponent) { return min(126, max(-126, 14 - exponent)); }
@@ -152,9 +155,9 @@ __device__ inline void zero_row(half_bits* to, int d64, int lane) {
 // 5 us so instead of 8 in two launches).
 constexpr int kGatherRows = 4;                        // per workgroup
 template <class T, bool kList>
-__global__ __launch_bounds__(256) void linear_gather(LinearRows in, Slots slots, SlotGradients grads) {
+__device__ __forceinline__ void gather_rows(const LinearRows& in, const Slots& slots, const SlotGradients& grads, int block) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int first = blockIdx.x * kGatherRows, row = first + wave;
+    const int first = block * kGatherRows, row = first + wave;
     int before = 0, token = -1;
     if (kList) {
         for (int i = threadIdx.x; i < min(first, in.rows); i += 256) before += token_at(in, i) >= 0;
@@ -227,16 +230,26 @@ __global__ __launch_bounds__(256) void linear_gather(LinearRows in, Slots slots,
         of.g = ldexpf(of.g, shift);
         of.h = ldexpf(of.h, shift);
         grads.z_shift[slot] = shift;
-        // (the largest of whole numbers: their order does not matter)
-        if (bound > 0.f && largest > 0.f) atomicMax(slots.most, exponent_of(largest) - shift);
+        const int exponent = bound > 0.f && largest > 0.f ? exponent_of(largest) - shift : kNoExponent;
+        if (kList) grads.exponent[slot] = exponent;
+        else if (exponent > kNoExponent) atomicMax(slots.most, exponent);        // (the largest of whole numbers: their order does not matter)
     }
     grads.of[slot] = of;
 }
 
 // h 2^(14 - most - z_shift) as pairs: dz 2^z_shift times it adds up over rows of any sizes.
-__global__ __launch_bounds__(256) void linear_weigh(LinearRows in, Slots slots, SlotGradients grads) {
-    const int lane = threadIdx.x & 63, row = blockIdx.x * kGatherRows + (int)(threadIdx.x >> 6);
-    const int live = *slots.live, most = *slots.most;
+__device__ __forceinline__ void weigh_rows(const LinearRows& in, const Slots& slots, const SlotGradients& grads, int block) {
+    const int lane = threadIdx.x & 63, row = block * kGatherRows + (int)(threadIdx.x >> 6);
+    const int live = *slots.live;
+    int most;
+    if (slots.counts == nullptr) {                        // a short list: each workgroup looks for the largest exponent itself
+        float x = (float)kNoExponent;
+        for (int i = threadIdx.x; i < live; i += 256) x = fmaxf(x, (float)grads.exponent[i]);
+        most = (int)block_max(x);
+        if (block == 0 && threadIdx.x == 0) *slots.most = most;
+    } else {
+        most = *slots.most;
+    }
     if (row >= in.rows) {
         const int slot = live + row - in.rows;
         if (slot >= min(slots.padded, (live + 255) / 256 * 256)) return;
@@ -253,51 +266,70 @@ __global__ __launch_bounds__(256) void linear_weigh(LinearRows in, Slots slots, 
 
 // ---- weights that have to be copied ----------------------------------------------------------------
 
-// 4096 values of a row at a time.
-__global__ __launch_bounds__(256) void linear_absmax(const float* w, int64_t ld, int rows, int cols, float* parts) {
-    const int per_row = (cols + 4095) / 4096;
+__device__ __forceinline__ void absmax_part(const WeightAbsmax& q, int block) {
+    const int lanes = q.split.lanes, chunks = q.split.chunks;
     float most = 0.f;
-    for (int64_t at = blockIdx.x; at < (int64_t)rows * per_row; at += gridDim.x) {
-        const int row = (int)(at / per_row), i = (int)(at % per_row) * 4096 + threadIdx.x * 4;
+    for (int at = block; at < q.split.blocks; at += q.parts) {
+        const int row = (at / chunks << (8 - lanes)) + (int)(threadIdx.x >> lanes);
+        const int64_t i = (((int64_t)(at % chunks) << (lanes + 2)) + (threadIdx.x & ((1 << lanes) - 1))) * 4;       // four loads, 4 << lanes apart
+        if (row >= q.rows) continue;
         f32x4 x[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) x[q] = i + q * 1024 < cols ? load_4(w + row * ld + i + q * 1024, cols - i - q * 1024) : f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int e = 0; e < 4; ++e) {
+            const int64_t c = i + ((int64_t)e << (lanes + 2));
+            x[e] = c < q.cols ? load_4(q.w + row * q.ld + c, (int)(q.cols - c)) : f32x4{0.f, 0.f, 0.f, 0.f};
+        }
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            most = fmaxf(fmaxf(most, fmaxf(finite_abs(x[q][0]), finite_abs(x[q][1]))), fmaxf(finite_abs(x[q][2]), finite_abs(x[q][3])));
+        for (int e = 0; e < 4; ++e)
+            most = fmaxf(fmaxf(most, fmaxf(finite_abs(x[e][0]), finite_abs(x[e][1]))), fmaxf(finite_abs(x[e][2]), finite_abs(x[e][3])));
     }
-    most = wave_max(most);
-    __shared__ float lds[4];
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = most;
-    __syncthreads();
-    if (threadIdx.x == 0) parts[blockIdx.x] = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+    most = block_max(most);
+    if (threadIdx.x == 0) q.out[block] = most;
 }
-__global__ __launch_bounds__(kAbsmaxParts) void linear_unit(const float* parts, int n, float* unit) {
-    float most = wave_max(threadIdx.x < (unsigned)n ? parts[threadIdx.x] : 0.f);
-    __shared__ float lds[kAbsmaxParts / 64];
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = most;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    for (int w = 0; w < kAbsmaxParts / 64; ++w) most = fmaxf(most, lds[w]);
-    *unit = most > 0.f ? ldexpf(1.f, -shift_for(exponent_of(most))) : 1.f;
-}
-// rows x cols of the source to rows of ld_to, zeros behind cols; a workgroup takes 2048 values of a row.
 template <class T>
-__global__ __launch_bounds__(256) void linear_copy(const T* w, int64_t ld, int rows, int cols, half_bits* to, half_bits* low, int64_t ld_to,
-                                                   const float* unit) {
-    const int row = blockIdx.y * 65535 + blockIdx.z;
-    const int i = blockIdx.x * 2048 + threadIdx.x * 8;
-    if (row >= rows || i >= ld_to) return;
-    const T* const from = w + row * ld + i;
-    const int n = cols - i;
-    half_bits* const out = to + row * ld_to + i;
+__device__ __forceinline__ void copy_piece(const WeightPiece& q, int block) {
+    float scale = 1.f;
+    if constexpr (sizeof(T) == 4) {
+        float most = 0.f;
+        for (int i = threadIdx.x; i < q.absmax_parts; i += 256) most = fmaxf(most, q.absmax[i]);
+        most = block_max(most);
+        const int shift = most > 0.f ? shift_for(exponent_of(most)) : 0;
+        scale = ldexpf(1.f, shift);
+        if (block == 0 && threadIdx.x == 0) *q.unit = ldexpf(1.f, -shift);
+    }
+    const int lanes = q.split.lanes, row = (block / q.split.chunks << (8 - lanes)) + (int)(threadIdx.x >> lanes);
+    const int64_t i = (((int64_t)(block % q.split.chunks) << lanes) + (threadIdx.x & ((1 << lanes) - 1))) * 8;
+    if (row >= q.rows || i >= q.ld_to) return;
+    const T* const from = static_cast<const T*>(q.w) + row * q.ld + i;
+    const int n = (int)(q.cols - i);
+    half_bits* const out = q.to + row * q.ld_to + i;
     if constexpr (sizeof(T) == 2) {
         *reinterpret_cast<u32x4*>(out) = load_16B(from, n);
     } else {
-        const float scale = 1.f / *unit;                  // a power of two
         const f32x4 a = load_4(from, n), b = load_4(from + 4, n - 4);
-        store_pairs(out, low + row * ld_to + i, [&](int e) { return (e < 4 ? a[e] : b[e - 4]) * scale; });
+        store_pairs(out, q.low + row * q.ld_to + i, [&](int e) { return (e < 4 ? a[e] : b[e - 4]) * scale; });
     }
+}
+
+// ---- before the products: two launches at most, of work that does not wait for one another ------------------
+
+// Rows to slots, and beside it the largest value of an fp32 weight or the first piece of a bf16 one.
+template <class T, bool kList>
+__global__ __launch_bounds__(256) void linear_gather(LinearRows in, Slots slots, SlotGradients grads, int rows_blocks, WeightAbsmax absmax, WeightPiece piece) {
+    const int block = blockIdx.x;
+    if (block < rows_blocks) return gather_rows<T, kList>(in, slots, grads, block);
+    if constexpr (sizeof(T) == 4) absmax_part(absmax, block - rows_blocks);
+    else copy_piece<T>(piece, block - rows_blocks);
+}
+// fp32: rows weighted for dW, and the first piece of the weight.
+__global__ __launch_bounds__(256) void linear_weigh(LinearRows in, Slots slots, SlotGradients grads, int rows_blocks, WeightPiece piece) {
+    const int block = blockIdx.x;
+    if (block < rows_blocks) return weigh_rows(in, slots, grads, block);
+    copy_piece<float>(piece, block - rows_blocks);
+}
+template <class T>
+__global__ __launch_bounds__(256) void linear_copy(WeightPiece piece) {
+    copy_piece<T>(piece, blockIdx.x);
 }
 
 // ---- joining the parts -------------------------------------------------------------------------------
@@ -346,23 +378,38 @@ __global__ __launch_bounds__(256) void linear_join(LinearRows in, const int32_t*
 
 // ---- few rows --------------------------------------------------------------------------------------
 
+// The 16 bytes of a row of d values that begin at value k, zeros behind its end; the row is that long at least, and nothing outside it is read.
+template <class T>
+__device__ __forceinline__ u32x4 load_tail(const T* row, int k, int d) {
+    constexpr int kE = 16 / sizeof(T);
+    const int from = min(k, d - kE), drop = (k - from) * (int)sizeof(T) * 8;        // bits that belong before k
+    const u32x4 x = load_16B(row + from, kE);
+    const uint64_t lo = (uint64_t)x[1] << 32 | x[0], hi = (uint64_t)x[3] << 32 | x[2];
+    const uint64_t l = drop == 0 ? lo : drop < 64 ? lo >> drop | hi << (64 - drop) : drop < 128 ? hi >> (drop - 64) : 0;
+    const uint64_t h = drop < 64 ? hi >> drop : 0;
+    return u32x4{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+}
+
 // z of up to 16 rows and a block of the vocabulary.  The four wavefronts of a workgroup take every fourth slice of the reduction index, their sums
 // are added in LDS.  A slice is 4 lane groups x kE values of k (kE = 16 bytes of them).
 //   [V][d]: a lane brings in kE values of k of one column and is its fragment; four fragments of 16 columns share one of the hidden rows.
 //   [d][V]: a lane brings in kE columns at kE values of k and has the fragments of kE columns, bf16 after exchanging halves between pairs of rows.
+// More than 16 rows are groups of 16 whose workgroups follow one another on an XCD, so that the projection comes out of its cache after the first.
 template <class T, int kLayout>
-__global__ __launch_bounds__(256) void few_rows(LinearRows in, const T* w, int64_t ld, PartSums out, float* token_z, float c) {
+__global__ __launch_bounds__(256) void few_rows(LinearRows in, const T* w, int64_t ld, PartSums out, float* token_z, float c, int groups) {
     constexpr int kE = 16 / sizeof(T), kSlice = 4 * kE;
     constexpr int kTiles = kLayout == PCM_WEIGHT_OUT_IN ? 4 : kE, kLoads = kLayout == PCM_WEIGHT_OUT_IN ? 4 : kE;
     constexpr int kColumns = kTiles * 16;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane >> 4, at = lane & 15;
-    const int n0 = blockIdx.x * kColumns;
+    const int block = blockIdx.x / (kNumXcd * groups) * kNumXcd + blockIdx.x % kNumXcd, row0 = blockIdx.x / kNumXcd % groups * kFewRows;
+    const int n0 = block * kColumns;
+    if (n0 >= in.V) return;
     f32x4 acc[kTiles];
 #pragma unroll
     for (int j = 0; j < kTiles; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     // (lanes of rows that are not there take the last one's values along)
-    const T* const h_row = static_cast<const T*>(in.hidden) + min(at, in.rows - 1) * in.ld;
-    const bool has_row = at < in.rows;
+    const T* const h_row = static_cast<const T*>(in.hidden) + min(row0 + at, in.rows - 1) * in.ld;
+    const bool has_row = row0 + at < in.rows;
     // [d][V]: where the vocabulary ends lanes move back to its last kE columns and count those that are their own.
     const bool moves = kLayout == PCM_WEIGHT_IN_OUT && in.V >= kE;
     auto first_column = [&](int lane_of_16) { return moves ? min(n0 + lane_of_16 * kE, in.V - kE) : n0 + lane_of_16 * kE; };
@@ -377,8 +424,22 @@ __global__ __launch_bounds__(256) void few_rows(LinearRows in, const T* w, int64
             x.w[q] = load_16B(kLayout == PCM_WEIGHT_OUT_IN ? w + min(n0 + q * 16 + at, in.V - 1) * ld + k : w + (k + q) * ld + first_column(at), kE);
         x.h = load_16B(h_row + k, kE);
     };
+    // the slice in which k ends: rows that are shorter than 16 bytes are read value by value
+    const bool shifts = in.d >= kE && (kLayout == PCM_WEIGHT_OUT_IN || moves);
     auto load_edge = [&](Slice& x, int k0) __attribute__((always_inline)) {
         const int k = k0 + group * kE;
+        if (shifts) {
+#pragma unroll
+            for (int q = 0; q < kLoads; ++q) {
+                if (kLayout == PCM_WEIGHT_OUT_IN) x.w[q] = load_tail(w + min(n0 + q * 16 + at, in.V - 1) * ld, k, in.d);
+                else {
+                    x.w[q] = load_16B(w + min(k + q, in.d - 1) * ld + first_column(at), kE);
+                    if (k + q >= in.d) x.w[q] = u32x4{0, 0, 0, 0};
+                }
+            }
+            x.h = load_tail(h_row, k, in.d);
+            return;
+        }
 #pragma unroll
         for (int q = 0; q < kLoads; ++q) {
             const int v = kLayout == PCM_WEIGHT_OUT_IN ? n0 + q * 16 + at : first_column(at), row = kLayout == PCM_WEIGHT_OUT_IN ? k : k + q;
@@ -440,7 +501,7 @@ __global__ __launch_bounds__(256) void few_rows(LinearRows in, const T* w, int64
     __syncthreads();
     // a lane has row `at` and, of tile j, columns 4 group + t of 16
     constexpr int kMine = kTiles / 4;
-    const int token = has_row ? token_at(in, at) : -1;
+    const int token = has_row ? token_at(in, row0 + at) : -1;
     float z[kMine][4], m = -__builtin_huge_valf();
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
@@ -452,7 +513,7 @@ __global__ __launch_bounds__(256) void few_rows(LinearRows in, const T* w, int64
             const bool own = v < in.V && (kLayout == PCM_WEIGHT_OUT_IN || v >= n0 + column * kE);
             z[i][t] = own ? total[t] : -__builtin_huge_valf();
             m = fmaxf(m, z[i][t]);
-            if (own && v == token) token_z[at] = z[i][t];
+            if (own && v == token) token_z[row0 + at] = z[i][t];
         }
     }
     m = fmaxf(m, __shfl_xor(m, 16, 64));
@@ -476,15 +537,17 @@ __global__ __launch_bounds__(256) void few_rows(LinearRows in, const T* w, int64
     if (threadIdx.x >= 16 || !has_row) return;
     RowSums a = part[0][at];
     for (int q = 1; q < 4; ++q) merge(a, part[q][at], c);
-    out.of[blockIdx.x * out.ld + at] = f32x4{a.m, a.s, a.t, 0.f};
+    out.of[block * out.ld + row0 + at] = f32x4{a.m, a.s, a.t, 0.f};
 }
 
 int few_columns(int dtype, int layout) { return layout == PCM_WEIGHT_OUT_IN || dtype == PCM_F32 ? 64 : 128; }
 template <class T>
 void launch_few(const LinearRows& in, const void* w, int64_t ld, int layout, const PartSums& parts, float* token_z, float c, hipStream_t s) {
     const T* const p = static_cast<const T*>(w);
-    if (layout == PCM_WEIGHT_OUT_IN) few_rows<T, PCM_WEIGHT_OUT_IN><<<(unsigned)parts.parts, 256, 0, s>>>(in, p, ld, parts, token_z, c);
-    else few_rows<T, PCM_WEIGHT_IN_OUT><<<(unsigned)parts.parts, 256, 0, s>>>(in, p, ld, parts, token_z, c);
+    const int groups = ceil_div(in.rows, kFewRows);
+    const unsigned grid = (unsigned)(groups == 1 ? parts.parts : round_up(parts.parts, kNumXcd) * groups);
+    if (layout == PCM_WEIGHT_OUT_IN) few_rows<T, PCM_WEIGHT_OUT_IN><<<grid, 256, 0, s>>>(in, p, ld, parts, token_z, c, groups);
+    else few_rows<T, PCM_WEIGHT_IN_OUT><<<grid, 256, 0, s>>>(in, p, ld, parts, token_z, c, groups);
 }
 
 // ---- the forward call --------------------------------------------------------------------------------
@@ -508,10 +571,10 @@ struct ForwardPlan {
 ForwardPlan plan_forward(void* workspace, int rows, const WeightSource& src) {
     Carver c(workspace);
     ForwardPlan f{};
-    f.few = rows <= kFewRows;
+    f.few = rows <= few_rows_most(src.dtype, src.layout);
     if (f.few) {
         f.parts = carve_parts(c, rows, ceil_div(src.V, few_columns(src.dtype, src.layout)));
-        f.token_z = c.take<float>(kFewRows);
+        f.token_z = c.take<float>((size_t)rows);
     } else {
         f.slots = carve_slots(c, rows, src.d, src.dtype);
         f.columns = src.in_place ? src.V : copy_columns(src);
@@ -531,7 +594,7 @@ template <bool kThirds>
 void forward_products(const ForwardPlan& f, const WeightSource& src, int rows, float c, hipStream_t s) {
     for (int first = 0; first < src.V; first += f.columns) {
         const int columns = std::min(f.columns, src.V - first);
-        const WeightOperand w = weight_piece(src, f.copy, first, columns, s);
+        const WeightOperand w = weight_operand(src, f.copy, first, columns, s);
         BoundedProblem<kThirds> p = slot_product<kThirds>(f.slots, kRowsAreM);
         p.M = rows <= 128 ? 128 : f.slots.padded;
         set_a(p, f.slots.h, f.slots.h_low, f.slots.d64);
@@ -577,34 +640,17 @@ SlotGradients carve_gradients(Carver& c, const Slots& slots, int dtype) {
     if (dtype == PCM_F32) {
         const size_t h = (size_t)slots.padded * slots.d64 + kTileM;
         g.z_shift = c.take<int32_t>((size_t)slots.padded);
+        g.exponent = c.take<int32_t>((size_t)slots.padded);
         g.w_h = c.take<half_bits>(h);
         g.w_h_low = c.take<half_bits>(h);
     }
     return g;
 }
-void gather_slots(const LinearRows& in, const Slots& slots, const SlotGradients* grads, int dtype, hipStream_t s) {
-    const unsigned lists = (unsigned)ceil_div(in.rows, kCountRows), blocks = (unsigned)ceil_div(in.rows + kTileM, kGatherRows);
-    const SlotGradients g = grads != nullptr ? *grads : SlotGradients{};
-    // (the exponent that fp32 gradients gather begins with the list)
-    const bool own_list = slots.counts == nullptr && !(dtype == PCM_F32 && grads != nullptr);
-    if (!own_list) {
-        if (slots.counts != nullptr) linear_counts<<<lists, 256, 0, s>>>(in, slots.counts);
-        linear_slots<<<lists, 256, 0, s>>>(in, slots);
-    }
-    if (dtype == PCM_F32) {
-        if (own_list) linear_gather<float, true><<<blocks, 256, 0, s>>>(in, slots, g);
-        else linear_gather<float, false><<<blocks, 256, 0, s>>>(in, slots, g);
-        if (grads != nullptr) linear_weigh<<<blocks, 256, 0, s>>>(in, slots, g);
-    } else {
-        if (own_list) linear_gather<half_bits, true><<<blocks, 256, 0, s>>>(in, slots, g);
-        else linear_gather<half_bits, false><<<blocks, 256, 0, s>>>(in, slots, g);
-    }
-}
-
 WeightSource weight_source(const void* w, int64_t ld, int dtype, int layout, int d, int V) {
     const int length = layout == PCM_WEIGHT_OUT_IN ? d : V;
     return WeightSource{w, ld, dtype, layout, d, V,
-                        dtype == PCM_BF16 && (reinterpret_cast<uintptr_t>(w) & 15u) == 0 && ld % 8 == 0 && length % 8 == 0};
+                        // (256 rows of a tile are addressed with 32 bits)
+                        dtype == PCM_BF16 && (reinterpret_cast<uintptr_t>(w) & 15u) == 0 && ld % 8 == 0 && length % 8 == 0 && ld < (1 << 23)};
 }
 // Pieces of at most 256 MB, in whole tiles.
 int copy_columns(const WeightSource& src) {
@@ -620,26 +666,50 @@ WeightCopy carve_weight(Carver& c, const WeightSource& src, int columns) {
     q.w = c.take<half_bits>((size_t)rows * q.ld);
     if (src.dtype == PCM_F32) {
         q.low = c.take<half_bits>((size_t)rows * q.ld);
+        const int rows_all = src.layout == PCM_WEIGHT_OUT_IN ? src.V : src.d, cols = src.layout == PCM_WEIGHT_OUT_IN ? src.d : src.V;
+        q.absmax_parts = std::min(kAbsmaxParts, RowSplit(rows_all, ceil_div(cols, 4), 4).blocks);
         q.absmax = c.take<float>(kAbsmaxParts);
         q.unit = c.take<float>(1);
     }
     return q;
 }
-void prepare_weight(const WeightSource& src, const WeightCopy& copy, hipStream_t s) {
-    if (src.dtype != PCM_F32) return;
-    const int rows = src.layout == PCM_WEIGHT_OUT_IN ? src.V : src.d, cols = src.layout == PCM_WEIGHT_OUT_IN ? src.d : src.V;
-    const int parts = (int)std::min<int64_t>((int64_t)rows * ceil_div(cols, 4096), kAbsmaxParts);
-    linear_absmax<<<(unsigned)parts, 256, 0, s>>>(static_cast<const float*>(src.w), src.ld, rows, cols, copy.absmax);
-    linear_unit<<<1, kAbsmaxParts, 0, s>>>(copy.absmax, parts, copy.unit);
+static WeightPiece piece_of(const WeightSource& src, const WeightCopy& copy, int first, int columns) {
+    const bool by_token = src.layout == PCM_WEIGHT_OUT_IN;
+    const int64_t at = by_token ? first * src.ld : first;
+    const int rows = by_token ? columns : src.d;
+    const void* const w = static_cast<const char*>(src.w) + at * (src.dtype == PCM_F32 ? 4 : 2);
+    return WeightPiece{w, src.ld, rows, by_token ? src.d : columns, copy.w, copy.low, copy.ld, RowSplit(rows, copy.ld, 8), copy.absmax, copy.absmax_parts, copy.unit};
 }
-WeightOperand weight_piece(const WeightSource& src, const WeightCopy& copy, int first, int columns, hipStream_t s) {
-    const int64_t at = src.layout == PCM_WEIGHT_OUT_IN ? first * src.ld : first;
-    if (src.in_place) return WeightOperand{static_cast<const half_bits*>(src.w) + at, nullptr, src.ld};
-    // everything that a bounded product asks for: its rows and its reduction index end with the copy's values
-    const int rows = src.layout == PCM_WEIGHT_OUT_IN ? columns : src.d, cols = src.layout == PCM_WEIGHT_OUT_IN ? src.d : columns;
-    const dim3 grid((unsigned)ceil_div((int)copy.ld, 2048), (unsigned)ceil_div(rows, 65535), (unsigned)std::min(rows, 65535));
-    if (src.dtype == PCM_F32) linear_copy<float><<<grid, 256, 0, s>>>(static_cast<const float*>(src.w) + at, src.ld, rows, cols, copy.w, copy.low, copy.ld, copy.unit);
-    else linear_copy<half_bits><<<grid, 256, 0, s>>>(static_cast<const half_bits*>(src.w) + at, src.ld, rows, cols, copy.w, nullptr, copy.ld, nullptr);
+void prepare_operands(const LinearRows& in, const Slots& slots, const SlotGradients* grads, const WeightSource& src, const WeightCopy& copy, int columns,
+                      hipStream_t s) {
+    const int rows_blocks = ceil_div(in.rows + kTileM, kGatherRows);
+    const SlotGradients g = grads != nullptr ? *grads : SlotGradients{};
+    const bool own_list = slots.counts == nullptr;
+    if (!own_list) {
+        const unsigned lists = (unsigned)ceil_div(in.rows, kCountRows);
+        linear_counts<<<lists, 256, 0, s>>>(in, slots.counts);
+        linear_slots<<<lists, 256, 0, s>>>(in, slots);
+    }
+    const WeightPiece piece = src.in_place ? WeightPiece{} : piece_of(src, copy, 0, std::min(columns, src.V));
+    if (src.dtype == PCM_F32) {
+        const int rows = src.layout == PCM_WEIGHT_OUT_IN ? src.V : src.d, cols = src.layout == PCM_WEIGHT_OUT_IN ? src.d : src.V;
+        const WeightAbsmax absmax{static_cast<const float*>(src.w), src.ld, rows, cols, copy.absmax_parts, RowSplit(rows, ceil_div(cols, 4), 4), copy.absmax};
+        if (own_list) linear_gather<float, true><<<rows_blocks + absmax.parts, 256, 0, s>>>(in, slots, g, rows_blocks, absmax, piece);
+        else linear_gather<float, false><<<rows_blocks + absmax.parts, 256, 0, s>>>(in, slots, g, rows_blocks, absmax, piece);
+        if (grads != nullptr) linear_weigh<<<rows_blocks + piece.split.blocks, 256, 0, s>>>(in, slots, g, rows_blocks, piece);
+        else linear_copy<float><<<piece.split.blocks, 256, 0, s>>>(piece);
+    } else {
+        if (own_list) linear_gather<half_bits, true><<<rows_blocks + piece.split.blocks, 256, 0, s>>>(in, slots, g, rows_blocks, WeightAbsmax{}, piece);
+        else linear_gather<half_bits, false><<<rows_blocks + piece.split.blocks, 256, 0, s>>>(in, slots, g, rows_blocks, WeightAbsmax{}, piece);
+    }
+}
+WeightOperand weight_operand(const WeightSource& src, const WeightCopy& copy, int first, int columns, hipStream_t s) {
+    if (src.in_place) return WeightOperand{static_cast<const half_bits*>(src.w) + (src.layout == PCM_WEIGHT_OUT_IN ? first * src.ld : first), nullptr, src.ld};
+    if (first > 0) {
+        const WeightPiece piece = piece_of(src, copy, first, columns);
+        if (src.dtype == PCM_F32) linear_copy<float><<<piece.split.blocks, 256, 0, s>>>(piece);
+        else linear_copy<half_bits><<<piece.split.blocks, 256, 0, s>>>(piece);
+    }
     return WeightOperand{copy.w, copy.low, copy.ld};
 }
 
@@ -655,7 +725,7 @@ int check_linear(const void* hidden, int64_t hidden_ld, const void* weight, int6
     if (!hidden || !weight || !tokens || (reinterpret_cast<uintptr_t>(hidden) & value) != 0 || (reinterpret_cast<uintptr_t>(weight) & value) != 0 ||
         (reinterpret_cast<uintptr_t>(tokens) & token) != 0)
         return PCM_EINVAL;
-    return rows > (1 << 24) || d > (1 << 16) || V > (1 << 22) || weight_ld > (1 << 24) ? PCM_EUNSUPPORTED : PCM_OK;
+    return rows > (1 << 24) || d > (1 << 16) || V > (1 << 22) ? PCM_EUNSUPPORTED : PCM_OK;
 }
 
 }  // namespace pcm
@@ -695,8 +765,7 @@ PCM_API int pcm_linear_logprobs(const void* hidden, int64_t hidden_ld, const voi
         linear_join<1><<<(unsigned)rows, 256, 0, s>>>(in, nullptr, f.parts, f.token_z, inv_t, out);
         return launch_status();
     }
-    gather_slots(in, f.slots, nullptr, dtype, s);
-    prepare_weight(src, f.copy, s);
+    prepare_operands(in, f.slots, nullptr, src, f.copy, f.columns, s);
     if (dtype == PCM_F32) forward_products<true>(f, src, (int)rows, c, s);
     else forward_products<false>(f, src, (int)rows, c, s);
     linear_join<4><<<(unsigned)ceil_div((int)rows, 4), 256, 0, s>>>(in, f.slots.slot_of, f.parts, f.token_z, inv_t, out);

@@ -235,6 +235,26 @@ void look_at_slots(const Slots& s, int rows, bool thirds, bool units) {
     if (thirds) touches("h, low parts", s.h_low, h, true), touches("units", s.h_unit, (int64_t)s.padded * 4, true);
 }
 
+void look_at_split(const RowSplit& s, int rows, int64_t cols, int each) {
+    if (s.lanes < 0 || s.lanes > 8 || ((int64_t)each * s.chunks << s.lanes) < cols || (int64_t)s.blocks / s.chunks * (256 >> s.lanes) < rows || s.blocks % s.chunks)
+        fail(kernel, "a split that does not cover the rows");
+}
+void look_at_piece(const WeightPiece& p, bool floats, int64_t blocks) {
+    if (p.w == nullptr) {
+        if (blocks != 0 || floats) fail(kernel, "a copy of nothing");
+        return;
+    }
+    ++pieces;
+    touches_rows("weight", p.w, p.rows, p.cols, p.ld, floats ? 4 : 2, false);
+    touches("the copy", p.to, p.rows * p.ld_to * 2, true);
+    if (floats) {
+        touches("the copy, low parts", p.low, p.rows * p.ld_to * 2, true);
+        touches("unit of W", p.unit, 4, true);
+        touches("largest values", p.absmax, (int64_t)p.absmax_parts * 4, false);
+    }
+    look_at_split(p.split, p.rows, p.ld_to, 8);
+    if (p.ld_to < p.cols || p.ld_to % 8 || blocks != p.split.blocks) fail(kernel, "a grid that does not fit the copy");
+}
 void look_at_launch(const std::string& raw, void** args, dim3 grid) {
     std::string name = without_spaces(raw);
     const size_t ends = name.find('<') < name.find('(') ? name.find(inside_angles(name)) + inside_angles(name).size() + 1 : name.find('(');
@@ -270,40 +290,37 @@ void look_at_launch(const std::string& raw, void** args, dim3 grid) {
         const LinearRows& in = *static_cast<LinearRows*>(args[0]);
         const Slots& s = *static_cast<Slots*>(args[1]);
         const SlotGradients& g = *static_cast<SlotGradients*>(args[2]);
-        const bool thirds = has(name, "float") || has(name, "linear_weigh");
+        const int rows_blocks = *static_cast<int*>(args[3]);
+        const bool weighs = has(name, "linear_weigh"), thirds = has(name, "float") || weighs;
         look_at_rows(in, thirds ? 4 : 2);
-        if (has(name, "linear_weigh")) {
+        touches("live", s.live, 4, !weighs);
+        if (weighs) {
             touches("weighted h", g.w_h, (int64_t)s.padded * s.d64 * 2, true);
             touches("weighted h, low parts", g.w_h_low, (int64_t)s.padded * s.d64 * 2, true);
             touches("shifts", g.z_shift, (int64_t)s.padded * 4, false);
-            touches("the exponent", s.most, 4, false);
+            touches("exponents", g.exponent, (int64_t)s.padded * 4, false);
+            touches("the exponent", s.most, 4, true);
+            look_at_piece(*static_cast<WeightPiece*>(args[4]), true, grid.x - rows_blocks);
         } else {
             look_at_slots(s, in.rows, thirds, true);
-            touches("live", s.live, 4, true);
             if (g.of) look_at_grads(g, s, in.rows);
-            if (g.of && thirds) touches("shifts", g.z_shift, (int64_t)s.padded * 4, true), touches("the exponent", s.most, 4, true);
+            if (g.of && thirds) touches("shifts", g.z_shift, (int64_t)s.padded * 4, true), touches("exponents", g.exponent, (int64_t)s.padded * 4, true), touches("the exponent", s.most, 4, true);
             if (g.dh) touches_rows("dhidden", g.dh, in.rows, in.d, g.dh_ld, thirds ? 4 : 2, true);
             rows_of_call = in.rows;
+            if (has(name, "true") != (s.counts == nullptr)) fail(kernel, "a list in the wrong place");
+            if (thirds) {
+                const WeightAbsmax& a = *static_cast<WeightAbsmax*>(args[4]);
+                touches_rows("weight", a.w, a.rows, a.cols, a.ld, 4, false);
+                touches("largest values", a.out, (int64_t)a.parts * 4, true);
+                look_at_split(a.split, a.rows, ((int64_t)a.cols + 3) / 4, 4);
+                if (a.parts < 1 || a.parts > kAbsmaxParts || a.parts != (int)grid.x - rows_blocks) fail(kernel, "a grid that does not fit the weight");
+            } else {
+                look_at_piece(*static_cast<WeightPiece*>(args[5]), false, grid.x - rows_blocks);
+            }
         }
-        if ((int64_t)grid.x * 4 < in.rows + kTileM) fail(kernel, "a grid that does not fit the rows");
-    } else if (has(name, "linear_absmax")) {
-        touches_rows("weight", *static_cast<float**>(args[0]), *static_cast<int*>(args[2]), *static_cast<int*>(args[3]), *static_cast<int64_t*>(args[1]), 4, false);
-        touches("largest values", *static_cast<float**>(args[4]), (int64_t)grid.x * 4, true);
-        if (grid.x > kAbsmaxParts) fail(kernel, "more parts than there is room for");
-    } else if (has(name, "linear_unit")) {
-        const int n = *static_cast<int*>(args[1]);
-        touches("largest values", *static_cast<float**>(args[0]), (int64_t)n * 4, false);
-        touches("unit of W", *static_cast<float**>(args[2]), 4, true);
-        if (n > kAbsmaxParts) fail(kernel, "more parts than threads");
+        if ((int64_t)rows_blocks * 4 < in.rows + kTileM) fail(kernel, "a grid that does not fit the rows");
     } else if (has(name, "linear_copy<")) {
-        ++pieces;
-        const int rows = *static_cast<int*>(args[2]), cols = *static_cast<int*>(args[3]);
-        const int64_t ld_to = *static_cast<int64_t*>(args[6]);
-        touches_rows("weight", *static_cast<void**>(args[0]), rows, cols, *static_cast<int64_t*>(args[1]), has(name, "float") ? 4 : 2, false);
-        touches("the copy", *static_cast<void**>(args[4]), rows * ld_to * 2, true);
-        if (has(name, "float")) touches("the copy, low parts", *static_cast<void**>(args[5]), rows * ld_to * 2, true), touches("unit of W", *static_cast<void**>(args[7]), 4, false);
-        if (ld_to < cols || ld_to % 8 || (int64_t)grid.x * 2048 < ld_to || (int64_t)grid.y * 65535 < rows || (grid.y == 1 && (int)grid.z < rows) || (grid.y > 1 && grid.z != 65535))
-            fail(kernel, "a grid that does not fit the copy");
+        look_at_piece(*static_cast<WeightPiece*>(args[0]), has(name, "float"), grid.x);
     } else if (has(name, "few_rows<")) {
         const LinearRows& in = *static_cast<LinearRows*>(args[0]);
         const PartSums& p = *static_cast<PartSums*>(args[3]);
@@ -312,7 +329,10 @@ void look_at_launch(const std::string& raw, void** args, dim3 grid) {
         touches_rows("weight", *static_cast<void**>(args[1]), by_token ? in.V : in.d, by_token ? in.d : in.V, *static_cast<int64_t*>(args[2]), floats ? 4 : 2, false);
         look_at_parts(p, true);
         touches("logits of tokens", *static_cast<float**>(args[4]), (int64_t)in.rows * 4, true);
-        if (in.rows > 16 || p.ld < in.rows || p.parts != (int)grid.x || (int64_t)grid.x * (by_token || floats ? 64 : 128) < in.V) fail(kernel, "a grid that does not fit the columns");
+        const int groups = *static_cast<int*>(args[6]), blocks = groups == 1 ? (int)grid.x : (int)grid.x / groups;
+        if (groups * kFewRows < in.rows || p.ld < in.rows || p.parts > blocks || (int64_t)p.parts * (by_token || floats ? 64 : 128) < in.V || (groups > 1 && blocks % kNumXcd) ||
+            grid.x % groups)
+            fail(kernel, "a grid that does not fit the rows and columns");
     } else if (has(name, "linear_join<")) {
         const LinearRows& in = *static_cast<LinearRows*>(args[0]);
         const int32_t* slot_of = *static_cast<int32_t**>(args[1]);
@@ -488,6 +508,14 @@ void bounds() {
                         expect(forward(c), PCM_OK);
                         expect(backward(c), PCM_OK);
                     }
+    // rows of the weight far apart
+    for (int layout = 0; layout < 2; ++layout)
+        for (int pad : {(1 << 22), (1 << 23) - 1000 - 8, (1 << 23) - 1000, 1 << 27})
+            for (int dtype : {PCM_F32, PCM_BF16}) {
+                const Linear c{300, 1000, 1000, dtype, layout, 1, pad, 0, true, dtype, 3};
+                expect(forward(c), PCM_OK);
+                expect(backward(c), PCM_OK);
+            }
     // the largest sizes, and many pieces
     for (int layout = 0; layout < 2; ++layout)
         for (int dtype : {PCM_F32, PCM_BF16})
