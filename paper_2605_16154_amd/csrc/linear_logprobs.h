@@ -43,7 +43,7 @@ struct SlotGradients {
     float inv_t;
     SlotGradient* of;                // [padded]
     // fp32
-    int32_t* z_shift;                // [padded]: a row of dz is held times 2^z_shift
+    int32_t* z_shift;                // [padded]: a row of dz is held times 2^z_shift; beyond any number for a row of zeros
     int32_t* exponent;               // [padded]: of h 2^-z_shift (short lists only, else the largest is gathered in slots.most)
     half_bits *w_h, *w_h_low;        // [padded, d64]: h 2^(14 - most - z_shift): what dz is multiplied with for dW
     void* dh;                        // [rows], dh_ld apart, or null: rows without a token are made zeros

@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256) void linear_counts(LinearRows in, int32_t* cou
     if (threadIdx.x == 0) counts[blockIdx.x] = n;
 }
 
-constexpr int kNoExponent = -(1 << 20);
+constexpr int kNoExponent = -(1 << 20), kNoGradient = 1 << 21;
 // Long lists: 1024 rows a workgroup, four neighbours a thread; where its rows begin among the slots it adds up from the counts of the launch before.
 __global__ __launch_bounds__(256) void linear_slots(LinearRows in, Slots slots) {
     int before = 0;
@@ -226,7 +226,8 @@ __device__ __forceinline__ void gather_rows(const LinearRows& in, const Slots& s
     if constexpr (sizeof(T) == 4) {
         // |p (log p + entropy)| is at most the larger of 1 / e and the entropy
         const float bound = fabsf(of.g) + fabsf(of.h) * (0.5f + fabsf(of.entropy));
-        const int shift = bound > 0.f && bound < __builtin_huge_valf() ? shift_for(exponent_of(bound)) : 0;
+        // (a row that no gradient reaches is not weighted by the others' power of two, which may be far too large for it)
+        const int shift = bound == 0.f ? kNoGradient : bound < __builtin_huge_valf() ? shift_for(exponent_of(bound)) : 0;
         of.g = ldexpf(of.g, shift);
         of.h = ldexpf(of.h, shift);
         grads.z_shift[slot] = shift;

@@ -341,3 +341,22 @@ def test_binding_refuses():
                dict(out={"dhidden": h.float()}), dict(accumulate=True, out={"dweight": torch.zeros_like(w)}), dict(temperature=-1.0)):
         with pytest.raises(pcm.PcmError):
             pcm.pcm_linear_logprobs_backward(h, w, t, kw.pop("lse", f), kw.pop("dlogp", f), **kw)
+
+
+@pytest.mark.parametrize("rows", [3, 40, 200, 5000])
+@pytest.mark.parametrize("layout", ["in_out", "out_in"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_with_a_gradient_of_zero_add_nothing(dtype, layout, rows):
+    """However large what they hold is beside the gradients of the others; and no gradient at all is zeros."""
+    import paper_2605_16154_amd as pcm
+    hidden, w, tokens, gen = _inputs(rows, 72, 130, dtype, layout)
+    idle = torch.arange(rows, device="cuda") % 3 == 1
+    hidden[idle] *= 1000
+    fwd = pcm.pcm_linear_logprobs(hidden, w, tokens)
+    g = torch.where(idle, 0.0, 1e-5 * torch.randn(rows, generator=gen, device="cuda"))
+    got = pcm.pcm_linear_logprobs_backward(hidden, w, tokens, fwd["lse"], g, fwd["entropy"], g)
+    assert not got["dhidden"][idle].any() and bool(torch.isfinite(got["dweight"]).all())
+    for name, want, tol in zip(("dhidden", "dweight"), *zip(*_bounds((hidden, w, tokens, gen), g, g, 1.0, dtype))):
+        assert np.all(np.abs(_np(got[name]) - want) <= tol), name
+    none = pcm.pcm_linear_logprobs_backward(hidden, w, tokens, fwd["lse"], 0 * g, fwd["entropy"], 0 * g)
+    assert not none["dhidden"].any() and not none["dweight"].any()
