@@ -545,15 +545,17 @@ PCM_API int pcm_muon_step(int n_tensors, const int* rows, const int* cols, const
  * With x_j = (hidden[r] . weight[:, j]) / temperature, j over the whole vocabulary:
  *   lse = log sum_j e^(x_j);   logp = x_token - lse;   entropy = lse - sum_j p_j x_j with p_j = e^(x_j - lse).
  * A row whose token is negative is left out (prompts, padding): its three results are 0, and what it holds is not met by any other.
- * Products and sums are fp32 or better (PCM_F32: each value as two of 11 significand bits, products of their high and low parts without the last).
+ * Products and sums are fp32 or better (PCM_F32: each value as two of 11 significand bits, products of their high and low parts without the last;
+ * of a value, what is below 2^-39 of the largest in its row of hidden, or in weight, is lost).
  *
  *   hidden    device [rows] rows of d values of dtype (PCM_F32 or PCM_BF16), hidden_ld >= d values apart
  *   weight    device, of dtype: PCM_WEIGHT_IN_OUT d rows of V values, PCM_WEIGHT_OUT_IN V rows of d values, weight_ld apart.  bf16 weights are read
- *             where they are if their address is a multiple of 16 bytes and weight_ld (below 2^23) and the length of a row of 8 values, else by way of the workspace
+ *             where they are if their address is a multiple of 16 bytes, weight_ld (below 2^23) and the length of a row are multiples of 8 values and
+ *             there is no gap between rows whose length is not one of 64, else by way of the workspace
  *   tokens    device [rows] of token_type; a token >= V counts as V-1
  *   temperature  finite, at least 2^-126
  *   logp, lse device f32 [rows];  entropy device f32 [rows] or NULL
- * A NaN or +inf among the logits makes the row's results NaN.  Last bits depend on how many rows there are.  rows = 0 is a valid call (of the
+ * A NaN or +inf among the logits makes the row's results NaN; an infinity in weight or in the row may.  Last bits depend on how many rows there are.  rows = 0 is a valid call (of the
  * gradient: dweight becomes zeros).
  * Limits: 1 <= d <= 2^16, 1 <= V <= 2^22, rows <= 2^24.
  * Workspace: the slots of the rows and 16 bytes per row and 64 or 128 columns, never the logits; of the weight, where it has to be copied,

@@ -106,7 +106,8 @@ enum Cut : int { kCutNone = 0, kCutHead = 1, kCutTail = 2 };
 
 // A product whose B operand lies in the caller's memory as it is: rows and reduction index of B end anywhere (in whole 16-byte pieces;
 // pointer and leading dimension multiples of 16 bytes), and what lies beyond reads as zero or, within a row's pitch or the next row, as what
-// is there.  So columns n >= N_real of the result hold anything, and the A operand has to be zero for k >= K_real up to the next multiple of 64.
+// is there.  So columns n >= N_real of the result hold anything, and the A operand has to be zero for k >= K_real up to the next multiple of 64,
+// where B may hold no NaN that would matter.
 // M, N, K1 as above, rounded up.
 // kThirds: operands are fp16 matrices, pairs hi + lo of 22 significand bits each; three reduction segments of K1 add up
 // hi hi, hi lo and lo hi (A2, B2; A3, B3).

@@ -246,7 +246,7 @@ PCM_API size_t pcm_linear_logprobs_backward_workspace_bytes(int64_t rows, int d,
                                                             int64_t weight_ld) {
     const void* const fine = reinterpret_cast<const void*>((uintptr_t)256);
     if (rows < 1 || check_linear(fine, d, weight, weight_ld, weight_layout, dtype, fine, PCM_TOKEN_U8, rows, d, V, 1.f) != PCM_OK) return 0;
-    return plan_backward(nullptr, (int)rows, weight_source(weight, weight_ld, dtype, weight_layout, d, V)).bytes;
+    return plan_backward(nullptr, (int)rows, weight_source(weight, weight_ld, dtype, weight_layout, d, V, true)).bytes;
 }
 
 PCM_API int pcm_linear_logprobs_backward(const void* hidden, int64_t hidden_ld, const void* weight, int64_t weight_ld, int weight_layout,
@@ -272,7 +272,7 @@ PCM_API int pcm_linear_logprobs_backward(const void* hidden, int64_t hidden_ld, 
         sum_parts(none, dweight, dweight_ld, dweight_dtype, s);
         return launch_status();
     }
-    const WeightSource src = weight_source(weight, weight_ld, dtype, weight_layout, d, V);
+    const WeightSource src = weight_source(weight, weight_ld, dtype, weight_layout, d, V, true);
     BackwardPlan b = plan_backward(workspace, (int)rows, src);
     if (!workspace_ok(workspace, workspace_bytes, b.bytes)) return PCM_EWORKSPACE;
     const LinearRows in{hidden, hidden_ld, tokens, token_type, (int)rows, d, V};

@@ -116,7 +116,8 @@ inline int round_up(int x, int to) { return (x + to - 1) / to * to; }
 
 Slots carve_slots(Carver& c, int rows, int d, int dtype);
 SlotGradients carve_gradients(Carver& c, const Slots& slots, int dtype);
-WeightSource weight_source(const void* w, int64_t ld, int dtype, int layout, int d, int V);
+// sums_along_rows: a product of the call has the row's index as its reduction index.
+WeightSource weight_source(const void* w, int64_t ld, int dtype, int layout, int d, int V, bool sums_along_rows);
 // columns: of the pieces that the caller works in.
 WeightCopy carve_weight(Carver& c, const WeightSource& src, int columns);
 int copy_columns(const WeightSource& src);               // of a piece that is copied

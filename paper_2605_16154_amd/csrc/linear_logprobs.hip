@@ -647,11 +647,13 @@ SlotGradients carve_gradients(Carver& c, const Slots& slots, int dtype) {
     }
     return g;
 }
-WeightSource weight_source(const void* w, int64_t ld, int dtype, int layout, int d, int V) {
+WeightSource weight_source(const void* w, int64_t ld, int dtype, int layout, int d, int V, bool sums_along_rows) {
     const int length = layout == PCM_WEIGHT_OUT_IN ? d : V;
-    return WeightSource{w, ld, dtype, layout, d, V,
-                        // (256 rows of a tile are addressed with 32 bits)
-                        dtype == PCM_BF16 && (reinterpret_cast<uintptr_t>(w) & 15u) == 0 && ld % 8 == 0 && length % 8 == 0 && ld < (1 << 23)};
+    // 256 rows of a tile are addressed with 32 bits
+    const bool reads = dtype == PCM_BF16 && (reinterpret_cast<uintptr_t>(w) & 15u) == 0 && ld % 8 == 0 && length % 8 == 0 && ld < (1 << 23);
+    // A sum along a row goes on to the next multiple of 64 with zeros times what is there: the next row, whose NaN all results have anyway, or a
+    // gap, whose none may have
+    return WeightSource{w, ld, dtype, layout, d, V, reads && (!sums_along_rows || ld == length || length % kTileK == 0)};
 }
 // Pieces of at most 256 MB, in whole tiles.
 int copy_columns(const WeightSource& src) {
@@ -740,7 +742,7 @@ PCM_API size_t pcm_linear_logprobs_workspace_bytes(int64_t rows, int d, int V, i
     // (the addresses that are not given are taken to be fine)
     const void* const fine = reinterpret_cast<const void*>((uintptr_t)256);
     if (rows < 1 || check_linear(fine, d, weight, weight_ld, weight_layout, dtype, fine, PCM_TOKEN_U8, rows, d, V, 1.f) != PCM_OK) return 0;
-    return plan_forward(nullptr, (int)rows, weight_source(weight, weight_ld, dtype, weight_layout, d, V)).bytes;
+    return plan_forward(nullptr, (int)rows, weight_source(weight, weight_ld, dtype, weight_layout, d, V, weight_layout == PCM_WEIGHT_OUT_IN)).bytes;
 }
 
 PCM_API int pcm_linear_logprobs(const void* hidden, int64_t hidden_ld, const void* weight, int64_t weight_ld, int weight_layout, int dtype,
@@ -752,7 +754,7 @@ PCM_API int pcm_linear_logprobs(const void* hidden, int64_t hidden_ld, const voi
     auto misaligned = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; };
     if (!logp || !lse || misaligned(logp) || misaligned(lse) || misaligned(entropy)) return PCM_EINVAL;
     if (rc != PCM_OK) return rc;
-    const WeightSource src = weight_source(weight, weight_ld, dtype, weight_layout, d, V);
+    const WeightSource src = weight_source(weight, weight_ld, dtype, weight_layout, d, V, weight_layout == PCM_WEIGHT_OUT_IN);
     const ForwardPlan f = plan_forward(workspace, (int)rows, src);
     if (!workspace_ok(workspace, workspace_bytes, f.bytes)) return PCM_EWORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);

@@ -360,3 +360,23 @@ def test_rows_with_a_gradient_of_zero_add_nothing(dtype, layout, rows):
         assert np.all(np.abs(_np(got[name]) - want) <= tol), name
     none = pcm.pcm_linear_logprobs_backward(hidden, w, tokens, fwd["lse"], 0 * g, fwd["entropy"], 0 * g)
     assert not none["dhidden"].any() and not none["dweight"].any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", ["in_out", "out_in"])
+@pytest.mark.parametrize("rows", [9, 150])
+def test_what_lies_between_rows_is_not_met(rows, layout, dtype):
+    import paper_2605_16154_amd as pcm
+    for d, V, pad in ((136, 520, 8), (72, 200, 56), (64, 256, 8), (65, 129, 7)):
+        hidden, w, tokens, gen = _inputs(rows, d, V, dtype, layout, pad=pad)
+        g = torch.randn(rows, generator=gen, device="cuda")
+        results = []
+        for fill in (0.0, float("nan")):
+            base = torch.full((rows, d + pad), fill, dtype=dtype, device="cuda")
+            wide = torch.full((V, d + pad) if layout == "out_in" else (d, V + pad), fill, dtype=dtype, device="cuda")
+            h = base[:, :d].copy_(hidden)
+            ww = wide[:, :d].copy_(w.t()).t() if layout == "out_in" else wide[:, :V].copy_(w)
+            f = pcm.pcm_linear_logprobs(h, ww, tokens)
+            results.append({**f, **pcm.pcm_linear_logprobs_backward(h, ww, tokens, f["lse"], g, f["entropy"], g)})
+        for k in results[0]:
+            assert torch.equal(results[0][k], results[1][k]), (d, V, k)
