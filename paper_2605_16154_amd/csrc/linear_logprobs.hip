@@ -723,12 +723,12 @@ int check_linear(const void* hidden, int64_t hidden_ld, const void* weight, int6
         (token_type != PCM_TOKEN_U8 && token_type != PCM_TOKEN_I32 && token_type != PCM_TOKEN_I64) || !(temperature >= 0x1p-126f) ||
         temperature == __builtin_huge_valf())
         return PCM_EINVAL;
-    if (rows == 0) return PCM_OK;
+    const int rc = rows > (1 << 24) || d > (1 << 16) || V > (1 << 22) ? PCM_EUNSUPPORTED : PCM_OK;
+    if (rows == 0) return rc;
     const uintptr_t value = dtype == PCM_F32 ? 3 : 1, token = token_type == PCM_TOKEN_U8 ? 0 : token_type == PCM_TOKEN_I32 ? 3 : 7;
-    if (!hidden || !weight || !tokens || (reinterpret_cast<uintptr_t>(hidden) & value) != 0 || (reinterpret_cast<uintptr_t>(weight) & value) != 0 ||
-        (reinterpret_cast<uintptr_t>(tokens) & token) != 0)
-        return PCM_EINVAL;
-    return rows > (1 << 24) || d > (1 << 16) || V > (1 << 22) ? PCM_EUNSUPPORTED : PCM_OK;
+    const bool fine = hidden && weight && tokens && (reinterpret_cast<uintptr_t>(hidden) & value) == 0 && (reinterpret_cast<uintptr_t>(weight) & value) == 0 &&
+                      (reinterpret_cast<uintptr_t>(tokens) & token) == 0;
+    return fine ? rc : PCM_EINVAL;
 }
 
 }  // namespace pcm
@@ -749,8 +749,7 @@ PCM_API int pcm_linear_logprobs(const void* hidden, int64_t hidden_ld, const voi
                                 const void* tokens, int token_type, int64_t rows, int d, int V, float temperature, float* logp, float* lse,
                                 float* entropy, void* workspace, size_t workspace_bytes, void* stream) {
     const int rc = check_linear(hidden, hidden_ld, weight, weight_ld, weight_layout, dtype, tokens, token_type, rows, d, V, temperature);
-    if (rc == PCM_EINVAL) return rc;
-    if (rows == 0) return PCM_OK;
+    if (rc == PCM_EINVAL || rows == 0) return rc;
     auto misaligned = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; };
     if (!logp || !lse || misaligned(logp) || misaligned(lse) || misaligned(entropy)) return PCM_EINVAL;
     if (rc != PCM_OK) return rc;

@@ -77,6 +77,13 @@ def test_no_rows(cdll):
     assert cdll.pcm_linear_logprobs_backward(*none.values()) == OK
 
 
+def test_no_rows_of_sizes_beyond_the_limits(cdll):
+    for change in (dict(d=1 << 30, hidden_ld=1 << 30, dhidden_ld=1 << 30), dict(V=1 << 30, weight_ld=1 << 30, dweight_ld=1 << 30)):
+        pick = lambda base: {**base, "rows": 0, **{k: v for k, v in change.items() if k in base}}
+        assert cdll.pcm_linear_logprobs(*pick(FORWARD).values()) == EUNSUPPORTED
+        assert cdll.pcm_linear_logprobs_backward(*pick({**BACKWARD, "dweight": None}).values()) == EUNSUPPORTED
+
+
 def test_logits_are_never_kept(cdll):
     """The forward call takes 16 bytes per row and 128 columns beside its rows, a copy of at most 256 MB, the gradient one GB of dz besides."""
     rows, d, V = 4096, 4096, 131072
