@@ -674,8 +674,8 @@ def pcm_linear_logprobs(hidden, weight, tokens, temperature: float = 1.0, want_e
         t = out.get(name)
         if t is None:
             out[name] = t = torch.empty(rows, dtype=_F32, device=dev)
-        elif tuple(t.shape) != (rows,):
-            raise PcmError(f"out[{name!r}] has shape {tuple(t.shape)}, expected {(rows,)}")
+        elif tuple(t.shape) != (rows,) or t.device != dev:
+            raise PcmError(f"out[{name!r}] has shape {tuple(t.shape)} on {t.device}, expected {(rows,)} on {dev}")
         p.append(_ptr(t, _F32, name))
     if not want_entropy:
         p.append(None)
@@ -715,6 +715,8 @@ def pcm_linear_logprobs_backward(hidden, weight, tokens, lse, dlogp, entropy: Op
         if t.shape != (rows,):
             raise PcmError("lse, dlogp, entropy and dentropy must be [rows]")
     out = {} if out is None else out
+    if any(t.device != dev for t in (lse, dlogp, entropy, dentropy, *out.values()) if t is not None):
+        raise PcmError("all tensors must be on the device of hidden")
     p_dh = p_dw = None
     dh_ld, dw_ld, dw_type = d, 0, PCM_F32
     if want_dhidden:

@@ -279,6 +279,7 @@ PCM_API int pcm_linear_logprobs_backward(const void* hidden, int64_t hidden_ld, 
     const float inv_t = 1.f / temperature, c = inv_t * kLog2E;
     b.grads.lse = lse; b.grads.dlogp = dlogp; b.grads.entropy = entropy; b.grads.dentropy = dentropy;
     b.grads.inv_t = inv_t;
+    if (!dweight) b.grads.w_h = nullptr;
     b.grads.dh = dhidden;
     b.grads.dh_ld = dhidden_ld;
     const BackwardOut out{dhidden, dhidden_ld, dweight, dweight_ld, dweight_dtype, accumulate};

@@ -45,7 +45,7 @@ struct SlotGradients {
     // fp32
     int32_t* z_shift;                // [padded]: a row of dz is held times 2^z_shift; beyond any number for a row of zeros
     int32_t* exponent;               // [padded]: of h 2^-z_shift (short lists only, else the largest is gathered in slots.most)
-    half_bits *w_h, *w_h_low;        // [padded, d64]: h 2^(14 - most - z_shift): what dz is multiplied with for dW
+    half_bits *w_h, *w_h_low;        // [padded, d64]: h 2^(14 - most - z_shift): what dz is multiplied with for dW (null: it is not asked for)
     void* dh;                        // [rows], dh_ld apart, or null: rows without a token are made zeros
     int64_t dh_ld;
 };

@@ -699,7 +699,7 @@ void prepare_operands(const LinearRows& in, const Slots& slots, const SlotGradie
         const WeightAbsmax absmax{static_cast<const float*>(src.w), src.ld, rows, cols, copy.absmax_parts, RowSplit(rows, ceil_div(cols, 4), 4), copy.absmax};
         if (own_list) linear_gather<float, true><<<rows_blocks + absmax.parts, 256, 0, s>>>(in, slots, g, rows_blocks, absmax, piece);
         else linear_gather<float, false><<<rows_blocks + absmax.parts, 256, 0, s>>>(in, slots, g, rows_blocks, absmax, piece);
-        if (grads != nullptr) linear_weigh<<<rows_blocks + piece.split.blocks, 256, 0, s>>>(in, slots, g, rows_blocks, piece);
+        if (g.w_h != nullptr) linear_weigh<<<rows_blocks + piece.split.blocks, 256, 0, s>>>(in, slots, g, rows_blocks, piece);
         else linear_copy<float><<<piece.split.blocks, 256, 0, s>>>(piece);
     } else {
         if (own_list) linear_gather<half_bits, true><<<rows_blocks + piece.split.blocks, 256, 0, s>>>(in, slots, g, rows_blocks, WeightAbsmax{}, piece);
