@@ -24,9 +24,10 @@ namespace {
 
 constexpr int kThreads = 256;
 static_assert(kManyChunk == kThreads * 8, "eight elements a lane");
-// Workgroups of the two passes.  Update of 341 M parameters in 32 / 203 M in 8 bits by 2048 / 1280 (five to a CU) / 1024 of them: 1910 / 1873 / 1880 and
-// 713 / 705 / 715 us.
-constexpr int kSumsqGrid = 1024, kUpdateGrid = 1280;
+constexpr int kSumsqGrid = 1024;
+// Workgroups of the update, and how many a CU has registers for.  Steps over 341 M parameters in 32 bits / over 203 M in 8 and their values read out, by 768 / 1024 /
+// 2048 workgroups, four to a CU: 2220 / 2203 / 2243 and 1039 / 982 / 978 us; by 1280, five to a CU, 2188 and 984.
+constexpr int kUpdateGrid32 = 1280, kUpdatePerCu32 = 5, kUpdateGrid8 = 2048, kUpdatePerCu8 = 4;
 constexpr int kSignField = 15, kSquareField = 31;
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -213,77 +214,87 @@ __device__ inline uint32_t block_max(uint32_t x) {
     x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x122, 0xf, 0xf, true));
     return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x121, 0xf, 0xf, true));
 }
-// Codes of eight values of a block whose exponent is `top`, without their signs, as values.  A code is the upper bits of an fp32 number whose exponent
-// begins at top - kField: an addition and a shift; below f = 1 with the implicit one put in and taken away again.  Blocks whose values do not fit
-// into that (close to the least numbers, or NaN) are rare and go the long way: the lanes of a wavefront together.
+// Eight values of a block whose exponent is `top`, from their codes.  A code is the upper bits of an fp32 number whose exponent field is f, numbers below the
+// normal ones for f = 0 included: in place, it is that number times a power of two.
 template <int kField>
-__device__ __forceinline__ void values_of(float (&x)[8], const uint32_t (&code)[8], int top) {
-    if (!__any(top == 255 || (top > 0 && top <= kField))) {
-        const uint32_t base = (uint32_t)(top - kField) << 3;
-        const float one = __builtin_bit_cast(float, (8 + base) << 20);
+__device__ __forceinline__ void values_of(float (&x)[8], u32x2 codes, int top) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const bool fine = code[e] < 8;
-            x[e] = __builtin_bit_cast(float, ((fine ? code[e] + 8 : code[e]) + base) << 20) - (fine ? one : 0.f);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float v = ldexpf((float)(code[e] >= 8 ? 8 + (code[e] & 7) : code[e]), max((int)(code[e] >> 3), 1) + top - kField - 130);
-            x[e] = top == 255 ? __builtin_nanf("") : v;
-        }
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t word = codes[e / 4];
+        const uint32_t bits = kField == kSquareField ? (word >> (e % 4 * 8) & 255u) << 20
+                                                     : (uint32_t)((int32_t)(word << (24 - e % 4 * 8)) >> 4) & 0x87f00000u;
+        x[e] = ldexpf(__builtin_bit_cast(float, bits), top - kField);
     }
+    if (!__any(top == 255)) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = top == 255 ? __builtin_nanf("") : x[e];
 }
-// Exponent of a block, from each lane's eight values (as bits without a sign) and their random bits (times 16).
-__device__ __forceinline__ int exponent_of(const uint32_t (&bits)[8], const uint32_t (&random)[8]) {
+// Exponent of a block, from each lane's eight values (as bits without a sign) and these with their random bits added.
+__device__ __forceinline__ int exponent_of(const uint32_t (&bits)[8], const uint32_t (&sum)[8]) {
     uint32_t most = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) most = max(most, bits[e] + random[e]);
+    for (int e = 0; e < 8; ++e) most = max(most, sum[e]);
     most = block_max(most);
     // zeros and what is below the normal numbers count as nothing, which matters where there is nothing else
     if (__any(most < 3u << 23)) {
         most = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) most = max(most, bits[e] < 1u << 23 ? 0u : bits[e] + random[e]);
+        for (int e = 0; e < 8; ++e) most = max(most, bits[e] < 1u << 23 ? 0u : sum[e]);
         most = block_max(most);
     }
     return (int)min(most >> 23, 255u);
 }
-// Codes of eight values, without signs.
+// Codes of eight values, without signs.  True where those of the wavefront are all of blocks of zeros or at least 8 (f > 0): an addition and a shift.
+// Others are rare, and the lanes go the long way together.
 template <int kField>
-__device__ __forceinline__ void codes_of(uint32_t (&code)[8], const uint32_t (&bits)[8], const uint32_t (&random)[8], int top) {
-    const int base = (top - kField) << 3;
-    bool fine = false;
+__device__ __forceinline__ bool codes_of(uint32_t (&code)[8], const uint32_t (&bits)[8], const uint32_t (&sum)[8], const uint32_t (&random)[8], int top) {
+    const int base = top > 0 ? (top - kField) << 3 : 1 << 12;
+    int least = base;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int c = (int)((bits[e] + random[e]) >> 20) - base;
-        fine |= c < 8 && bits[e] >= 1u << 23;
-        code[e] = bits[e] < 1u << 23 ? 0u : (uint32_t)c;
+        const int c = (int)(sum[e] >> 20) - base;
+        least = e == 0 ? c : min(least, c);
+        code[e] = (uint32_t)max(c, 0);
     }
+    if (!__any(top > 0 && (least < 8 || top <= kField || top == 255))) return true;
     // below 2^(top - kField + 1): multiples of 2^(top - kField - 2), of which 16 bits behind the point count
-    if (!__any(fine)) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        if (bits[e] < 1u << 23 || (int)code[e] >= 8) continue;
-        code[e] = ((uint32_t)ldexpf(__builtin_bit_cast(float, bits[e]), 16 + 129 + kField - top) + (random[e] >> 4)) >> 16;
-        if (kField == kSquareField) code[e] = max(code[e], 1u);
+        if (bits[e] < 1u << 23) code[e] = 0;
+        else if (code[e] < 8) {
+            code[e] = ((uint32_t)ldexpf(__builtin_bit_cast(float, bits[e]), 16 + 129 + kField - top) + (random[e] >> 4)) >> 16;
+            if (kField == kSquareField) code[e] = max(code[e], 1u);
+        }
     }
+    return false;
 }
-__device__ __forceinline__ void split_codes(uint32_t (&code)[8], u32x2 x) {
+// A lane's eight values of a block as codes; the first n count, the others pad a tensor.
+template <int kField>
+__device__ __forceinline__ u32x2 coded(int& top, const float (&x)[8], const uint32_t (&random)[8], int n) {
+    uint32_t bits[8], sum[8], code[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) code[e] = x[e / 4] >> (e % 4 * 8) & 255;
-}
-// m and v of eight elements.
-__device__ __forceinline__ void moments_of(float (&m)[8], float (&v)[8], u32x2 mc, u32x2 vc, int m_top, int v_top) {
-    uint32_t a[8], b[8], mag[8];
-    split_codes(a, mc);
-    split_codes(b, vc);
+    for (int e = 0; e < 8; ++e) bits[e] = __builtin_bit_cast(uint32_t, x[e]) & 0x7fffffffu;
+    if (__any(n < 8)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) mag[e] = a[e] & 127;
-    values_of<kSignField>(m, mag, m_top);
-    values_of<kSquareField>(v, b, v_top);
+        for (int e = 0; e < 8; ++e) bits[e] = e < n ? bits[e] : 0u;
+    }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) m[e] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, m[e]) | (a[e] & 128) << 24);
+    for (int e = 0; e < 8; ++e) sum[e] = bits[e] + random[e];
+    top = exponent_of(bits, sum);
+    const bool plain = codes_of<kField>(code, bits, sum, random, top);
+    if (kField == kSignField) {
+        const uint32_t sign = top > 0 ? 128u : 0u;            // (a code of 0 has none)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            code[e] = (plain ? code[e] : code[e] & 127u) | (__builtin_bit_cast(uint32_t, x[e]) >> 24 & (plain || code[e] != 0 ? sign : 0u));
+    } else if (!plain) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) code[e] &= 255u;
+    }
+    u32x2 out = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e / 4] |= code[e] << (e % 4 * 8);
+    return out;
 }
 
 // Norm and clip factor; every workgroup forms them from the partial sums by itself.  They are asked for before anything else.
@@ -356,37 +367,23 @@ struct Eight<8, kStream> {
         m_top = tops[0];
         v_top = tops[s.elements / kManyBlock];
     }
-    __device__ __forceinline__ void get(float (&mm)[8], float (&vv)[8]) const { moments_of(mm, vv, m, v, m_top, v_top); }
+    __device__ __forceinline__ void get(float (&mm)[8], float (&vv)[8]) const {
+        values_of<kSignField>(mm, m, m_top);
+        values_of<kSquareField>(vv, v, v_top);
+    }
     __device__ __forceinline__ void put(const ManyStep& s, const float (&mm)[8], const float (&vv)[8]) const {
         if (!in_block()) return;                              // by whole blocks, so the lanes of a block stay together
         const int64_t j = k.at + threadIdx.x * 8;
         const int n = k.count - (int)threadIdx.x * 8;
         const uint64_t group = (uint64_t)(j / 8);
         const PhiloxWords bits = philox4x32((uint32_t)group, (uint32_t)(group >> 32), s.step[0], s.step[1], s.seed[0], s.seed[1]);
-        uint32_t random[8], mb[8], vb[8], a[8], b[8];
+        uint32_t random[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            random[e] = (e % 2 ? bits.w[e / 2] >> 12 : bits.w[e / 2] << 4) & 0xffff0u;
-            mb[e] = __builtin_bit_cast(uint32_t, mm[e]) & 0x7fffffffu;
-            vb[e] = __builtin_bit_cast(uint32_t, vv[e]) & 0x7fffffffu;
-        }
-        if (__any(n < 8)) {                                   // what pads a tensor
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                mb[e] = e < n ? mb[e] : 0u;
-                vb[e] = e < n ? vb[e] : 0u;
-            }
-        }
-        const int m_new = exponent_of(mb, random), v_new = exponent_of(vb, random);
-        codes_of<kSignField>(a, mb, random, m_new);
-        codes_of<kSquareField>(b, vb, random, v_new);
-        u32x2 mc = {0, 0}, vc = {0, 0};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t sign = a[e] != 0 ? __builtin_bit_cast(uint32_t, mm[e]) >> 24 & 128u : 0u;
-            mc[e / 4] |= ((a[e] & 127u) | sign) << (e % 4 * 8);
-            vc[e / 4] |= (b[e] & 255u) << (e % 4 * 8);
-        }
+        for (int e = 0; e < 8; ++e) random[e] = (bits.w[e / 2] >> (e % 2 * 16) & 0xffffu) << 4;
+        int m_new, v_new;
+        const u32x2 mc = coded<kSignField>(m_new, mm, random, n);
+        __builtin_amdgcn_sched_barrier(0);                    // (registers for one of the two)
+        const u32x2 vc = coded<kSquareField>(v_new, vv, random, n);
         PCM_GLOBAL uint8_t* const state = (PCM_GLOBAL uint8_t*)s.state;
         store_codes<kStream>((eight_codes*)(state + j), mc);
         store_codes<kStream>((eight_codes*)(state + s.elements + j), vc);
@@ -400,7 +397,7 @@ struct Eight<8, kStream> {
 
 // A workgroup takes every gridDim-th chunk, the next one's values under way while one is worked on; the first one's while the norm is formed.
 template <int kBits, bool kStream>
-__global__ __launch_bounds__(kThreads, 5) void many_update(ManyStep s) {
+__global__ __launch_bounds__(kThreads, kBits == 8 ? kUpdatePerCu8 : kUpdatePerCu32) void many_update(ManyStep s) {
     constexpr bool kTogether = kBits == 8;
     const AdamConst& c = s.c;
     int64_t at = blockIdx.x;
@@ -421,10 +418,12 @@ __global__ __launch_bounds__(kThreads, 5) void many_update(ManyStep s) {
             const float y = g[e] * scale;
             m[e] = c.beta1 * m[e] + c.one_minus_beta1 * y;
             v[e] = c.beta2 * v[e] + c.one_minus_beta2 * (y * y);
-            // (8 bits: root and reciprocal of the hardware, 1 ulp each: with the exact ones 203 M parameters take 7 % longer)
+            // (8 bits: root and reciprocal of the hardware, 1 ulp each: with the exact ones the update of 203 M parameters takes 10 % longer)
             const float root = kBits == 8 ? __builtin_amdgcn_sqrtf(v[e]) : sqrtf(v[e]);
-            const float denom = root * c.inv_sqrt_bc2 + c.eps;
-            w[e] = now.w[e / 4][e % 4] * c.decay - c.step_size * (kBits == 8 ? m[e] * __builtin_amdgcn_rcpf(denom) : m[e] / denom);
+            const float old = now.w[e / 4][e % 4] * c.decay;
+            if constexpr (kBits == 8)
+                w[e] = __builtin_fmaf(-c.step_size, m[e] * __builtin_amdgcn_rcpf(__builtin_fmaf(root, c.inv_sqrt_bc2, c.eps)), old);
+            else w[e] = old - c.step_size * (m[e] / (root * c.inv_sqrt_bc2 + c.eps));
         }
         store_eight<kTogether, kStream && !kTogether>(now.k.weight, w, now.k.count);
         if (now.k.lowp != nullptr) store_bf16<kTogether>(now.k.lowp, w, now.k.count);
@@ -440,7 +439,8 @@ __global__ __launch_bounds__(kThreads) void many_states(const uint8_t* state, in
         const u32x2 mc = *reinterpret_cast<const u32x2*>(state + j), vc = *reinterpret_cast<const u32x2*>(state + elements + j);
         const int m_top = tops[0], v_top = tops[elements / kManyBlock];
         float m[8], v[8];
-        moments_of(m, v, mc, vc, m_top, v_top);
+        values_of<kSignField>(m, mc, m_top);
+        values_of<kSquareField>(v, vc, v_top);
         auto write = [&](void* out, const float (&x)[8]) {
             if (kBf16) {
                 u32x4 a;
@@ -613,7 +613,8 @@ PCM_API int pcm_adamw_many_step(const void* plan, const pcm_adamw_many_layout* l
         many_sumsq<<<(unsigned)a.parts, kThreads, 0, s>>>(a.chunks, a.n, partial);
     }
     StageTimer t(ST_OPT_ADAMW, s);
-    const unsigned grid = (unsigned)(a.n < 1 ? 1 : a.n < kUpdateGrid ? a.n : kUpdateGrid);
+    const int64_t most = layout->state_bits == 8 ? kUpdateGrid8 : kUpdateGrid32;
+    const unsigned grid = (unsigned)(a.n < 1 ? 1 : a.n < most ? a.n : most);
     const bool past = a.elements > kStreamElements;
     if (layout->state_bits == 32) {
         if (past) many_update<32, true><<<grid, kThreads, 0, s>>>(a);
