@@ -51,12 +51,7 @@ struct SlotGradients {
 };
 
 constexpr int kCountRows = 1024;
-// Rows that the projection streams past, 16 at a time, instead of being multiplied in tiles.  Calls with rows in bf16, streamed / in tiles: 16 rows of
-// 1024 -> 32003 21 / 43 us ([d, V]) and 21 / 26 ([V, d]), of 4096 -> 65536 100 / 115 and 122 / 140.  fp32 rows in tiles need the weight as pairs first, so more
-// of them stream: 64 of 1024 -> 32003 66 / 106 ([d, V]) and 91 / 104 ([V, d]), 100 104 / 106 and 152 / 103; 64 of 4096 -> 65536 451 / 1004 and
-// 653 / 1095, 100 745 / 1006 and 1078 / 1093.
 constexpr int kFewRows = 16;
-inline int few_rows_most(int dtype, int layout) { return dtype != PCM_F32 ? kFewRows : layout == 1 ? 64 : 96; }
 constexpr int kAbsmaxParts = 1024;
 constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -66,6 +61,16 @@ struct WeightSource {
     int dtype, layout, d, V;
     bool in_place;                   // bf16 that the products can read where it is
 };
+// Rows that the projection streams past, 16 at a time, instead of being multiplied in tiles.  Calls with rows in bf16, streamed / in tiles: 16 rows of
+// 1024 -> 32000 17 / 43 us ([d, V]) and 20 / 26 ([V, d]), of 4096 -> 65536 100 / 115 and 120 / 140; 32 rows 125 / 116 and 193 / 140.  Where the weight has to be
+// copied first more of them stream: bf16 [d, V], 64 of 1023 -> 32003 42 / 44 and of 4095 -> 65531 287 / 329, 80 50 / 43 and 353 / 326; fp32, which is
+// made pairs, 64 of 1024 -> 32003 68 / 105 ([d, V]) and 90 / 102 ([V, d]), 100 108 / 106 and 151 / 104, 64 of 4096 -> 65536 432 / 998 and 649 / 1092, 100
+// 732 / 1000 and 1073 / 1093.  (bf16 [V, d] whose rows begin anywhere: 16 of 1023 -> 32003 50 / 44, of 4095 -> 65531 276 / 370, 32 93 / 44 and 548 / 371.)
+inline int few_rows_most(const WeightSource& src) {
+    const bool by_token = src.layout == PCM_WEIGHT_OUT_IN;
+    if (src.dtype == PCM_F32) return by_token ? 64 : 96;
+    return src.in_place || by_token ? kFewRows : 64;
+}
 // Scratch for a copy of up to `columns` of the vocabulary, rows of it, or of d, `ld` apart.
 struct WeightCopy {
     half_bits *w, *low;

@@ -395,14 +395,17 @@ __device__ __forceinline__ u32x4 load_tail(const T* row, int k, int d) {
 // are added in LDS.  A slice is 4 lane groups x kE values of k (kE = 16 bytes of them).
 //   [V][d]: a lane brings in kE values of k of one column and is its fragment; four fragments of 16 columns share one of the hidden rows.
 //   [d][V]: a lane brings in kE columns at kE values of k and has the fragments of kE columns, bf16 after exchanging halves between pairs of rows.
-// More than 16 rows are groups of 16 whose workgroups follow one another on an XCD, so that the projection comes out of its cache after the first.
+// An XCD has neighbouring blocks: the lines that two of them share, where rows do not begin on a line, come out of its cache (7 fp32 rows of 1024 -> 32003 33.6 ->
+// 26.6 us with what follows; one bf16 row of 4096 -> 131072 204 -> 195).  More than 16 rows are groups of 16 whose workgroups follow one another on an XCD, so
+// that the projection comes from there after the first.
 template <class T, int kLayout>
 __global__ __launch_bounds__(256) void few_rows(LinearRows in, const T* w, int64_t ld, PartSums out, float* token_z, float c, int groups) {
     constexpr int kE = 16 / sizeof(T), kSlice = 4 * kE;
     constexpr int kTiles = kLayout == PCM_WEIGHT_OUT_IN ? 4 : kE, kLoads = kLayout == PCM_WEIGHT_OUT_IN ? 4 : kE;
     constexpr int kColumns = kTiles * 16;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = lane >> 4, at = lane & 15;
-    const int block = blockIdx.x / (kNumXcd * groups) * kNumXcd + blockIdx.x % kNumXcd, row0 = blockIdx.x / kNumXcd % groups * kFewRows;
+    const int each = (out.parts + kNumXcd - 1) / kNumXcd;              // blocks of an XCD
+    const int block = blockIdx.x % kNumXcd * each + blockIdx.x / (kNumXcd * groups), row0 = blockIdx.x / kNumXcd % groups * kFewRows;
     const int n0 = block * kColumns;
     if (n0 >= in.V) return;
     f32x4 acc[kTiles];
@@ -546,7 +549,7 @@ template <class T>
 void launch_few(const LinearRows& in, const void* w, int64_t ld, int layout, const PartSums& parts, float* token_z, float c, hipStream_t s) {
     const T* const p = static_cast<const T*>(w);
     const int groups = ceil_div(in.rows, kFewRows);
-    const unsigned grid = (unsigned)(groups == 1 ? parts.parts : round_up(parts.parts, kNumXcd) * groups);
+    const unsigned grid = (unsigned)(round_up(parts.parts, kNumXcd) * groups);
     if (layout == PCM_WEIGHT_OUT_IN) few_rows<T, PCM_WEIGHT_OUT_IN><<<grid, 256, 0, s>>>(in, p, ld, parts, token_z, c, groups);
     else few_rows<T, PCM_WEIGHT_IN_OUT><<<grid, 256, 0, s>>>(in, p, ld, parts, token_z, c, groups);
 }
@@ -572,7 +575,7 @@ struct ForwardPlan {
 ForwardPlan plan_forward(void* workspace, int rows, const WeightSource& src) {
     Carver c(workspace);
     ForwardPlan f{};
-    f.few = rows <= few_rows_most(src.dtype, src.layout);
+    f.few = rows <= few_rows_most(src);
     if (f.few) {
         f.parts = carve_parts(c, rows, ceil_div(src.V, few_columns(src.dtype, src.layout)));
         f.token_z = c.take<float>((size_t)rows);
