@@ -66,10 +66,12 @@ struct WeightSource {
 // copied first more of them stream: bf16 [d, V], 64 of 1023 -> 32003 42 / 44 and of 4095 -> 65531 287 / 329, 80 50 / 43 and 353 / 326; fp32, which is
 // made pairs, 64 of 1024 -> 32003 68 / 105 ([d, V]) and 90 / 102 ([V, d]), 100 108 / 106 and 151 / 104, 64 of 4096 -> 65536 432 / 998 and 649 / 1092, 100
 // 732 / 1000 and 1073 / 1093.  (bf16 [V, d] whose rows begin anywhere: 16 of 1023 -> 32003 50 / 44, of 4095 -> 65531 276 / 370, 32 93 / 44 and 548 / 371.)
-inline int few_rows_most(const WeightSource& src) {
+// And fp32 rows, up to as many as were measured, as long as what streams past all groups is 128 MB: 1024 rows of 256 -> 1024 17 / 26 and 23 / 26, 256 of 512 -> 4096 23 / 33
+// and 31 / 32, 512 39 / 35 and 55 / 34.
+inline bool streams(int rows, const WeightSource& src) {
     const bool by_token = src.layout == PCM_WEIGHT_OUT_IN;
-    if (src.dtype == PCM_F32) return by_token ? 64 : 96;
-    return src.in_place || by_token ? kFewRows : 64;
+    if (src.dtype != PCM_F32) return rows <= (src.in_place || by_token ? kFewRows : 64);
+    return rows <= (by_token ? 64 : 96) || (rows <= 1024 && (int64_t)ceil_div(rows, kFewRows) * src.d * src.V * 4 <= 128 << 20);
 }
 // Scratch for a copy of up to `columns` of the vocabulary, rows of it, or of d, `ld` apart.
 struct WeightCopy {

@@ -4,7 +4,7 @@
 //   products   z = h W on the matrix cores; the epilogue turns a wavefront's block of logits into three numbers per row: largest logit, sum of
 //              2^a and of 2^a a, a = (z - largest) log2 e / temperature; the token's logit is written down where it passes by
 //   join       the blocks of a row -> log-sum-exp, log p, entropy
-// Few rows (few_rows_most) have the projection streamed past them, 16 in the registers of a wavefront, bound by its bytes.
+// Few rows (streams()) have the projection streamed past them, 16 in the registers of a wavefront, bound by its bytes.
 #include "linear_epilogues.h"
 
 #include <type_traits>
@@ -575,7 +575,7 @@ struct ForwardPlan {
 ForwardPlan plan_forward(void* workspace, int rows, const WeightSource& src) {
     Carver c(workspace);
     ForwardPlan f{};
-    f.few = rows <= few_rows_most(src);
+    f.few = streams(rows, src);
     if (f.few) {
         f.parts = carve_parts(c, rows, ceil_div(src.V, few_columns(src.dtype, src.layout)));
         f.token_z = c.take<float>((size_t)rows);

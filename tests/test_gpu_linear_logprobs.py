@@ -380,3 +380,21 @@ def test_what_lies_between_rows_is_not_met(rows, layout, dtype):
             results.append({**f, **pcm.pcm_linear_logprobs_backward(h, ww, tokens, f["lse"], g, f["entropy"], g)})
         for k in results[0]:
             assert torch.equal(results[0][k], results[1][k]), (d, V, k)
+
+
+@pytest.mark.parametrize("layout", ["in_out", "out_in"])
+@pytest.mark.parametrize("rows,d,V,masked", [(1025, 1, 1, 0.0), (1030, 7, 2, 0.5), (1100, 65, 129, 0.0), (1279, 64, 255, 0.9), (1281, 320, 513, 0.3), (2000, 129, 1023, 0.99)])
+def test_forward_of_more_fp32_rows_than_stream(rows, d, V, masked, layout):
+    _forward(_inputs(rows, d, V, F32, layout, masked=masked, pad=1), 0.8)
+
+
+def test_streamed_rows_and_rows_in_tiles_agree():
+    """Rows on either side of where fp32 calls change from one to the other; the masked one that tells them apart is not met."""
+    import paper_2605_16154_amd as pcm
+    for layout, few in (("in_out", 96), ("out_in", 64)):
+        hidden, w, tokens, _ = _inputs(few + 1, 1024, 8192, F32, layout)
+        tokens[few] = -1
+        a, b = pcm.pcm_linear_logprobs(hidden[:few], w, tokens[:few]), pcm.pcm_linear_logprobs(hidden, w, tokens)
+        E = _z_error(_np(hidden), _np(w), F32, 1.0).max()
+        for k in a:
+            assert float((a[k] - b[k][:few]).abs().max()) <= 2 * (4 * E + 2.0 ** -19) * 11, k
