@@ -55,7 +55,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 
 // The logits of a tile, a wavefront's block of which is a part of its rows.  Vector instructions that no product runs beside: 11.5 issue
 // slots per logit (the accumulator moved twice, half a maximum, difference, product, exponential, sum, moment and its guard).  A lane has a quarter of 16 neighbours' rows
-// to itself; the quarters meet at the end, all rows together, so that the exchanges wait for one another only there.
+// to itself; the quarters meet at the end, all rows together, so that the exchanges wait for one another only there.  8.7 us of the 57 that a tile takes whose
+// reduction is 2048 long (main loop 45 at the clock that the power cap leaves, start 2.8).
 struct EpiRowStats {
     PartSums out;
     float* token_z;                      // [padded]
@@ -127,7 +128,7 @@ struct RowResults {
 // ---- dz -------------------------------------------------------------------------------------------
 
 // Vector instructions that no product runs beside: 10 issue slots per logit (the accumulator's move, log p, exponential, factor, product, rounding and
-// the way through LDS).
+// the way through LDS).  With what it writes 7.8 us of a tile's 50 (reduction 1536 long), as pairs 10 to 12 of 85.
 struct LogitGradient {
     const SlotGradient* of;
     const int32_t* token;
@@ -264,7 +265,8 @@ __device__ inline uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16
 // What a product over all rows is to be multiplied by: 2^(most - 14) for pairs.
 __device__ inline float weight_gradient_unit(const int32_t* most) { return most == nullptr || *most <= -(1 << 20) ? 1.f : ldexpf(1.f, *most - 14); }
 
-// acc into rows and columns of a matrix that end anywhere, at any alignment of its type, through LDS so that whole lines leave.
+// acc into rows and columns of a matrix that end anywhere, at any alignment of its type, through LDS so that whole lines leave (bf16 3 to 3.5 us a tile,
+// fp32 8).
 template <class T>
 struct EpiStoreAnywhere;
 template <>

@@ -4,6 +4,7 @@
 //   products   z = h W on the matrix cores; the epilogue turns a wavefront's block of logits into three numbers per row: largest logit, sum of
 //              2^a and of 2^a a, a = (z - largest) log2 e / temperature; the token's logit is written down where it passes by
 //   join       the blocks of a row -> log-sum-exp, log p, entropy
+// 4096 bf16 rows of 4096 -> 65536: 22 + 1,560 + 15 us, 1.4 PFLOP/s, bound by the power cap (as the gradient's products).
 // Few rows (streams()) have the projection streamed past them, 16 in the registers of a wavefront, bound by its bytes.
 #include "linear_epilogues.h"
 
@@ -314,7 +315,8 @@ __device__ __forceinline__ void copy_piece(const WeightPiece& q, int block) {
 
 // ---- before the products: two launches at most, of work that does not wait for one another ------------------
 
-// Rows to slots, and beside it the largest value of an fp32 weight or the first piece of a bf16 one.
+// Rows to slots, and beside it the largest value of an fp32 weight or the first piece of a bf16 one.  4096 bf16 rows of 4096 22 us; 1111 fp32 rows of 1001 and
+// a weight of 1001 x 32003 37, and 47 in the second launch, 4.6 TB/s together.
 template <class T, bool kList>
 __global__ __launch_bounds__(256) void linear_gather(LinearRows in, Slots slots, SlotGradients grads, int rows_blocks, WeightAbsmax absmax, WeightPiece piece) {
     const int block = blockIdx.x;
@@ -335,7 +337,7 @@ __global__ __launch_bounds__(256) void linear_copy(WeightPiece piece) {
 
 // ---- joining the parts -------------------------------------------------------------------------------
 
-// Results of a row from its parts: kRows rows a workgroup, the other threads parts of them.
+// Results of a row from its parts: kRows rows a workgroup, the other threads parts of them (one row of 2,048 parts 5.5 us, 4096 of 512 15).
 template <int kRows>
 __global__ __launch_bounds__(256) void linear_join(LinearRows in, const int32_t* slot_of, PartSums parts, const float* token_z, float inv_t,
                                                    RowResults out) {
