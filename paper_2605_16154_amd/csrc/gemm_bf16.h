@@ -116,23 +116,29 @@ struct BoundedProblem : GemmProblem {
     static constexpr bool kBoundedB = true, kHalves = kThirds;
     int N_real, K_real;
     const bf16 *A3, *B3;
-    // > 0: the product is done in as many parts, splits at most, as suit the rows that are there (parts_for; what a part costs beside its steps)
+    // > 0: the product is done in as many parts, splits at most, as suit the rows that are there (parts_for; what a part costs beside its steps, in eighths of one)
     int part_cost, part_steps;       // part_steps: the steps that this goes by
 };
 // Parts of a reduction of `steps` for `tiles` tiles: the fewest steps in a row over all rounds of 256 workgroups, ten more for the start
-// and end of each, and what the parts cost when they are written and added up: part_cost each and six for the launch.
+// and end of each, and what the parts cost when they are written and added up: part_cost eighths of a step each and 14 steps for the launch.  Looked at
+// are one part, those that just fill some rounds, and numbers in steps of a half: the host and the device come to the same.
 __host__ __device__ inline int parts_for(int tiles, int steps, int most, int part_cost) {
-    int best = 1, least = 0x7fffffff;
     if (tiles > 2048) return 1;                          // eight rounds and more even out
-    for (int n = 1; n <= most; ++n) {
-        const int rounds = (tiles * n + 255) / 256, cost = rounds * ((steps + n - 1) / n + 10) + (n > 1 ? n * part_cost + 6 : 0);
+    int best = 1, least = ((tiles + 255) / 256 * (steps + 10)) * 8;
+    auto look = [&](int n) {
+        if (n < 2 || n > most) return;
+        const int rounds = (tiles * n + 255) / 256, cost = (rounds * ((steps + n - 1) / n + 10) + 14) * 8 + n * part_cost;
         if (cost < least) {
             least = cost;
             best = n;
         }
-    }
+    };
+    for (int n = 2; n <= most; n *= 2) look(n), look(n + n / 2);
+    for (int rounds = 1; rounds <= 8; ++rounds) look(256 * rounds / tiles);
     return best;
 }
+// Workgroups that a part of so many tiles takes: a whole number for each XCD, unless there are fewer tiles than XCDs.
+__host__ __device__ inline int part_workgroups(int tiles) { return tiles < kNumXcd ? tiles : (tiles + kNumXcd - 1) / kNumXcd * kNumXcd; }
 enum RowsRole : int { kRowsUnused = 0, kRowsAreM = 1, kRowsAreK = 2 };
 
 // Accumulators of a wavefront: kW x kW tiles of 16 x 16.  Tile (i, j), register t of a lane is
@@ -367,9 +373,12 @@ __device__ __forceinline__ void gemm_tile(const Problem& p, const Epilogue& epi,
         if (p.part_cost > 0) {
             const int live_tiles = live_m * tiles_n;
             splits = parts_for(live_tiles, p.part_steps, p.splits, p.part_cost);
-            n_tiles = (live_tiles + kNumXcd - 1) / kNumXcd * kNumXcd;
+            n_tiles = part_workgroups(live_tiles);
             if (n_tiles == 0 || block >= n_tiles * splits) return;
             split = block / n_tiles;
+            // (the tiles that are one more for some XCDs go to others in the next part)
+            block -= split * n_tiles;
+            if (live_tiles >= kNumXcd) block = block / kNumXcd * kNumXcd + (block + split * (kNumXcd - live_tiles % kNumXcd)) % kNumXcd;
         }
     }
     int tm, tn;

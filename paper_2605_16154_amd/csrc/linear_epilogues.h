@@ -130,11 +130,15 @@ struct RowResults {
 // Vector instructions that no product runs beside: 10 issue slots per logit (the accumulator's move, log p, exponential, factor, product, rounding and
 // the way through LDS).  With what it writes 7.8 us of a tile's 50 (reduction 1536 long), as pairs 10 to 12 of 85.
 struct LogitGradient {
+    const int32_t* live;
     const SlotGradient* of;
     const int32_t* token;
     const float *h_unit, *w_unit;        // fp32, or null: powers of two
     float c;                             // log2 e / temperature
     int first, columns;                  // of the vocabulary in this piece
+    // Whether anything reads the rows of a wavefront's block: those that hold a row, and the rest of its step of 64 in the sum over rows.
+    template <int kW>
+    __device__ __forceinline__ bool read(const TileCoord<kW>& tc) const { return tc.row0() < (*live + kTileK - 1) / kTileK * kTileK; }
     // What is to be known of rows 16 i + (lane & 15) of a wavefront's block, asked for all at once.
     struct Row {
         float scale, lse2, along, rest, g;
@@ -211,6 +215,7 @@ struct EpiLogitGradient {
     }
     template <int kW>
     __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* lds) const {
+        if (!gradient.read(tc)) return;
         char* st = wave_stage(tc, lds);
         if (tc.col0() + kWaveRows<kW> <= gradient.columns) rows<true>(tc, acc, st);
         else rows<false>(tc, acc, st);
@@ -252,6 +257,7 @@ struct EpiLogitGradientPairs {
     }
     template <int kW>
     __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* lds) const {
+        if (!gradient.read(tc)) return;
         char* st = wave_stage(tc, lds);
         if (tc.col0() + kWaveRows<kW> <= gradient.columns) rows<true>(tc, acc, st);
         else rows<false>(tc, acc, st);
@@ -361,9 +367,10 @@ struct EpiHidden {
         char* st = wave_stage(tc, lds);
         const int col0 = tc.col0(), c = tc.lane % kLanes * 4, n_cols = min(RW, cols - col0);
         const bool direct = whole && tc.splits == 1;
-        const int rows = direct ? *live : 0x7fffffff;
+        const int rows = *live;
         float* const C = parts.of + tc.split * parts.part;
         if (tc.m0 == 0 && tc.n0 == 0 && tc.split == 0 && threadIdx.x == 0) *parts.used = tc.splits;
+        if (tc.row0() >= rows) return;
         // where the block's rows go, one or two to a lane (negative: nowhere); the lanes that write a row ask those
         constexpr int kHeld = (RW + 63) / 64;
         int to_row[kHeld];

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(256) void linear_sum_parts(PartSum q, T* out, int64
         if (slot < 0) continue;                            // zeros already
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         const float* from = q.parts + (int64_t)slot * q.ld + i;
-#pragma unroll 4
+#pragma unroll 16
         for (int p = 0; p < n; ++p) x += *reinterpret_cast<const f32x4*>(from + p * q.part);
         if (q.z_shift != nullptr) x *= ldexpf(*q.w_unit, -q.z_shift[slot]);
         x *= unit;
@@ -53,18 +53,20 @@ void sum_parts(PartSum q, void* out, int64_t ld, int dtype, hipStream_t s) {
 // ---- host side --------------------------------------------------------------------------------------
 
 // Tile and parts of the reduction of a product of M x N whose reduction takes `steps`, by an estimate: a step of the large tile takes 0.94 us, of the
-// small one 0.46 (see tile_for); parts are written and read at 4.8 TB/s.
-constexpr int kMostParts = 16;
+// small one 0.46 (see tile_for); parts are written and read at 4.8 TB/s, in at most 256 MB.
+constexpr int kMostParts = 128;
 struct ProductPlan {
-    int kW, parts, cost;             // parts; what one costs, in steps
+    int kW, parts, cost;             // parts; what one costs, in eighths of a step
     ProductPlan() : kW(kSmallTile), parts(1), cost(1) {}
     ProductPlan(int M, int N, int steps) {
         double best = 1e30;
+        const int most = (int)std::min<int64_t>({kMostParts, std::max(1, steps / 8), std::max<int64_t>(1, ((int64_t)64 << 20) / ((int64_t)M * N))});
         for (const int tile : {kLargeTile, kSmallTile}) {
+            if (M % (32 * tile) != 0) continue;
             const double step = tile == kLargeTile ? 0.94 : 0.46;
-            const int tiles = ceil_div(M, 32 * tile) * ceil_div(N, 32 * tile), each = 1 + (int)(2.0 * M * N * 4.0 / 4.8e6 / step);
-            const int n = parts_for(tiles, steps, std::min(kMostParts, std::max(1, steps / 8)), each);
-            const double time = step * (((tiles * n + 255) / 256) * (ceil_div(steps, n) + 10) + (n > 1 ? n * each + 6 : 0));
+            const int tiles = ceil_div(M, 32 * tile) * ceil_div(N, 32 * tile), each = 1 + (int)(8 * 2.0 * M * N * 4.0 / 4.8e6 / step);
+            const int n = parts_for(tiles, steps, most, each);
+            const double time = step * (((tiles * n + 255) / 256) * (ceil_div(steps, n) + 10) + (n > 1 ? n * each / 8.0 + 14 : 0));
             if (time < best) {
                 best = time;
                 kW = tile;
@@ -77,6 +79,7 @@ struct ProductPlan {
 
 struct BackwardPlan {
     int columns;                     // of a piece
+    int rows;                        // of the products that have them
     int64_t z_ld;
     Slots slots;
     SlotGradients grads;
@@ -113,7 +116,8 @@ BackwardPlan plan_backward(void* workspace, int rows, const WeightSource& src) {
     h.part = (int64_t)b.slots.padded * h.ld;
     h.used = b.slots.parts;
     b.dh_steps = b.columns / kTileK * (width == 4 ? 3 : 1);
-    b.dh = ProductPlan(b.slots.padded, (int)h.ld, b.dh_steps);
+    b.rows = rows <= 128 ? 128 : b.slots.padded;
+    b.dh = ProductPlan(b.rows, (int)h.ld, b.dh_steps);
     const int tile = 32 * b.dh.kW;
     // Fewer rows with a token than rows take more parts: as many as fill the chip with one tile of rows, in at most 256 MB
     const int64_t room = ((int64_t)64 << 20) / h.part, alone = ceil_div(256, (kTileM / tile) * ceil_div(src.d, tile));
@@ -138,12 +142,12 @@ struct BackwardOut {
 };
 
 template <bool kThirds, int kLayW>
-void logit_gradient(const BackwardPlan& b, const WeightSource& src, const WeightOperand& w, int rows, int first, int columns, float c, hipStream_t s) {
+void logit_gradient(const BackwardPlan& b, const WeightSource& src, const WeightOperand& w, int first, int columns, float c, hipStream_t s) {
     BoundedProblem<kThirds> p = slot_product<kThirds>(b.slots, kRowsAreM);
-    p.M = rows <= 128 ? 128 : b.slots.padded;
+    p.M = b.rows;
     set_a(p, b.slots.h, b.slots.h_low, b.slots.d64);
     set_b<kLayW>(p, w.w, w.low, w.ld, columns, src.d);
-    const LogitGradient gradient{b.grads.of, b.slots.token, kThirds ? b.slots.h_unit : nullptr, kThirds ? b.copy.unit : nullptr, c, first, columns};
+    const LogitGradient gradient{b.slots.live, b.grads.of, b.slots.token, kThirds ? b.slots.h_unit : nullptr, kThirds ? b.copy.unit : nullptr, c, first, columns};
     if constexpr (kThirds) {
         const EpiLogitGradientPairs epi{gradient, reinterpret_cast<f16*>(b.z), reinterpret_cast<f16*>(b.z_low), b.z_ld};
         SlotProduct<kThirds, kRowsByK, kLayW, EpiLogitGradientPairs>(p, b.z_tile, epi).launch(s);
@@ -157,7 +161,7 @@ template <bool kThirds, int kLayW>
 auto hidden_gradient(const BackwardPlan& b, const WeightSource& src, const WeightOperand& w, int first, int columns, const BackwardOut& out) {
     using T = std::conditional_t<kThirds, float, uint16_t>;
     BoundedProblem<kThirds> p = slot_product<kThirds>(b.slots, kRowsAreM);
-    p.M = b.slots.padded;
+    p.M = b.rows;
     p.splits = b.dh_parts.most;
     p.part_cost = b.dh.cost;
     p.part_steps = b.dh_steps;
@@ -220,10 +224,10 @@ void backward(const BackwardPlan& b, const WeightSource& src, int rows, float c,
         const int columns = std::min(b.columns, src.V - first);
         const WeightOperand w = weight_operand(src, b.copy, first, columns, s);
         if (src.layout == PCM_WEIGHT_OUT_IN) {
-            logit_gradient<kThirds, kRowsByK>(b, src, w, rows, first, columns, c, s);
+            logit_gradient<kThirds, kRowsByK>(b, src, w, first, columns, c, s);
             piece_gradients<kThirds, kKByRows>(b, src, w, first, columns, out, s);
         } else {
-            logit_gradient<kThirds, kKByRows>(b, src, w, rows, first, columns, c, s);
+            logit_gradient<kThirds, kKByRows>(b, src, w, first, columns, c, s);
             piece_gradients<kThirds, kRowsByK>(b, src, w, first, columns, out, s);
         }
     }

@@ -194,11 +194,11 @@ struct SlotProduct {
         grid = (unsigned)tiles * (unsigned)p.splits;
         if (p.splits == 1) p.part_cost = 0;
         if (p.part_cost == 0) return;
-        grid = (unsigned)round_up(tiles, kNumXcd);         // the most that any number of rows takes
-        const int each = kTileM / (32 * kW) * tiles_n;     // of 256 rows
-        for (int live = std::min(p.M / kTileM, 2048 / each + 1); live > 0; --live) {
-            const int n = live * each;
-            grid = std::max(grid, (unsigned)(round_up(n, kNumXcd) * parts_for(n, p.part_steps, p.splits, p.part_cost)));
+        grid = (unsigned)part_workgroups(tiles);           // the most that any number of rows takes
+        const int rows_m = p.M / (32 * kW), each = kTileM / (32 * kW);      // row tiles, and those of 256 rows
+        for (int live = std::min(ceil_div(rows_m, each), 2048 / (each * tiles_n) + 1); live > 0; --live) {
+            const int n = std::min(rows_m, live * each) * tiles_n;
+            grid = std::max(grid, (unsigned)(part_workgroups(n) * parts_for(n, p.part_steps, p.splits, p.part_cost)));
         }
     }
     int steps() const { return p.K1 / kTileK * (kThirds ? 3 : 1) / p.splits; }

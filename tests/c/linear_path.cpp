@@ -112,7 +112,7 @@ void look_at_product(const BoundedProblem<kThirds>& p, int lay_a, int lay_b, int
         need = 0;
         for (int rows = 1; rows <= p.kept_max; rows += kTileM) {
             const int n = std::min(p.M / tile, (rows + kTileM - 1) / kTileM * (kTileM / tile)) * (p.N / tile);
-            need = std::max<int64_t>(need, (int64_t)(n + kNumXcd - 1) / kNumXcd * kNumXcd * parts_for(n, p.part_steps, p.splits, p.part_cost));
+            need = std::max<int64_t>(need, (int64_t)part_workgroups(n) * parts_for(n, p.part_steps, p.splits, p.part_cost));
         }
     }
     if (exact ? blocks != need : blocks < need) fail(kernel, "a grid that does not fit the product");
