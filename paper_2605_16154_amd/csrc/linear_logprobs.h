@@ -30,6 +30,7 @@ struct Slots {
     int32_t* live;                   // [1]: how many slots hold a row
     int32_t* parts;                  // [1]: backward: in how many parts the product for dhidden was done
     int32_t* most;                   // [1]: fp32, backward: the largest exponent of h 2^-z_shift
+    int32_t* mosts;                  // [kMosts], kMostPitch apart: of workgroups' shares of the rows (long lists only)
     int32_t* slot_of;                // [rows]: -1 for a row without a token
     int32_t* row_of;                 // [padded]: of the slots below live
     int32_t* token;                  // [padded]: in 0 .. V - 1; -1 from live up to the next multiple of 256
@@ -51,6 +52,8 @@ struct SlotGradients {
 };
 
 constexpr int kCountRows = 1024;
+// (one number for all took 90 us of 7,500 rows' atomics)
+constexpr int kMosts = 64, kMostPitch = 32;
 constexpr int kFewRows = 16;
 constexpr int kAbsmaxParts = 1024;
 constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;

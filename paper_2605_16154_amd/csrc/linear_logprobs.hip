@@ -78,10 +78,9 @@ __global__ __launch_bounds__(256) void linear_slots(LinearRows in, Slots slots) 
             slots.token[slot++] = token[e];
         }
     }
-    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 255) {
-        *slots.live = slot;
-        *slots.most = kNoExponent;
-    }
+    if (blockIdx.x != gridDim.x - 1) return;
+    if (threadIdx.x == 255) *slots.live = slot;
+    if (threadIdx.x < kMosts) slots.mosts[threadIdx.x * kMostPitch] = kNoExponent;
 }
 
 // Exponent e with 2^e <= x < 2^(e + 1); x > 0 and finite.
@@ -234,7 +233,10 @@ __device__ __forceinline__ void gather_rows(const LinearRows& in, const Slots& s
         grads.z_shift[slot] = shift;
         const int exponent = bound > 0.f && largest > 0.f ? exponent_of(largest) - shift : kNoExponent;
         if (kList) grads.exponent[slot] = exponent;
-        else if (exponent > kNoExponent) atomicMax(slots.most, exponent);        // (the largest of whole numbers: their order does not matter)
+        else {                                            // (the largest of whole numbers: their order does not matter)
+            int32_t* const most = slots.mosts + block % kMosts * kMostPitch;
+            if (exponent > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, exponent);
+        }
     }
     grads.of[slot] = of;
 }
@@ -243,15 +245,12 @@ __device__ __forceinline__ void gather_rows(const LinearRows& in, const Slots& s
 __device__ __forceinline__ void weigh_rows(const LinearRows& in, const Slots& slots, const SlotGradients& grads, int block) {
     const int lane = threadIdx.x & 63, row = block * kGatherRows + (int)(threadIdx.x >> 6);
     const int live = *slots.live;
-    int most;
-    if (slots.counts == nullptr) {                        // a short list: each workgroup looks for the largest exponent itself
-        float x = (float)kNoExponent;
-        for (int i = threadIdx.x; i < live; i += 256) x = fmaxf(x, (float)grads.exponent[i]);
-        most = (int)block_max(x);
-        if (block == 0 && threadIdx.x == 0) *slots.most = most;
-    } else {
-        most = *slots.most;
-    }
+    // (a short list: each workgroup looks for the largest exponent itself)
+    const bool shares = slots.counts != nullptr;
+    float x = (float)kNoExponent;
+    for (int i = threadIdx.x; i < (shares ? kMosts : live); i += 256) x = fmaxf(x, (float)(shares ? slots.mosts[i * kMostPitch] : grads.exponent[i]));
+    const int most = (int)block_max(x);
+    if (block == 0 && threadIdx.x == 0) *slots.most = most;
     if (row >= in.rows) {
         const int slot = live + row - in.rows;
         if (slot >= min(slots.padded, (live + 255) / 256 * 256)) return;
@@ -637,7 +636,10 @@ Slots carve_slots(Carver& c, int rows, int d, int dtype) {
         q.h_low = c.take<half_bits>(h);
         q.h_unit = c.take<float>((size_t)q.padded);
     }
-    if (rows > 4 * kCountRows) q.counts = c.take<int32_t>((size_t)ceil_div(rows, kCountRows));
+    if (rows > 4 * kCountRows) {
+        q.counts = c.take<int32_t>((size_t)ceil_div(rows, kCountRows));
+        q.mosts = c.take<int32_t>(kMosts * kMostPitch);
+    }
     return q;
 }
 SlotGradients carve_gradients(Carver& c, const Slots& slots, int dtype) {

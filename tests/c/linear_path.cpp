@@ -282,7 +282,7 @@ void look_at_launch(const std::string& raw, void** args, dim3 grid) {
         const LinearRows& in = *static_cast<LinearRows*>(args[0]);
         const Slots& s = *static_cast<Slots*>(args[1]);
         touches("live", s.live, 4, true);
-        touches("the exponent", s.most, 4, true);
+        touches("shares of the exponent", s.mosts, kMosts * kMostPitch * 4, true);
         look_at_slots(s, in.rows, false, false);
         if (s.counts) touches("counts", s.counts, (int64_t)grid.x * 4, false);
         if ((int64_t)grid.x * kCountRows < in.rows) fail(kernel, "a grid that does not fit the rows");
@@ -300,11 +300,13 @@ void look_at_launch(const std::string& raw, void** args, dim3 grid) {
             touches("shifts", g.z_shift, (int64_t)s.padded * 4, false);
             touches("exponents", g.exponent, (int64_t)s.padded * 4, false);
             touches("the exponent", s.most, 4, true);
+            if (s.counts) touches("shares of the exponent", s.mosts, kMosts * kMostPitch * 4, false);
             look_at_piece(*static_cast<WeightPiece*>(args[4]), true, grid.x - rows_blocks);
         } else {
             look_at_slots(s, in.rows, thirds, true);
             if (g.of) look_at_grads(g, s, in.rows);
-            if (g.of && thirds) touches("shifts", g.z_shift, (int64_t)s.padded * 4, true), touches("exponents", g.exponent, (int64_t)s.padded * 4, true), touches("the exponent", s.most, 4, true);
+            if (g.of && thirds) touches("shifts", g.z_shift, (int64_t)s.padded * 4, true), touches("exponents", g.exponent, (int64_t)s.padded * 4, true);
+            if (g.of && thirds && s.counts) touches("shares of the exponent", s.mosts, kMosts * kMostPitch * 4, true);
             if (g.dh) touches_rows("dhidden", g.dh, in.rows, in.d, g.dh_ld, thirds ? 4 : 2, true);
             rows_of_call = in.rows;
             if (has(name, "true") != (s.counts == nullptr)) fail(kernel, "a list in the wrong place");
