@@ -272,7 +272,7 @@ __device__ inline uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16
 __device__ inline float weight_gradient_unit(const int32_t* most) { return most == nullptr || *most <= -(1 << 20) ? 1.f : ldexpf(1.f, *most - 14); }
 
 // acc into rows and columns of a matrix that end anywhere, at any alignment of its type, through LDS so that whole lines leave (bf16 3 to 3.5 us a tile,
-// fp32 8).
+// fp32 8; bf16 rows that begin anywhere, by 16 bytes instead of value by value, 876 rows of 3077 -> 51202 two pieces of 291 -> 217 us).
 template <class T>
 struct EpiStoreAnywhere;
 template <>
@@ -292,13 +292,21 @@ struct EpiStoreAnywhere<uint16_t> {                        // bf16
             __builtin_amdgcn_sched_barrier(0);             // one tile row's conversions at a time
         }
         __builtin_amdgcn_wave_barrier();
-        uint16_t* const to = C + (int64_t)row0 * ldc + col0;
         if (n_cols == RW && ((reinterpret_cast<uintptr_t>(C) | (uintptr_t)(ldc * 2)) & 15u) == 0) {
-            copy_rows_out<RW, RW * 2>(st, kStride, reinterpret_cast<char*>(to), ldc * 2, n_rows, tc.lane);
+            copy_rows_out<RW, RW * 2>(st, kStride, reinterpret_cast<char*>(C + (int64_t)row0 * ldc + col0), ldc * 2, n_rows, tc.lane);
             return;
         }
-        for (int r = 0; r < n_rows; ++r)
-            for (int c = tc.lane; c < n_cols; c += 64) to[r * ldc + c] = *reinterpret_cast<const uint16_t*>(st + r * kStride + c * 2);
+        typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+        constexpr int kLanes = RW / 8;                     // of a row, eight columns each
+        const int c = tc.lane % kLanes * 8;
+        for (int r = tc.lane / kLanes; r < n_rows; r += 64 / kLanes) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(st + r * kStride + c * 2);
+            uint16_t* const to = C + (int64_t)(row0 + r) * ldc + col0 + c;
+            if (c + 8 <= n_cols) *reinterpret_cast<u32x4_any*>(to) = x;
+            else
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < n_cols) to[e] = (uint16_t)(x[e / 2] >> (e % 2 * 16));
+        }
     }
 };
 template <>
