@@ -46,10 +46,10 @@ __device__ __forceinline__ RowSums sums_of(float m, float c, F z) {
     return r;
 }
 
-// The largest of three, NaN aside (fmaxf would first quieten each operand, an instruction more).
+// The largest of three, NaN if one of them is (fmaxf would let a NaN go, and first quieten each operand, an instruction more).
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
 
@@ -99,7 +99,7 @@ struct EpiRowStats {
                 m = max3(z(j, 2), z(j, 3), m);
             }
             r[i] = sums_of<kW>(m, c * unit[i], z);
-            if (!kWhole && m == -__builtin_huge_valf()) r[i].s = r[i].t = 0.f;       // no column of this lane's
+            if (!kWhole && m == -__builtin_huge_valf()) r[i].s = r[i].t = 0.f;       // no column of this lane's (m of a NaN is NaN, and so are its sums)
             r[i].m = m * unit[i];
             if (__any(at[i] >= 0 && at[i] < RW)) {
                 float x = 0.f;
