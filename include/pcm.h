@@ -565,7 +565,8 @@ PCM_API int pcm_muon_step(int n_tensors, const int* rows, const int* cols, const
  *   dz_j = ([j = token] dlogp - p_j (dlogp + dentropy (log p_j + entropy))) / temperature;  dhidden = dz weight^T;  dweight = hidden^T dz.
  * The logits are formed again, piece by piece of the vocabulary; of dz at most 1 GB or 256 columns are in memory at a time, in bf16 (PCM_BF16:
  * each value is rounded once, 2^-9 of it; PCM_F32: pairs as above).
- *   lse, entropy     device f32 [rows], as the forward call left them (log p carries the rounding of lse: 2^-24 |lse|);  entropy NULL exactly if dentropy is
+ *   lse, entropy     device f32 [rows], as the forward call left them;  entropy NULL exactly if dentropy is.  log p is the difference of a logit, formed again,
+ *                    and lse: it carries the roundings of both, 2^-22 of their sizes, and is not let above 0 in PCM_F32 nor where |lse| >= 1024
  *   dlogp, dentropy  device f32 [rows]; those of rows without a token are not looked at;  dentropy NULL: no gradient through the entropy
  *   dhidden          device [rows] rows of d values of dtype, dhidden_ld apart, or NULL; zeros for rows without a token
  *   dweight          device, layout of weight, dweight_ld apart, of dweight_dtype (PCM_F32, or PCM_BF16 for bf16 weights), or NULL.  The

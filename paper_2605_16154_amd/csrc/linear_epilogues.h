@@ -53,6 +53,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return r;
 }
 
+__device__ __forceinline__ float at_most(float x, float most) {    // (NaN stays)
+    float r;
+    asm("v_minimum3_f32 %0, %1, %2, %2" : "=v"(r) : "v"(x), "v"(most));
+    return r;
+}
+
 // The logits of a tile, a wavefront's block of which is a part of its rows.  Vector instructions that no product runs beside: 11.5 issue
 // slots per logit (the accumulator moved twice, half a maximum, difference, product, exponential, sum, moment and its guard).  A lane has a quarter of 16 neighbours' rows
 // to itself; the quarters meet at the end, all rows together, so that the exchanges wait for one another only there.  8.7 us of the 57 that a tile takes whose
@@ -129,6 +135,11 @@ struct RowResults {
 
 // Vector instructions that no product runs beside: 10 issue slots per logit (the accumulator's move, log p, exponential, factor, product, rounding and
 // the way through LDS).  With what it writes 7.8 us of a tile's 50 (reduction 1536 long), as pairs 10 to 12 of 85.
+// log p is a difference of rounded numbers and may come out above 0, where p has to stay at 1: far above where lse is large (2^-22 of it and more).  As pairs dz
+// would leave the range that the power of two of its row was chosen for, so there every log p is bounded (630 us for 625 in 1111 fp32 rows of 1001 -> 32003); in bf16
+// those of rows with |lse| from 1024 on are, in the loop that also serves blocks which the vocabulary does not fill (in all of them: 553 us for 545 in 2072 rows of
+// 1536 -> 50021).
+constexpr float kFarLse2 = 1024.f * kLog2E;
 struct LogitGradient {
     const int32_t* live;
     const SlotGradient* of;
@@ -142,8 +153,16 @@ struct LogitGradient {
     // What is to be known of rows 16 i + (lane & 15) of a wavefront's block, asked for all at once.
     struct Row {
         float scale, lse2, along, rest, g;
+        float most;                      // that log p may be
         int at;                          // of the token in this block
     };
+    template <int kW>
+    static __device__ __forceinline__ bool any_bounded(const Row (&row)[kW]) {
+        bool x = false;
+#pragma unroll
+        for (int i = 0; i < kW; ++i) x |= row[i].most == 0.f;
+        return __any(x);
+    }
     template <int kW>
     __device__ __forceinline__ void load(Row (&row)[kW], const TileCoord<kW>& tc) const {
         const float w_scale = w_unit != nullptr ? *w_unit : 1.f;
@@ -160,13 +179,14 @@ struct LogitGradient {
         for (int i = 0; i < kW; ++i) {
             row[i].scale = c * (unit[i] * w_scale);
             row[i].lse2 = G[i].lse2;
+            row[i].most = h_unit != nullptr || fabsf(G[i].lse2) >= kFarLse2 ? 0.f : __builtin_huge_valf();
             row[i].along = G[i].h * kLn2;
             row[i].rest = __builtin_fmaf(G[i].h, G[i].entropy, G[i].g);
             row[i].g = G[i].g;
         }
     }
     // dz of a row: store(tile column j, four neighbours).  Rows behind the last slot are zeros times W with a gradient of zero.
-    template <bool kWhole, int kW, class F>
+    template <bool kWhole, bool kBounded, int kW, class F>
     __device__ __forceinline__ void row(const Row& q, const TileCoord<kW>& tc, const Accumulators<kW>& acc, int i, F store) const {
         constexpr int RW = kWaveRows<kW>;
         const int quarter = tc.lane >> 4;
@@ -175,7 +195,7 @@ struct LogitGradient {
         for (int j = 0; j < kW; ++j)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const float a = __builtin_fmaf(accumulator(acc[i][j][t]), q.scale, -q.lse2);
+                const float log2p = __builtin_fmaf(accumulator(acc[i][j][t]), q.scale, -q.lse2), a = kBounded ? at_most(log2p, q.most) : log2p;
                 // (where p is 0 log p may be -inf, which is not to become a NaN)
                 const float x = -__builtin_amdgcn_exp2f(a) * __builtin_fmaf(q.along, fmaxf(a, -150.f), q.rest);
                 r[j][t] = kWhole || tc.col0() + j * 16 + quarter * 4 + t < columns ? x : 0.f;
@@ -197,16 +217,14 @@ struct EpiLogitGradient {
     LogitGradient gradient;
     bf16* dz;
     int64_t ld;
-    template <bool kWhole, int kW>
-    __device__ __forceinline__ void rows(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* st) const {
+    template <bool kPlain, int kW>
+    __device__ __forceinline__ void rows(const LogitGradient::Row (&row)[kW], const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* st) const {
         constexpr int RW = kWaveRows<kW>, kStride = RW * 2 + 16;
-        LogitGradient::Row row[kW];
-        gradient.load(row, tc);
         const int col0 = tc.col0();
 #pragma unroll
         for (int i = 0; i < kW; ++i) {
             char* const to = st + (i * 16 + (tc.lane & 15)) * kStride + 4 * (tc.lane >> 4) * 2;
-            gradient.row<kWhole>(row[i], tc, acc, i, [&](int j, const f32x4& r) __attribute__((always_inline)) {
+            gradient.row<kPlain, !kPlain>(row[i], tc, acc, i, [&](int j, const f32x4& r) __attribute__((always_inline)) {
                 *reinterpret_cast<bf16x4*>(to + j * 32) = to_bf16x4(r[0], r[1], r[2], r[3]);
             });
         }
@@ -217,8 +235,10 @@ struct EpiLogitGradient {
     __device__ __forceinline__ void operator()(const TileCoord<kW>& tc, const Accumulators<kW>& acc, char* lds) const {
         if (!gradient.read(tc)) return;
         char* st = wave_stage(tc, lds);
-        if (tc.col0() + kWaveRows<kW> <= gradient.columns) rows<true>(tc, acc, st);
-        else rows<false>(tc, acc, st);
+        LogitGradient::Row row[kW];
+        gradient.load(row, tc);
+        if (tc.col0() + kWaveRows<kW> <= gradient.columns && !gradient.any_bounded(row)) rows<true>(row, tc, acc, st);
+        else rows<false>(row, tc, acc, st);
     }
 };
 // dz 2^z_shift as hi + lo of fp16.
@@ -237,7 +257,7 @@ struct EpiLogitGradientPairs {
 #pragma unroll
             for (int ii = 0; ii < 4; ++ii) {
                 char* const to = st + (ii * 16 + (tc.lane & 15)) * kStride + 4 * (tc.lane >> 4) * 2;
-                gradient.row<kWhole>(row[half * 4 + ii], tc, acc, half * 4 + ii, [&](int j, const f32x4& r) __attribute__((always_inline)) {
+                gradient.row<kWhole, true>(row[half * 4 + ii], tc, acc, half * 4 + ii, [&](int j, const f32x4& r) __attribute__((always_inline)) {
                     f16x4 h, l;
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
