@@ -589,7 +589,9 @@ PCM_API int pcm_linear_logprobs_backward(const void* hidden, int64_t hidden_ld, 
 
 /* ------------------------------------------------------------------------------------------
  * pcm_adamw_many_step -- pcm_adamw_clip_step over all tensors of a model at once: any number of them, of any sizes and alignments, with
- * gradients in fp32 or bf16 and moments in 32 or in 8 bits.  Norm, clipping and update as there, the norm over all tensors together.
+ * gradients in fp32 or bf16 and moments in 32 or in 8 bits.  Norm, clipping and update as there, the norm over all tensors together, with two
+ * differences: where gradients are clipped and the norm is NaN, all weights and moments become NaN (there the gradients are then taken as they are); with
+ * moments in 8 bits root and reciprocal of the update are those of the hardware, 1 ulp each.
  *
  * A plan is made once for the tensors (again when their addresses change) and holds what a step needs to find them; the moments are one
  * flat block.  Both belong to the caller:

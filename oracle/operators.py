@@ -176,7 +176,7 @@ def adamw_many_eight(weights, grads, state, step, seed, lr, beta1, beta2, eps, w
     -> (weights in 64 bits, state, norm)"""
     f = np.float32
     norm = np.sqrt(sum(float((np.asarray(g, np.float64) ** 2).sum()) for g in grads))
-    scale = f(1.0) if max_grad_norm is None else f(min(1.0, max_grad_norm / (norm + 1e-6)))
+    scale = f(1.0) if max_grad_norm is None else f(np.minimum(1.0, max_grad_norm / (norm + 1e-6)))
     m_old = moment_values(state[0], state[2], M_FIELD).astype(f)
     v_old = moment_values(state[1], state[3], V_FIELD).astype(f)
     m, v, out, at = np.zeros_like(m_old), np.zeros_like(v_old), [], 0

@@ -889,7 +889,8 @@ def pcm_adamw_many_step(plan: AdamwManyPlan, step: int, lr: float = 1e-5, beta1:
                         grad_norm_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """Global-norm clipping + AdamW over the tensors of a plan (updated in place); -> grad norm f32[1].
 
-    max_grad_norm None: no clipping, and the norm only if `grad_norm_out` is given.  `seed` goes into the rounding of 8-bit moments."""
+    max_grad_norm None: no clipping, and the norm only if `grad_norm_out` is given.  With clipping, a norm that is NaN makes every weight and moment NaN.
+    `seed` goes into the rounding of 8-bit moments."""
     dev = plan.state.device
     _on_current_device(dev, "pcm_adamw_many_step")
     if max_grad_norm is not None and grad_norm_out is None:

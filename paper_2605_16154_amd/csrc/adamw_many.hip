@@ -315,7 +315,9 @@ struct ClipFactor {
         if (s.parts == 0) return 1.f;
         const double norm = sqrt(block_sum((part[0] + part[1]) + (part[2] + part[3])));
         if (s.norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *s.norm_out = (float)norm;
-        return (float)fmin(1.0, s.max_norm / (norm + 1e-6));
+        // (a norm that is NaN makes the factor NaN: fmin alone would let every gradient through at its full size)
+        if (s.max_norm == __builtin_huge_val()) return 1.f;
+        return norm == norm ? (float)fmin(1.0, s.max_norm / (norm + 1e-6)) : __builtin_nanf("");
     }
 };
 static_assert(ClipFactor::kEach == 4, "");
