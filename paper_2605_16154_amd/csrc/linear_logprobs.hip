@@ -177,7 +177,7 @@ __device__ __forceinline__ void gather_rows(const LinearRows& in, const Slots& s
         if (sizeof(T) == 4) zero_row(slots.h_low + (int64_t)slot * slots.d64, slots.d64, lane);
         if (lane == 0) {
             slots.token[slot] = -1;
-            if (sizeof(T) == 4) slots.h_unit[slot] = 1.f;
+            if (sizeof(T) == 4) slots.h_unit[slot] = 0.f;      // (1 times the weight's over a low temperature may be infinite, and 0 times that no number)
             if (grads.of != nullptr) grads.of[slot] = SlotGradient{0.f, 0.f, 0.f, 0.f};
             if (sizeof(T) == 4 && grads.of != nullptr) grads.z_shift[slot] = 0;
         }
