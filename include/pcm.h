@@ -614,6 +614,7 @@ PCM_API int pcm_linear_logprobs_backward(const void* hidden, int64_t hidden_ld, 
  *   grads, grad_dtypes host arrays: device pointers and pcm_dtype of each;  weights host array of device pointers f32, updated in place
  *   weights_bf16       NULL, or a host array of device pointers (entries may be NULL) that receive the new weights, rounded to nearest even
  *   max_grad_norm      infinity: no clipping; without grad_norm_out the norm is then not formed and needs no workspace
+ *   eps                at least 2^-126
  *   seed               of the rounding of 8-bit moments
  * Errors: PCM_EINVAL also where tensors of a plan that are written share memory with any other, for a layout that pcm_adamw_many_describe did
  * not make and for hyper-parameters out of range; PCM_EWORKSPACE for a plan buffer that is too small.  Steps on the same state have to be ordered.

@@ -521,6 +521,9 @@ bool share_memory(Extent* x, int64_t n) {
     return false;
 }
 
+// The update has eps in fp32; where neither moment has met a gradient it divides by nothing else, and the hardware's reciprocal takes what is below the
+// normal numbers for 0.
+constexpr double kLeastEps = 0x1p-126;
 // Parameters beyond which a step's arrays outgrow the 256 MB memory-side cache.
 constexpr int64_t kStreamElements = 20 << 20;
 
@@ -592,7 +595,7 @@ PCM_API int pcm_adamw_many_step(const void* plan, const pcm_adamw_many_layout* l
                                 double beta2, double eps, double weight_decay, double max_grad_norm, uint64_t seed, float* grad_norm_out,
                                 void* workspace, size_t workspace_bytes, void* stream) {
     if (!layout_ok(layout) || !adam_arguments_ok(step, lr, beta1, beta2, eps, weight_decay, max_grad_norm) || !aligned(plan, 8) ||
-        !aligned(state, 16) || !aligned(grad_norm_out, 4))
+        !aligned(state, 16) || !aligned(grad_norm_out, 4) || !(eps >= kLeastEps))
         return PCM_EINVAL;
     if (layout->chunks > 0 && (!plan || !state)) return PCM_EINVAL;
     const bool want_norm = max_grad_norm < __builtin_huge_val() || grad_norm_out != nullptr;
