@@ -895,6 +895,8 @@ def pcm_adamw_many_step(plan: AdamwManyPlan, step: int, lr: float = 1e-5, beta1:
     _on_current_device(dev, "pcm_adamw_many_step")
     if max_grad_norm is not None and grad_norm_out is None:
         grad_norm_out = torch.empty(1, dtype=_F32, device=dev)
+    elif grad_norm_out is not None and (grad_norm_out.numel() == 0 or grad_norm_out.device != dev):
+        raise PcmError(f"grad_norm_out must hold a number on {dev}")
     entry, stream = lib().pcm_adamw_many_step, _stream()
     head = (plan.table.data_ptr(), C.byref(plan.layout), plan.state.data_ptr(), step, lr, beta1, beta2, eps, weight_decay,
             float("inf") if max_grad_norm is None else max_grad_norm, seed & 0xFFFFFFFFFFFFFFFF, _ptr(grad_norm_out, _F32, "grad_norm_out"))

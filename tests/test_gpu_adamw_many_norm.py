@@ -67,3 +67,13 @@ def test_an_infinite_gradient_makes_the_others_nothing(bits):
     gone = torch.isnan(m)
     assert bool(gone[at]) and int(gone.sum()) == (1 if bits == 32 else 128) and torch.equal(gone, torch.isnan(v))
     assert not m[~gone].any() and not v[~gone].any()
+
+
+def test_a_norm_that_has_no_place_is_refused():
+    pcm, plan, grads, weights, copies = _plan(32)
+    before = torch.cat(weights)
+    for clip in (None, 1.0):
+        for out in (torch.empty(0, device="cuda"), torch.empty(1)):
+            with pytest.raises(pcm.PcmError):
+                pcm.pcm_adamw_many_step(plan, 1, max_grad_norm=clip, grad_norm_out=out, **HP)
+    assert torch.equal(torch.cat(weights), before)
