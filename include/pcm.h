@@ -564,7 +564,7 @@ PCM_API int pcm_muon_step(int n_tensors, const int* rows, const int* cols, const
  * pcm_linear_logprobs_backward -- the gradient of a loss from its gradients in logp and entropy, as pcm_token_logprobs_backward:
  *   dz_j = ([j = token] dlogp - p_j (dlogp + dentropy (log p_j + entropy))) / temperature;  dhidden = dz weight^T;  dweight = hidden^T dz.
  * The logits are formed again, piece by piece of the vocabulary; of dz at most 1 GB or 256 columns are in memory at a time, in bf16 (PCM_BF16:
- * each value is rounded once, 2^-9 of it; PCM_F32: pairs as above).
+ * each value is rounded once, 2^-8 of it at most; PCM_F32: pairs as above; of what the rows add to dweight, what is below 2^-38 of the largest row's is lost).
  *   lse, entropy     device f32 [rows], as the forward call left them;  entropy NULL exactly if dentropy is.  log p is the difference of a logit, formed again,
  *                    and lse: it carries the roundings of both, 2^-22 of their sizes, and is not let above 0 in PCM_F32 nor where |lse| >= 1024
  *   dlogp, dentropy  device f32 [rows]; those of rows without a token are not looked at;  dentropy NULL: no gradient through the entropy
@@ -572,6 +572,8 @@ PCM_API int pcm_muon_step(int n_tensors, const int* rows, const int* cols, const
  *   dweight          device, layout of weight, dweight_ld apart, of dweight_dtype (PCM_F32, or PCM_BF16 for bf16 weights), or NULL.  The
  *                    sum over all rows is formed in fp32 and rounded once.  accumulate != 0 (PCM_F32 only): it is added to what is there
  * Not both NULL.  Values between rows are left as they are.  Results may not share memory with what is read.
+ * Workspace: the rows' slots (PCM_F32: twice), dz, the copy of the weight as above and fp32 parts of both results, at most 256 MB of each (of dhidden over
+ * several pieces one part at least): up to about 1.8 GB for the rows of a training batch.
  * ------------------------------------------------------------------------------------------ */
 typedef enum { PCM_WEIGHT_IN_OUT = 0, PCM_WEIGHT_OUT_IN = 1 } pcm_weight_layout;
 PCM_API size_t pcm_linear_logprobs_workspace_bytes(int64_t rows, int d, int V, int dtype, int weight_layout, const void* weight,

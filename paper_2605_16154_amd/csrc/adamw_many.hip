@@ -14,7 +14,8 @@
 // holds the values below 2^(E - F + 1) at the spacing of f = 1, down to zero.  Values are rounded to one of their two neighbours with 16 random bits,
 // so that their expectation is the value: v moves by a thousandth of itself per step, a hundredth of the spacing, and rounding to nearest
 // would keep it where it is for good.  v > 0 never becomes 0, which would make the update m / eps.  The update itself takes m and v
-// before they are rounded.  All of it is integer arithmetic and fp32 without fused multiply-add: bits do not depend on the launch.
+// before they are rounded.  Moments and codes are integer arithmetic and fp32 without fused multiply-add, so that their bits are those of the definition (the weights
+// of this form take the hardware's root and reciprocal and a fused multiply-add); none depend on the launch.
 #include "adamw_many.h"
 
 #include <algorithm>

@@ -212,7 +212,8 @@ struct LogitGradient {
     }
 };
 
-// dz as bf16.
+// dz as bf16, once rounded: what the products with bf16 rows and weights take.  Kept in more bits it would be a second product for each result (hi + lo) or fp32
+// copies of rows and weights.  Both results of 256 to 2072 rows are then off by 2.3e-3 to 2.5e-3 of their size against 64 bits, by 1.7e-3 from their own rounding alone.
 struct EpiLogitGradient {
     LogitGradient gradient;
     bf16* dz;

@@ -93,7 +93,6 @@ struct BackwardPlan {
     int pieces, dh_steps;            // dh_steps: of the first piece, in which all pieces' parts are chosen
     size_t bytes;
 };
-// `dw_direct`: whole products go straight to dweight.
 BackwardPlan plan_backward(void* workspace, int rows, const WeightSource& src) {
     Carver c(workspace);
     BackwardPlan b{};

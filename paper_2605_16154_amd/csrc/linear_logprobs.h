@@ -4,8 +4,8 @@
 // the others and nothing that those hold is met.  How many there are is known on the device only; products skip tiles beyond.
 //
 // fp32: operands are pairs of fp16 matrices, value times a power of two = hi + lo, 22 significand bits, and a product is three of fp16 with
-// fp32 sums: a third of the 16-bit rate, several times that of fp32 instructions.  What is lost is below 2^-22 of a value, or 2^-40 of the
-// largest one that shares its power of two: a row of h and of dz has one each, W has one.
+// fp32 sums: a third of the 16-bit rate, several times that of fp32 instructions.  What is lost is below 2^-22 of a value, or 2^-39 of the
+// largest one that shares its power of two: a row of h and of dz has one each, W has one, and so have all rows of h as they are weighted for dW.
 #pragma once
 
 #include "gemm_bf16.h"
@@ -64,13 +64,17 @@ struct WeightSource {
     int dtype, layout, d, V;
     bool in_place;                   // bf16 that the products can read where it is
 };
-// Rows that the projection streams past, 16 at a time, instead of being multiplied in tiles.  Calls with rows in bf16, streamed / in tiles: 16 rows of
-// 1024 -> 32000 17 / 43 us ([d, V]) and 20 / 26 ([V, d]), of 4096 -> 65536 100 / 115 and 120 / 140; 32 rows 125 / 116 and 193 / 140.  Where the weight has to be
-// copied first more of them stream: bf16 [d, V], 64 of 1023 -> 32003 42 / 44 and of 4095 -> 65531 287 / 329, 80 50 / 43 and 353 / 326; fp32, which is
-// made pairs, 64 of 1024 -> 32003 68 / 105 ([d, V]) and 90 / 102 ([V, d]), 100 108 / 106 and 151 / 104, 64 of 4096 -> 65536 432 / 998 and 649 / 1092, 100
-// 732 / 1000 and 1073 / 1093.  (bf16 [V, d] whose rows begin anywhere: 16 of 1023 -> 32003 50 / 44, of 4095 -> 65531 276 / 370, 32 93 / 44 and 548 / 371.)
-// And fp32 rows, up to as many as were measured, as long as what streams past all groups is 128 MB: 1024 rows of 256 -> 1024 17 / 26 and 23 / 26, 256 of 512 -> 4096 23 / 33
-// and 31 / 32, 512 39 / 35 and 55 / 34.
+// Whether the projection streams past the rows, 16 at a time, or they are multiplied in tiles.  Streaming reads W once per 16 rows (from the cache after the
+// first); tiles need W in place or a copy first, of fp32 as pairs after a pass for its largest value.  So
+//   bf16            up to 16 rows
+//   bf16, copied    [d, V] up to 64, [V, d] up to 16: there a lane's 16 bytes begin anywhere and neighbours' lie far apart, which takes three times as long
+//   fp32            [d, V] up to 96, [V, d] up to 64, and up to 1024 (as many as were measured) as long as what streams past all groups is 128 MB
+// Calls streamed / in tiles, us, [d, V] and [V, d]:
+//   bf16          16 rows of 1024 -> 32000 17 / 43 and 20 / 26, of 4096 -> 65536 100 / 115 and 120 / 140; 32 rows 125 / 116 and 193 / 140
+//   bf16, copied  [d, V] 64 of 1023 -> 32003 42 / 44, of 4095 -> 65531 287 / 329; 80 50 / 43 and 353 / 326
+//                 [V, d] 16 of 1023 -> 32003 50 / 44, of 4095 -> 65531 276 / 370; 32 93 / 44 and 548 / 371
+//   fp32          64 of 1024 -> 32003 68 / 105 and 90 / 102, of 4096 -> 65536 432 / 998 and 649 / 1092; 100 108 / 106 and 151 / 104, 732 / 1000 and 1073 / 1093
+//                 1024 of 256 -> 1024 17 / 26 and 23 / 26; 256 of 512 -> 4096 23 / 33 and 31 / 32, 512 39 / 35 and 55 / 34
 inline bool streams(int rows, const WeightSource& src) {
     const bool by_token = src.layout == PCM_WEIGHT_OUT_IN;
     if (src.dtype != PCM_F32) return rows <= (src.in_place || by_token ? kFewRows : 64);

@@ -4,7 +4,8 @@
 //   products   z = h W on the matrix cores; the epilogue turns a wavefront's block of logits into three numbers per row: largest logit, sum of
 //              2^a and of 2^a a, a = (z - largest) log2 e / temperature; the token's logit is written down where it passes by
 //   join       the blocks of a row -> log-sum-exp, log p, entropy
-// 4096 bf16 rows of 4096 -> 65536: 22 + 1,560 + 15 us, 1.4 PFLOP/s, bound by the power cap (as the gradient's products).
+// 4096 bf16 rows of 4096 -> 65536: 1,600 to 1,620 us a call in a row of them, 22 and 14 of it before and after the product, 1.4 PFLOP/s, bound by the power cap (as the
+// gradient's products).
 // Few rows (streams()) have the projection streamed past them, 16 in the registers of a wavefront, bound by its bytes.
 #include "linear_epilogues.h"
 
